@@ -60,10 +60,12 @@ extern "C" {
 #define MRL_DEV_BAD_TOKEN_ID 1
 #define MRL_DEV_TIMEOUT 2
 #define MRL_DEV_BAD_WORD_MAP 4
+#define MRL_DEV_NONFINITE_GRAD 8     /* mrl_adamw_step: *grad_scale is not finite; the step was skipped */
 
-/* element types of logits / dlogits */
+/* element types of logits / dlogits, rows, weights, gradients */
 #define MRL_F32 0
 #define MRL_BF16 1
+#define MRL_E4M3 2   /* 8-bit codes (OCP e4m3: 4 exponent bits, 3 mantissa bits, largest value 448); where an entry point says so */
 
 /* mrl_adv_params.mode: which normalisation of the group-centred reward (Sec. 3; App. A) */
 #define MRL_ADV_MEAN_ONLY 0     /* A = r - mean                                  (Sec. 3, A-tilde)    */
@@ -113,6 +115,52 @@ extern "C" {
 #define MRL_WS_POLICY_LOSS 1
 #define MRL_WS_FUSED_LMHEAD 2
 #define MRL_WS_THL_WORD_ALIGN 3         /* N = total number of words of the batch; V, H, dtype, S unused */
+#define MRL_WS_RMSNORM_BWD 4            /* N rows of H columns; V, dtype, S unused */
+#define MRL_WS_GRAD_NORM 5              /* a constant; the sizes are unused */
+#define MRL_WS_ADAMW 6                  /* a constant; the sizes are unused */
+
+/* mrl_adamw_params.rounding: how what is kept in fewer bits than float32 is rounded */
+#define MRL_ROUND_NEAREST 0
+#define MRL_ROUND_SEEDED 1   /* up or down with the probability of the remainder, from the seed: equal in the mean */
+
+#define MRL_STATE_BLOCK 256  /* elements of a tensor that share the scale of an 8-bit optimiser state */
+
+typedef struct mrl_norm_params {
+  float eps;                /* added to the mean square; > 0 (forward only) */
+  float weight_offset;      /* the gain is weight + weight_offset: 0, or 1 where the weight is stored as its distance from 1 */
+  int32_t group;            /* columns that share a scale of y8: 0 (the whole row), 32, 64, 128 or 256 (forward only) */
+  uint32_t flags;           /* backward only: MRL_FLAG_ACCUMULATE_DW (dweight is added to, not overwritten) */
+} mrl_norm_params;
+
+/* One tensor of mrl_grad_norm / mrl_adamw_step.  Contiguous; every pointer [device]. */
+typedef struct mrl_tensor_slot {
+  const void* grad;         /* grad_dtype [numel] */
+  void* param;              /* param_dtype [numel] */
+  float* master;            /* float32 [numel], nullable: the weights in full precision.  Where given, the step is taken
+                               on them and param receives them rounded to nearest (param_dtype BF16 only) */
+  void* m;                  /* first moment:  float32 [numel], or e4m3 codes uint8 [numel] with m_scale */
+  void* v;                  /* second moment: float32 [numel], or e4m3 codes of its SQUARE ROOT uint8 [numel] with v_scale */
+  float* m_scale;           /* [ceil(numel / MRL_STATE_BLOCK)] with 8-bit states, else unused */
+  float* v_scale;
+  int64_t numel;
+  uint64_t rng_first;       /* MRL_ROUND_SEEDED: position of the tensor in the step's stream of random words; element i uses
+                               word rng_first + i / 2, so give tensors ranges ceil(numel / 2) apart */
+  float weight_decay;
+  int32_t grad_dtype;       /* MRL_F32 or MRL_BF16 */
+  int32_t param_dtype;      /* MRL_F32 or MRL_BF16 */
+  int32_t state_dtype;      /* MRL_F32 or MRL_E4M3 */
+} mrl_tensor_slot;
+
+typedef struct mrl_adamw_params {
+  double lr, beta1, beta2, eps;   /* 0 <= beta < 1, eps > 0 */
+  int64_t step;             /* number of this step, from 1 (bias corrections, seeded rounding); unused with step_dev */
+  uint64_t seed;            /* MRL_ROUND_SEEDED */
+  int32_t rounding;         /* MRL_ROUND_*: of 8-bit states, and of bf16 parameters without a master copy */
+  uint32_t flags;           /* 0 */
+  const float* lr_dev;      /* [device] float32 [1], nullable: read in place of lr when the work runs */
+  int64_t* step_dev;        /* [device] int64 [1], nullable: steps taken so far; the call adds 1 (unless it skips the step)
+                               and uses the result.  For steps replayed from a CUDA graph */
+} mrl_adamw_params;
 
 typedef struct mrl_adv_params {
   int32_t mode;             /* MRL_ADV_* */
@@ -404,10 +452,105 @@ int mrl_thl_word_align_logprobs(const float* src_logp, const int32_t* src_word, 
                                 void* stream);
 
 /*
+ * mrl_rmsnorm_residual_fwd -- the residual's addition and the root-mean-square norm in front of the output layer:
+ * what makes the `hidden` rows of mrl_fused_lmhead_loss_fwd_bwd.  (The paper's learners are stock models whose last layer
+ * before the LM head is this norm; the paper itself says nothing about it.)
+ *
+ *   h[t, i] = x[t, i] + residual[t, i]
+ *   rstd_t  = 1 / sqrt(mean_i h[t, i]^2 + eps)
+ *   y[t, i] = h[t, i] * rstd_t * (weight[i] + weight_offset)
+ * and, for 8-bit rows, with the columns cut into groups (the last one may be short):
+ *   scales[t, k] = max(max over group k of |y[t, i]| / 448, 2^-126),   y8[t, i] = e4m3(y[t, i] / scales[t, k])
+ * h and y are held in float32 and rounded once, to nearest even: the norm is taken of the unrounded sum, y8 of the
+ * unrounded y.  NaN and infinities propagate as the formulas say; the maxima pass over NaN.  A row whose sum of
+ * squares leaves float32 (elements above about 1e18) is summed again after division by a power of two.
+ *
+ *   x, residual [device] dtype [N, ld_x], [N, ld_res]; residual nullable (h = x)
+ *   dtype    MRL_BF16 or MRL_F32
+ *   weight   [device] w_dtype [H], MRL_BF16 or MRL_F32
+ *   np       [host]
+ *   h_out    [device] dtype [N, ld_h], nullable; may equal x or residual (with its row stride)
+ *   y        [device] dtype [N, ld_y], nullable; may equal x or residual (with its row stride)
+ *   y8       [device] uint8 [N, ld_y8], nullable; e4m3 codes
+ *   scales   [device] float32 [N, ceil(H / group)] (group 0: [N, 1]), contiguous; required with y8
+ *   rstd     [device] float32 [N], nullable; the backward pass reads it
+ * One output at least has to be given; outputs must not overlap one another, nor an input otherwise than said.
+ * Bitwise reproducible.  One read of each input where H <= 16,384.  N = 0 is a no-op.  H < 1, a row stride below H, a
+ * null required pointer, eps that is not finite and positive, an unknown group -> MRL_ERR_INVALID_ARG.
+ */
+int mrl_rmsnorm_residual_fwd(const void* x, int64_t ld_x, const void* residual, int64_t ld_res, int32_t dtype,
+                             const void* weight, int32_t w_dtype, int64_t N, int32_t H, const mrl_norm_params* np,
+                             void* h_out, int64_t ld_h, void* y, int64_t ld_y, void* y8, int64_t ld_y8, float* scales,
+                             float* rstd, void* stream);
+
+/*
+ * mrl_rmsnorm_residual_bwd -- its gradients: takes the `dHidden` of mrl_fused_lmhead_loss_fwd_bwd.
+ * With w_i = weight[i] + weight_offset and xhat[t, i] = h[t, i] * rstd_t:
+ *   dx[t, i]   = dh[t, i] + rstd_t (w_i dy[t, i] - xhat[t, i] mean_j(w_j dy[t, j] xhat[t, j]))
+ *   dweight[i] = sum_t dy[t, i] xhat[t, i]
+ * dx is the gradient of x and of residual alike (h is their sum).
+ *
+ *   dy      [device] dtype [N, ld_dy]  gradient of y
+ *   dh      [device] dtype [N, ld_dh]  gradient that reaches h from elsewhere (the residual stream); nullable = 0
+ *   h       [device] dtype [N, ld_h]   the forward pass's h_out (its x where there was no residual)
+ *   rstd    [device] float32 [N]       of the forward pass
+ *   np      [host]  weight_offset and flags
+ *   dx      [device] dtype [N, ld_dx]; may equal dy, dh or h (with its row stride)
+ *   dweight [device] float32 [H], nullable; overwritten, or added to under MRL_FLAG_ACCUMULATE_DW
+ *   workspace: mrl_workspace_bytes(MRL_WS_RMSNORM_BWD, N, 0, H, 0, 0); may be NULL where dweight is
+ * float32 arithmetic and sums in a fixed order: bitwise reproducible.  N = 0: dweight is zeroed unless accumulated.
+ */
+int mrl_rmsnorm_residual_bwd(const void* dy, int64_t ld_dy, const void* dh, int64_t ld_dh, const void* h, int64_t ld_h,
+                             int32_t dtype, const void* weight, int32_t w_dtype, const float* rstd, int64_t N, int32_t H,
+                             const mrl_norm_params* np, void* dx, int64_t ld_dx, float* dweight, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/*
+ * mrl_grad_norm -- the 2-norm of a step's gradients over all tensors and the factor that clips it (App. A: clipping at
+ * 1.0 before the update).
+ *   norm = sqrt(sum over all elements of g^2),   coef = max_norm > 0 ? max_norm / max(norm, max_norm) : 1
+ * coef is NaN where the norm is not finite: mrl_adamw_step then skips the step.
+ *
+ *   slots   [host] n_slots tensors; grad, grad_dtype and numel are read (numel 0: grad may be NULL)
+ *   norm, coef [device] float32 [1], each nullable, not both
+ *   workspace: mrl_workspace_bytes(MRL_WS_GRAD_NORM, 0, 0, 0, 0, 0)
+ * Squares are summed in float32 over short runs (in float64 where they would leave float32) and the runs in float64 in a
+ * fixed order: bitwise reproducible.  n_slots = 0: norm 0.
+ */
+int mrl_grad_norm(const mrl_tensor_slot* slots, int32_t n_slots, float max_norm, float* norm, float* coef,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * mrl_adamw_step -- one AdamW step (App. A: AdamW, lr 1e-6) over many tensors at once: takes the dW of
+ * mrl_fused_lmhead_loss_fwd_bwd and the dweight of mrl_rmsnorm_residual_bwd.
+ *   g = grad * grad_scale,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+ *   p = p - lr (weight_decay p + (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps))
+ * float32 arithmetic.  p is master where given, else param; bf16 param is rounded once.  8-bit states: per
+ * MRL_STATE_BLOCK elements of the tensor, scale = max(max |s| / 448, 2^-126) and code = e4m3(s / scale), s = m or sqrt(v); a v
+ * above zero never gets the code of zero (its update would be unbounded).  States start as zeros (codes and scales).
+ *
+ * MRL_ROUND_SEEDED.  At lr 1e-6 nearest rounding loses every update of a bf16 weight, and an 8-bit moving average stands
+ * still: its change per step is below half a code.  Seeded rounding keeps both equal to the exact value in the mean:
+ * the remainder is compared with 16 bits of the word splitmix64(splitmix64(splitmix64(seed) + step) + rng_first + i / 2)
+ * -- from bit 32 (i mod 2): 16 for m, then 16 for v; the parameter uses m's bits in reverse order.
+ *
+ *   slots      [host] n_slots tensors; they must not overlap
+ *   ap         [host]
+ *   grad_scale [device] float32 [1], nullable = 1.  Not finite: nothing is written, MRL_DEV_NONFINITE_GRAD is set
+ *   status     [device] int32 [1], nullable
+ *   workspace: mrl_workspace_bytes(MRL_WS_ADAMW, 0, 0, 0, 0, 0); may be NULL unless lr_dev or step_dev is given
+ * Elementwise, so bitwise reproducible.  A non-finite gradient that grad_scale does not announce spoils its element (8-bit
+ * states: its block).  n_slots = 0 with step_dev still counts the step.
+ */
+int mrl_adamw_step(const mrl_tensor_slot* slots, int32_t n_slots, const mrl_adamw_params* ap, const float* grad_scale,
+                   int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * mrl_profile_dominant_kernel -- instrumentation for benchmarks; the paper has no counterpart.
  * Registers n pairs of CUDA events (cudaEvent_t passed as void*, created and owned by the caller).
  * From then on every launch of an entry point's dominant kernel (the per-row kernel of
- * mrl_token_logprobs / mrl_policy_loss_fwd_bwd; each tensor-core kernel of the fused LM head)
+ * mrl_token_logprobs / mrl_policy_loss_fwd_bwd; each tensor-core kernel of the fused LM head; the row or element
+ * kernels of the norm, the gradient norm and the update)
  * records start_events[i % n] just before and stop_events[i % n] just after it on the call's
  * stream, i counting such launches since registration.  n = 0 (or null arrays) unregisters.
  * The arrays [host] must stay alive while registered.  Process-wide and not thread-safe.

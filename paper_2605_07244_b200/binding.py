@@ -13,7 +13,7 @@ import torch
 from .build import LIB_PATH
 
 OK = 0
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2
 ADV_MEAN_ONLY, ADV_GROUP_ZNORM, ADV_BATCH_ZNORM = 0, 1, 2
 PICK_NONE, PICK_FIRST, PICK_SHORTEST, PICK_ALL, PICK_SEEDED = 0, 1, 2, 3, 4
 AGG_TOKEN_MEAN, AGG_SEQ_MEAN_TOKEN_MEAN = 0, 1
@@ -21,12 +21,16 @@ RATIO_TOKEN, RATIO_SEQUENCE = 0, 1
 KL_K1, KL_K2, KL_K3 = 0, 1, 2
 FLAG_ACCUMULATE_LOSS, FLAG_SKIP_ZERO_ROWS, FLAG_ACCUMULATE_DW, FLAG_PAIR_TILES = 1, 2, 4, 8
 WS_TOKEN_LOGPROBS, WS_POLICY_LOSS, WS_FUSED_LMHEAD, WS_THL_WORD_ALIGN = 0, 1, 2, 3
-DEV_BAD_TOKEN_ID, DEV_TIMEOUT, DEV_BAD_WORD_MAP = 1, 2, 4
+WS_RMSNORM_BWD, WS_GRAD_NORM, WS_ADAMW = 4, 5, 6
+DEV_BAD_TOKEN_ID, DEV_TIMEOUT, DEV_BAD_WORD_MAP, DEV_NONFINITE_GRAD = 1, 2, 4, 8
+ROUND_NEAREST, ROUND_SEEDED = 0, 1
+STATE_BLOCK = 256
 
 EXPORTS = ("mrl_group_advantages", "mrl_token_logprobs", "mrl_policy_loss_fwd_bwd",
            "mrl_fused_lmhead_loss_fwd_bwd", "mrl_workspace_bytes", "mrl_status_string", "mrl_version",
            "mrl_profile_dominant_kernel", "mrl_policy_loss_fwd_bwd_static", "mrl_thl_word_align_logprobs",
-           "mrl_policy_loss_fwd_bwd_host", "mrl_host_pipeline_workspace_bytes", "mrl_profile_last_kernel")
+           "mrl_policy_loss_fwd_bwd_host", "mrl_host_pipeline_workspace_bytes", "mrl_profile_last_kernel",
+           "mrl_rmsnorm_residual_fwd", "mrl_rmsnorm_residual_bwd", "mrl_grad_norm", "mrl_adamw_step")
 STATIC_MAX_ROWS, STATIC_MAX_SEQS = 65536, 65536
 ERR_STATIC_SCRATCH_TOO_SMALL = 8
 
@@ -43,6 +47,23 @@ class LossParams(C.Structure):
                 ("nll_coeff", C.c_float), ("ratio_level", C.c_int32), ("entropy", C.c_void_p),
                 ("logp_ref", C.c_void_p), ("kl_coeff", C.c_float), ("kl_estimator", C.c_int32),
                 ("kl_loss", C.c_void_p)]
+
+
+class NormParams(C.Structure):
+    _fields_ = [("eps", C.c_float), ("weight_offset", C.c_float), ("group", C.c_int32), ("flags", C.c_uint32)]
+
+
+class TensorSlotStruct(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("param", C.c_void_p), ("master", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("numel", C.c_int64), ("rng_first", C.c_uint64),
+                ("weight_decay", C.c_float), ("grad_dtype", C.c_int32), ("param_dtype", C.c_int32),
+                ("state_dtype", C.c_int32)]
+
+
+class AdamwParams(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("step", C.c_int64), ("seed", C.c_uint64), ("rounding", C.c_int32), ("flags", C.c_uint32),
+                ("lr_dev", C.c_void_p), ("step_dev", C.c_void_p)]
 
 
 class MrlError(RuntimeError):
@@ -84,6 +105,16 @@ def lib() -> C.CDLL:
         L.mrl_thl_word_align_logprobs.argtypes = [vp, vp, vp, vp, vp, vp, i32, i64, i64, i64, C.c_float, vp, vp, vp, vp,
                                                   vp, sz, vp]
         L.mrl_thl_word_align_logprobs.restype = C.c_int
+        L.mrl_rmsnorm_residual_fwd.argtypes = [vp, i64, vp, i64, i32, vp, i32, i64, i32, C.POINTER(NormParams), vp, i64,
+                                               vp, i64, vp, i64, vp, vp, vp]
+        L.mrl_rmsnorm_residual_fwd.restype = C.c_int
+        L.mrl_rmsnorm_residual_bwd.argtypes = [vp, i64, vp, i64, vp, i64, i32, vp, i32, vp, i64, i32, C.POINTER(NormParams),
+                                               vp, i64, vp, vp, sz, vp]
+        L.mrl_rmsnorm_residual_bwd.restype = C.c_int
+        L.mrl_grad_norm.argtypes = [C.POINTER(TensorSlotStruct), i32, C.c_float, vp, vp, vp, sz, vp]
+        L.mrl_grad_norm.restype = C.c_int
+        L.mrl_adamw_step.argtypes = [C.POINTER(TensorSlotStruct), i32, C.POINTER(AdamwParams), vp, vp, vp, sz, vp]
+        L.mrl_adamw_step.restype = C.c_int
         L.mrl_workspace_bytes.argtypes = [i32, i64, i32, i32, i32, i32]
         L.mrl_workspace_bytes.restype = sz
         L.mrl_status_string.argtypes = [C.c_int]
@@ -233,6 +264,136 @@ def mrl_thl_word_align_logprobs(src_logp, src_word, src_cu, tgt_word, tgt_cu, wo
                                              float(ignore_value), _p(out),
                                              _p(src_total), _p(tgt_total), _p(status), _p(workspace), ws_bytes,
                                              _stream(stream)), "mrl_thl_word_align_logprobs")
+
+
+# ---- the norm before the LM head, the gradient norm and the update: the argument checks that need the tensors' shapes
+
+_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+_CODE_TYPES = (torch.float8_e4m3fn, torch.uint8)      # how e4m3 codes may be held
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _raw_stream(stream, device):
+    """The stream handle: the current stream of the tensors' device, which has to be the current device."""
+    if device.type != "cuda":
+        raise MrlError(1, f"tensors on {device}")
+    if device.index != torch.cuda.current_device():
+        raise MrlError(1, f"tensors on {device}, which is not the current device")
+    return torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream
+
+
+def _rows(t, N, H, dtypes, device, where):
+    """Row stride of an [N, H] tensor whose columns are adjacent."""
+    if t is None:
+        return H
+    if t.dtype not in dtypes:
+        raise MrlError(3, where)
+    if t.shape != (N, H) or (H > 1 and t.stride(1) != 1) or t.device != device:
+        raise MrlError(1, where)
+    ld = t.stride(0) if N > 1 else H
+    if ld < H:
+        raise MrlError(1, where)
+    return ld
+
+
+def _vector(t, n, dtypes, device, where):
+    """Address of a contiguous tensor of n elements."""
+    if t is None:
+        return None
+    if t.dtype not in dtypes:
+        raise MrlError(3, where)
+    if t.numel() != n or not t.is_contiguous() or t.device != device:
+        raise MrlError(1, where)
+    return t.data_ptr()
+
+
+_F32_ONLY = (torch.float32,)
+
+
+def mrl_rmsnorm_residual_fwd(x, residual, weight, np: NormParams, h_out=None, y=None, y8=None, scales=None, rstd=None,
+                             stream=None):
+    N, H = x.shape
+    where, dev, own = "mrl_rmsnorm_residual_fwd", x.device, (x.dtype,)
+    code = _CODES.get(x.dtype)
+    if code is None:
+        raise MrlError(3, where)
+    st = _raw_stream(stream, dev)
+    groups = -(-H // np.group) if np.group > 0 else 1
+    _check(lib().mrl_rmsnorm_residual_fwd(
+        x.data_ptr(), _rows(x, N, H, own, dev, where), _ptr(residual), _rows(residual, N, H, own, dev, where), code,
+        _vector(weight, H, _CODES, dev, where), _CODES[weight.dtype], N, H, np, _ptr(h_out),
+        _rows(h_out, N, H, own, dev, where), _ptr(y), _rows(y, N, H, own, dev, where), _ptr(y8),
+        _rows(y8, N, H, _CODE_TYPES, dev, where), _vector(scales, N * groups, _F32_ONLY, dev, where),
+        _vector(rstd, N, _F32_ONLY, dev, where), st), where)
+
+
+def mrl_rmsnorm_residual_bwd(dy, dh, h, weight, rstd, np: NormParams, dx, dweight=None, workspace=None, stream=None):
+    N, H = dy.shape
+    where, dev, own = "mrl_rmsnorm_residual_bwd", dy.device, (dy.dtype,)
+    code = _CODES.get(dy.dtype)
+    if code is None:
+        raise MrlError(3, where)
+    st = _raw_stream(stream, dev)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().mrl_rmsnorm_residual_bwd(
+        dy.data_ptr(), _rows(dy, N, H, own, dev, where), _ptr(dh), _rows(dh, N, H, own, dev, where), h.data_ptr(),
+        _rows(h, N, H, own, dev, where), code, _vector(weight, H, _CODES, dev, where), _CODES[weight.dtype],
+        _vector(rstd, N, _F32_ONLY, dev, where), N, H, np, dx.data_ptr(), _rows(dx, N, H, own, dev, where),
+        _vector(dweight, H, _F32_ONLY, dev, where), _ptr(workspace), ws_bytes, st), where)
+
+
+class TensorSlot:
+    """One tensor of mrl_grad_norm / mrl_adamw_step: contiguous CUDA tensors of one size.  A gradient norm needs `grad`
+    alone; 8-bit states are uint8 or float8_e4m3fn tensors with `m_scale`, `v_scale` of ceil(numel / STATE_BLOCK)."""
+
+    def __init__(self, grad, param=None, master=None, m=None, v=None, m_scale=None, v_scale=None, weight_decay=0.0,
+                 rng_first=0):
+        n, dev, where = grad.numel(), grad.device, "TensorSlot"
+        s = self.struct = TensorSlotStruct()
+        s.grad = _vector(grad, n, _CODES, dev, where)
+        s.grad_dtype = _CODES[grad.dtype]
+        s.param = _vector(param, n, _CODES, dev, where)
+        s.param_dtype = F32 if param is None else _CODES[param.dtype]
+        s.master = _vector(master, n, _F32_ONLY, dev, where)
+        s.state_dtype = E4M3 if m is not None and m.dtype in _CODE_TYPES else F32
+        kind = _CODE_TYPES if s.state_dtype == E4M3 else _F32_ONLY
+        s.m, s.v = _vector(m, n, kind, dev, where), _vector(v, n, kind, dev, where)
+        blocks = -(-n // STATE_BLOCK)
+        s.m_scale, s.v_scale = (_vector(t, blocks, _F32_ONLY, dev, where) for t in (m_scale, v_scale))
+        s.numel, s.rng_first, s.weight_decay = n, rng_first, weight_decay
+        self.device = dev
+        self.tensors = (grad, param, master, m, v, m_scale, v_scale)
+
+
+class TensorList:
+    """The table of a step's tensors, built once; it keeps them alive."""
+
+    def __init__(self, slots):
+        self.slots = list(slots)
+        if any(s.device != self.slots[0].device for s in self.slots):
+            raise MrlError(1, "TensorList: tensors on several devices")
+        self.device = self.slots[0].device if self.slots else torch.device("cuda", torch.cuda.current_device())
+        self.n = len(self.slots)
+        self.table = (TensorSlotStruct * self.n)(*[s.struct for s in self.slots])
+
+
+def mrl_grad_norm(tensors: TensorList, max_norm: float, norm=None, coef=None, workspace=None, stream=None):
+    where, dev = "mrl_grad_norm", tensors.device
+    st = _raw_stream(stream, dev)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().mrl_grad_norm(tensors.table, tensors.n, max_norm, _vector(norm, 1, _F32_ONLY, dev, where),
+                               _vector(coef, 1, _F32_ONLY, dev, where), _ptr(workspace), ws_bytes, st), where)
+
+
+def mrl_adamw_step(tensors: TensorList, ap: AdamwParams, grad_scale=None, status=None, workspace=None, stream=None):
+    where, dev = "mrl_adamw_step", tensors.device
+    st = _raw_stream(stream, dev)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().mrl_adamw_step(tensors.table, tensors.n, ap, _vector(grad_scale, 1, _F32_ONLY, dev, where),
+                                _vector(status, 1, (torch.int32,), dev, where), _ptr(workspace), ws_bytes, st), where)
 
 
 class DominantKernelTimer:

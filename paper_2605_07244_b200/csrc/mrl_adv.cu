@@ -20,15 +20,6 @@ __device__ __forceinline__ unsigned long long warp_min_u64(unsigned long long v)
   return v;
 }
 
-// SplitMix64 output function (Steele, Lea, Flood 2014).
-__device__ __forceinline__ unsigned long long splitmix64(unsigned long long x) {
-  x += 0x9E3779B97F4A7C15ull;
-  unsigned long long z = x;
-  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
-  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
-  return z ^ (z >> 31);
-}
-
 // mean and sum of squared deviations of x[0..n) (strided by lane), two passes
 __device__ __forceinline__ void warp_mean_ss(const float* x, int n, int lane, float& mean, float& ss) {
   float s = 0.f;
@@ -93,7 +84,7 @@ __global__ void __launch_bounds__(32) adv_prompt_kernel(
   if (fire && ap.sgt_pick != MRL_PICK_NONE) {
     chosen = (int)(best & 0xffffffffull);
     if (ap.sgt_pick == MRL_PICK_SEEDED) {
-      const unsigned long long h = splitmix64(((ap.seed & 0xffffffffull) << 32) | (unsigned long long)(uint32_t)p);
+      const unsigned long long h = mrl::splitmix64(((ap.seed & 0xffffffffull) << 32) | (unsigned long long)(uint32_t)p);
       int k = (int)(h % (unsigned long long)n_succ);
       chosen = -1;
       for (int i = 0; i < MG; ++i) {  // every lane walks the same short list

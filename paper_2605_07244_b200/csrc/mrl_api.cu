@@ -4,6 +4,9 @@
 size_t mrl_policy_loss_workspace_bytes(long long N, int S);
 size_t mrl_fused_lmhead_workspace_bytes(long long N, int V, int H, int S);
 size_t mrl_thl_workspace_bytes(long long total_words);
+size_t mrl_rmsnorm_bwd_workspace_bytes(long long N, int H);
+size_t mrl_grad_norm_workspace_bytes();
+size_t mrl_adamw_workspace_bytes();
 
 extern "C" size_t mrl_workspace_bytes(int32_t which, int64_t N, int32_t V, int32_t H, int32_t dtype, int32_t S) {
   (void)dtype;
@@ -17,6 +20,12 @@ extern "C" size_t mrl_workspace_bytes(int32_t which, int64_t N, int32_t V, int32
       return mrl_fused_lmhead_workspace_bytes(N, V, H, S);
     case MRL_WS_THL_WORD_ALIGN:
       return mrl_thl_workspace_bytes(N);
+    case MRL_WS_RMSNORM_BWD:
+      return mrl_rmsnorm_bwd_workspace_bytes(N, H);
+    case MRL_WS_GRAD_NORM:
+      return mrl_grad_norm_workspace_bytes();
+    case MRL_WS_ADAMW:
+      return mrl_adamw_workspace_bytes();
     default:
       return 0;
   }

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -109,6 +110,29 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
   return r;
+}
+
+// Two floats to e4m3 codes, to nearest even, at most 448 in magnitude, NaN kept: low byte = a, next byte = b
+__device__ __forceinline__ uint32_t pack_e4m3x2(float a, float b) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+  return r;
+}
+__device__ __forceinline__ float2 unpack_e4m3x2(uint16_t codes) {
+  uint32_t h2;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"(codes));
+  return __half22float2(*reinterpret_cast<const __half2*>(&h2));  // every e4m3 value is a half
+}
+// The scale of a group of e4m3 codes: its largest magnitude lands on 448.  Not below 2^-126, so that 1 / scale is finite.
+__device__ __forceinline__ float e4m3_scale(float amax) { return fmaxf(amax / 448.0f, 1.17549435e-38f); }
+
+// SplitMix64 output function (Steele, Lea, Flood 2014).
+__host__ __device__ __forceinline__ uint64_t splitmix64(uint64_t x) {
+  x += 0x9E3779B97F4A7C15ull;
+  uint64_t z = x;
+  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+  return z ^ (z >> 31);
 }
 
 // Running log-sum-exp state in the base-2 domain: sum_i 2^(x_i - m), x = z * log2(e).
