@@ -4,6 +4,8 @@
 // Forward: h = x + r, rstd = 1 / sqrt(mean h^2 + eps), y = h rstd (w + o), optionally as e4m3 codes with a scale per group.
 // Backward: with g = (w + o) dy and xhat = h rstd, dx = dh + rstd (g - xhat mean(g xhat)), dw = sum over rows of dy xhat.
 // A few operations per element against 6 to 9 bytes: bound by HBM.
+#include <type_traits>
+
 #include "mrl_common.cuh"
 
 namespace {
@@ -12,8 +14,9 @@ using namespace mrl;
 
 constexpr int kSms = 148;
 constexpr int kLoopThreads = 512;
-constexpr int kRowCols = 16;                       // columns a thread holds in registers
-constexpr int kRowMax = kRowCols * 1024;           // the widest row that one CTA holds
+constexpr int kRowCols = 32;                       // columns a thread holds in registers
+constexpr int kRowMax = kRowCols * 512;            // the widest row that one CTA holds
+constexpr int kFwdRegs = 64, kBwdRegs = 80;        // registers of a thread of the row kernels
 
 template <typename T>
 __device__ __forceinline__ float load_f(const T* p);
@@ -53,6 +56,7 @@ struct NormFwdArgs {
   int H, group;
   bool w_bf16;
   float eps, offset, inv_h;
+  int stages;  // rows on their way or worked on (row kernels)
 };
 
 struct NormBwdArgs {
@@ -64,6 +68,7 @@ struct NormBwdArgs {
   int H;
   bool w_bf16;
   float offset, inv_h;
+  int stages;
 };
 
 // Rows of any length and alignment, one element per thread and step; the inputs are read again in each pass.
@@ -150,91 +155,196 @@ __global__ void __launch_bounds__(kLoopThreads) rmsnorm_bwd_loop_kernel(NormBwdA
   }
 }
 
-// kE adjacent elements of a row as 32-bit words: one load or store of 32, 16, 4 or 2 bytes.
-template <typename T, int kE>
-struct RowVec {
-  static constexpr int kBytes = kE * (int)sizeof(T);
-  static constexpr int kWords = kBytes < 4 ? 1 : kBytes / 4;
-  uint32_t w[kWords];
+// Two floats in a register pair: Blackwell adds, multiplies and fuses them with one instruction (the row kernels issue
+// enough for this to show).
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 make_f2(float lo, float hi) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 split_f2(f2 v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ f2 add_f2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 mul_f2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 fma_f2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f2 bf16x2_to_f2(uint32_t w) { return make_f2(bf16lo_to_f32(w), bf16hi_to_f32(w)); }
+__device__ __forceinline__ uint32_t f2_to_bf16x2(f2 v) {
+  const float2 u = split_f2(v);
+  return pack_bf16x2(u.x, u.y);
+}
+__device__ __forceinline__ float abs_max(float m, f2 v) {
+  const float2 u = split_f2(v);
+  return fmaxf(m, fmaxf(fabsf(u.x), fabsf(u.y)));
+}
 
-  // (not the read-only path: outputs may lie over inputs)
-  __device__ __forceinline__ void load(const T* p) {
-    if constexpr (kBytes == 32)
-      asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
-                   : "l"(p));
-    else if constexpr (kBytes == 16)
-      asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
-    else if constexpr (kBytes == 4)
-      asm volatile("ld.global.b32 %0, [%1];" : "=r"(w[0]) : "l"(p));
-    else {
-      uint16_t h;
-      asm volatile("ld.global.b16 %0, [%1];" : "=h"(h) : "l"(p));
-      w[0] = h;
-    }
-  }
-  __device__ __forceinline__ void store(T* p) const {
-    if constexpr (kBytes == 32)
-      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
-                   "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                   : "memory");
-    else if constexpr (kBytes == 16)
-      asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-    else if constexpr (kBytes == 4)
-      asm volatile("st.global.b32 [%0], %1;" ::"l"(p), "r"(w[0]) : "memory");
-    else
-      asm volatile("st.global.b16 [%0], %1;" ::"l"(p), "h"((uint16_t)w[0]) : "memory");
-  }
+// The unit of work of the row kernels: 16 adjacent bytes of a row (whole granules), or two elements 32 columns apart.
+template <typename T, bool kOdd>
+struct Unit {
+  static constexpr int kCols = kOdd ? 2 : 16 / (int)sizeof(T);  // columns
+  static constexpr int kPairs = kCols / 2;
+  static constexpr int kStep = 32 * kCols;                      // columns of a warp
+  static constexpr int kUnits = kRowCols / kCols;               // per thread and row
+  f2 p[kPairs];
+
   __device__ __forceinline__ void zero() {
 #pragma unroll
-    for (int k = 0; k < kWords; ++k) w[k] = 0;
+    for (int k = 0; k < kPairs; ++k) p[k] = 0ull;
   }
-  __device__ __forceinline__ float at(int j) const {
-    if constexpr (sizeof(T) == 4)
-      return __uint_as_float(w[j]);
-    else
-      return (j & 1) ? bf16hi_to_f32(w[j >> 1]) : bf16lo_to_f32(w[j >> 1]);
+  // from 16 bytes
+  __device__ __forceinline__ void set(uint4 q) {
+    if constexpr (sizeof(T) == 4) {
+      p[0] = make_f2(__uint_as_float(q.x), __uint_as_float(q.y));
+      p[1] = make_f2(__uint_as_float(q.z), __uint_as_float(q.w));
+    } else if constexpr (!kOdd) {
+      p[0] = bf16x2_to_f2(q.x), p[1] = bf16x2_to_f2(q.y), p[2] = bf16x2_to_f2(q.z), p[3] = bf16x2_to_f2(q.w);
+    }
   }
-  __device__ __forceinline__ void set(const float* v) {
-#pragma unroll
-    for (int k = 0; k < kWords; ++k) {
-      if constexpr (sizeof(T) == 4)
-        w[k] = __float_as_uint(v[k]);
-      else
-        w[k] = pack_bf16x2(v[2 * k], kE > 1 ? v[2 * k + 1] : 0.f);
+  __device__ __forceinline__ uint4 bits() const {
+    if constexpr (sizeof(T) == 4) {
+      const float2 a = split_f2(p[0]), b = split_f2(p[1 % kPairs]);
+      return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
+    } else {
+      return make_uint4(f2_to_bf16x2(p[0]), f2_to_bf16x2(p[1 % kPairs]), f2_to_bf16x2(p[2 % kPairs]), f2_to_bf16x2(p[3 % kPairs]));
+    }
+  }
+  // `at`: the unit's place in shared memory; in0 / in1: its first / second half lies inside the row
+  __device__ __forceinline__ void load(const char* at, bool in0, bool in1) {
+    if constexpr (!kOdd) {
+      if (in0) set(*reinterpret_cast<const uint4*>(at)); else zero();
+    } else {
+      const T* e = reinterpret_cast<const T*>(at);
+      p[0] = make_f2(in0 ? load_f(e) : 0.f, in1 ? load_f(e + 32) : 0.f);
+    }
+  }
+  // to shared memory (odd rows: their copy) or global memory
+  __device__ __forceinline__ void store(T* to, bool in0, bool in1) const {
+    if constexpr (!kOdd) {
+      if (in0) *reinterpret_cast<uint4*>(to) = bits();
+    } else {
+      const float2 u = split_f2(p[0]);
+      if (in0) store_f(to, u.x);
+      if (in1) store_f(to + 32, u.y);
     }
   }
 };
 
-// kE gains from column c on (weight + offset); the weight stays in L1.
-template <int kE>
-__device__ __forceinline__ void load_gain(const void* w, bool w_bf16, float offset, int c, float* g) {
-  if constexpr (kE == 1) {
-    g[0] = weight_at(w, w_bf16, c) + offset;
-  } else if (w_bf16) {
-    const uint2* p = reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(w) + c);
-#pragma unroll
-    for (int k = 0; k < kE / 4; ++k) {
-      const uint2 u = __ldg(p + k);
-      g[4 * k] = bf16lo_to_f32(u.x) + offset;
-      g[4 * k + 1] = bf16hi_to_f32(u.x) + offset;
-      g[4 * k + 2] = bf16lo_to_f32(u.y) + offset;
-      g[4 * k + 3] = bf16hi_to_f32(u.y) + offset;
+// The gains (weight + offset) of the unit at column c, 0 behind the row; the weight stays in L1.
+template <typename U, bool kOdd, typename W>
+__device__ __forceinline__ void load_gain(const W* w, float offset, int c, bool in0, bool in1, U* g) {
+  const W* p = w + c;
+  const f2 o2 = make_f2(offset, offset);
+  if constexpr (kOdd) {
+    float a = 0.f, b = 0.f;
+    if constexpr (sizeof(W) == 2) {
+      if (in0) a = bf16lo_to_f32(__ldg(reinterpret_cast<const uint16_t*>(p)));
+      if (in1) b = bf16lo_to_f32(__ldg(reinterpret_cast<const uint16_t*>(p) + 32));
+    } else {
+      if (in0) a = __ldg(p);
+      if (in1) b = __ldg(p + 32);
     }
+    g->p[0] = make_f2(a, b);
   } else {
-    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(w) + c);
+    g->zero();
+    if (in0) {
+      if constexpr (sizeof(W) == 2) {
 #pragma unroll
-    for (int k = 0; k < kE / 4; ++k) {
-      const float4 u = __ldg(p + k);
-      g[4 * k] = u.x + offset;
-      g[4 * k + 1] = u.y + offset;
-      g[4 * k + 2] = u.z + offset;
-      g[4 * k + 3] = u.w + offset;
+        for (int k = 0; k < U::kPairs / 2; ++k) {
+          const uint2 q = __ldg(reinterpret_cast<const uint2*>(p) + k);
+          g->p[2 * k] = bf16x2_to_f2(q.x);
+          g->p[2 * k + 1] = bf16x2_to_f2(q.y);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < U::kPairs / 2; ++k) {
+          const float4 q = __ldg(reinterpret_cast<const float4*>(p) + k);
+          g->p[2 * k] = make_f2(q.x, q.y);
+          g->p[2 * k + 1] = make_f2(q.z, q.w);
+        }
+      }
     }
+  }
+  if (offset != 0.f) {
+#pragma unroll
+    for (int k = 0; k < U::kPairs; ++k) g->p[k] = add_f2(g->p[k], o2);
   }
 }
 
-// As block_reduce, for a kernel that never reuses `red` before another barrier: one barrier, none for a single warp.
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// 16 bytes from global to shared memory without a register; reads the first `bytes` of them, zeros for the rest
+__device__ __forceinline__ void copy_async(void* dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(dst)), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// waits until at most `newer` of the thread's later groups are still under way
+__device__ __forceinline__ void copy_wait(int newer) {
+  switch (newer) {
+    case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+    case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+    case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+    default: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+  }
+}
+
+// Where a row's bytes lie in a copy of the 16-byte granules that hold them (rows of any alignment).
+struct Image {
+  char* first;   // granule with the row's first byte
+  int off, len;  // first byte inside it; bytes of the row
+};
+template <typename P>
+__device__ __forceinline__ Image image_of(P* base, long long element, int H) {
+  char* p = const_cast<char*>(reinterpret_cast<const char*>(base + element));
+  const int off = (int)(reinterpret_cast<uintptr_t>(p) & 15);
+  return Image{p - off, off, H * (int)sizeof(P)};
+}
+// Granules of a row into its copy.  Bytes of the row before it come along where it starts inside a granule, except before
+// the first row, which is none of the tensor's memory; nothing behind the row's end is read.
+template <typename T>
+__device__ __forceinline__ void image_load(char* dst, const Image& im, bool first_row) {
+  const int end = im.off + im.len;
+  for (int k = threadIdx.x; 16 * k < end; k += blockDim.x) {
+    if (k == 0 && first_row && im.off != 0) {
+      for (int b = im.off; b < min(16, end); b += (int)sizeof(T)) *reinterpret_cast<T*>(dst + b) = *reinterpret_cast<const T*>(im.first + b);
+    } else {
+      copy_async(dst + 16 * k, im.first + 16 * k, min(16, end - 16 * k));
+    }
+  }
+}
+// The copy's granules to the row: whole ones at once, the first and the last by element.
+template <typename P>
+__device__ __forceinline__ void image_store(const char* src, const Image& im) {
+  const int end = im.off + im.len;
+  for (int k = threadIdx.x; 16 * k < end; k += blockDim.x) {
+    const int lo = max(im.off, 16 * k), hi = min(end, 16 * k + 16);
+    if (hi - lo == 16) {
+      *reinterpret_cast<uint4*>(im.first + 16 * k) = *reinterpret_cast<const uint4*>(src + 16 * k);
+    } else {
+      for (int b = lo; b < hi; b += (int)sizeof(P)) *reinterpret_cast<P*>(im.first + b) = *reinterpret_cast<const P*>(src + b);
+    }
+  }
+}
+// The scale of 8-bit rows (two units in the last place of max / 448 at most), and a magnitude as an ordered integer, 0 for NaN.
+__device__ __forceinline__ float row_scale(float top) { return fmaxf(top * (1.0f / 448.0f), 1.17549435e-38f); }
+__device__ __forceinline__ uint32_t peak_bits(float v) { return __float_as_uint(fmaxf(fabsf(v), 0.f)); }
+__host__ __device__ __forceinline__ int image_bytes(int H, int elem) { return (H * elem + 30) / 16 * 16; }
+
+// Sum / maximum of non-negative values over the CTA in a fixed order: one barrier, none for a single warp.  `red` holds 16 floats,
+// 0 where there is no warp, and is not written again before another barrier.
 template <bool kMax>
 __device__ __forceinline__ float row_reduce(float v, float* red) {
 #pragma unroll
@@ -242,241 +352,399 @@ __device__ __forceinline__ float row_reduce(float v, float* red) {
     const float u = __shfl_xor_sync(0xffffffffu, v, o);
     v = kMax ? fmaxf(v, u) : v + u;
   }
-  const int warps = blockDim.x >> 5;
-  if (warps == 1) {
+  if (blockDim.x == 32) {
     __syncwarp();
     return v;
   }
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
   __syncthreads();
-  float r = red[0];
-  for (int k = 1; k < warps; ++k) r = kMax ? fmaxf(r, red[k]) : r + red[k];
-  return r;
+  const float4* q = reinterpret_cast<const float4*>(red);
+  float4 s = q[0];
+  if (blockDim.x > 128) {
+#pragma unroll
+    for (int k = 1; k < 4; ++k) {
+      const float4 u = q[k];
+      s.x = kMax ? fmaxf(s.x, u.x) : s.x + u.x;
+      s.y = kMax ? fmaxf(s.y, u.y) : s.y + u.y;
+      s.z = kMax ? fmaxf(s.z, u.z) : s.z + u.z;
+      s.w = kMax ? fmaxf(s.w, u.w) : s.w + u.w;
+    }
+  }
+  return kMax ? fmaxf(fmaxf(s.x, s.y), fmaxf(s.z, s.w)) : (s.x + s.y) + (s.z + s.w);
 }
 
-// One CTA per row, the row in registers between its one read and its writes: kV vectors of kE columns per thread, vector v
-// of thread t at column (v * blockDim.x + t) * kE.
-template <typename T, int kE, int kV, int kMaxThreads, int kMinCtas>
-__global__ void __launch_bounds__(kMaxThreads, kMinCtas) rmsnorm_fwd_row_kernel(const __grid_constant__ NormFwdArgs a) {
-  using Vec = RowVec<T, kE>;
-  __shared__ float red[4][32];
+// Rows of up to kRowMax columns, each read once and written once.  A CTA walks rows blockIdx.x, + gridDim.x, ...; the rows to
+// come are under way into shared memory (`stages` of them, 16-byte asynchronous copies), so the bytes in flight do not
+// depend on registers.  kOdd = false: rows of 16-byte granules; a thread copies the granules whose columns it works on
+// and needs no barrier to read them.  kOdd = true: rows of any alignment; the granules are copied as they lie and read by
+// column after a barrier, and outputs go the same way back.
+// Columns: a warp owns 32 * kRowCols adjacent ones, unit u of a lane lies u * kStep behind its first.  A warp whose columns
+// all lie inside the row runs without tests (kFull).
+template <typename T, bool kOdd>
+__global__ void __maxnreg__(kFwdRegs) rmsnorm_fwd_row_kernel(const __grid_constant__ NormFwdArgs a) {
+  using U = Unit<T, kOdd>;
+  constexpr int kUnits = U::kUnits, kStep = U::kStep, kPairs = U::kPairs, kHalf = kOdd ? 32 : 0;
+  extern __shared__ __align__(16) char smem[];
+  __shared__ __align__(16) float red[2][4][16];
   __shared__ uint32_t peak[kRowMax / 32];
   const int tid = threadIdx.x, nt = blockDim.x;
+  const int c0 = (tid >> 5) * (kUnits * kStep) + (tid & 31) * (kOdd ? 1 : U::kCols);
+  const bool full = ((tid >> 5) + 1) * (kUnits * kStep) <= a.H;
+  const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : nt * kRowCols * (int)sizeof(T);
+  const int stage = a.res != nullptr ? 2 * slot : slot;
+  char* img_h = smem + a.stages * stage;
+  char* img_y = img_h + (a.h_out != nullptr ? slot : 0);
+  char* img_q = img_y + (a.y != nullptr ? slot : 0);
   const int group = a.group > 0 ? a.group : a.H, groups = (a.H + group - 1) / group;
   // lanes whose columns share a scale sit side by side; more than a warp of them meet in shared memory
-  const bool meet = a.y8 != nullptr && a.group > 32 * kE;
-  for (long long row = blockIdx.x; row < a.N; row += gridDim.x) {
-    float h[kV][kE];
-    {
-      Vec x[kV], r[kV];
+  const bool meet = a.y8 != nullptr && a.group > (kOdd ? 32 : kStep);
+  for (int k = tid; k < 128; k += nt) (&red[0][0][0])[k] = 0.f;
+  __syncthreads();
+
+  const auto fetch = [&](long long row, int s) {
+    if (row < a.N) {
+      char* dst = smem + s * stage;
+      const T* x = static_cast<const T*>(a.x);
+      const T* r = static_cast<const T*>(a.res);
+      if constexpr (kOdd) {
+        image_load<T>(dst, image_of(x, row * a.ld_x, a.H), row == 0);
+        if (r != nullptr) image_load<T>(dst + slot, image_of(r, row * a.ld_res, a.H), row == 0);
+      } else {
+        dst += tid * 16;
+        x += row * a.ld_x + c0;
 #pragma unroll
-      for (int v = 0; v < kV; ++v) {
-        const int c = (v * nt + tid) * kE;
-        x[v].zero();
-        if (c < a.H) x[v].load(static_cast<const T*>(a.x) + row * a.ld_x + c);
-      }
-      if (a.res != nullptr) {
+        for (int u = 0; u < kUnits; ++u)
+          if (full || c0 + u * kStep < a.H) copy_async(dst + u * nt * 16, x + u * kStep, 16);
+        if (r != nullptr) {
+          r += row * a.ld_res + c0;
 #pragma unroll
-        for (int v = 0; v < kV; ++v) {
-          const int c = (v * nt + tid) * kE;
-          r[v].zero();
-          if (c < a.H) r[v].load(static_cast<const T*>(a.res) + row * a.ld_res + c);
+          for (int u = 0; u < kUnits; ++u)
+            if (full || c0 + u * kStep < a.H) copy_async(dst + slot + u * nt * 16, r + u * kStep, 16);
         }
       }
-#pragma unroll
-      for (int v = 0; v < kV; ++v)
-#pragma unroll
-        for (int j = 0; j < kE; ++j) h[v][j] = a.res != nullptr ? x[v].at(j) + r[v].at(j) : x[v].at(j);
     }
+    copy_commit();
+  };
+
+  for (int s = 0; s + 1 < a.stages; ++s) fetch(blockIdx.x + (long long)s * gridDim.x, s);
+  int s = 0, turn = 0;
+  for (long long row = blockIdx.x; row < a.N; row += gridDim.x, turn ^= 1) {
+    fetch(row + (long long)(a.stages - 1) * gridDim.x, s == 0 ? a.stages - 1 : s - 1);
+    copy_wait(a.stages - 1);
+    if (kOdd) __syncthreads();
+    const char* in_x = smem + s * stage + (kOdd ? c0 * (int)sizeof(T) : tid * 16);
+    const char* in_r = in_x + slot;
+    if (kOdd) {
+      in_x += image_of(static_cast<const T*>(a.x), row * a.ld_x, a.H).off;
+      in_r += image_of(static_cast<const T*>(a.res), row * a.ld_res, a.H).off;
+    }
+    s = s + 1 == a.stages ? 0 : s + 1;
+    const int unit_bytes = kOdd ? kStep * (int)sizeof(T) : nt * 16;
+
+    U h[kUnits];
+    f2 acc[2] = {0ull, 0ull};
+    const auto read = [&](auto all) {
+      constexpr bool kFull = decltype(all)::value;
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u) {
+        const bool in0 = kFull || c0 + u * kStep < a.H, in1 = kFull || c0 + u * kStep + kHalf < a.H;
+        h[u].load(in_x + u * unit_bytes, in0, in1);
+        if (a.res != nullptr) {
+          U r;
+          r.load(in_r + u * unit_bytes, in0, in1);
+#pragma unroll
+          for (int k = 0; k < kPairs; ++k) h[u].p[k] = add_f2(h[u].p[k], r.p[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kPairs; ++k) acc[(u * kPairs + k) & 1] = fma_f2(h[u].p[k], h[u].p[k], acc[(u * kPairs + k) & 1]);
+      }
+    };
+    if (full) read(std::true_type{}); else read(std::false_type{});
     if (meet)
       for (int k = tid; k < groups; k += nt) peak[k] = 0;
-    float ss = 0.f;
-#pragma unroll
-    for (int v = 0; v < kV; ++v)
-#pragma unroll
-      for (int j = 0; j < kE; ++j) ss = fmaf(h[v][j], h[v][j], ss);
-    ss = row_reduce<false>(ss, red[0]);
+    const float2 part = split_f2(add_f2(acc[0], acc[1]));
+    const float ss = row_reduce<false>(part.x + part.y, red[turn][0]);
     float rstd = rsqrtf(fmaf(ss, a.inv_h, a.eps));
     if (ss == INFINITY) {  // the squares may have left float32 although the row has not
       float m = 0.f;
 #pragma unroll
-      for (int v = 0; v < kV; ++v)
+      for (int u = 0; u < kUnits; ++u)
 #pragma unroll
-        for (int j = 0; j < kE; ++j) m = fmaxf(m, fabsf(h[v][j]));
-      m = row_reduce<true>(m, red[1]);
+        for (int k = 0; k < kPairs; ++k) m = abs_max(m, h[u].p[k]);
+      m = row_reduce<true>(m, red[turn][1]);
       if (m < INFINITY) {
-        const float s = scalbnf(1.f, -ilogbf(m));
+        const float f = scalbnf(1.f, -ilogbf(m));
         float q = 0.f;
 #pragma unroll
-        for (int v = 0; v < kV; ++v)
+        for (int u = 0; u < kUnits; ++u)
 #pragma unroll
-          for (int j = 0; j < kE; ++j) q = fmaf(h[v][j] * s, h[v][j] * s, q);
-        q = row_reduce<false>(q, red[2]);
-        rstd = s * rsqrtf(fmaf(q, a.inv_h, a.eps * s * s));
+          for (int k = 0; k < kPairs; ++k) {
+            const float2 v = split_f2(h[u].p[k]);
+            q = fmaf(v.x * f, v.x * f, fmaf(v.y * f, v.y * f, q));
+          }
+        q = row_reduce<false>(q, red[turn][2]);
+        rstd = f * rsqrtf(fmaf(q, a.inv_h, a.eps * f * f));
       }
     }
     if (tid == 0 && a.rstd != nullptr) a.rstd[row] = rstd;
-    if (a.h_out != nullptr) {
+
+    const f2 rstd2 = make_f2(rstd, rstd);
+    T* to_h = static_cast<T*>(a.h_out) + row * a.ld_h + c0;
+    T* to_y = static_cast<T*>(a.y) + row * a.ld_y + c0;
+    if (kOdd) {
+      to_h = reinterpret_cast<T*>(img_h + image_of(static_cast<T*>(a.h_out), row * a.ld_h, a.H).off) + c0;
+      to_y = reinterpret_cast<T*>(img_y + image_of(static_cast<T*>(a.y), row * a.ld_y, a.H).off) + c0;
+    }
+    const auto write = [&](auto all, auto w) {
+      constexpr bool kFull = decltype(all)::value;
 #pragma unroll
-      for (int v = 0; v < kV; ++v) {
-        const int c = (v * nt + tid) * kE;
-        Vec o;
-        o.set(h[v]);
-        if (c < a.H) o.store(static_cast<T*>(a.h_out) + row * a.ld_h + c);
+      for (int u = 0; u < kUnits; ++u) {
+        const bool in0 = kFull || c0 + u * kStep < a.H, in1 = kFull || c0 + u * kStep + kHalf < a.H;
+        if (a.h_out != nullptr) h[u].store(to_h + u * kStep, in0, in1);
+        U g;
+        load_gain<U, kOdd>(w, a.offset, c0 + u * kStep, in0, in1, &g);
+#pragma unroll
+        for (int k = 0; k < kPairs; ++k) h[u].p[k] = mul_f2(mul_f2(h[u].p[k], rstd2), g.p[k]);
+        if (a.y != nullptr) h[u].store(to_y + u * kStep, in0, in1);
       }
-    }
-    float top = 0.f;  // of the row (one scale for all columns)
-#pragma unroll
-    for (int v = 0; v < kV; ++v) {
-      const int c = (v * nt + tid) * kE;
-      float g[kE];
-      if (c < a.H) {
-        load_gain<kE>(a.w, a.w_bf16, a.offset, c, g);
-#pragma unroll
-        for (int j = 0; j < kE; ++j) h[v][j] = h[v][j] * rstd * g[j];
-      }  // (columns behind the row hold 0)
-      if (a.y != nullptr) {
-        Vec o;
-        o.set(h[v]);
-        if (c < a.H) o.store(static_cast<T*>(a.y) + row * a.ld_y + c);
-      }
-    }
-    if (a.y8 == nullptr) {
-      if (row + gridDim.x < a.N) __syncthreads();
-      continue;
-    }
-    float inv[kV];
-    if (a.group == 0) {
-#pragma unroll
-      for (int v = 0; v < kV; ++v)
-#pragma unroll
-        for (int j = 0; j < kE; ++j) top = fmaxf(top, fabsf(h[v][j]));
-      top = row_reduce<true>(top, red[3]);
-      const float scale = e4m3_scale(top);
-      if (tid == 0) a.scales[row] = scale;
-#pragma unroll
-      for (int v = 0; v < kV; ++v) inv[v] = 1.f / scale;
+    };
+    if (a.w_bf16) {
+      if (full) write(std::true_type{}, static_cast<const __nv_bfloat16*>(a.w));
+      else write(std::false_type{}, static_cast<const __nv_bfloat16*>(a.w));
     } else {
-      const int lanes = min(32, group / kE);
+      if (full) write(std::true_type{}, static_cast<const float*>(a.w));
+      else write(std::false_type{}, static_cast<const float*>(a.w));
+    }
+
+    if (a.y8 != nullptr) {
+      const int shift = 31 - __clz(group);  // of a group that is a power of two
+      float row_inv = 0.f;
+      if (a.group == 0) {
+        float top = 0.f;
 #pragma unroll
-      for (int v = 0; v < kV; ++v) {
-        float m = 0.f;
+        for (int u = 0; u < kUnits; ++u)
 #pragma unroll
-        for (int j = 0; j < kE; ++j) m = fmaxf(m, fabsf(h[v][j]));
-        for (int o = lanes >> 1; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        const int c = (v * nt + tid) * kE;
-        if (meet) {
-          if ((tid & 31) == 0 && c < a.H) atomicMax(&peak[c / group], __float_as_uint(m));
-        } else {
-          const float scale = e4m3_scale(m);
-          if (c < a.H && c % group == 0) a.scales[row * groups + c / group] = scale;
-          inv[v] = 1.f / scale;
-        }
-      }
-      if (meet) {
-        __syncthreads();
+          for (int k = 0; k < kPairs; ++k) top = abs_max(top, h[u].p[k]);
+        const float scale = row_scale(row_reduce<true>(top, red[turn][3]));
+        if (tid == 0) a.scales[row] = scale;
+        row_inv = __fdividef(1.f, scale);
+      } else if (meet) {
 #pragma unroll
-        for (int v = 0; v < kV; ++v) {
-          const int c = (v * nt + tid) * kE;
-          if (c < a.H) {
-            const float scale = e4m3_scale(__uint_as_float(peak[c / group]));
-            if (c % group == 0) a.scales[row * groups + c / group] = scale;
-            inv[v] = 1.f / scale;
+        for (int u = 0; u < kUnits; ++u) {
+          const int c = c0 + u * kStep;
+          if constexpr (kOdd) {
+            const float2 v = split_f2(h[u].p[0]);
+            const uint32_t m0 = __reduce_max_sync(0xffffffffu, peak_bits(v.x)), m1 = __reduce_max_sync(0xffffffffu, peak_bits(v.y));
+            if ((tid & 31) == 0 && c < a.H) atomicMax(&peak[c >> shift], m0);
+            if ((tid & 31) == 0 && c + 32 < a.H) atomicMax(&peak[(c + 32) >> shift], m1);
+          } else {
+            float m = 0.f;
+#pragma unroll
+            for (int k = 0; k < kPairs; ++k) m = abs_max(m, h[u].p[k]);
+            const uint32_t m0 = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
+            if ((tid & 31) == 0 && c < a.H) atomicMax(&peak[c >> shift], m0);
           }
         }
+        __syncthreads();
+      }
+      float* scales = a.scales + row * groups;
+      uint8_t* q = a.y8 + row * a.ld_y8 + c0;
+      if (kOdd) q = reinterpret_cast<uint8_t*>(img_q) + image_of(a.y8, row * a.ld_y8, a.H).off + c0;
+      const int lanes = kOdd ? 32 : min(32, group / U::kCols);
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u) {
+        const int c = c0 + u * kStep;
+        // the scale of columns c on, and in odd rows of column c + 32
+        float inv0 = row_inv, inv1 = row_inv;
+        if (a.group != 0) {
+          float m0 = 0.f, m1 = 0.f;
+          if (meet) {
+            if (c < a.H) m0 = __uint_as_float(peak[c >> shift]);
+            if (kOdd && c + 32 < a.H) m1 = __uint_as_float(peak[(c + 32) >> shift]);
+          } else if constexpr (kOdd) {
+            const float2 v = split_f2(h[u].p[0]);
+            m0 = __uint_as_float(__reduce_max_sync(0xffffffffu, peak_bits(v.x)));
+            m1 = __uint_as_float(__reduce_max_sync(0xffffffffu, peak_bits(v.y)));
+          } else {
+#pragma unroll
+            for (int k = 0; k < kPairs; ++k) m0 = abs_max(m0, h[u].p[k]);
+            for (int o = lanes >> 1; o > 0; o >>= 1) m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, o));
+          }
+          m0 = row_scale(m0);
+          m1 = row_scale(m1);
+          if (c < a.H && (c & (group - 1)) == 0) scales[c >> shift] = m0;
+          if (kOdd && c + 32 < a.H && ((c + 32) & (group - 1)) == 0) scales[(c + 32) >> shift] = m1;
+          inv0 = __fdividef(1.f, m0);
+          inv1 = __fdividef(1.f, m1);
+        }
+        if constexpr (kOdd) {
+          const float2 v = split_f2(h[u].p[0]);
+          const uint32_t code = pack_e4m3x2(v.x * inv0, v.y * inv1);
+          if (c < a.H) q[u * kStep] = (uint8_t)code;
+          if (c + 32 < a.H) q[u * kStep + 32] = (uint8_t)(code >> 8);
+        } else if (c < a.H) {
+          uint32_t o[kPairs / 2];
+#pragma unroll
+          for (int k = 0; k < kPairs / 2; ++k) {
+            const f2 i2 = make_f2(inv0, inv0);
+            const float2 v = split_f2(mul_f2(h[u].p[2 * k], i2)), w = split_f2(mul_f2(h[u].p[2 * k + 1], i2));
+            o[k] = pack_e4m3x2(v.x, v.y) | pack_e4m3x2(w.x, w.y) << 16;
+          }
+          if constexpr (kPairs == 4)
+            *reinterpret_cast<uint2*>(q + u * kStep) = make_uint2(o[0], o[1]);
+          else
+            *reinterpret_cast<uint32_t*>(q + u * kStep) = o[0];
+        }
       }
     }
-#pragma unroll
-    for (int v = 0; v < kV; ++v) {
-      const int c = (v * nt + tid) * kE;
-      if (c >= a.H) continue;
-      uint8_t* q = a.y8 + row * a.ld_y8 + c;
-      if constexpr (kE == 1) {
-        *q = (uint8_t)pack_e4m3x2(h[v][0] * inv[v], 0.f);
-      } else {
-        uint32_t o[kE / 4];
-#pragma unroll
-        for (int k = 0; k < kE / 4; ++k)
-          o[k] = pack_e4m3x2(h[v][4 * k] * inv[v], h[v][4 * k + 1] * inv[v]) |
-                 pack_e4m3x2(h[v][4 * k + 2] * inv[v], h[v][4 * k + 3] * inv[v]) << 16;
-        if constexpr (kE == 16)
-          *reinterpret_cast<uint4*>(q) = make_uint4(o[0], o[1], o[2], o[3]);
-        else if constexpr (kE == 8)
-          *reinterpret_cast<uint2*>(q) = make_uint2(o[0], o[1]);
-        else
-          *reinterpret_cast<uint32_t*>(q) = o[0];
-      }
+    if constexpr (kOdd) {
+      __syncthreads();
+      if (a.h_out != nullptr) image_store<T>(img_h, image_of(static_cast<T*>(a.h_out), row * a.ld_h, a.H));
+      if (a.y != nullptr) image_store<T>(img_y, image_of(static_cast<T*>(a.y), row * a.ld_y, a.H));
+      if (a.y8 != nullptr) image_store<uint8_t>(img_q, image_of(a.y8, row * a.ld_y8, a.H));
+    } else if (meet) {
+      __syncthreads();  // the next row clears the peaks
     }
-    if (row + gridDim.x < a.N) __syncthreads();
   }
 }
 
-// Backward of rows held in registers.  A CTA walks rows blockIdx.x, + gridDim.x, ...; each thread keeps the dweight sums of
-// its columns in registers over all of them and writes them once.
-template <typename T, int kE, int kV, int kMaxThreads, int kMinCtas>
-__global__ void __launch_bounds__(kMaxThreads, kMinCtas) rmsnorm_bwd_row_kernel(const __grid_constant__ NormBwdArgs a) {
-  using Vec = RowVec<T, kE>;
-  __shared__ float red[2][32];
+// Backward, with rows on their way as above.  Each thread keeps the dweight sums of its columns in registers over all of
+// the CTA's rows and writes them once; what a row needs after its sum is read from shared memory again.
+template <typename T, bool kOdd>
+__global__ void __maxnreg__(kBwdRegs) rmsnorm_bwd_row_kernel(const __grid_constant__ NormBwdArgs a) {
+  using U = Unit<T, kOdd>;
+  constexpr int kUnits = U::kUnits, kStep = U::kStep, kPairs = U::kPairs, kHalf = kOdd ? 32 : 0;
+  extern __shared__ __align__(16) char smem[];
+  __shared__ __align__(16) float red[2][16];
   const int tid = threadIdx.x, nt = blockDim.x;
-  float dw[kV][kE];
+  const int c0 = (tid >> 5) * (kUnits * kStep) + (tid & 31) * (kOdd ? 1 : U::kCols);
+  const bool full = ((tid >> 5) + 1) * (kUnits * kStep) <= a.H;
+  const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : nt * kRowCols * (int)sizeof(T);
+  const int stage = a.dh != nullptr ? 3 * slot : 2 * slot;
+  char* img = smem + a.stages * stage;
+  if (tid < 32) (&red[0][0])[tid] = 0.f;
+  __syncthreads();
+
+  const auto fetch = [&](long long row, int s) {
+    if (row < a.N) {
+      char* dst = smem + s * stage;
+      const void* const from[3] = {a.dy, a.h, a.dh};
+      const long long ld[3] = {a.ld_dy, a.ld_h, a.ld_dh};
 #pragma unroll
-  for (int v = 0; v < kV; ++v)
+      for (int k = 0; k < 3; ++k) {
+        if (from[k] == nullptr) continue;
+        const T* p = static_cast<const T*>(from[k]);
+        if constexpr (kOdd) {
+          image_load<T>(dst + k * slot, image_of(p, row * ld[k], a.H), row == 0);
+        } else {
+          p += row * ld[k] + c0;
 #pragma unroll
-    for (int j = 0; j < kE; ++j) dw[v][j] = 0.f;
-  int turn = 0;  // the reduction's scratch alternates: one barrier per row
-  for (long long row = blockIdx.x; row < a.N; row += gridDim.x, turn ^= 1) {
-    Vec dy[kV], h[kV], dh[kV];
-#pragma unroll
-    for (int v = 0; v < kV; ++v) {
-      const int c = (v * nt + tid) * kE;
-      dy[v].zero();
-      h[v].zero();
-      dh[v].zero();
-      if (c < a.H) {
-        dy[v].load(static_cast<const T*>(a.dy) + row * a.ld_dy + c);
-        h[v].load(static_cast<const T*>(a.h) + row * a.ld_h + c);
-        if (a.dh != nullptr) dh[v].load(static_cast<const T*>(a.dh) + row * a.ld_dh + c);
-      }
-    }
-    const float rstd = a.rstd[row];
-    float sum = 0.f;
-#pragma unroll
-    for (int v = 0; v < kV; ++v) {
-      const int c = (v * nt + tid) * kE;
-      if (c < a.H) {
-        float g[kE];
-        load_gain<kE>(a.w, a.w_bf16, a.offset, c, g);
-#pragma unroll
-        for (int j = 0; j < kE; ++j) {
-          const float d = dy[v].at(j), xhat = h[v].at(j) * rstd;
-          sum = fmaf(d * g[j], xhat, sum);
-          dw[v][j] = fmaf(d, xhat, dw[v][j]);
+          for (int u = 0; u < kUnits; ++u)
+            if (full || c0 + u * kStep < a.H) copy_async(dst + k * slot + (u * nt + tid) * 16, p + u * kStep, 16);
         }
       }
     }
-    const float mean = row_reduce<false>(sum, red[turn]) * a.inv_h;
+    copy_commit();
+  };
+
+  f2 dw[kUnits][kPairs];
 #pragma unroll
-    for (int v = 0; v < kV; ++v) {
-      const int c = (v * nt + tid) * kE;
-      if (c < a.H) {
-        float g[kE];
-        load_gain<kE>(a.w, a.w_bf16, a.offset, c, g);
+  for (int u = 0; u < kUnits; ++u)
 #pragma unroll
-        for (int j = 0; j < kE; ++j) g[j] = fmaf(dy[v].at(j) * g[j] - h[v].at(j) * rstd * mean, rstd, dh[v].at(j));
-        Vec o;
-        o.set(g);
-        o.store(static_cast<T*>(a.dx) + row * a.ld_dx + c);
+    for (int k = 0; k < kPairs; ++k) dw[u][k] = 0ull;
+  for (int s = 0; s + 1 < a.stages; ++s) fetch(blockIdx.x + (long long)s * gridDim.x, s);
+  int s = 0, turn = 0;
+  for (long long row = blockIdx.x; row < a.N; row += gridDim.x, turn ^= 1) {
+    fetch(row + (long long)(a.stages - 1) * gridDim.x, s == 0 ? a.stages - 1 : s - 1);
+    const float rstd = a.rstd[row];
+    copy_wait(a.stages - 1);
+    if (kOdd) __syncthreads();
+    const char* in_d = smem + s * stage + (kOdd ? c0 * (int)sizeof(T) : tid * 16);
+    const char *in_h = in_d + slot, *in_e = in_h + slot;
+    if (kOdd) {
+      in_d += image_of(static_cast<const T*>(a.dy), row * a.ld_dy, a.H).off;
+      in_h += image_of(static_cast<const T*>(a.h), row * a.ld_h, a.H).off;
+      in_e += image_of(static_cast<const T*>(a.dh), row * a.ld_dh, a.H).off;
+    }
+    s = s + 1 == a.stages ? 0 : s + 1;
+    const int unit_bytes = kOdd ? kStep * (int)sizeof(T) : nt * 16;
+
+    const f2 rstd2 = make_f2(rstd, rstd);
+    f2 acc[2] = {0ull, 0ull};
+    const auto read = [&](auto all, auto w) {
+      constexpr bool kFull = decltype(all)::value;
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u) {
+        const bool in0 = kFull || c0 + u * kStep < a.H, in1 = kFull || c0 + u * kStep + kHalf < a.H;
+        U d, x, g;
+        d.load(in_d + u * unit_bytes, in0, in1);
+        x.load(in_h + u * unit_bytes, in0, in1);
+        load_gain<U, kOdd>(w, a.offset, c0 + u * kStep, in0, in1, &g);
+#pragma unroll
+        for (int k = 0; k < kPairs; ++k) {
+          const f2 v = mul_f2(d.p[k], mul_f2(x.p[k], rstd2));
+          dw[u][k] = add_f2(dw[u][k], v);
+          acc[k & 1] = fma_f2(v, g.p[k], acc[k & 1]);
+        }
       }
+    };
+    if (a.w_bf16) {
+      if (full) read(std::true_type{}, static_cast<const __nv_bfloat16*>(a.w));
+      else read(std::false_type{}, static_cast<const __nv_bfloat16*>(a.w));
+    } else {
+      if (full) read(std::true_type{}, static_cast<const float*>(a.w));
+      else read(std::false_type{}, static_cast<const float*>(a.w));
+    }
+    const float2 part = split_f2(add_f2(acc[0], acc[1]));
+    const float mean = row_reduce<false>(part.x + part.y, red[turn]) * a.inv_h;
+
+    T* out = static_cast<T*>(a.dx) + row * a.ld_dx + c0;
+    if (kOdd) out = reinterpret_cast<T*>(img + image_of(static_cast<T*>(a.dx), row * a.ld_dx, a.H).off) + c0;
+    const f2 minus2 = make_f2(-rstd * mean, -rstd * mean);
+    const auto write = [&](auto all, auto w) {
+      constexpr bool kFull = decltype(all)::value;
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u) {
+        const bool in0 = kFull || c0 + u * kStep < a.H, in1 = kFull || c0 + u * kStep + kHalf < a.H;
+        U d, x, g;
+        d.load(in_d + u * unit_bytes, in0, in1);
+        x.load(in_h + u * unit_bytes, in0, in1);
+        load_gain<U, kOdd>(w, a.offset, c0 + u * kStep, in0, in1, &g);  // again, from L1: cheaper than its registers
+#pragma unroll
+        for (int k = 0; k < kPairs; ++k) d.p[k] = fma_f2(x.p[k], minus2, mul_f2(d.p[k], g.p[k]));
+        if (a.dh != nullptr) {
+          x.load(in_e + u * unit_bytes, in0, in1);
+#pragma unroll
+          for (int k = 0; k < kPairs; ++k) d.p[k] = fma_f2(d.p[k], rstd2, x.p[k]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < kPairs; ++k) d.p[k] = mul_f2(d.p[k], rstd2);
+        }
+        d.store(out + u * kStep, in0, in1);
+      }
+    };
+    if (a.w_bf16) {
+      if (full) write(std::true_type{}, static_cast<const __nv_bfloat16*>(a.w));
+      else write(std::false_type{}, static_cast<const __nv_bfloat16*>(a.w));
+    } else {
+      if (full) write(std::true_type{}, static_cast<const float*>(a.w));
+      else write(std::false_type{}, static_cast<const float*>(a.w));
+    }
+    if constexpr (kOdd) {
+      __syncthreads();
+      image_store<T>(img, image_of(static_cast<T*>(a.dx), row * a.ld_dx, a.H));
     }
   }
   if (a.partial != nullptr) {
-    float* part = a.partial + (size_t)blockIdx.x * a.H;
+    float* to = a.partial + (size_t)blockIdx.x * a.H + c0;
 #pragma unroll
-    for (int v = 0; v < kV; ++v) {
-      const int c = (v * nt + tid) * kE;
-      if (c < a.H) {
+    for (int u = 0; u < kUnits; ++u) {
 #pragma unroll
-        for (int j = 0; j < kE; ++j) part[c + j] = dw[v][j];
+      for (int k = 0; k < kPairs; ++k) {
+        const float2 v = split_f2(dw[u][k]);
+        const int c = c0 + u * kStep + 2 * k;
+        if (c < a.H) to[u * kStep + 2 * k] = v.x;
+        if (c + (kOdd ? 32 : 1) < a.H) to[u * kStep + 2 * k + (kOdd ? 32 : 1)] = v.y;
       }
     }
   }
@@ -500,54 +768,68 @@ __global__ void __launch_bounds__(256) rmsnorm_dw_kernel(const float* __restrict
 
 int row_threads(int H) { return (H + kRowCols * 32 - 1) / (kRowCols * 32) * 32; }
 
-// CTAs of the backward kernels, and rows of dweight partials: as many as are resident together.
-int bwd_ctas(long long N, int H) {
-  int per_sm = 2;
-  if (H <= kRowMax) {
-    per_sm = 768 / row_threads(H);
-    per_sm = per_sm < 1 ? 1 : (per_sm > 16 ? 16 : per_sm);
-  }
-  return (int)(N < (long long)kSms * per_sm ? N : (long long)kSms * per_sm);
-}
-
-bool aligned(const void* p, long long ld, int bytes, int elem) {
+bool aligned(const void* p, long long ld, int elem, int bytes) {
   return p == nullptr || ((reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0 && (ld * elem) % bytes == 0);
 }
 
-// Bytes of the widest vector that every row of the call allows: 32, 16, or one element.
-int fwd_vector(const NormFwdArgs& a, int elem) {
-  for (int bytes = 32; bytes >= 16; bytes >>= 1) {
-    const int e = bytes / elem;
-    if (a.H % e == 0 && aligned(a.x, a.ld_x, bytes, elem) && aligned(a.res, a.ld_res, bytes, elem) &&
-        aligned(a.h_out, a.ld_h, bytes, elem) && aligned(a.y, a.ld_y, bytes, elem) && aligned(a.y8, a.ld_y8, e, 1) &&
-        aligned(a.w, 0, 16, 1))
-      return bytes;
-  }
-  return elem;
+// How a row kernel is launched.  CTAs per SM: as many as their registers allow and as leave each at least two rows in shared
+// memory; stages: what fits then, 4 at most.
+struct RowPlan {
+  int threads, ctas_per_sm, stages, smem;
+};
+constexpr int kSmemPerSm = 227 * 1024, kSmemCta = 227 * 1024 - 4096;  // (4 KB: the kernels' own arrays and the system's)
+RowPlan plan_rows(int H, int regs, int stage_bytes, int out_bytes) {
+  RowPlan p;
+  p.threads = row_threads(H);
+  int c = 65536 / (regs * p.threads);
+  if (c > 32) c = 32;
+  const int own = 4096;
+  while (c > 1 && c * (2 * stage_bytes + out_bytes + own) > kSmemPerSm) --c;
+  const int s = stage_bytes > 0 ? (kSmemPerSm / c - own - out_bytes) / stage_bytes : 1;
+  p.stages = s > 4 ? 4 : (s < 1 ? 1 : s);
+  p.ctas_per_sm = c;
+  p.smem = p.stages * stage_bytes + out_bytes;
+  return p;
 }
-int bwd_vector(const NormBwdArgs& a, int elem) {
-  for (int bytes = 32; bytes >= 16; bytes >>= 1)
-    if (a.H % (bytes / elem) == 0 && aligned(a.dy, a.ld_dy, bytes, elem) && aligned(a.dh, a.ld_dh, bytes, elem) &&
-        aligned(a.h, a.ld_h, bytes, elem) && aligned(a.dx, a.ld_dx, bytes, elem) && aligned(a.w, 0, 16, 1))
-      return bytes;
-  return elem;
-}
+// CTAs of the backward kernels, and rows of dweight partials; the most that any alignment and type of the rows leads to.
+int bwd_ctas(long long N, int per_sm) { return (int)(N < (long long)kSms * per_sm ? N : (long long)kSms * per_sm); }
+int bwd_ctas_most(long long N, int H) { return bwd_ctas(N, H <= kRowMax ? plan_rows(H, kBwdRegs, 0, 0).ctas_per_sm : 2); }
 
-template <typename T, int kE>
-void launch_fwd_rows(const NormFwdArgs& a, unsigned grid, cudaStream_t st) {
-  const int nt = row_threads(a.H);
-  if (nt <= 256)
-    rmsnorm_fwd_row_kernel<T, kE, kRowCols / kE, 256, 5><<<grid, nt, 0, st>>>(a);
-  else
-    rmsnorm_fwd_row_kernel<T, kE, kRowCols / kE, 1024, 1><<<grid, nt, 0, st>>>(a);
+template <typename K>
+int allow_smem(K kernel, std::atomic<uint64_t>& done) {
+  return mrl_once_per_device(done, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemCta); });
 }
-template <typename T, int kE>
-void launch_bwd_rows(const NormBwdArgs& a, int grid, cudaStream_t st) {
-  const int nt = row_threads(a.H);
-  if (nt <= 256)
-    rmsnorm_bwd_row_kernel<T, kE, kRowCols / kE, 256, 3><<<grid, nt, 0, st>>>(a);
-  else
-    rmsnorm_bwd_row_kernel<T, kE, kRowCols / kE, 1024, 1><<<grid, nt, 0, st>>>(a);
+// -1: the rows do not fit; the looping kernel takes them.
+template <typename T, bool kOdd>
+int launch_fwd_rows(NormFwdArgs a, cudaStream_t st) {
+  const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : row_threads(a.H) * kRowCols * (int)sizeof(T);
+  const int out = kOdd ? ((a.h_out != nullptr) + (a.y != nullptr)) * slot + (a.y8 != nullptr ? image_bytes(a.H, 1) : 0) : 0;
+  const RowPlan p = plan_rows(a.H, kFwdRegs, a.res != nullptr ? 2 * slot : slot, out);
+  if (p.smem > kSmemCta) return -1;
+  a.stages = p.stages;
+  const long long most = (long long)kSms * p.ctas_per_sm;
+  static std::atomic<uint64_t> done;
+  const int rc = allow_smem(rmsnorm_fwd_row_kernel<T, kOdd>, done);
+  if (rc != MRL_OK) return rc;
+  mrl_profile_before(st, "rmsnorm_fwd_row_kernel");
+  rmsnorm_fwd_row_kernel<T, kOdd><<<(unsigned)(a.N < most ? a.N : most), p.threads, p.smem, st>>>(a);
+  mrl_profile_after(st);
+  return cudaGetLastError() == cudaSuccess ? MRL_OK : MRL_ERR_CUDA;
+}
+template <typename T, bool kOdd>
+int launch_bwd_rows(NormBwdArgs a, int* ctas, cudaStream_t st) {
+  const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : row_threads(a.H) * kRowCols * (int)sizeof(T);
+  const RowPlan p = plan_rows(a.H, kBwdRegs, (a.dh != nullptr ? 3 : 2) * slot, kOdd ? slot : 0);
+  if (p.smem > kSmemCta) return -1;
+  a.stages = p.stages;
+  *ctas = bwd_ctas(a.N, p.ctas_per_sm);
+  static std::atomic<uint64_t> done;
+  const int rc = allow_smem(rmsnorm_bwd_row_kernel<T, kOdd>, done);
+  if (rc != MRL_OK) return rc;
+  mrl_profile_before(st, "rmsnorm_bwd_row_kernel");
+  rmsnorm_bwd_row_kernel<T, kOdd><<<*ctas, p.threads, p.smem, st>>>(a);
+  mrl_profile_after(st);
+  return cudaGetLastError() == cudaSuccess ? MRL_OK : MRL_ERR_CUDA;
 }
 
 bool row_type_ok(int32_t dtype) { return dtype == MRL_BF16 || dtype == MRL_F32; }
@@ -556,7 +838,7 @@ bool row_type_ok(int32_t dtype) { return dtype == MRL_BF16 || dtype == MRL_F32; 
 
 size_t mrl_rmsnorm_bwd_workspace_bytes(long long N, int H) {
   if (N <= 0 || H <= 0) return 0;
-  return mrl_align_up((size_t)bwd_ctas(N, H) * (size_t)H * 4, 256);
+  return mrl_align_up((size_t)bwd_ctas_most(N, H) * (size_t)H * 4, 256);
 }
 
 extern "C" int mrl_rmsnorm_residual_fwd(const void* x, int64_t ld_x, const void* residual, int64_t ld_res, int32_t dtype,
@@ -575,26 +857,27 @@ extern "C" int mrl_rmsnorm_residual_fwd(const void* x, int64_t ld_x, const void*
   if (h_out != nullptr && h_out == y) return MRL_ERR_INVALID_ARG;
   if (x == nullptr || weight == nullptr) return MRL_ERR_INVALID_ARG;
   NormFwdArgs a{x, residual, weight, h_out, y, static_cast<uint8_t*>(y8), scales, rstd, ld_x, ld_res, ld_h, ld_y, ld_y8, N,
-                H, np->group, w_dtype == MRL_BF16, np->eps, np->weight_offset, 1.0f / (float)H};
+                H, np->group, w_dtype == MRL_BF16, np->eps, np->weight_offset, 1.0f / (float)H, 0};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const unsigned grid = (unsigned)(N < 0x7fffffffll ? N : 0x7fffffffll);
   const bool bf16 = dtype == MRL_BF16;
+  const int elem = bf16 ? 2 : 4;
+  int rc = -1;
   if (H <= kRowMax) {
-    const int bytes = fwd_vector(a, bf16 ? 2 : 4);
-    mrl_profile_before(st, "rmsnorm_fwd_row_kernel");
-    if (bf16 && bytes == 32) launch_fwd_rows<__nv_bfloat16, 16>(a, grid, st);
-    else if (bf16 && bytes == 16) launch_fwd_rows<__nv_bfloat16, 8>(a, grid, st);
-    else if (bf16) launch_fwd_rows<__nv_bfloat16, 1>(a, grid, st);
-    else if (bytes == 32) launch_fwd_rows<float, 8>(a, grid, st);
-    else if (bytes == 16) launch_fwd_rows<float, 4>(a, grid, st);
-    else launch_fwd_rows<float, 1>(a, grid, st);
-  } else {
-    mrl_profile_before(st, "rmsnorm_fwd_loop_kernel");
+    const bool whole = H % (16 / elem) == 0 && aligned(x, ld_x, elem, 16) && aligned(residual, ld_res, elem, 16) &&
+                       aligned(h_out, ld_h, elem, 16) && aligned(y, ld_y, elem, 16) && aligned(y8, ld_y8, 1, 16 / elem) &&
+                       aligned(weight, 0, 1, 16);
     if (bf16)
-      rmsnorm_fwd_loop_kernel<__nv_bfloat16><<<grid, kLoopThreads, 0, st>>>(a);
+      rc = whole ? launch_fwd_rows<__nv_bfloat16, false>(a, st) : launch_fwd_rows<__nv_bfloat16, true>(a, st);
     else
-      rmsnorm_fwd_loop_kernel<float><<<grid, kLoopThreads, 0, st>>>(a);
+      rc = whole ? launch_fwd_rows<float, false>(a, st) : launch_fwd_rows<float, true>(a, st);
   }
+  if (rc >= 0) return rc;
+  const unsigned grid = (unsigned)(N < 0x7fffffffll ? N : 0x7fffffffll);
+  mrl_profile_before(st, "rmsnorm_fwd_loop_kernel");
+  if (bf16)
+    rmsnorm_fwd_loop_kernel<__nv_bfloat16><<<grid, kLoopThreads, 0, st>>>(a);
+  else
+    rmsnorm_fwd_loop_kernel<float><<<grid, kLoopThreads, 0, st>>>(a);
   mrl_profile_after(st);
   return cudaGetLastError() == cudaSuccess ? MRL_OK : MRL_ERR_CUDA;
 }
@@ -619,30 +902,32 @@ extern "C" int mrl_rmsnorm_residual_bwd(const void* dy, int64_t ld_dy, const voi
     if (workspace == nullptr || workspace_bytes < mrl_rmsnorm_bwd_workspace_bytes(N, H)) return MRL_ERR_WORKSPACE_TOO_SMALL;
     if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return MRL_ERR_INVALID_ARG;
   }
-  const int grid = bwd_ctas(N, H);
   NormBwdArgs a{dy, dh, h, weight, rstd, dx, dweight != nullptr ? static_cast<float*>(workspace) : nullptr, ld_dy, ld_dh,
-                ld_h, ld_dx, N, H, w_dtype == MRL_BF16, np->weight_offset, 1.0f / (float)H};
+                ld_h, ld_dx, N, H, w_dtype == MRL_BF16, np->weight_offset, 1.0f / (float)H, 0};
   const bool bf16 = dtype == MRL_BF16;
+  const int elem = bf16 ? 2 : 4;
+  int rc = -1, ctas = 0;
   if (H <= kRowMax) {
-    const int bytes = bwd_vector(a, bf16 ? 2 : 4);
-    mrl_profile_before(st, "rmsnorm_bwd_row_kernel");
-    if (bf16 && bytes == 32) launch_bwd_rows<__nv_bfloat16, 16>(a, grid, st);
-    else if (bf16 && bytes == 16) launch_bwd_rows<__nv_bfloat16, 8>(a, grid, st);
-    else if (bf16) launch_bwd_rows<__nv_bfloat16, 1>(a, grid, st);
-    else if (bytes == 32) launch_bwd_rows<float, 8>(a, grid, st);
-    else if (bytes == 16) launch_bwd_rows<float, 4>(a, grid, st);
-    else launch_bwd_rows<float, 1>(a, grid, st);
-  } else {
+    const bool whole = H % (16 / elem) == 0 && aligned(dy, ld_dy, elem, 16) && aligned(dh, ld_dh, elem, 16) &&
+                       aligned(h, ld_h, elem, 16) && aligned(dx, ld_dx, elem, 16) && aligned(weight, 0, 1, 16);
+    if (bf16)
+      rc = whole ? launch_bwd_rows<__nv_bfloat16, false>(a, &ctas, st) : launch_bwd_rows<__nv_bfloat16, true>(a, &ctas, st);
+    else
+      rc = whole ? launch_bwd_rows<float, false>(a, &ctas, st) : launch_bwd_rows<float, true>(a, &ctas, st);
+  }
+  if (rc < 0) {
+    ctas = bwd_ctas_most(N, H);
     mrl_profile_before(st, "rmsnorm_bwd_loop_kernel");
     if (bf16)
-      rmsnorm_bwd_loop_kernel<__nv_bfloat16><<<grid, kLoopThreads, 0, st>>>(a);
+      rmsnorm_bwd_loop_kernel<__nv_bfloat16><<<ctas, kLoopThreads, 0, st>>>(a);
     else
-      rmsnorm_bwd_loop_kernel<float><<<grid, kLoopThreads, 0, st>>>(a);
+      rmsnorm_bwd_loop_kernel<float><<<ctas, kLoopThreads, 0, st>>>(a);
+    mrl_profile_after(st);
+    rc = cudaGetLastError() == cudaSuccess ? MRL_OK : MRL_ERR_CUDA;
   }
-  mrl_profile_after(st);
-  MRL_CUDA_OK(cudaGetLastError());
+  if (rc != MRL_OK) return rc;
   if (dweight != nullptr) {
-    rmsnorm_dw_kernel<<<(H + 31) / 32, 256, 0, st>>>(a.partial, grid, H, dweight, accumulate);
+    rmsnorm_dw_kernel<<<(H + 31) / 32, 256, 0, st>>>(a.partial, ctas, H, dweight, accumulate);
     MRL_CUDA_OK(cudaGetLastError());
   }
   return MRL_OK;
