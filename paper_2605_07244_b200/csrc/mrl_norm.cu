@@ -14,8 +14,8 @@ using namespace mrl;
 
 constexpr int kSms = 148;
 constexpr int kLoopThreads = 512;
-constexpr int kRowCols = 32;                       // columns a thread holds in registers
-constexpr int kRowMax = kRowCols * 512;            // the widest row that one CTA holds
+constexpr int kWide = 32, kNarrow = 8;              // columns of a thread of the row kernels
+constexpr int kRowMax = kWide * 512;               // the widest row that one CTA holds
 constexpr int kFwdRegs = 64, kBwdRegs = 80;        // registers of a thread of the row kernels
 
 template <typename T>
@@ -199,7 +199,6 @@ struct Unit {
   static constexpr int kCols = kOdd ? 2 : 16 / (int)sizeof(T);  // columns
   static constexpr int kPairs = kCols / 2;
   static constexpr int kStep = 32 * kCols;                      // columns of a warp
-  static constexpr int kUnits = kRowCols / kCols;               // per thread and row
   f2 p[kPairs];
 
   __device__ __forceinline__ void zero() {
@@ -373,6 +372,12 @@ __device__ __forceinline__ float row_reduce(float v, float* red) {
   return kMax ? fmaxf(fmaxf(s.x, s.y), fmaxf(s.z, s.w)) : (s.x + s.y) + (s.z + s.w);
 }
 
+// Copies of a row that a stage holds.
+__host__ __device__ __forceinline__ int fwd_slots(const NormFwdArgs& a, bool odd) {
+  const int in = 1 + (a.res != nullptr), out = (a.h_out != nullptr) + (a.y != nullptr);
+  return odd && out > in ? out : in;
+}
+
 // Rows of up to kRowMax columns, each read once and written once.  A CTA walks rows blockIdx.x, + gridDim.x, ...; the rows to
 // come are under way into shared memory (`stages` of them, 16-byte asynchronous copies), so the bytes in flight do not
 // depend on registers.  kOdd = false: rows of 16-byte granules; a thread copies the granules whose columns it works on
@@ -380,10 +385,10 @@ __device__ __forceinline__ float row_reduce(float v, float* red) {
 // column after a barrier, and outputs go the same way back.
 // Columns: a warp owns 32 * kRowCols adjacent ones, unit u of a lane lies u * kStep behind its first.  A warp whose columns
 // all lie inside the row runs without tests (kFull).
-template <typename T, bool kOdd>
+template <typename T, bool kOdd, int kRowCols>
 __global__ void __maxnreg__(kFwdRegs) rmsnorm_fwd_row_kernel(const __grid_constant__ NormFwdArgs a) {
   using U = Unit<T, kOdd>;
-  constexpr int kUnits = U::kUnits, kStep = U::kStep, kPairs = U::kPairs, kHalf = kOdd ? 32 : 0;
+  constexpr int kUnits = kRowCols / U::kCols, kStep = U::kStep, kPairs = U::kPairs, kHalf = kOdd ? 32 : 0;
   extern __shared__ __align__(16) char smem[];
   __shared__ __align__(16) float red[2][4][16];
   __shared__ uint32_t peak[kRowMax / 32];
@@ -391,10 +396,8 @@ __global__ void __maxnreg__(kFwdRegs) rmsnorm_fwd_row_kernel(const __grid_consta
   const int c0 = (tid >> 5) * (kUnits * kStep) + (tid & 31) * (kOdd ? 1 : U::kCols);
   const bool full = ((tid >> 5) + 1) * (kUnits * kStep) <= a.H;
   const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : nt * kRowCols * (int)sizeof(T);
-  const int stage = a.res != nullptr ? 2 * slot : slot;
-  char* img_h = smem + a.stages * stage;
-  char* img_y = img_h + (a.h_out != nullptr ? slot : 0);
-  char* img_q = img_y + (a.y != nullptr ? slot : 0);
+  const int stage = fwd_slots(a, kOdd) * slot;
+  char* img_q = smem + a.stages * stage;
   const int group = a.group > 0 ? a.group : a.H, groups = (a.H + group - 1) / group;
   // lanes whose columns share a scale sit side by side; more than a warp of them meet in shared memory
   const bool meet = a.y8 != nullptr && a.group > (kOdd ? 32 : kStep);
@@ -429,10 +432,21 @@ __global__ void __maxnreg__(kFwdRegs) rmsnorm_fwd_row_kernel(const __grid_consta
   for (int s = 0; s + 1 < a.stages; ++s) fetch(blockIdx.x + (long long)s * gridDim.x, s);
   int s = 0, turn = 0;
   for (long long row = blockIdx.x; row < a.N; row += gridDim.x, turn ^= 1) {
-    fetch(row + (long long)(a.stages - 1) * gridDim.x, s == 0 ? a.stages - 1 : s - 1);
-    copy_wait(a.stages - 1);
-    if (kOdd) __syncthreads();
-    const char* in_x = smem + s * stage + (kOdd ? c0 * (int)sizeof(T) : tid * 16);
+    if (kOdd) {
+      // the copies of this row are there for all, and those of the last row, outputs by now, have been read
+      if (a.stages > 1) copy_wait(a.stages - 2);
+      __syncthreads();
+      fetch(row + (long long)(a.stages - 1) * gridDim.x, s == 0 ? a.stages - 1 : s - 1);
+      if (a.stages == 1) {
+        copy_wait(0);
+        __syncthreads();
+      }
+    } else {
+      fetch(row + (long long)(a.stages - 1) * gridDim.x, s == 0 ? a.stages - 1 : s - 1);
+      copy_wait(a.stages - 1);
+    }
+    char* here = smem + s * stage;
+    const char* in_x = here + (kOdd ? c0 * (int)sizeof(T) : tid * 16);
     const char* in_r = in_x + slot;
     if (kOdd) {
       in_x += image_of(static_cast<const T*>(a.x), row * a.ld_x, a.H).off;
@@ -489,11 +503,12 @@ __global__ void __maxnreg__(kFwdRegs) rmsnorm_fwd_row_kernel(const __grid_consta
     if (tid == 0 && a.rstd != nullptr) a.rstd[row] = rstd;
 
     const f2 rstd2 = make_f2(rstd, rstd);
+    const int y_at = a.h_out != nullptr ? slot : 0;  // odd rows: outputs take the place of the row's inputs, which have all been read
     T* to_h = static_cast<T*>(a.h_out) + row * a.ld_h + c0;
     T* to_y = static_cast<T*>(a.y) + row * a.ld_y + c0;
     if (kOdd) {
-      to_h = reinterpret_cast<T*>(img_h + image_of(static_cast<T*>(a.h_out), row * a.ld_h, a.H).off) + c0;
-      to_y = reinterpret_cast<T*>(img_y + image_of(static_cast<T*>(a.y), row * a.ld_y, a.H).off) + c0;
+      to_h = reinterpret_cast<T*>(here + image_of(static_cast<T*>(a.h_out), row * a.ld_h, a.H).off) + c0;
+      to_y = reinterpret_cast<T*>(here + y_at + image_of(static_cast<T*>(a.y), row * a.ld_y, a.H).off) + c0;
     }
     const auto write = [&](auto all, auto w) {
       constexpr bool kFull = decltype(all)::value;
@@ -599,8 +614,8 @@ __global__ void __maxnreg__(kFwdRegs) rmsnorm_fwd_row_kernel(const __grid_consta
     }
     if constexpr (kOdd) {
       __syncthreads();
-      if (a.h_out != nullptr) image_store<T>(img_h, image_of(static_cast<T*>(a.h_out), row * a.ld_h, a.H));
-      if (a.y != nullptr) image_store<T>(img_y, image_of(static_cast<T*>(a.y), row * a.ld_y, a.H));
+      if (a.h_out != nullptr) image_store<T>(here, image_of(static_cast<T*>(a.h_out), row * a.ld_h, a.H));
+      if (a.y != nullptr) image_store<T>(here + y_at, image_of(static_cast<T*>(a.y), row * a.ld_y, a.H));
       if (a.y8 != nullptr) image_store<uint8_t>(img_q, image_of(a.y8, row * a.ld_y8, a.H));
     } else if (meet) {
       __syncthreads();  // the next row clears the peaks
@@ -610,10 +625,10 @@ __global__ void __maxnreg__(kFwdRegs) rmsnorm_fwd_row_kernel(const __grid_consta
 
 // Backward, with rows on their way as above.  Each thread keeps the dweight sums of its columns in registers over all of
 // the CTA's rows and writes them once; what a row needs after its sum is read from shared memory again.
-template <typename T, bool kOdd>
+template <typename T, bool kOdd, int kRowCols>
 __global__ void __maxnreg__(kBwdRegs) rmsnorm_bwd_row_kernel(const __grid_constant__ NormBwdArgs a) {
   using U = Unit<T, kOdd>;
-  constexpr int kUnits = U::kUnits, kStep = U::kStep, kPairs = U::kPairs, kHalf = kOdd ? 32 : 0;
+  constexpr int kUnits = kRowCols / U::kCols, kStep = U::kStep, kPairs = U::kPairs, kHalf = kOdd ? 32 : 0;
   extern __shared__ __align__(16) char smem[];
   __shared__ __align__(16) float red[2][16];
   const int tid = threadIdx.x, nt = blockDim.x;
@@ -621,7 +636,6 @@ __global__ void __maxnreg__(kBwdRegs) rmsnorm_bwd_row_kernel(const __grid_consta
   const bool full = ((tid >> 5) + 1) * (kUnits * kStep) <= a.H;
   const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : nt * kRowCols * (int)sizeof(T);
   const int stage = a.dh != nullptr ? 3 * slot : 2 * slot;
-  char* img = smem + a.stages * stage;
   if (tid < 32) (&red[0][0])[tid] = 0.f;
   __syncthreads();
 
@@ -655,10 +669,20 @@ __global__ void __maxnreg__(kBwdRegs) rmsnorm_bwd_row_kernel(const __grid_consta
   for (int s = 0; s + 1 < a.stages; ++s) fetch(blockIdx.x + (long long)s * gridDim.x, s);
   int s = 0, turn = 0;
   for (long long row = blockIdx.x; row < a.N; row += gridDim.x, turn ^= 1) {
-    fetch(row + (long long)(a.stages - 1) * gridDim.x, s == 0 ? a.stages - 1 : s - 1);
     const float rstd = a.rstd[row];
-    copy_wait(a.stages - 1);
-    if (kOdd) __syncthreads();
+    if (kOdd) {  // as in the forward kernel
+      if (a.stages > 1) copy_wait(a.stages - 2);
+      __syncthreads();
+      fetch(row + (long long)(a.stages - 1) * gridDim.x, s == 0 ? a.stages - 1 : s - 1);
+      if (a.stages == 1) {
+        copy_wait(0);
+        __syncthreads();
+      }
+    } else {
+      fetch(row + (long long)(a.stages - 1) * gridDim.x, s == 0 ? a.stages - 1 : s - 1);
+      copy_wait(a.stages - 1);
+    }
+    char* img = smem + a.stages * stage;
     const char* in_d = smem + s * stage + (kOdd ? c0 * (int)sizeof(T) : tid * 16);
     const char *in_h = in_d + slot, *in_e = in_h + slot;
     if (kOdd) {
@@ -766,7 +790,9 @@ __global__ void __launch_bounds__(256) rmsnorm_dw_kernel(const float* __restrict
   }
 }
 
-int row_threads(int H) { return (H + kRowCols * 32 - 1) / (kRowCols * 32) * 32; }
+int row_threads(int H, int cols) { return (H + cols * 32 - 1) / (cols * 32) * 32; }
+// Few rows, or short ones, are spread over more threads.
+int row_cols(long long N, int H) { return H <= 512 || (H <= 512 * kNarrow && N <= 2 * kSms) ? kNarrow : kWide; }
 
 bool aligned(const void* p, long long ld, int elem, int bytes) {
   return p == nullptr || ((reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0 && (ld * elem) % bytes == 0);
@@ -778,9 +804,9 @@ struct RowPlan {
   int threads, ctas_per_sm, stages, smem;
 };
 constexpr int kSmemPerSm = 227 * 1024, kSmemCta = 227 * 1024 - 4096;  // (4 KB: the kernels' own arrays and the system's)
-RowPlan plan_rows(int H, int regs, int stage_bytes, int out_bytes) {
+RowPlan plan_rows(int threads, int regs, int stage_bytes, int out_bytes) {
   RowPlan p;
-  p.threads = row_threads(H);
+  p.threads = threads;
   int c = 65536 / (regs * p.threads);
   if (c > 32) c = 32;
   const int own = 4096;
@@ -793,43 +819,55 @@ RowPlan plan_rows(int H, int regs, int stage_bytes, int out_bytes) {
 }
 // CTAs of the backward kernels, and rows of dweight partials; the most that any alignment and type of the rows leads to.
 int bwd_ctas(long long N, int per_sm) { return (int)(N < (long long)kSms * per_sm ? N : (long long)kSms * per_sm); }
-int bwd_ctas_most(long long N, int H) { return bwd_ctas(N, H <= kRowMax ? plan_rows(H, kBwdRegs, 0, 0).ctas_per_sm : 2); }
+int bwd_ctas_most(long long N, int H) { return bwd_ctas(N, H <= kRowMax ? plan_rows(row_threads(H, kWide), kBwdRegs, 0, 0).ctas_per_sm : 2); }
 
 template <typename K>
 int allow_smem(K kernel, std::atomic<uint64_t>& done) {
   return mrl_once_per_device(done, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemCta); });
 }
 // -1: the rows do not fit; the looping kernel takes them.
-template <typename T, bool kOdd>
+template <typename T, bool kOdd, int kCols>
 int launch_fwd_rows(NormFwdArgs a, cudaStream_t st) {
-  const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : row_threads(a.H) * kRowCols * (int)sizeof(T);
-  const int out = kOdd ? ((a.h_out != nullptr) + (a.y != nullptr)) * slot + (a.y8 != nullptr ? image_bytes(a.H, 1) : 0) : 0;
-  const RowPlan p = plan_rows(a.H, kFwdRegs, a.res != nullptr ? 2 * slot : slot, out);
+  const int threads = row_threads(a.H, kCols);
+  const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : threads * kCols * (int)sizeof(T);
+  const RowPlan p = plan_rows(threads, kFwdRegs, fwd_slots(a, kOdd) * slot, kOdd && a.y8 != nullptr ? image_bytes(a.H, 1) : 0);
   if (p.smem > kSmemCta) return -1;
   a.stages = p.stages;
   const long long most = (long long)kSms * p.ctas_per_sm;
   static std::atomic<uint64_t> done;
-  const int rc = allow_smem(rmsnorm_fwd_row_kernel<T, kOdd>, done);
+  const int rc = allow_smem(rmsnorm_fwd_row_kernel<T, kOdd, kCols>, done);
   if (rc != MRL_OK) return rc;
   mrl_profile_before(st, "rmsnorm_fwd_row_kernel");
-  rmsnorm_fwd_row_kernel<T, kOdd><<<(unsigned)(a.N < most ? a.N : most), p.threads, p.smem, st>>>(a);
+  rmsnorm_fwd_row_kernel<T, kOdd, kCols><<<(unsigned)(a.N < most ? a.N : most), p.threads, p.smem, st>>>(a);
   mrl_profile_after(st);
   return cudaGetLastError() == cudaSuccess ? MRL_OK : MRL_ERR_CUDA;
 }
-template <typename T, bool kOdd>
+template <typename T, bool kOdd, int kCols>
 int launch_bwd_rows(NormBwdArgs a, int* ctas, cudaStream_t st) {
-  const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : row_threads(a.H) * kRowCols * (int)sizeof(T);
-  const RowPlan p = plan_rows(a.H, kBwdRegs, (a.dh != nullptr ? 3 : 2) * slot, kOdd ? slot : 0);
+  const int threads = row_threads(a.H, kCols);
+  const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : threads * kCols * (int)sizeof(T);
+  const RowPlan p = plan_rows(threads, kBwdRegs, (a.dh != nullptr ? 3 : 2) * slot, kOdd ? slot : 0);
   if (p.smem > kSmemCta) return -1;
   a.stages = p.stages;
   *ctas = bwd_ctas(a.N, p.ctas_per_sm);
   static std::atomic<uint64_t> done;
-  const int rc = allow_smem(rmsnorm_bwd_row_kernel<T, kOdd>, done);
+  const int rc = allow_smem(rmsnorm_bwd_row_kernel<T, kOdd, kCols>, done);
   if (rc != MRL_OK) return rc;
   mrl_profile_before(st, "rmsnorm_bwd_row_kernel");
-  rmsnorm_bwd_row_kernel<T, kOdd><<<*ctas, p.threads, p.smem, st>>>(a);
+  rmsnorm_bwd_row_kernel<T, kOdd, kCols><<<*ctas, p.threads, p.smem, st>>>(a);
   mrl_profile_after(st);
   return cudaGetLastError() == cudaSuccess ? MRL_OK : MRL_ERR_CUDA;
+}
+template <typename T>
+int launch_fwd(const NormFwdArgs& a, bool odd, cudaStream_t st) {
+  if (row_cols(a.N, a.H) == kNarrow) return odd ? launch_fwd_rows<T, true, kNarrow>(a, st) : launch_fwd_rows<T, false, kNarrow>(a, st);
+  return odd ? launch_fwd_rows<T, true, kWide>(a, st) : launch_fwd_rows<T, false, kWide>(a, st);
+}
+template <typename T>
+int launch_bwd(const NormBwdArgs& a, bool odd, int* ctas, cudaStream_t st) {
+  if (row_cols(a.N, a.H) == kNarrow)
+    return odd ? launch_bwd_rows<T, true, kNarrow>(a, ctas, st) : launch_bwd_rows<T, false, kNarrow>(a, ctas, st);
+  return odd ? launch_bwd_rows<T, true, kWide>(a, ctas, st) : launch_bwd_rows<T, false, kWide>(a, ctas, st);
 }
 
 bool row_type_ok(int32_t dtype) { return dtype == MRL_BF16 || dtype == MRL_F32; }
@@ -866,10 +904,7 @@ extern "C" int mrl_rmsnorm_residual_fwd(const void* x, int64_t ld_x, const void*
     const bool whole = H % (16 / elem) == 0 && aligned(x, ld_x, elem, 16) && aligned(residual, ld_res, elem, 16) &&
                        aligned(h_out, ld_h, elem, 16) && aligned(y, ld_y, elem, 16) && aligned(y8, ld_y8, 1, 16 / elem) &&
                        aligned(weight, 0, 1, 16);
-    if (bf16)
-      rc = whole ? launch_fwd_rows<__nv_bfloat16, false>(a, st) : launch_fwd_rows<__nv_bfloat16, true>(a, st);
-    else
-      rc = whole ? launch_fwd_rows<float, false>(a, st) : launch_fwd_rows<float, true>(a, st);
+    rc = bf16 ? launch_fwd<__nv_bfloat16>(a, !whole, st) : launch_fwd<float>(a, !whole, st);
   }
   if (rc >= 0) return rc;
   const unsigned grid = (unsigned)(N < 0x7fffffffll ? N : 0x7fffffffll);
@@ -910,10 +945,7 @@ extern "C" int mrl_rmsnorm_residual_bwd(const void* dy, int64_t ld_dy, const voi
   if (H <= kRowMax) {
     const bool whole = H % (16 / elem) == 0 && aligned(dy, ld_dy, elem, 16) && aligned(dh, ld_dh, elem, 16) &&
                        aligned(h, ld_h, elem, 16) && aligned(dx, ld_dx, elem, 16) && aligned(weight, 0, 1, 16);
-    if (bf16)
-      rc = whole ? launch_bwd_rows<__nv_bfloat16, false>(a, &ctas, st) : launch_bwd_rows<__nv_bfloat16, true>(a, &ctas, st);
-    else
-      rc = whole ? launch_bwd_rows<float, false>(a, &ctas, st) : launch_bwd_rows<float, true>(a, &ctas, st);
+    rc = bf16 ? launch_bwd<__nv_bfloat16>(a, !whole, &ctas, st) : launch_bwd<float>(a, !whole, &ctas, st);
   }
   if (rc < 0) {
     ctas = bwd_ctas_most(N, H);
