@@ -126,6 +126,40 @@ __device__ __forceinline__ float2 unpack_e4m3x2(uint16_t codes) {
 // The scale of a group of e4m3 codes: its largest magnitude lands on 448.  Not below 2^-126, so that 1 / scale is finite.
 __device__ __forceinline__ float e4m3_scale(float amax) { return fmaxf(amax / 448.0f, 1.17549435e-38f); }
 
+// Two floats in a register pair: Blackwell adds, multiplies and fuses them with one instruction (kernels that stream with
+// little arithmetic per byte still issue enough of it for this to show).
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 make_f2(float lo, float hi) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 split_f2(f2 v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ f2 add_f2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 mul_f2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 fma_f2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f2 bf16x2_to_f2(uint32_t w) { return make_f2(bf16lo_to_f32(w), bf16hi_to_f32(w)); }
+__device__ __forceinline__ uint32_t f2_to_bf16x2(f2 v) {
+  const float2 u = split_f2(v);
+  return pack_bf16x2(u.x, u.y);
+}
+
 // SplitMix64 output function (Steele, Lea, Flood 2014).
 __host__ __device__ __forceinline__ uint64_t splitmix64(uint64_t x) {
   x += 0x9E3779B97F4A7C15ull;

@@ -65,6 +65,31 @@ __device__ __forceinline__ float sqrt_approx(float x) {
   return y;
 }
 
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+constexpr float kRootMin = 1e-25f, kRootMax = 1e37f;  // where newton_root holds: s^2 and the residual stay normal
+
+__device__ __forceinline__ f2 newton_root(f2 v) {
+  const float2 u = split_f2(v);
+  float a, b;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(u.x));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(u.y));
+  const f2 y = make_f2(a, b), s = mul_f2(v, y), half = mul_f2(y, make_f2(-0.5f, -0.5f));
+  return fma_f2(fma_f2(s, s, v ^ 0x8000000080000000ull), half, s);  // s + (v - s^2) / (2 s), the signs moved together
+}
+__device__ __forceinline__ float newton_over_448(float x) {
+  const float c = 1.0f / 448.0f, q = x * c;
+  return fmaf(fmaf(-448.0f, q, x), c, q);
+}
+__device__ __forceinline__ float newton_reciprocal(float x) {
+  const float y = rcp_approx(x);
+  return fmaf(y, fmaf(-x, y, 1.0f), y);
+}
+
 __device__ __forceinline__ double block_sum(double v, double* red) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -118,55 +143,50 @@ struct AdamwArgs {
   bool seeded;
 };
 
-// ---- eight adjacent elements of a lane; a warp works on the 256 that share the scales of an 8-bit state
+// ---- eight adjacent elements of a lane, as four pairs; a warp works on the 256 that share the scales of an 8-bit state
 
-// kN = 8 elements: whole (one or two wide accesses) where `vec`, else one by one below n.
+// Whole (one or two wide accesses) where `vec`, else one by one below n and 0 from there.
 template <typename T>
-__device__ __forceinline__ void load8(const void* base, long long i, int n, bool vec, float (&x)[8]) {
+__device__ __forceinline__ void load8(const void* base, long long i, int n, bool vec, f2 (&x)[4]) {
   const T* p = static_cast<const T*>(base) + i;
   if (vec) {
     if constexpr (sizeof(T) == 4) {
-      uint32_t w[8];
-      asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
-                   : "l"(p));
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(w[j]);
+      asm volatile("ld.global.L1::no_allocate.v4.b64 {%0, %1, %2, %3}, [%4];" : "=l"(x[0]), "=l"(x[1]), "=l"(x[2]), "=l"(x[3]) : "l"(p));
     } else {
       uint32_t w[4];
       asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        x[2 * j] = bf16lo_to_f32(w[j]);
-        x[2 * j + 1] = bf16hi_to_f32(w[j]);
-      }
+      for (int j = 0; j < 4; ++j) x[j] = bf16x2_to_f2(w[j]);
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      x[j] = 0.f;
-      if (j < n) {
-        if constexpr (sizeof(T) == 4) x[j] = p[j]; else x[j] = __bfloat162float(p[j]);
-      }
+    for (int j = 0; j < 4; ++j) {
+      float u[2] = {0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if (2 * j + k < n) {
+          if constexpr (sizeof(T) == 4) u[k] = p[2 * j + k]; else u[k] = __bfloat162float(p[2 * j + k]);
+        }
+      x[j] = make_f2(u[0], u[1]);
     }
   }
 }
-__device__ __forceinline__ void store8(float* base, long long i, int n, bool vec, const float (&x)[8]) {
-  float* p = base + i;
+__device__ __forceinline__ void store8(void* base, long long i, int n, bool vec, const f2 (&x)[4]) {
+  float* p = static_cast<float*>(base) + i;
   if (vec) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(__float_as_uint(x[0])),
-                 "r"(__float_as_uint(x[1])), "r"(__float_as_uint(x[2])), "r"(__float_as_uint(x[3])), "r"(__float_as_uint(x[4])),
-                 "r"(__float_as_uint(x[5])), "r"(__float_as_uint(x[6])), "r"(__float_as_uint(x[7]))
-                 : "memory");
+    asm volatile("st.global.v4.b64 [%0], {%1, %2, %3, %4};" ::"l"(p), "l"(x[0]), "l"(x[1]), "l"(x[2]), "l"(x[3]) : "memory");
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < n) p[j] = x[j];
+    for (int j = 0; j < 4; ++j) {
+      const float2 u = split_f2(x[j]);
+      if (2 * j < n) p[2 * j] = u.x;
+      if (2 * j + 1 < n) p[2 * j + 1] = u.y;
+    }
   }
 }
 // words of two bf16 each
-__device__ __forceinline__ void store8(__nv_bfloat16* base, long long i, int n, bool vec, const uint32_t (&w)[4]) {
-  uint16_t* p = reinterpret_cast<uint16_t*>(base) + i;
+__device__ __forceinline__ void store8_bf16(void* base, long long i, int n, bool vec, const uint32_t (&w)[4]) {
+  uint16_t* p = static_cast<uint16_t*>(base) + i;
   if (vec) {
     *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
   } else {
@@ -194,42 +214,216 @@ __device__ __forceinline__ void store_codes(void* base, long long i, int n, bool
       if (j < n) p[j] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
   }
 }
-__device__ __forceinline__ void decode(uint2 codes, float scale, float (&x)[8]) {
+__device__ __forceinline__ void decode(uint2 codes, float scale, f2 (&x)[4]) {
+  const f2 s2 = make_f2(scale, scale);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const float2 u = unpack_e4m3x2((uint16_t)((j < 2 ? codes.x : codes.y) >> (16 * (j & 1))));
-    x[2 * j] = __fmul_rn(u.x, scale);
-    x[2 * j + 1] = __fmul_rn(u.y, scale);
+    x[j] = mul_f2(make_f2(u.x, u.y), s2);
   }
 }
 
-// |y| (at most about 448) with the part below an e4m3 step rounded up with probability remainder / step: the 16 bits are
-// added below the last kept bit and the rest is cut.  Below 2^-6 the codes are 2^-9 apart, as they are from 2^-6 to 2^-5: the
-// value is moved there and back.  y that is not finite comes back as it is.
-__device__ __forceinline__ float e4m3_dither(float y, uint32_t bits16) {
-  const float a = fabsf(y);
-  const bool small = a < 0.015625f;
-  const float up = small ? 0.015625f : 0.f;
-  const float z = __uint_as_float((__float_as_uint(a + up) + (bits16 << 4)) & 0xfff00000u) - up;
-  return a < INFINITY ? copysignf(z, y) : y;
-}
-// Codes of eight values at most 448 / inv in magnitude.  kFloor: what is above zero stays above zero.
-template <bool kFloor>
-__device__ __forceinline__ void encode(const float (&x)[8], float inv, bool seeded, const uint32_t (&bits)[8], int shift, uint32_t (&codes)[2]) {
-  codes[0] = codes[1] = 0;
+// IEEE square roots of eight values: v * rsqrt(v), brought to the nearest float by one Newton step on the fused residual
+// v - s^2 (Markstein 1990; equal to sqrtf for every float in its range, see the tests).  Values near zero, where the
+// residual would leave float32, and infinities go through sqrtf.
+__device__ __forceinline__ void root8(const f2 (&v)[4], f2 (&root)[4]) {
+  float lo = INFINITY, hi = 0.f;
 #pragma unroll
-  for (int j = 0; j < 8; j += 2) {
-    float a = __fmul_rn(x[j], inv), b = __fmul_rn(x[j + 1], inv);
-    if (seeded) {
-      a = e4m3_dither(a, (bits[j] >> shift) & 0xffffu);
-      b = e4m3_dither(b, (bits[j + 1] >> shift) & 0xffffu);
+  for (int j = 0; j < 4; ++j) {
+    const float2 u = split_f2(v[j]);
+    lo = fminf(lo, fminf(u.x, u.y));
+    hi = fmaxf(hi, fmaxf(u.x, u.y));
+    root[j] = newton_root(v[j]);
+  }
+  if (!(lo >= kRootMin && hi <= kRootMax)) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 u = split_f2(v[j]);
+      root[j] = make_f2(__fsqrt_rn(u.x), __fsqrt_rn(u.y));
     }
-    uint32_t c = pack_e4m3x2(a, b);
-    if (kFloor) {
-      if ((c & 0xffu) == 0 && x[j] > 0.f) c |= 1u;
-      if ((c & 0xff00u) == 0 && x[j + 1] > 0.f) c |= 0x100u;
+  }
+}
+// The scale of a block and its reciprocal as IEEE quotients, corrected on their fused residuals the same way.
+__device__ __forceinline__ void block_scale(float amax, float* scale, float* inv) {
+  *scale = newton_over_448(amax);
+  *inv = newton_reciprocal(*scale);
+  if (!(amax >= 1e-30f && amax <= 1e30f)) {
+    *scale = e4m3_scale(amax);
+    *inv = __frcp_rn(*scale);
+  }
+}
+
+// |y| (at most about 448, not NaN) with the part below an e4m3 step rounded up with probability remainder / step: the 16
+// bits are added below the last kept bit and the rest is cut.  Below 2^-6 the codes are 2^-9 apart, as they are from 2^-6
+// to 2^-5: the value is moved there and back.
+__device__ __forceinline__ float e4m3_dither(float y, uint32_t bits16) {
+  const float up = fabsf(y) < 0.015625f ? 0.015625f : 0.f;
+  return copysignf(__uint_as_float((__float_as_uint(fabsf(y) + up) + (bits16 << 4)) & 0xfff00000u) - up, y);
+}
+// the same from 2^-6 on
+__device__ __forceinline__ float e4m3_dither_normal(float y, uint32_t bits16) {
+  return __uint_as_float((__float_as_uint(y) + (bits16 << 4)) & 0xfff00000u);
+}
+// Codes of x / scale, |x| at most 448 scale.  bits: 16 of each element, the lower ones for the first moment, the upper ones
+// for the (root of the) second, of which a value above zero keeps a code above zero.
+template <bool kSecond>
+__device__ __forceinline__ void encode(const f2 (&x)[4], float inv, bool seeded, const uint32_t (&bits)[8], uint32_t (&codes)[2]) {
+  const f2 inv2 = make_f2(inv, inv);
+  f2 y[4];
+  float least = INFINITY;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    y[j] = mul_f2(x[j], inv2);
+    const float2 u = split_f2(y[j]);
+    least = fminf(least, fminf(fabsf(u.x), fabsf(u.y)));
+  }
+  const auto bits16 = [&](int j) { return kSecond ? bits[j] >> 16 : bits[j] & 0xffffu; };
+  codes[0] = codes[1] = 0;
+  if (seeded && least >= 0.015625f) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 u = split_f2(y[j]);
+      codes[j >> 1] |= pack_e4m3x2(e4m3_dither_normal(u.x, bits16(2 * j)), e4m3_dither_normal(u.y, bits16(2 * j + 1))) << (16 * (j & 1));
     }
-    codes[j >> 2] |= c << (8 * (j & 3));
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 u = split_f2(y[j]);
+    const float a = seeded ? e4m3_dither(u.x, bits16(2 * j)) : u.x, b = seeded ? e4m3_dither(u.y, bits16(2 * j + 1)) : u.y;
+    codes[j >> 1] |= pack_e4m3x2(a, b) << (16 * (j & 1));
+  }
+  if (kSecond && least < 0.001953125f) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float2 u = split_f2(x[j >> 1]);
+      if (((codes[j >> 2] >> (8 * (j & 3))) & 0xffu) == 0 && (j & 1 ? u.y : u.x) > 0.f) codes[j >> 2] |= 1u << (8 * (j & 3));
+    }
+  }
+}
+
+// One block of MRL_STATE_BLOCK elements by a warp.  The moments are rounded operation by operation as the formula stands
+// (no fused multiply-add) and the 8-bit states take the IEEE root and quotients: the codes, which feed the next step, are
+// then the same for every evaluation of the formula in float32, and a value on the border between two codes does not
+// depend on how an expression was contracted.
+template <bool kParamBf16, bool kMaster, bool kGradBf16, bool kCodes>
+__device__ __forceinline__ void adamw_block(const Slot& s, const AdamwArgs& a, const Hyper& hy, float gs, long long base) {
+  using G = typename std::conditional<kGradBf16, __nv_bfloat16, float>::type;
+  using P = typename std::conditional<kParamBf16, __nv_bfloat16, float>::type;
+  const long long i = base + (threadIdx.x & 31) * 8;
+  const int n = (int)(s.numel - i < 8 ? (s.numel > i ? s.numel - i : 0) : 8);
+  const bool vec = s.aligned && n == 8;
+  f2 g[4], m[4], v[4], p[4];
+  load8<G>(s.grad, i, n, vec, g);
+  uint2 cm, cv;
+  float sm = 0.f, sv = 0.f;
+  if constexpr (kCodes) {
+    cm = load_codes(s.m, i, n, vec);
+    cv = load_codes(s.v, i, n, vec);
+    sm = s.m_scale[base / MRL_STATE_BLOCK];
+    sv = s.v_scale[base / MRL_STATE_BLOCK];
+  } else {
+    load8<float>(s.m, i, n, vec, m);
+    load8<float>(s.v, i, n, vec, v);
+  }
+  if constexpr (kMaster)
+    load8<float>(s.master, i, n, vec, p);
+  else
+    load8<P>(s.param, i, n, vec, p);
+  uint32_t bits[8];  // of each element: 16 for m, 16 for v above them
+  if (a.seeded && (kCodes || (kParamBf16 && !kMaster))) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const unsigned long long w = splitmix64(hy.key + s.rng_first + (unsigned long long)(i / 2 + j));
+      bits[2 * j] = (uint32_t)w;
+      bits[2 * j + 1] = (uint32_t)(w >> 32);
+    }
+  }
+  if constexpr (kCodes) {
+    decode(cm, sm, m);
+    decode(cv, sv, v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = mul_f2(v[j], v[j]);
+  }
+  f2 root[4];
+  const f2 gs2 = make_f2(gs, gs), b1 = make_f2(a.beta1, a.beta1), o1 = make_f2(a.one_beta1, a.one_beta1);
+  const f2 b2 = make_f2(a.beta2, a.beta2), o2 = make_f2(a.one_beta2, a.one_beta2);
+  const f2 rc2 = make_f2(hy.root_c2, hy.root_c2), eps2 = make_f2(a.eps, a.eps), lr2 = make_f2(-hy.lr_c1, -hy.lr_c1);
+  const f2 keep2 = make_f2(-hy.lr * s.decay, -hy.lr * s.decay);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const f2 gj = mul_f2(g[j], gs2);
+    m[j] = add_f2(mul_f2(b1, m[j]), mul_f2(o1, gj));
+    v[j] = add_f2(mul_f2(b2, v[j]), mul_f2(o2, mul_f2(gj, gj)));
+  }
+  if constexpr (kCodes) root8(v, root);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (!kCodes) {
+      const float2 u = split_f2(v[j]);
+      root[j] = make_f2(sqrt_approx(u.x), sqrt_approx(u.y));
+    }
+    const float2 den = split_f2(fma_f2(root[j], rc2, eps2));
+    const f2 quot = mul_f2(mul_f2(m[j], lr2), make_f2(rcp_approx(den.x), rcp_approx(den.y)));
+    p[j] = add_f2(p[j], fma_f2(keep2, p[j], quot));
+  }
+  if constexpr (kMaster) store8(s.master, i, n, vec, p);
+  if constexpr (kParamBf16) {
+    uint32_t w[4];
+    f2 nothing = 0ull;  // 0, or NaN where a value is not finite
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      w[j] = f2_to_bf16x2(p[j]);
+      if (!kMaster) nothing = fma_f2(p[j], 0ull, nothing);
+    }
+    if (!kMaster && a.seeded) {  // the 16 bits that are cut decide against m's in reverse order
+      const float2 none = split_f2(nothing);
+      if (none.x + none.y == 0.f) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 u = split_f2(p[j]);
+          w[j] = __byte_perm(__float_as_uint(u.x) + (__brev(bits[2 * j]) >> 16), __float_as_uint(u.y) + (__brev(bits[2 * j + 1]) >> 16), 0x7632);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 u = split_f2(p[j]);
+          const uint32_t lo = __float_as_uint(u.x) + (__brev(bits[2 * j]) >> 16), hi = __float_as_uint(u.y) + (__brev(bits[2 * j + 1]) >> 16);
+          if (fabsf(u.x) < INFINITY) w[j] = (w[j] & 0xffff0000u) | lo >> 16;
+          if (fabsf(u.y) < INFINITY) w[j] = (w[j] & 0xffffu) | (hi & 0xffff0000u);
+        }
+      }
+    }
+    store8_bf16(s.param, i, n, vec, w);
+  } else {
+    store8(s.param, i, n, vec, p);
+  }
+  if constexpr (kCodes) {
+    uint32_t am = 0, av = 0;  // magnitudes as ordered integers; NaN lies above infinity
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 um = split_f2(m[j]), ur = split_f2(root[j]);
+      am = max(am, max(__float_as_uint(um.x) & 0x7fffffffu, __float_as_uint(um.y) & 0x7fffffffu));
+      av = max(av, max(__float_as_uint(ur.x) & 0x7fffffffu, __float_as_uint(ur.y) & 0x7fffffffu));
+    }
+    am = __reduce_max_sync(0xffffffffu, am);
+    av = __reduce_max_sync(0xffffffffu, av);
+    float inv_m, inv_v;
+    block_scale(__uint_as_float(am), &sm, &inv_m);
+    block_scale(__uint_as_float(av), &sv, &inv_v);
+    if ((threadIdx.x & 31) == 0) {
+      s.m_scale[base / MRL_STATE_BLOCK] = sm;
+      s.v_scale[base / MRL_STATE_BLOCK] = sv;
+    }
+    uint32_t codes[2];
+    const bool seeded = a.seeded && am < 0x7f800000u && av < 0x7f800000u;  // (the dither's arithmetic on bits is for numbers)
+    encode<false>(m, inv_m, seeded, bits, codes);
+    store_codes(s.m, i, n, vec, codes);
+    encode<true>(root, inv_v, seeded, bits, codes);
+    store_codes(s.v, i, n, vec, codes);
+  } else {
+    store8(s.m, i, n, vec, m);
+    store8(s.v, i, n, vec, v);
   }
 }
 
@@ -239,8 +433,7 @@ template <typename G>
 __device__ __forceinline__ double chunk_squares(const Slot& s, long long lo, long long hi) {
   double sum = 0.0;
   for (long long base = lo; base < hi; base += kChunk * 4) {
-    float x[4][8];
-    float run = 0.f;
+    f2 x[4][4], run2[2] = {0ull, 0ull};
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const long long i = base + k * kChunk + threadIdx.x * 8;
@@ -250,14 +443,19 @@ __device__ __forceinline__ double chunk_squares(const Slot& s, long long lo, lon
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) run = fmaf(x[k][j], x[k][j], run);
+      for (int j = 0; j < 4; ++j) run2[j & 1] = fma_f2(x[k][j], x[k][j], run2[j & 1]);
+    const float2 part = split_f2(add_f2(run2[0], run2[1]));
+    const float run = part.x + part.y;
     if (run >= 1e-30f && run <= 1e38f) {
       sum += (double)run;
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum = fma((double)x[k][j], (double)x[k][j], sum);
+        for (int j = 0; j < 4; ++j) {
+          const float2 u = split_f2(x[k][j]);
+          sum = fma((double)u.x, (double)u.x, fma((double)u.y, (double)u.y, sum));
+        }
     }
   }
   return sum;
@@ -277,104 +475,6 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const __grid_consta
   }
   sum = block_sum(sum, red);
   if (threadIdx.x == 0) partial[blockIdx.x] = first_launch ? sum : partial[blockIdx.x] + sum;
-}
-
-// One block of MRL_STATE_BLOCK elements by a warp.  The moments are rounded operation by operation as the formula stands
-// (no fused multiply-add) and the 8-bit states take the IEEE root and quotients: the codes, which feed the next step, are
-// then the same for every evaluation of the formula in float32, and a value on the border between two codes does not
-// depend on how an expression was contracted.
-template <bool kParamBf16, bool kMaster, bool kGradBf16, bool kCodes>
-__device__ __forceinline__ void adamw_block(const Slot& s, const AdamwArgs& a, const Hyper& hy, float gs, long long base) {
-  using G = typename std::conditional<kGradBf16, __nv_bfloat16, float>::type;
-  using P = typename std::conditional<kParamBf16, __nv_bfloat16, float>::type;
-  const long long i = base + (threadIdx.x & 31) * 8;
-  const int n = (int)(s.numel - i < 8 ? (s.numel > i ? s.numel - i : 0) : 8);
-  const bool vec = s.aligned && n == 8;
-  float g[8], m[8], v[8], p[8];
-  load8<G>(s.grad, i, n, vec, g);
-  uint2 cm, cv;
-  float sm = 0.f, sv = 0.f;
-  if constexpr (kCodes) {
-    cm = load_codes(s.m, i, n, vec);
-    cv = load_codes(s.v, i, n, vec);
-    sm = s.m_scale[base / MRL_STATE_BLOCK];
-    sv = s.v_scale[base / MRL_STATE_BLOCK];
-  } else {
-    load8<float>(s.m, i, n, vec, m);
-    load8<float>(s.v, i, n, vec, v);
-  }
-  if constexpr (kMaster)
-    load8<float>(s.master, i, n, vec, p);
-  else
-    load8<P>(s.param, i, n, vec, p);
-  if constexpr (kCodes) {
-    decode(cm, sm, m);
-    decode(cv, sv, v);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(v[j], v[j]);
-  }
-  float root[8];
-  const float decay = hy.lr * s.decay;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float gj = __fmul_rn(g[j], gs);
-    m[j] = __fadd_rn(__fmul_rn(a.beta1, m[j]), __fmul_rn(a.one_beta1, gj));
-    v[j] = __fadd_rn(__fmul_rn(a.beta2, v[j]), __fmul_rn(a.one_beta2, __fmul_rn(gj, gj)));
-    if constexpr (kCodes) root[j] = __fsqrt_rn(v[j]); else root[j] = sqrt_approx(v[j]);
-    p[j] -= fmaf(decay, p[j], __fdividef(hy.lr_c1 * m[j], fmaf(root[j], hy.root_c2, a.eps)));
-  }
-  uint32_t bits[8];  // of each element: 16 for m, 16 for v above them
-  if (a.seeded && (kCodes || (kParamBf16 && !kMaster))) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const unsigned long long w = splitmix64(hy.key + s.rng_first + (unsigned long long)(i / 2 + j));
-      bits[2 * j] = (uint32_t)w;
-      bits[2 * j + 1] = (uint32_t)(w >> 32);
-    }
-  }
-  if constexpr (kMaster) store8(s.master, i, n, vec, p);
-  if constexpr (kParamBf16) {
-    uint32_t w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      w[j] = pack_bf16x2(p[2 * j], p[2 * j + 1]);
-      if (!kMaster && a.seeded) {  // the 16 bits that are cut decide against m's in reverse order
-        const uint32_t lo = __float_as_uint(p[2 * j]) + (__brev(bits[2 * j]) >> 16);
-        const uint32_t hi = __float_as_uint(p[2 * j + 1]) + (__brev(bits[2 * j + 1]) >> 16);
-        if (fabsf(p[2 * j]) < INFINITY && fabsf(p[2 * j + 1]) < INFINITY) {
-          w[j] = __byte_perm(lo, hi, 0x7632);
-        } else {  // not finite: as it is
-          if (fabsf(p[2 * j]) < INFINITY) w[j] = (w[j] & 0xffff0000u) | lo >> 16;
-          if (fabsf(p[2 * j + 1]) < INFINITY) w[j] = (w[j] & 0xffffu) | (hi & 0xffff0000u);
-        }
-      }
-    }
-    store8(static_cast<__nv_bfloat16*>(s.param), i, n, vec, w);
-  } else {
-    store8(static_cast<float*>(s.param), i, n, vec, p);
-  }
-  if constexpr (kCodes) {
-    uint32_t am = 0, av = 0;  // magnitudes as ordered integers
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      am = max(am, __float_as_uint(m[j]) & 0x7fffffffu);
-      av = max(av, __float_as_uint(root[j]) & 0x7fffffffu);
-    }
-    sm = e4m3_scale(__uint_as_float(__reduce_max_sync(0xffffffffu, am)));
-    sv = e4m3_scale(__uint_as_float(__reduce_max_sync(0xffffffffu, av)));
-    if ((threadIdx.x & 31) == 0) {
-      s.m_scale[base / MRL_STATE_BLOCK] = sm;
-      s.v_scale[base / MRL_STATE_BLOCK] = sv;
-    }
-    uint32_t codes[2];
-    encode<false>(m, __frcp_rn(sm), a.seeded, bits, 0, codes);
-    store_codes(s.m, i, n, vec, codes);
-    encode<true>(root, __frcp_rn(sv), a.seeded, bits, 16, codes);
-    store_codes(s.v, i, n, vec, codes);
-  } else {
-    store8(static_cast<float*>(s.m), i, n, vec, m);
-    store8(static_cast<float*>(s.v), i, n, vec, v);
-  }
 }
 
 // The tensors of one kind (types of gradient, parameter and states), which share the launch and its registers.
