@@ -14,10 +14,12 @@ using namespace mrl;
 
 constexpr int kThreads = 256;
 constexpr int kChunk = 8 * MRL_STATE_BLOCK;   // elements of a CTA at least: a state block per warp
+constexpr int kChunksMost = 4;
 constexpr int kSlotsFew = 16, kSlots = 352;   // tensors per launch: the tables stay below the 32,764 bytes of kernel arguments
 constexpr int kSms = 148;
 constexpr int kNormCtas = kSms * 8;
-constexpr int kAdamwCtas = 4;                 // per SM
+constexpr int kCodesCtas = 3;                 // per SM, of the update with 8-bit states
+constexpr bool kCodesAhead = true;
 
 struct Slot {
   const void* grad;
@@ -145,32 +147,40 @@ struct AdamwArgs {
 
 // ---- eight adjacent elements of a lane, as four pairs; a warp works on the 256 that share the scales of an 8-bit state
 
-// Whole (one or two wide accesses) where `vec`, else one by one below n and 0 from there.
+// As they lie in memory: eight words of float32, four of two bf16.  Whole (one wide access) where `vec`, else one by one below n
+// and 0 from there.
 template <typename T>
-__device__ __forceinline__ void load8(const void* base, long long i, int n, bool vec, f2 (&x)[4]) {
-  const T* p = static_cast<const T*>(base) + i;
-  if (vec) {
-    if constexpr (sizeof(T) == 4) {
-      asm volatile("ld.global.L1::no_allocate.v4.b64 {%0, %1, %2, %3}, [%4];" : "=l"(x[0]), "=l"(x[1]), "=l"(x[2]), "=l"(x[3]) : "l"(p));
+struct Raw8 {
+  static constexpr int kWords = (int)sizeof(T) * 2;
+  uint32_t w[kWords];
+
+  __device__ __forceinline__ void load(const void* base, long long i, int n, bool vec) {
+    const T* p = static_cast<const T*>(base) + i;
+    if (vec) {
+      if constexpr (sizeof(T) == 4)
+        asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                     : "l"(p));
+      else
+        asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
     } else {
-      uint32_t w[4];
-      asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = bf16x2_to_f2(w[j]);
-    }
-  } else {
+      for (int k = 0; k < kWords; ++k) w[k] = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float u[2] = {0.f, 0.f};
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-        if (2 * j + k < n) {
-          if constexpr (sizeof(T) == 4) u[k] = p[2 * j + k]; else u[k] = __bfloat162float(p[2 * j + k]);
+      for (int j = 0; j < 8; ++j)
+        if (j < n) {
+          if constexpr (sizeof(T) == 4) w[j] = reinterpret_cast<const uint32_t*>(p)[j];
+          else w[j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[j] << (16 * (j & 1));
         }
-      x[j] = make_f2(u[0], u[1]);
     }
   }
-}
+  __device__ __forceinline__ f2 pair(int j) const {
+    if constexpr (sizeof(T) == 4)
+      return make_f2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
+    else
+      return bf16x2_to_f2(w[j]);
+  }
+};
 __device__ __forceinline__ void store8(void* base, long long i, int n, bool vec, const f2 (&x)[4]) {
   float* p = static_cast<float*>(base) + i;
   if (vec) {
@@ -306,44 +316,65 @@ __device__ __forceinline__ void encode(const f2 (&x)[4], float inv, bool seeded,
 // (no fused multiply-add) and the 8-bit states take the IEEE root and quotients: the codes, which feed the next step, are
 // then the same for every evaluation of the formula in float32, and a value on the border between two codes does not
 // depend on how an expression was contracted.
-template <bool kParamBf16, bool kMaster, bool kGradBf16, bool kCodes>
-__device__ __forceinline__ void adamw_block(const Slot& s, const AdamwArgs& a, const Hyper& hy, float gs, long long base) {
-  using G = typename std::conditional<kGradBf16, __nv_bfloat16, float>::type;
-  using P = typename std::conditional<kParamBf16, __nv_bfloat16, float>::type;
+// kKind: kind_of().
+template <int kKind>
+struct AdamwBlock {
+  static constexpr bool kParamBf16 = (kKind & 1) != 0, kMaster = (kKind & 2) != 0, kCodes = (kKind & 8) != 0;
+  using G = typename std::conditional<(kKind & 4) != 0, __nv_bfloat16, float>::type;
+  using P = typename std::conditional<kParamBf16 && !kMaster, __nv_bfloat16, float>::type;
+  Raw8<G> g;
+  Raw8<P> p;
+  Raw8<float> m, v;  // float32 states
+  uint2 cm, cv;      // or codes
+  float sm, sv;
+
+  __device__ __forceinline__ void load(const Slot& s, long long base) {
+    const long long i = base + (threadIdx.x & 31) * 8;
+    const int n = (int)(s.numel - i < 8 ? (s.numel > i ? s.numel - i : 0) : 8);
+    const bool vec = s.aligned && n == 8;
+    g.load(s.grad, i, n, vec);
+    if constexpr (kCodes) {
+      cm = load_codes(s.m, i, n, vec);
+      cv = load_codes(s.v, i, n, vec);
+      sm = s.m_scale[base / MRL_STATE_BLOCK];
+      sv = s.v_scale[base / MRL_STATE_BLOCK];
+    } else {
+      m.load(s.m, i, n, vec);
+      v.load(s.v, i, n, vec);
+    }
+    p.load(kMaster ? (const void*)s.master : (const void*)s.param, i, n, vec);
+  }
+};
+
+template <int kKind>
+__device__ __forceinline__ void adamw_block(const Slot& s, const AdamwArgs& a, const Hyper& hy, float gs, long long base, const AdamwBlock<kKind>& in) {
+  using In = AdamwBlock<kKind>;
+  constexpr bool kParamBf16 = In::kParamBf16, kMaster = In::kMaster, kCodes = In::kCodes;
   const long long i = base + (threadIdx.x & 31) * 8;
   const int n = (int)(s.numel - i < 8 ? (s.numel > i ? s.numel - i : 0) : 8);
   const bool vec = s.aligned && n == 8;
-  f2 g[4], m[4], v[4], p[4];
-  load8<G>(s.grad, i, n, vec, g);
-  uint2 cm, cv;
-  float sm = 0.f, sv = 0.f;
-  if constexpr (kCodes) {
-    cm = load_codes(s.m, i, n, vec);
-    cv = load_codes(s.v, i, n, vec);
-    sm = s.m_scale[base / MRL_STATE_BLOCK];
-    sv = s.v_scale[base / MRL_STATE_BLOCK];
-  } else {
-    load8<float>(s.m, i, n, vec, m);
-    load8<float>(s.v, i, n, vec, v);
-  }
-  if constexpr (kMaster)
-    load8<float>(s.master, i, n, vec, p);
-  else
-    load8<P>(s.param, i, n, vec, p);
+  f2 m[4], v[4], p[4];
   uint32_t bits[8];  // of each element: 16 for m, 16 for v above them
   if (a.seeded && (kCodes || (kParamBf16 && !kMaster))) {
+    const unsigned long long first = hy.key + s.rng_first + (unsigned long long)(i / 2);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const unsigned long long w = splitmix64(hy.key + s.rng_first + (unsigned long long)(i / 2 + j));
+      const unsigned long long w = splitmix64(first + j);
       bits[2 * j] = (uint32_t)w;
       bits[2 * j + 1] = (uint32_t)(w >> 32);
     }
   }
   if constexpr (kCodes) {
-    decode(cm, sm, m);
-    decode(cv, sv, v);
+    decode(in.cm, in.sm, m);
+    decode(in.cv, in.sv, v);
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = mul_f2(v[j], v[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      m[j] = in.m.pair(j);
+      v[j] = in.v.pair(j);
+    }
   }
   f2 root[4];
   const f2 gs2 = make_f2(gs, gs), b1 = make_f2(a.beta1, a.beta1), o1 = make_f2(a.one_beta1, a.one_beta1);
@@ -352,7 +383,8 @@ __device__ __forceinline__ void adamw_block(const Slot& s, const AdamwArgs& a, c
   const f2 keep2 = make_f2(-hy.lr * s.decay, -hy.lr * s.decay);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const f2 gj = mul_f2(g[j], gs2);
+    const f2 gj = mul_f2(in.g.pair(j), gs2);
+    p[j] = in.p.pair(j);
     m[j] = add_f2(mul_f2(b1, m[j]), mul_f2(o1, gj));
     v[j] = add_f2(mul_f2(b2, v[j]), mul_f2(o2, mul_f2(gj, gj)));
   }
@@ -408,7 +440,7 @@ __device__ __forceinline__ void adamw_block(const Slot& s, const AdamwArgs& a, c
     }
     am = __reduce_max_sync(0xffffffffu, am);
     av = __reduce_max_sync(0xffffffffu, av);
-    float inv_m, inv_v;
+    float sm, sv, inv_m, inv_v;
     block_scale(__uint_as_float(am), &sm, &inv_m);
     block_scale(__uint_as_float(av), &sv, &inv_v);
     if ((threadIdx.x & 31) == 0) {
@@ -433,17 +465,18 @@ template <typename G>
 __device__ __forceinline__ double chunk_squares(const Slot& s, long long lo, long long hi) {
   double sum = 0.0;
   for (long long base = lo; base < hi; base += kChunk * 4) {
-    f2 x[4][4], run2[2] = {0ull, 0ull};
+    Raw8<G> x[4];
+    f2 run2[2] = {0ull, 0ull};
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const long long i = base + k * kChunk + threadIdx.x * 8;
       const int n = (int)(hi - i < 8 ? (hi > i ? hi - i : 0) : 8);
-      load8<G>(s.grad, i, n, s.aligned && n == 8, x[k]);
+      x[k].load(s.grad, i, n, s.aligned && n == 8);
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) run2[j & 1] = fma_f2(x[k][j], x[k][j], run2[j & 1]);
+      for (int j = 0; j < 4; ++j) run2[j & 1] = fma_f2(x[k].pair(j), x[k].pair(j), run2[j & 1]);
     const float2 part = split_f2(add_f2(run2[0], run2[1]));
     const float run = part.x + part.y;
     if (run >= 1e-30f && run <= 1e38f) {
@@ -453,7 +486,7 @@ __device__ __forceinline__ double chunk_squares(const Slot& s, long long lo, lon
       for (int k = 0; k < 4; ++k)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float2 u = split_f2(x[k][j]);
+          const float2 u = split_f2(x[k].pair(j));
           sum = fma((double)u.x, (double)u.x, fma((double)u.y, (double)u.y, sum));
         }
     }
@@ -479,7 +512,7 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const __grid_consta
 
 // The tensors of one kind (types of gradient, parameter and states), which share the launch and its registers.
 template <int kKind, int kN>
-__global__ void __launch_bounds__(kThreads, kAdamwCtas) adamw_kernel(const __grid_constant__ Table<kN> t, const __grid_constant__ AdamwArgs a) {
+__global__ void __launch_bounds__(kThreads, kKind & 8 ? kCodesCtas : 4) adamw_kernel(const __grid_constant__ Table<kN> t, const __grid_constant__ AdamwArgs a) {
   const float gs = a.grad_scale != nullptr ? *a.grad_scale : 1.f;
   if (!(fabsf(gs) < INFINITY)) {
     if (blockIdx.x == 0 && threadIdx.x == 0 && a.status != nullptr) atomicOr(a.status, MRL_DEV_NONFINITE_GRAD);
@@ -489,8 +522,22 @@ __global__ void __launch_bounds__(kThreads, kAdamwCtas) adamw_kernel(const __gri
   const int k = slot_of(t, blockIdx.x);
   const Slot& s = t.slot[k];
   const long long lo = (long long)(blockIdx.x - t.first[k]) * t.chunk, hi = min(lo + t.chunk, s.numel);
-  for (long long base = lo + (threadIdx.x >> 5) * MRL_STATE_BLOCK; base < hi; base += kThreads / 32 * MRL_STATE_BLOCK)
-    adamw_block<(kKind & 1) != 0, (kKind & 2) != 0, (kKind & 4) != 0, (kKind & 8) != 0>(s, a, hy, gs, base);
+  constexpr bool kAhead = (kKind & 8) != 0 && kCodesAhead;
+  long long base = lo + (threadIdx.x >> 5) * MRL_STATE_BLOCK;
+  constexpr int kNext = kThreads / 32 * MRL_STATE_BLOCK;
+  if (base >= hi) return;
+  AdamwBlock<kKind> in;
+  in.load(s, base);
+  for (;;) {
+    // the next block is on its way while this one is worked on
+    AdamwBlock<kKind> next;
+    const bool more = base + kNext < hi;
+    if (kAhead && more) next.load(s, base + kNext);
+    adamw_block<kKind>(s, a, hy, gs, base, in);
+    if (!more) break;
+    base += kNext;
+    if (kAhead) in = next; else in.load(s, base);
+  }
 }
 
 bool grad_type_ok(int32_t dtype) { return dtype == MRL_BF16 || dtype == MRL_F32; }
@@ -536,7 +583,7 @@ int fill_table(const mrl_tensor_slot* slots, int n, int at, int chunk, int only,
 int chunk_of(const mrl_tensor_slot* slots, int n) {
   long long total = 0;
   for (int k = 0; k < n; ++k) total += slots[k].numel;
-  return total <= (long long)kSms * 8 * 4 * kChunk ? kChunk : 4 * kChunk;
+  return total <= (long long)kSms * 8 * 4 * kChunk ? kChunk : kChunksMost * kChunk;
 }
 
 template <int kN>
