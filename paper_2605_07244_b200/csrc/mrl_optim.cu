@@ -14,12 +14,11 @@ using namespace mrl;
 
 constexpr int kThreads = 256;
 constexpr int kChunk = 8 * MRL_STATE_BLOCK;   // elements of a CTA at least: a state block per warp
-constexpr int kChunksMost = 4;
+constexpr int kChunksMost = 8;
 constexpr int kSlotsFew = 16, kSlots = 352;   // tensors per launch: the tables stay below the 32,764 bytes of kernel arguments
 constexpr int kSms = 148;
 constexpr int kNormCtas = kSms * 8;
 constexpr int kCodesCtas = 3;                 // per SM, of the update with 8-bit states
-constexpr bool kCodesAhead = true;
 
 struct Slot {
   const void* grad;
@@ -154,8 +153,8 @@ struct Raw8 {
   static constexpr int kWords = (int)sizeof(T) * 2;
   uint32_t w[kWords];
 
-  __device__ __forceinline__ void load(const void* base, long long i, int n, bool vec) {
-    const T* p = static_cast<const T*>(base) + i;
+  __device__ __forceinline__ void load(const void* at, int n, bool vec) {
+    const T* p = static_cast<const T*>(at);
     if (vec) {
       if constexpr (sizeof(T) == 4)
         asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -181,8 +180,8 @@ struct Raw8 {
       return bf16x2_to_f2(w[j]);
   }
 };
-__device__ __forceinline__ void store8(void* base, long long i, int n, bool vec, const f2 (&x)[4]) {
-  float* p = static_cast<float*>(base) + i;
+__device__ __forceinline__ void store8(void* at, int n, bool vec, const f2 (&x)[4]) {
+  float* p = static_cast<float*>(at);
   if (vec) {
     asm volatile("st.global.v4.b64 [%0], {%1, %2, %3, %4};" ::"l"(p), "l"(x[0]), "l"(x[1]), "l"(x[2]), "l"(x[3]) : "memory");
   } else {
@@ -195,8 +194,8 @@ __device__ __forceinline__ void store8(void* base, long long i, int n, bool vec,
   }
 }
 // words of two bf16 each
-__device__ __forceinline__ void store8_bf16(void* base, long long i, int n, bool vec, const uint32_t (&w)[4]) {
-  uint16_t* p = static_cast<uint16_t*>(base) + i;
+__device__ __forceinline__ void store8_bf16(void* at, int n, bool vec, const uint32_t (&w)[4]) {
+  uint16_t* p = static_cast<uint16_t*>(at);
   if (vec) {
     *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
   } else {
@@ -205,8 +204,8 @@ __device__ __forceinline__ void store8_bf16(void* base, long long i, int n, bool
       if (j < n) p[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
   }
 }
-__device__ __forceinline__ uint2 load_codes(const void* base, long long i, int n, bool vec) {
-  const uint8_t* p = static_cast<const uint8_t*>(base) + i;
+__device__ __forceinline__ uint2 load_codes(const void* at, int n, bool vec) {
+  const uint8_t* p = static_cast<const uint8_t*>(at);
   if (vec) return *reinterpret_cast<const uint2*>(p);
   uint32_t w[2] = {0, 0};
 #pragma unroll
@@ -214,8 +213,8 @@ __device__ __forceinline__ uint2 load_codes(const void* base, long long i, int n
     if (j < n) w[j >> 2] |= (uint32_t)p[j] << (8 * (j & 3));
   return make_uint2(w[0], w[1]);
 }
-__device__ __forceinline__ void store_codes(void* base, long long i, int n, bool vec, const uint32_t (&w)[2]) {
-  uint8_t* p = static_cast<uint8_t*>(base) + i;
+__device__ __forceinline__ void store_codes(void* at, int n, bool vec, const uint32_t (&w)[2]) {
+  uint8_t* p = static_cast<uint8_t*>(at);
   if (vec) {
     *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
   } else {
@@ -233,24 +232,33 @@ __device__ __forceinline__ void decode(uint2 codes, float scale, f2 (&x)[4]) {
   }
 }
 
-// IEEE square roots of eight values: v * rsqrt(v), brought to the nearest float by one Newton step on the fused residual
+// IEEE square roots of eight values whose smallest and largest are given: v * rsqrt(v), brought to the nearest float by one Newton step on the fused residual
 // v - s^2 (Markstein 1990; equal to sqrtf for every float in its range, see the tests).  Values near zero, where the
 // residual would leave float32, and infinities go through sqrtf.
-__device__ __forceinline__ void root8(const f2 (&v)[4], f2 (&root)[4]) {
-  float lo = INFINITY, hi = 0.f;
+__device__ __forceinline__ void root8(const f2 (&v)[4], uint32_t least, uint32_t most, f2 (&root)[4]) {
+  if (least >= __float_as_uint(kRootMin) && most <= __float_as_uint(kRootMax)) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float2 u = split_f2(v[j]);
-    lo = fminf(lo, fminf(u.x, u.y));
-    hi = fmaxf(hi, fmaxf(u.x, u.y));
-    root[j] = newton_root(v[j]);
-  }
-  if (!(lo >= kRootMin && hi <= kRootMax)) {
+    for (int j = 0; j < 4; ++j) root[j] = newton_root(v[j]);
+  } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float2 u = split_f2(v[j]);
       root[j] = make_f2(__fsqrt_rn(u.x), __fsqrt_rn(u.y));
     }
+  }
+}
+// The smallest and the largest magnitude of eight values as ordered integers; NaN lies above infinity.
+template <bool kSigned>
+__device__ __forceinline__ void bounds8(const f2 (&x)[4], uint32_t* least, uint32_t* most) {
+  *least = 0xffffffffu;
+  *most = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 u = split_f2(x[j]);
+    uint32_t a = __float_as_uint(u.x), b = __float_as_uint(u.y);
+    if (kSigned) a &= 0x7fffffffu, b &= 0x7fffffffu;
+    *least = min(min(a, b), *least);
+    *most = max(max(a, b), *most);
   }
 }
 // The scale of a block and its reciprocal as IEEE quotients, corrected on their fused residuals the same way.
@@ -277,29 +285,22 @@ __device__ __forceinline__ float e4m3_dither_normal(float y, uint32_t bits16) {
 // Codes of x / scale, |x| at most 448 scale.  bits: 16 of each element, the lower ones for the first moment, the upper ones
 // for the (root of the) second, of which a value above zero keeps a code above zero.
 template <bool kSecond>
-__device__ __forceinline__ void encode(const f2 (&x)[4], float inv, bool seeded, const uint32_t (&bits)[8], uint32_t (&codes)[2]) {
+__device__ __forceinline__ void encode(const f2 (&x)[4], float least, float inv, bool seeded, const uint32_t (&bits)[8], uint32_t (&codes)[2]) {
   const f2 inv2 = make_f2(inv, inv);
-  f2 y[4];
-  float least = INFINITY;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    y[j] = mul_f2(x[j], inv2);
-    const float2 u = split_f2(y[j]);
-    least = fminf(least, fminf(fabsf(u.x), fabsf(u.y)));
-  }
+  least *= inv;
   const auto bits16 = [&](int j) { return kSecond ? bits[j] >> 16 : bits[j] & 0xffffu; };
   codes[0] = codes[1] = 0;
   if (seeded && least >= 0.015625f) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float2 u = split_f2(y[j]);
+      const float2 u = split_f2(mul_f2(x[j], inv2));
       codes[j >> 1] |= pack_e4m3x2(e4m3_dither_normal(u.x, bits16(2 * j)), e4m3_dither_normal(u.y, bits16(2 * j + 1))) << (16 * (j & 1));
     }
     return;
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const float2 u = split_f2(y[j]);
+    const float2 u = split_f2(mul_f2(x[j], inv2));
     const float a = seeded ? e4m3_dither(u.x, bits16(2 * j)) : u.x, b = seeded ? e4m3_dither(u.y, bits16(2 * j + 1)) : u.y;
     codes[j >> 1] |= pack_e4m3x2(a, b) << (16 * (j & 1));
   }
@@ -328,38 +329,75 @@ struct AdamwBlock {
   uint2 cm, cv;      // or codes
   float sm, sv;
 
-  __device__ __forceinline__ void load(const Slot& s, long long base) {
-    const long long i = base + (threadIdx.x & 31) * 8;
-    const int n = (int)(s.numel - i < 8 ? (s.numel > i ? s.numel - i : 0) : 8);
-    const bool vec = s.aligned && n == 8;
-    g.load(s.grad, i, n, vec);
-    if constexpr (kCodes) {
-      cm = load_codes(s.m, i, n, vec);
-      cv = load_codes(s.v, i, n, vec);
-      sm = s.m_scale[base / MRL_STATE_BLOCK];
-      sv = s.v_scale[base / MRL_STATE_BLOCK];
-    } else {
-      m.load(s.m, i, n, vec);
-      v.load(s.v, i, n, vec);
+  // Where a lane's eight elements are; moved from block to block.
+  struct Cursor {
+    const G* g;
+    P* p;               // what the step is taken on: the master weights where there are any
+    __nv_bfloat16* low; // and the parameter then
+    char *m, *v;
+    float *ms, *vs;
+    unsigned long long word;  // position in the stream of random words
+    int left;           // elements from the block's start to the end of the chunk
+    bool aligned;
+
+    __device__ __forceinline__ Cursor(const Slot& s, long long base, long long end, unsigned long long key) {
+      const long long i = base + (threadIdx.x & 31) * 8;
+      constexpr int kState = kCodes ? 1 : 4;
+      g = static_cast<const G*>(s.grad) + i;
+      p = static_cast<P*>(kMaster ? (void*)s.master : s.param) + i;
+      low = static_cast<__nv_bfloat16*>(s.param) + i;
+      m = static_cast<char*>(s.m) + i * kState;
+      v = static_cast<char*>(s.v) + i * kState;
+      ms = s.m_scale + base / MRL_STATE_BLOCK;
+      vs = s.v_scale + base / MRL_STATE_BLOCK;
+      word = key + s.rng_first + (unsigned long long)(i / 2);
+      left = (int)(end - base);
+      aligned = s.aligned;
     }
-    p.load(kMaster ? (const void*)s.master : (const void*)s.param, i, n, vec);
+    __device__ __forceinline__ void advance(int blocks) {
+      constexpr int kState = kCodes ? 1 : 4;
+      const int e = blocks * MRL_STATE_BLOCK;
+      g += e, p += e, m += e * kState, v += e * kState, word += e / 2, left -= e;
+      if constexpr (kMaster) low += e;
+      if constexpr (kCodes) ms += blocks, vs += blocks;
+    }
+    __device__ __forceinline__ int count() const { return min(8, max(0, left - (int)(threadIdx.x & 31) * 8)); }
+    __device__ __forceinline__ bool vec() const { return aligned && left >= MRL_STATE_BLOCK; }  // the same for the warp
+  };
+
+  // `ahead` blocks behind the cursor
+  __device__ __forceinline__ void load(const Cursor& c, int ahead) {
+    constexpr int kState = kCodes ? 1 : 4;
+    const int e = ahead * MRL_STATE_BLOCK, left = c.left - e;
+    const int n = min(8, max(0, left - (int)(threadIdx.x & 31) * 8));
+    const bool vec = c.aligned && left >= MRL_STATE_BLOCK;
+    g.load(c.g + e, n, vec);
+    if constexpr (kCodes) {
+      cm = load_codes(c.m + e, n, vec);
+      cv = load_codes(c.v + e, n, vec);
+      sm = c.ms[ahead];
+      sv = c.vs[ahead];
+    } else {
+      m.load(c.m + e * kState, n, vec);
+      v.load(c.v + e * kState, n, vec);
+    }
+    p.load(c.p + e, n, vec);
   }
 };
 
 template <int kKind>
-__device__ __forceinline__ void adamw_block(const Slot& s, const AdamwArgs& a, const Hyper& hy, float gs, long long base, const AdamwBlock<kKind>& in) {
+__device__ __forceinline__ void adamw_block(const AdamwArgs& a, const Hyper& hy, float gs, float decay, const typename AdamwBlock<kKind>::Cursor& c,
+                                            const AdamwBlock<kKind>& in) {
   using In = AdamwBlock<kKind>;
   constexpr bool kParamBf16 = In::kParamBf16, kMaster = In::kMaster, kCodes = In::kCodes;
-  const long long i = base + (threadIdx.x & 31) * 8;
-  const int n = (int)(s.numel - i < 8 ? (s.numel > i ? s.numel - i : 0) : 8);
-  const bool vec = s.aligned && n == 8;
+  const int n = c.count();
+  const bool vec = c.vec();
   f2 m[4], v[4], p[4];
   uint32_t bits[8];  // of each element: 16 for m, 16 for v above them
   if (a.seeded && (kCodes || (kParamBf16 && !kMaster))) {
-    const unsigned long long first = hy.key + s.rng_first + (unsigned long long)(i / 2);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const unsigned long long w = splitmix64(first + j);
+      const unsigned long long w = splitmix64(c.word + j);
       bits[2 * j] = (uint32_t)w;
       bits[2 * j + 1] = (uint32_t)(w >> 32);
     }
@@ -380,7 +418,7 @@ __device__ __forceinline__ void adamw_block(const Slot& s, const AdamwArgs& a, c
   const f2 gs2 = make_f2(gs, gs), b1 = make_f2(a.beta1, a.beta1), o1 = make_f2(a.one_beta1, a.one_beta1);
   const f2 b2 = make_f2(a.beta2, a.beta2), o2 = make_f2(a.one_beta2, a.one_beta2);
   const f2 rc2 = make_f2(hy.root_c2, hy.root_c2), eps2 = make_f2(a.eps, a.eps), lr2 = make_f2(-hy.lr_c1, -hy.lr_c1);
-  const f2 keep2 = make_f2(-hy.lr * s.decay, -hy.lr * s.decay);
+  const f2 keep2 = make_f2(-hy.lr * decay, -hy.lr * decay);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const f2 gj = mul_f2(in.g.pair(j), gs2);
@@ -388,7 +426,12 @@ __device__ __forceinline__ void adamw_block(const Slot& s, const AdamwArgs& a, c
     m[j] = add_f2(mul_f2(b1, m[j]), mul_f2(o1, gj));
     v[j] = add_f2(mul_f2(b2, v[j]), mul_f2(o2, mul_f2(gj, gj)));
   }
-  if constexpr (kCodes) root8(v, root);
+  uint32_t least_m = 0, most_m = 0, least_v = 0, most_v = 0;
+  if constexpr (kCodes) {
+    bounds8<true>(m, &least_m, &most_m);
+    bounds8<false>(v, &least_v, &most_v);
+    root8(v, least_v, most_v, root);
+  }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     if constexpr (!kCodes) {
@@ -399,7 +442,7 @@ __device__ __forceinline__ void adamw_block(const Slot& s, const AdamwArgs& a, c
     const f2 quot = mul_f2(mul_f2(m[j], lr2), make_f2(rcp_approx(den.x), rcp_approx(den.y)));
     p[j] = add_f2(p[j], fma_f2(keep2, p[j], quot));
   }
-  if constexpr (kMaster) store8(s.master, i, n, vec, p);
+  if constexpr (kMaster) store8(c.p, n, vec, p);
   if constexpr (kParamBf16) {
     uint32_t w[4];
     f2 nothing = 0ull;  // 0, or NaN where a value is not finite
@@ -426,36 +469,29 @@ __device__ __forceinline__ void adamw_block(const Slot& s, const AdamwArgs& a, c
         }
       }
     }
-    store8_bf16(s.param, i, n, vec, w);
+    store8_bf16(kMaster ? (void*)c.low : (void*)c.p, n, vec, w);
   } else {
-    store8(s.param, i, n, vec, p);
+    store8(c.p, n, vec, p);
   }
   if constexpr (kCodes) {
-    uint32_t am = 0, av = 0;  // magnitudes as ordered integers; NaN lies above infinity
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 um = split_f2(m[j]), ur = split_f2(root[j]);
-      am = max(am, max(__float_as_uint(um.x) & 0x7fffffffu, __float_as_uint(um.y) & 0x7fffffffu));
-      av = max(av, max(__float_as_uint(ur.x) & 0x7fffffffu, __float_as_uint(ur.y) & 0x7fffffffu));
-    }
-    am = __reduce_max_sync(0xffffffffu, am);
-    av = __reduce_max_sync(0xffffffffu, av);
+    most_m = __reduce_max_sync(0xffffffffu, most_m);
+    most_v = __reduce_max_sync(0xffffffffu, most_v);
     float sm, sv, inv_m, inv_v;
-    block_scale(__uint_as_float(am), &sm, &inv_m);
-    block_scale(__uint_as_float(av), &sv, &inv_v);
+    block_scale(__uint_as_float(most_m), &sm, &inv_m);
+    block_scale(__fsqrt_rn(__uint_as_float(most_v)), &sv, &inv_v);  // (the largest root is the root of the largest)
     if ((threadIdx.x & 31) == 0) {
-      s.m_scale[base / MRL_STATE_BLOCK] = sm;
-      s.v_scale[base / MRL_STATE_BLOCK] = sv;
+      *c.ms = sm;
+      *c.vs = sv;
     }
     uint32_t codes[2];
-    const bool seeded = a.seeded && am < 0x7f800000u && av < 0x7f800000u;  // (the dither's arithmetic on bits is for numbers)
-    encode<false>(m, inv_m, seeded, bits, codes);
-    store_codes(s.m, i, n, vec, codes);
-    encode<true>(root, inv_v, seeded, bits, codes);
-    store_codes(s.v, i, n, vec, codes);
+    const bool seeded = a.seeded && most_m < 0x7f800000u && most_v < 0x7f800000u;  // (the dither's arithmetic on bits is for numbers)
+    encode<false>(m, __uint_as_float(least_m), inv_m, seeded, bits, codes);
+    store_codes(c.m, n, vec, codes);
+    encode<true>(root, sqrt_approx(__uint_as_float(least_v)) * 0.9999f, inv_v, seeded, bits, codes);
+    store_codes(c.v, n, vec, codes);
   } else {
-    store8(s.m, i, n, vec, m);
-    store8(s.v, i, n, vec, v);
+    store8(c.m, n, vec, m);
+    store8(c.v, n, vec, v);
   }
 }
 
@@ -471,7 +507,7 @@ __device__ __forceinline__ double chunk_squares(const Slot& s, long long lo, lon
     for (int k = 0; k < 4; ++k) {
       const long long i = base + k * kChunk + threadIdx.x * 8;
       const int n = (int)(hi - i < 8 ? (hi > i ? hi - i : 0) : 8);
-      x[k].load(s.grad, i, n, s.aligned && n == 8);
+      x[k].load(static_cast<const G*>(s.grad) + i, n, s.aligned && n == 8);
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k)
@@ -522,21 +558,23 @@ __global__ void __launch_bounds__(kThreads, kKind & 8 ? kCodesCtas : 4) adamw_ke
   const int k = slot_of(t, blockIdx.x);
   const Slot& s = t.slot[k];
   const long long lo = (long long)(blockIdx.x - t.first[k]) * t.chunk, hi = min(lo + t.chunk, s.numel);
-  constexpr bool kAhead = (kKind & 8) != 0 && kCodesAhead;
-  long long base = lo + (threadIdx.x >> 5) * MRL_STATE_BLOCK;
-  constexpr int kNext = kThreads / 32 * MRL_STATE_BLOCK;
-  if (base >= hi) return;
+  constexpr bool kAhead = (kKind & 8) != 0;
+  constexpr int kNext = kThreads / 32;
+  typename AdamwBlock<kKind>::Cursor c(s, lo + (threadIdx.x >> 5) * MRL_STATE_BLOCK, hi, hy.key);
+  if (c.left <= 0) return;
+  const float decay = s.decay;
   AdamwBlock<kKind> in;
-  in.load(s, base);
+  in.load(c, 0);
+#pragma unroll 1
   for (;;) {
     // the next block is on its way while this one is worked on
     AdamwBlock<kKind> next;
-    const bool more = base + kNext < hi;
-    if (kAhead && more) next.load(s, base + kNext);
-    adamw_block<kKind>(s, a, hy, gs, base, in);
+    const bool more = c.left > kNext * MRL_STATE_BLOCK;
+    if (kAhead && more) next.load(c, kNext);
+    adamw_block<kKind>(a, hy, gs, decay, c, in);
     if (!more) break;
-    base += kNext;
-    if (kAhead) in = next; else in.load(s, base);
+    c.advance(kNext);
+    if (kAhead) in = next; else in.load(c, 0);
   }
 }
 
