@@ -111,9 +111,9 @@ def lib() -> C.CDLL:
         L.mrl_rmsnorm_residual_bwd.argtypes = [vp, i64, vp, i64, vp, i64, i32, vp, i32, vp, i64, i32, C.POINTER(NormParams),
                                                vp, i64, vp, vp, sz, vp]
         L.mrl_rmsnorm_residual_bwd.restype = C.c_int
-        L.mrl_grad_norm.argtypes = [C.POINTER(TensorSlotStruct), i32, C.c_float, vp, vp, vp, sz, vp]
+        L.mrl_grad_norm.argtypes = [vp, i32, C.c_float, vp, vp, vp, sz, vp]
         L.mrl_grad_norm.restype = C.c_int
-        L.mrl_adamw_step.argtypes = [C.POINTER(TensorSlotStruct), i32, C.POINTER(AdamwParams), vp, vp, vp, sz, vp]
+        L.mrl_adamw_step.argtypes = [vp, i32, C.POINTER(AdamwParams), vp, vp, vp, sz, vp]
         L.mrl_adamw_step.restype = C.c_int
         L.mrl_workspace_bytes.argtypes = [i32, i64, i32, i32, i32, i32]
         L.mrl_workspace_bytes.restype = sz
@@ -266,46 +266,54 @@ def mrl_thl_word_align_logprobs(src_logp, src_word, src_cu, tgt_word, tgt_cu, wo
                                              _stream(stream)), "mrl_thl_word_align_logprobs")
 
 
-# ---- the norm before the LM head, the gradient norm and the update: the argument checks that need the tensors' shapes
+# ---- the norm before the LM head, the gradient norm and the update: the argument checks that need the tensors' shapes.
+# (Written for little time per call: the smallest calls take the GPU three microseconds.)
 
 _CODES = {torch.float32: F32, torch.bfloat16: BF16}
 _CODE_TYPES = (torch.float8_e4m3fn, torch.uint8)      # how e4m3 codes may be held
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+def _stream_of(device: int, stream, where):
+    """Handle of `stream`, or of the current stream of the tensors' device, which has to be the current device."""
+    if device < 0 or device != torch.cuda.current_device():
+        raise MrlError(1, f"{where}: tensors of the current device are wanted")
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
-def _raw_stream(stream, device):
-    """The stream handle: the current stream of the tensors' device, which has to be the current device."""
-    if device.type != "cuda":
-        raise MrlError(1, f"tensors on {device}")
-    if device.index != torch.cuda.current_device():
-        raise MrlError(1, f"tensors on {device}, which is not the current device")
-    return torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream
-
-
-def _rows(t, N, H, dtypes, device, where):
-    """Row stride of an [N, H] tensor whose columns are adjacent."""
+def _row_stride(t, shape, dtype, device, where):
+    """Row stride of a tensor of [N, H] rows whose columns are adjacent; 0 for none."""
     if t is None:
-        return H
-    if t.dtype not in dtypes:
+        return 0
+    if t.dtype is not dtype and not (dtype is None and t.dtype in _CODE_TYPES):
         raise MrlError(3, where)
-    if t.shape != (N, H) or (H > 1 and t.stride(1) != 1) or t.device != device:
+    if t.shape != shape or t.get_device() != device:
         raise MrlError(1, where)
-    ld = t.stride(0) if N > 1 else H
-    if ld < H:
+    if t.is_contiguous():
+        return shape[1]
+    ld, step = t.stride()
+    if (shape[1] > 1 and step != 1) or (shape[0] > 1 and ld < shape[1]):
         raise MrlError(1, where)
-    return ld
+    return ld if shape[0] > 1 else shape[1]
+
+
+def _float_vector(t, n, device, where):
+    """Address of a contiguous float32 tensor of n elements."""
+    if t is None:
+        return None
+    if t.dtype is not torch.float32:
+        raise MrlError(3, where)
+    if t.numel() != n or t.get_device() != device or not t.is_contiguous():
+        raise MrlError(1, where)
+    return t.data_ptr()
 
 
 def _vector(t, n, dtypes, device, where):
-    """Address of a contiguous tensor of n elements."""
+    """Address of a contiguous tensor of n elements of one of the types."""
     if t is None:
         return None
     if t.dtype not in dtypes:
         raise MrlError(3, where)
-    if t.numel() != n or not t.is_contiguous() or t.device != device:
+    if t.numel() != n or t.get_device() != device or not t.is_contiguous():
         raise MrlError(1, where)
     return t.data_ptr()
 
@@ -315,34 +323,45 @@ _F32_ONLY = (torch.float32,)
 
 def mrl_rmsnorm_residual_fwd(x, residual, weight, np: NormParams, h_out=None, y=None, y8=None, scales=None, rstd=None,
                              stream=None):
-    N, H = x.shape
-    where, dev, own = "mrl_rmsnorm_residual_fwd", x.device, (x.dtype,)
-    code = _CODES.get(x.dtype)
+    where = "mrl_rmsnorm_residual_fwd"
+    shape, dtype, dev = x.shape, x.dtype, x.get_device()
+    N, H = shape
+    code = _CODES.get(dtype)
     if code is None:
         raise MrlError(3, where)
-    st = _raw_stream(stream, dev)
-    groups = -(-H // np.group) if np.group > 0 else 1
-    _check(lib().mrl_rmsnorm_residual_fwd(
-        x.data_ptr(), _rows(x, N, H, own, dev, where), _ptr(residual), _rows(residual, N, H, own, dev, where), code,
-        _vector(weight, H, _CODES, dev, where), _CODES[weight.dtype], N, H, np, _ptr(h_out),
-        _rows(h_out, N, H, own, dev, where), _ptr(y), _rows(y, N, H, own, dev, where), _ptr(y8),
-        _rows(y8, N, H, _CODE_TYPES, dev, where), _vector(scales, N * groups, _F32_ONLY, dev, where),
-        _vector(rstd, N, _F32_ONLY, dev, where), st), where)
+    st = _stream_of(dev, stream, where)
+    w = _vector(weight, H, _CODES, dev, where)
+    ld_x, ld_r = _row_stride(x, shape, dtype, dev, where), _row_stride(residual, shape, dtype, dev, where)
+    ld_h, ld_y = _row_stride(h_out, shape, dtype, dev, where), _row_stride(y, shape, dtype, dev, where)
+    ld_8 = _row_stride(y8, shape, None, dev, where)
+    group = np.group
+    code = lib().mrl_rmsnorm_residual_fwd(
+        x.data_ptr(), ld_x, None if residual is None else residual.data_ptr(), ld_r, code, w, _CODES[weight.dtype], N, H, np,
+        None if h_out is None else h_out.data_ptr(), ld_h, None if y is None else y.data_ptr(), ld_y,
+        None if y8 is None else y8.data_ptr(), ld_8,
+        _float_vector(scales, N * (-(-H // group) if group > 0 else 1), dev, where), _float_vector(rstd, N, dev, where), st)
+    if code != OK:
+        raise MrlError(code, where)
 
 
 def mrl_rmsnorm_residual_bwd(dy, dh, h, weight, rstd, np: NormParams, dx, dweight=None, workspace=None, stream=None):
-    N, H = dy.shape
-    where, dev, own = "mrl_rmsnorm_residual_bwd", dy.device, (dy.dtype,)
-    code = _CODES.get(dy.dtype)
+    where = "mrl_rmsnorm_residual_bwd"
+    shape, dtype, dev = dy.shape, dy.dtype, dy.get_device()
+    N, H = shape
+    code = _CODES.get(dtype)
     if code is None:
         raise MrlError(3, where)
-    st = _raw_stream(stream, dev)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().mrl_rmsnorm_residual_bwd(
-        dy.data_ptr(), _rows(dy, N, H, own, dev, where), _ptr(dh), _rows(dh, N, H, own, dev, where), h.data_ptr(),
-        _rows(h, N, H, own, dev, where), code, _vector(weight, H, _CODES, dev, where), _CODES[weight.dtype],
-        _vector(rstd, N, _F32_ONLY, dev, where), N, H, np, dx.data_ptr(), _rows(dx, N, H, own, dev, where),
-        _vector(dweight, H, _F32_ONLY, dev, where), _ptr(workspace), ws_bytes, st), where)
+    st = _stream_of(dev, stream, where)
+    w = _vector(weight, H, _CODES, dev, where)
+    ld_dy, ld_dh = _row_stride(dy, shape, dtype, dev, where), _row_stride(dh, shape, dtype, dev, where)
+    ld_h, ld_dx = _row_stride(h, shape, dtype, dev, where), _row_stride(dx, shape, dtype, dev, where)
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    code = lib().mrl_rmsnorm_residual_bwd(
+        dy.data_ptr(), ld_dy, None if dh is None else dh.data_ptr(), ld_dh, h.data_ptr(), ld_h, code, w, _CODES[weight.dtype],
+        _float_vector(rstd, N, dev, where), N, H, np, dx.data_ptr(), ld_dx, _float_vector(dweight, H, dev, where), ws, ws_bytes,
+        st)
+    if code != OK:
+        raise MrlError(code, where)
 
 
 class TensorSlot:
@@ -351,7 +370,7 @@ class TensorSlot:
 
     def __init__(self, grad, param=None, master=None, m=None, v=None, m_scale=None, v_scale=None, weight_decay=0.0,
                  rng_first=0):
-        n, dev, where = grad.numel(), grad.device, "TensorSlot"
+        n, dev, where = grad.numel(), grad.get_device(), "TensorSlot"
         s = self.struct = TensorSlotStruct()
         s.grad = _vector(grad, n, _CODES, dev, where)
         s.grad_dtype = _CODES[grad.dtype]
@@ -375,25 +394,30 @@ class TensorList:
         self.slots = list(slots)
         if any(s.device != self.slots[0].device for s in self.slots):
             raise MrlError(1, "TensorList: tensors on several devices")
-        self.device = self.slots[0].device if self.slots else torch.device("cuda", torch.cuda.current_device())
+        self.device = self.slots[0].device if self.slots else torch.cuda.current_device()
         self.n = len(self.slots)
         self.table = (TensorSlotStruct * self.n)(*[s.struct for s in self.slots])
+        self.address = C.addressof(self.table) if self.n else None
 
 
 def mrl_grad_norm(tensors: TensorList, max_norm: float, norm=None, coef=None, workspace=None, stream=None):
     where, dev = "mrl_grad_norm", tensors.device
-    st = _raw_stream(stream, dev)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().mrl_grad_norm(tensors.table, tensors.n, max_norm, _vector(norm, 1, _F32_ONLY, dev, where),
-                               _vector(coef, 1, _F32_ONLY, dev, where), _ptr(workspace), ws_bytes, st), where)
+    st = _stream_of(dev, stream, where)
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    code = lib().mrl_grad_norm(tensors.address, tensors.n, max_norm, _float_vector(norm, 1, dev, where),
+                               _float_vector(coef, 1, dev, where), ws, ws_bytes, st)
+    if code != OK:
+        raise MrlError(code, where)
 
 
 def mrl_adamw_step(tensors: TensorList, ap: AdamwParams, grad_scale=None, status=None, workspace=None, stream=None):
     where, dev = "mrl_adamw_step", tensors.device
-    st = _raw_stream(stream, dev)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().mrl_adamw_step(tensors.table, tensors.n, ap, _vector(grad_scale, 1, _F32_ONLY, dev, where),
-                                _vector(status, 1, (torch.int32,), dev, where), _ptr(workspace), ws_bytes, st), where)
+    st = _stream_of(dev, stream, where)
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    code = lib().mrl_adamw_step(tensors.address, tensors.n, ap, _float_vector(grad_scale, 1, dev, where),
+                                _vector(status, 1, (torch.int32,), dev, where), ws, ws_bytes, st)
+    if code != OK:
+        raise MrlError(code, where)
 
 
 class DominantKernelTimer:
