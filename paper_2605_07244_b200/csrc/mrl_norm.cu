@@ -14,9 +14,9 @@ using namespace mrl;
 
 constexpr int kSms = 148;
 constexpr int kLoopThreads = 512;
-constexpr int kWide = 32, kNarrow = 8;              // columns of a thread of the row kernels
-constexpr int kRowMax = kWide * 512;               // the widest row that one CTA holds
-constexpr int kFwdRegs = 64, kBwdRegs = 80;        // registers of a thread of the row kernels
+constexpr int kFwdWide = 32, kBwdWide = 16, kNarrow = 8;  // columns of a thread of the row kernels
+constexpr int kRowMax = 16384;                            // the widest row that one CTA holds
+constexpr int kFwdRegs = 64, kBwdRegs = 64;               // registers of a thread of the row kernels
 
 template <typename T>
 __device__ __forceinline__ float load_f(const T* p);
@@ -309,7 +309,7 @@ __device__ __forceinline__ float row_scale(float top) { return fmaxf(top * (1.0f
 __device__ __forceinline__ uint32_t peak_bits(float v) { return __float_as_uint(fmaxf(fabsf(v), 0.f)); }
 __host__ __device__ __forceinline__ int image_bytes(int H, int elem) { return (H * elem + 30) / 16 * 16; }
 
-// Sum / maximum of non-negative values over the CTA in a fixed order: one barrier, none for a single warp.  `red` holds 16 floats,
+// Sum / maximum of non-negative values over the CTA in a fixed order: one barrier, none for a single warp.  `red` holds 32 floats,
 // 0 where there is no warp, and is not written again before another barrier.
 template <bool kMax>
 __device__ __forceinline__ float row_reduce(float v, float* red) {
@@ -326,16 +326,19 @@ __device__ __forceinline__ float row_reduce(float v, float* red) {
   __syncthreads();
   const float4* q = reinterpret_cast<const float4*>(red);
   float4 s = q[0];
-  if (blockDim.x > 128) {
+  const auto more = [&](int from, int to) {
 #pragma unroll
-    for (int k = 1; k < 4; ++k) {
+    for (int k = from; k < to; ++k) {
       const float4 u = q[k];
       s.x = kMax ? fmaxf(s.x, u.x) : s.x + u.x;
       s.y = kMax ? fmaxf(s.y, u.y) : s.y + u.y;
       s.z = kMax ? fmaxf(s.z, u.z) : s.z + u.z;
       s.w = kMax ? fmaxf(s.w, u.w) : s.w + u.w;
     }
-  }
+  };
+  if (blockDim.x > 128) more(1, 2);
+  if (blockDim.x > 256) more(2, 4);
+  if (blockDim.x > 512) more(4, 8);
   return kMax ? fmaxf(fmaxf(s.x, s.y), fmaxf(s.z, s.w)) : (s.x + s.y) + (s.z + s.w);
 }
 
@@ -357,7 +360,7 @@ __global__ void __maxnreg__(kFwdRegs) rmsnorm_fwd_row_kernel(const __grid_consta
   using U = Unit<T, kOdd>;
   constexpr int kUnits = kRowCols / U::kCols, kStep = U::kStep, kPairs = U::kPairs, kHalf = kOdd ? 32 : 0;
   extern __shared__ __align__(16) char smem[];
-  __shared__ __align__(16) float red[2][4][16];
+  __shared__ __align__(16) float red[2][4][32];
   __shared__ uint32_t peak[kRowMax / 32];
   const int tid = threadIdx.x, nt = blockDim.x;
   const int c0 = (tid >> 5) * (kUnits * kStep) + (tid & 31) * (kOdd ? 1 : U::kCols);
@@ -368,7 +371,7 @@ __global__ void __maxnreg__(kFwdRegs) rmsnorm_fwd_row_kernel(const __grid_consta
   const int group = a.group > 0 ? a.group : a.H, groups = (a.H + group - 1) / group;
   // lanes whose columns share a scale sit side by side; more than a warp of them meet in shared memory
   const bool meet = a.y8 != nullptr && a.group > (kOdd ? 32 : kStep);
-  for (int k = tid; k < 128; k += nt) (&red[0][0][0])[k] = 0.f;
+  for (int k = tid; k < 256; k += nt) (&red[0][0][0])[k] = 0.f;
   __syncthreads();
 
   const auto fetch = [&](long long row, int s) {
@@ -597,13 +600,13 @@ __global__ void __maxnreg__(kBwdRegs) rmsnorm_bwd_row_kernel(const __grid_consta
   using U = Unit<T, kOdd>;
   constexpr int kUnits = kRowCols / U::kCols, kStep = U::kStep, kPairs = U::kPairs, kHalf = kOdd ? 32 : 0;
   extern __shared__ __align__(16) char smem[];
-  __shared__ __align__(16) float red[2][16];
+  __shared__ __align__(16) float red[2][32];
   const int tid = threadIdx.x, nt = blockDim.x;
   const int c0 = (tid >> 5) * (kUnits * kStep) + (tid & 31) * (kOdd ? 1 : U::kCols);
   const bool full = ((tid >> 5) + 1) * (kUnits * kStep) <= a.H;
   const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : nt * kRowCols * (int)sizeof(T);
   const int stage = a.dh != nullptr ? 3 * slot : 2 * slot;
-  if (tid < 32) (&red[0][0])[tid] = 0.f;
+  for (int k = tid; k < 64; k += nt) (&red[0][0])[k] = 0.f;
   __syncthreads();
 
   const auto fetch = [&](long long row, int s) {
@@ -741,25 +744,34 @@ __global__ void __maxnreg__(kBwdRegs) rmsnorm_bwd_row_kernel(const __grid_consta
   }
 }
 
-// dweight[i] = sum over the CTAs' partials, in their order within each of 8 lanes and then over the lanes.
-__global__ void __launch_bounds__(256) rmsnorm_dw_kernel(const float* __restrict__ partial, int rows, int H,
-                                                         float* __restrict__ dw, bool accumulate) {
-  __shared__ float red[8][33];
-  const int col = blockIdx.x * 32 + (threadIdx.x & 31), lane = threadIdx.x >> 5;
+// dweight[i] = sum over the CTAs' partials, in their order within each of 32 lanes and then over the lanes.
+__global__ void __launch_bounds__(1024) rmsnorm_dw_kernel(const float* __restrict__ partial, int rows, int H,
+                                                          float* __restrict__ dw, bool accumulate) {
+  __shared__ float red[32][33];
+  const int x = threadIdx.x & 31, lane = threadIdx.x >> 5, col = blockIdx.x * 32 + x;
   float s = 0.f;
-  if (col < H)
-    for (int k = lane; k < rows; k += 8) s += partial[(size_t)k * H + col];
-  red[lane][threadIdx.x & 31] = s;
-  __syncthreads();
-  if (lane == 0 && col < H) {
-    for (int k = 1; k < 8; ++k) s += red[k][threadIdx.x];
-    dw[col] = accumulate ? dw[col] + s : s;
+  if (col < H) {
+    int k = lane;
+    for (; k + 96 < rows; k += 128) {  // four loads under way
+      const float a = partial[(size_t)k * H + col], b = partial[(size_t)(k + 32) * H + col];
+      const float c = partial[(size_t)(k + 64) * H + col], d = partial[(size_t)(k + 96) * H + col];
+      s += a, s += b, s += c, s += d;
+    }
+    for (; k < rows; k += 32) s += partial[(size_t)k * H + col];
   }
+  red[lane][x] = s;
+  __syncthreads();
+  // a warp adds up one column: 32 lanes in a tree
+  float t = red[x][lane];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+  const int out = blockIdx.x * 32 + lane;
+  if (x == 0 && out < H) dw[out] = accumulate ? dw[out] + t : t;
 }
 
 int row_threads(int H, int cols) { return (H + cols * 32 - 1) / (cols * 32) * 32; }
 // Few rows, or short ones, are spread over more threads.
-int row_cols(long long N, int H) { return H <= 512 || (H <= 512 * kNarrow && N <= 2 * kSms) ? kNarrow : kWide; }
+int row_cols(long long N, int H, int wide) { return H <= 512 || (H <= 512 * kNarrow && N <= 2 * kSms) ? kNarrow : wide; }
 
 bool aligned(const void* p, long long ld, int elem, int bytes) {
   return p == nullptr || ((reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0 && (ld * elem) % bytes == 0);
@@ -786,7 +798,7 @@ RowPlan plan_rows(int threads, int regs, int stage_bytes, int out_bytes) {
 }
 // CTAs of the backward kernels, and rows of dweight partials; the most that any alignment and type of the rows leads to.
 int bwd_ctas(long long N, int per_sm) { return (int)(N < (long long)kSms * per_sm ? N : (long long)kSms * per_sm); }
-int bwd_ctas_most(long long N, int H) { return bwd_ctas(N, H <= kRowMax ? plan_rows(row_threads(H, kWide), kBwdRegs, 0, 0).ctas_per_sm : 2); }
+int bwd_ctas_most(long long N, int H) { return bwd_ctas(N, H <= kRowMax ? plan_rows(row_threads(H, kBwdWide), kBwdRegs, 0, 0).ctas_per_sm : 2); }
 
 template <typename K>
 int allow_smem(K kernel, std::atomic<uint64_t>& done) {
@@ -827,14 +839,15 @@ int launch_bwd_rows(NormBwdArgs a, int* ctas, cudaStream_t st) {
 }
 template <typename T>
 int launch_fwd(const NormFwdArgs& a, bool odd, cudaStream_t st) {
-  if (row_cols(a.N, a.H) == kNarrow) return odd ? launch_fwd_rows<T, true, kNarrow>(a, st) : launch_fwd_rows<T, false, kNarrow>(a, st);
-  return odd ? launch_fwd_rows<T, true, kWide>(a, st) : launch_fwd_rows<T, false, kWide>(a, st);
+  if (row_cols(a.N, a.H, kFwdWide) == kNarrow)
+    return odd ? launch_fwd_rows<T, true, kNarrow>(a, st) : launch_fwd_rows<T, false, kNarrow>(a, st);
+  return odd ? launch_fwd_rows<T, true, kFwdWide>(a, st) : launch_fwd_rows<T, false, kFwdWide>(a, st);
 }
 template <typename T>
 int launch_bwd(const NormBwdArgs& a, bool odd, int* ctas, cudaStream_t st) {
-  if (row_cols(a.N, a.H) == kNarrow)
+  if (row_cols(a.N, a.H, kBwdWide) == kNarrow)
     return odd ? launch_bwd_rows<T, true, kNarrow>(a, ctas, st) : launch_bwd_rows<T, false, kNarrow>(a, ctas, st);
-  return odd ? launch_bwd_rows<T, true, kWide>(a, ctas, st) : launch_bwd_rows<T, false, kWide>(a, ctas, st);
+  return odd ? launch_bwd_rows<T, true, kBwdWide>(a, ctas, st) : launch_bwd_rows<T, false, kBwdWide>(a, ctas, st);
 }
 
 bool row_type_ok(int32_t dtype) { return dtype == MRL_BF16 || dtype == MRL_F32; }
@@ -926,7 +939,7 @@ extern "C" int mrl_rmsnorm_residual_bwd(const void* dy, int64_t ld_dy, const voi
   }
   if (rc != MRL_OK) return rc;
   if (dweight != nullptr) {
-    rmsnorm_dw_kernel<<<(H + 31) / 32, 256, 0, st>>>(a.partial, ctas, H, dweight, accumulate);
+    rmsnorm_dw_kernel<<<(H + 31) / 32, 1024, 0, st>>>(a.partial, ctas, H, dweight, accumulate);
     MRL_CUDA_OK(cudaGetLastError());
   }
   return MRL_OK;
