@@ -52,6 +52,22 @@ struct MrlCarver {
   }
 };
 
+// Launches a kernel that may start while the one before it in the stream is still running: it waits by itself
+// (mrl::wait_for_previous) before it reads what that one writes, and its launch costs no time in between.
+template <typename... Params, typename... Args>
+static inline cudaError_t mrl_launch_behind(void (*kernel)(Params...), unsigned grid, unsigned threads, cudaStream_t st, Args... args) {
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.stream = st;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+
 // Per-row scratch of the loss passes (carved from the caller's workspace) and the host steps around the row kernels.
 struct MrlLossWs {
   float *rowA, *rowcu, *rowcn;        // A_t, c_t u_t, cn_t
@@ -98,6 +114,11 @@ __device__ __forceinline__ float ex2_approx(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+
+// mrl_launch_behind: in the first kernel, the second one may be launched once all CTAs have come here; in the second, the
+// first one has ended and its writes are there.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // base-2 log-sum-exp (in units of MRL_LOG2E) -> nats
 __device__ __forceinline__ float lse2_to_nats(float lse2) { return fmaf(lse2, MRL_NAT_HI, lse2 * MRL_NAT_LO); }

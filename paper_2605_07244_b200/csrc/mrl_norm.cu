@@ -14,7 +14,7 @@ using namespace mrl;
 
 constexpr int kSms = 148;
 constexpr int kLoopThreads = 512;
-constexpr int kFwdWide = 32, kBwdWide = 16, kNarrow = 8;  // columns of a thread of the row kernels
+constexpr int kWide = 32, kMiddle = 16, kNarrow = 8;      // columns of a thread of the row kernels
 constexpr int kRowMax = 16384;                            // the widest row that one CTA holds
 constexpr int kFwdRegs = 64, kBwdRegs = 64;               // registers of a thread of the row kernels
 
@@ -135,6 +135,7 @@ __global__ void __launch_bounds__(kLoopThreads) rmsnorm_bwd_loop_kernel(NormBwdA
   __shared__ float red[32];
   const int tid = threadIdx.x, nt = blockDim.x;
   float* part = a.partial != nullptr ? a.partial + (size_t)blockIdx.x * a.H : nullptr;
+  let_next_start();
   for (long long row = blockIdx.x; row < a.N; row += gridDim.x) {
     const T* dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
     const T* hr = static_cast<const T*>(a.h) + row * a.ld_h;
@@ -606,6 +607,7 @@ __global__ void __maxnreg__(kBwdRegs) rmsnorm_bwd_row_kernel(const __grid_consta
   const bool full = ((tid >> 5) + 1) * (kUnits * kStep) <= a.H;
   const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : nt * kRowCols * (int)sizeof(T);
   const int stage = a.dh != nullptr ? 3 * slot : 2 * slot;
+  let_next_start();
   for (int k = tid; k < 64; k += nt) (&red[0][0])[k] = 0.f;
   __syncthreads();
 
@@ -745,10 +747,10 @@ __global__ void __maxnreg__(kBwdRegs) rmsnorm_bwd_row_kernel(const __grid_consta
 }
 
 // dweight[i] = sum over the CTAs' partials, in their order within each of 32 lanes and then over the lanes.
-__global__ void __launch_bounds__(1024) rmsnorm_dw_kernel(const float* __restrict__ partial, int rows, int H,
-                                                          float* __restrict__ dw, bool accumulate) {
+__global__ void __launch_bounds__(1024) rmsnorm_dw_kernel(const float* partial, int rows, int H, float* dw, bool accumulate) {
   __shared__ float red[32][33];
   const int x = threadIdx.x & 31, lane = threadIdx.x >> 5, col = blockIdx.x * 32 + x;
+  wait_for_previous();
   float s = 0.f;
   if (col < H) {
     int k = lane;
@@ -770,8 +772,17 @@ __global__ void __launch_bounds__(1024) rmsnorm_dw_kernel(const float* __restric
 }
 
 int row_threads(int H, int cols) { return (H + cols * 32 - 1) / (cols * 32) * 32; }
-// Few rows, or short ones, are spread over more threads.
-int row_cols(long long N, int H, int wide) { return H <= 512 || (H <= 512 * kNarrow && N <= 2 * kSms) ? kNarrow : wide; }
+// Columns of a thread.  Few rows, or short ones, are spread over more threads (one row of 4,096: 2.5 us with 8 columns, 3.4
+// with 32; 262,144 rows of 64: 93 us with 8, 133 with 16).  Forward, 32 columns are fastest for rows of 2 to 16 KB in 16-byte
+// granules once there are many (65,536 x 4,096 bf16: 341 us with 32, 374 with 16; 32,768 x 8,192: 338, 357), 16 for wider rows
+// (16,384 x 16,384: 356, 339), for fewer (1,024 x 4,096: 8.9, 7.6) and for odd ones (65,552 x 4,095: 727, 633).  Backward,
+// whose sums take registers, 16 (65,536 x 4,096: 394 with 32, 367 with 16).
+bool few_or_short(long long N, int H) { return H <= 512 || (H <= 512 * kNarrow && N <= 2 * kSms); }
+int fwd_cols(long long N, int H, int elem, bool odd) {
+  if (few_or_short(N, H)) return kNarrow;
+  return !odd && N > 2048 && H * elem >= 2048 && H * elem <= 16384 ? kWide : kMiddle;
+}
+int bwd_cols(long long N, int H) { return few_or_short(N, H) ? kNarrow : kMiddle; }
 
 bool aligned(const void* p, long long ld, int elem, int bytes) {
   return p == nullptr || ((reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0 && (ld * elem) % bytes == 0);
@@ -797,8 +808,12 @@ RowPlan plan_rows(int threads, int regs, int stage_bytes, int out_bytes) {
   return p;
 }
 // CTAs of the backward kernels, and rows of dweight partials; the most that any alignment and type of the rows leads to.
-int bwd_ctas(long long N, int per_sm) { return (int)(N < (long long)kSms * per_sm ? N : (long long)kSms * per_sm); }
-int bwd_ctas_most(long long N, int H) { return bwd_ctas(N, H <= kRowMax ? plan_rows(row_threads(H, kBwdWide), kBwdRegs, 0, 0).ctas_per_sm : 2); }
+// Four rows a CTA at least once every SM has one: the partials cost as much as rows.
+int bwd_ctas(long long N, int per_sm) {
+  const long long most = (long long)kSms * per_sm, few = N / 4 > kSms ? N / 4 : kSms;
+  return (int)(N < few ? N : (few < most ? few : most));
+}
+int bwd_ctas_most(long long N, int H) { return bwd_ctas(N, H <= kRowMax ? plan_rows(row_threads(H, kMiddle), kBwdRegs, 0, 0).ctas_per_sm : 2); }
 
 template <typename K>
 int allow_smem(K kernel, std::atomic<uint64_t>& done) {
@@ -839,15 +854,17 @@ int launch_bwd_rows(NormBwdArgs a, int* ctas, cudaStream_t st) {
 }
 template <typename T>
 int launch_fwd(const NormFwdArgs& a, bool odd, cudaStream_t st) {
-  if (row_cols(a.N, a.H, kFwdWide) == kNarrow)
-    return odd ? launch_fwd_rows<T, true, kNarrow>(a, st) : launch_fwd_rows<T, false, kNarrow>(a, st);
-  return odd ? launch_fwd_rows<T, true, kFwdWide>(a, st) : launch_fwd_rows<T, false, kFwdWide>(a, st);
+  switch (fwd_cols(a.N, a.H, sizeof(T), odd)) {
+    case kNarrow: return odd ? launch_fwd_rows<T, true, kNarrow>(a, st) : launch_fwd_rows<T, false, kNarrow>(a, st);
+    case kMiddle: return odd ? launch_fwd_rows<T, true, kMiddle>(a, st) : launch_fwd_rows<T, false, kMiddle>(a, st);
+    default: return launch_fwd_rows<T, false, kWide>(a, st);
+  }
 }
 template <typename T>
 int launch_bwd(const NormBwdArgs& a, bool odd, int* ctas, cudaStream_t st) {
-  if (row_cols(a.N, a.H, kBwdWide) == kNarrow)
+  if (bwd_cols(a.N, a.H) == kNarrow)
     return odd ? launch_bwd_rows<T, true, kNarrow>(a, ctas, st) : launch_bwd_rows<T, false, kNarrow>(a, ctas, st);
-  return odd ? launch_bwd_rows<T, true, kBwdWide>(a, ctas, st) : launch_bwd_rows<T, false, kBwdWide>(a, ctas, st);
+  return odd ? launch_bwd_rows<T, true, kMiddle>(a, ctas, st) : launch_bwd_rows<T, false, kMiddle>(a, ctas, st);
 }
 
 bool row_type_ok(int32_t dtype) { return dtype == MRL_BF16 || dtype == MRL_F32; }
@@ -939,8 +956,7 @@ extern "C" int mrl_rmsnorm_residual_bwd(const void* dy, int64_t ld_dy, const voi
   }
   if (rc != MRL_OK) return rc;
   if (dweight != nullptr) {
-    rmsnorm_dw_kernel<<<(H + 31) / 32, 1024, 0, st>>>(a.partial, ctas, H, dweight, accumulate);
-    MRL_CUDA_OK(cudaGetLastError());
+    MRL_CUDA_OK(mrl_launch_behind(rmsnorm_dw_kernel, (unsigned)((H + 31) / 32), 1024, st, a.partial, ctas, H, dweight, accumulate));
   }
   return MRL_OK;
 }
