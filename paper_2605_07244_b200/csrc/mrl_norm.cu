@@ -284,25 +284,24 @@ __device__ __forceinline__ Image image_of(P* base, long long element, int H) {
 template <typename T>
 __device__ __forceinline__ void image_load(char* dst, const Image& im, bool first_row) {
   const int end = im.off + im.len;
-  for (int k = threadIdx.x; 16 * k < end; k += blockDim.x) {
-    if (k == 0 && first_row && im.off != 0) {
-      for (int b = im.off; b < min(16, end); b += (int)sizeof(T)) *reinterpret_cast<T*>(dst + b) = *reinterpret_cast<const T*>(im.first + b);
-    } else {
-      copy_async(dst + 16 * k, im.first + 16 * k, min(16, end - 16 * k));
-    }
+  const bool by_element = first_row && im.off != 0;
+  for (int k = threadIdx.x + by_element; 16 * k < end; k += blockDim.x) copy_async(dst + 16 * k, im.first + 16 * k, min(16, end - 16 * k));
+  if (by_element) {
+    const int b = im.off + (int)threadIdx.x * (int)sizeof(T);
+    if (b < min(16, end)) *reinterpret_cast<T*>(dst + b) = *reinterpret_cast<const T*>(im.first + b);
   }
 }
-// The copy's granules to the row: whole ones at once, the first and the last by element.
+// The copy's granules to the row: whole ones at once, what the row has of its first and last one by element.
 template <typename P>
 __device__ __forceinline__ void image_store(const char* src, const Image& im) {
-  const int end = im.off + im.len;
-  for (int k = threadIdx.x; 16 * k < end; k += blockDim.x) {
-    const int lo = max(im.off, 16 * k), hi = min(end, 16 * k + 16);
-    if (hi - lo == 16) {
-      *reinterpret_cast<uint4*>(im.first + 16 * k) = *reinterpret_cast<const uint4*>(src + 16 * k);
-    } else {
-      for (int b = lo; b < hi; b += (int)sizeof(P)) *reinterpret_cast<P*>(im.first + b) = *reinterpret_cast<const P*>(src + b);
-    }
+  const int end = im.off + im.len, from = im.off != 0, to = end / 16;
+  for (int k = from + (int)threadIdx.x; k < to; k += blockDim.x)
+    *reinterpret_cast<uint4*>(im.first + 16 * k) = *reinterpret_cast<const uint4*>(src + 16 * k);
+  if (threadIdx.x < 32) {
+    const int j = (threadIdx.x & 15) * (int)sizeof(P), tail = max(to, from) * 16 + j, head = im.off + j;
+    const bool first = threadIdx.x < 16;
+    const int b = first ? head : tail;
+    if (first ? im.off != 0 && b < min(16, end) : b < end) *reinterpret_cast<P*>(im.first + b) = *reinterpret_cast<const P*>(src + b);
   }
 }
 // The scale of 8-bit rows (two units in the last place of max / 448 at most), and a magnitude as an ordered integer, 0 for NaN.
