@@ -14,7 +14,6 @@ using namespace mrl;
 
 constexpr int kThreads = 256;
 constexpr int kChunk = 8 * MRL_STATE_BLOCK;   // elements of a CTA at least: a state block per warp
-constexpr int kChunksMost = 8;
 constexpr int kSlotsFew = 16, kSlots = 160;   // tensors per launch: the tables stay below the 32,764 bytes of kernel arguments
 constexpr int kSms = 148;
 constexpr int kNormCtas = kSms * 8;
@@ -397,15 +396,6 @@ __device__ __forceinline__ void adamw_block(const AdamwArgs& a, const Hyper& hy,
   const int n = c.count();
   const bool vec = c.vec();
   f2 m[4], v[4], p[4];
-  uint32_t bits[8];  // of each element: 16 for m, 16 for v above them
-  if (a.seeded && (kCodes || (kParamBf16 && !kMaster))) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const unsigned long long w = splitmix64(c.word + j);
-      bits[2 * j] = (uint32_t)w;
-      bits[2 * j + 1] = (uint32_t)(w >> 32);
-    }
-  }
   if constexpr (kCodes) {
     decode(in.cm, in.sm, m);
     decode(in.cv, in.sv, v);
@@ -445,6 +435,15 @@ __device__ __forceinline__ void adamw_block(const AdamwArgs& a, const Hyper& hy,
     const float2 den = split_f2(fma_f2(root[j], rc2, eps2));
     const f2 quot = mul_f2(mul_f2(m[j], lr2), make_f2(rcp_approx(den.x), rcp_approx(den.y)));
     p[j] = add_f2(p[j], fma_f2(keep2, p[j], quot));
+  }
+  uint32_t bits[8];  // of each element: 16 for m, 16 for v above them
+  if (a.seeded && (kCodes || (kParamBf16 && !kMaster))) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const unsigned long long w = splitmix64(c.word + j);
+      bits[2 * j] = (uint32_t)w;
+      bits[2 * j + 1] = (uint32_t)(w >> 32);
+    }
   }
   if constexpr (kMaster) store8(c.p, n, vec, p);
   if constexpr (kParamBf16) {
@@ -649,17 +648,17 @@ int fill_table(const mrl_tensor_slot* slots, int n, int at, int chunk, int only,
   return at;
 }
 
-// Elements of a chunk: small ones while there are few, for the sake of parallel CTAs.
-int chunk_of(const mrl_tensor_slot* slots, int n) {
+// Elements of a chunk: small ones while there are few, for the sake of parallel CTAs; `most` times as many otherwise.
+int chunk_of(const mrl_tensor_slot* slots, int n, int most) {
   long long total = 0;
   for (int k = 0; k < n; ++k) total += slots[k].numel;
-  return total <= (long long)kSms * 8 * 4 * kChunk ? kChunk : kChunksMost * kChunk;
+  return total <= (long long)kSms * 8 * 4 * kChunk ? kChunk : most * kChunk;
 }
 
 template <int kN>
 int launch_grad_norm(const mrl_tensor_slot* slots, int n, float max_norm, float* norm, float* coef, double* partial, cudaStream_t st) {
   Table<kN> t;
-  const int chunk = chunk_of(slots, n);
+  const int chunk = chunk_of(slots, n, 8);
   int ctas = 0;
   for (int at = 0; at < n || ctas == 0;) {
     at = fill_table(slots, n, at, chunk, -1, &t);
@@ -774,11 +773,13 @@ extern "C" int mrl_adamw_step(const mrl_tensor_slot* slots, int32_t n_slots, con
   }
   int count[16] = {0};
   for (int k = 0; k < n_slots; ++k) count[kind_of(slots[k])] += slots[k].numel > 0;
-  const int chunk = chunk_of(slots, n_slots);
+  // (output layer, 622 M elements: 2,583 us with chunks of 4 and float32 states, 2,624 with 8; 8-bit, whose next block is on its
+  // way while one is worked on: 1,525 and 1,391)
+  const int chunk[2] = {chunk_of(slots, n_slots, 4), chunk_of(slots, n_slots, 8)};
   int rc = MRL_OK;
   const auto run = [&](auto kind) {
     constexpr int kKind = decltype(kind)::value;
-    if (rc == MRL_OK) rc = launch_adamw<kKind>(slots, n_slots, count[kKind], chunk, a, st);
+    if (rc == MRL_OK) rc = launch_adamw<kKind>(slots, n_slots, count[kKind], chunk[kKind >> 3], a, st);
   };
   run(std::integral_constant<int, 0>{}), run(std::integral_constant<int, 1>{}), run(std::integral_constant<int, 3>{});
   run(std::integral_constant<int, 4>{}), run(std::integral_constant<int, 5>{}), run(std::integral_constant<int, 7>{});
