@@ -318,6 +318,15 @@ def _vector(t, n, dtypes, device, where):
     return t.data_ptr()
 
 
+def _workspace(t, device, where):
+    """Address and bytes of a workspace."""
+    if t is None:
+        return None, 0
+    if t.get_device() != device:
+        raise MrlError(1, where)
+    return t.data_ptr(), t.nbytes
+
+
 _F32_ONLY = (torch.float32,)
 
 
@@ -355,7 +364,7 @@ def mrl_rmsnorm_residual_bwd(dy, dh, h, weight, rstd, np: NormParams, dx, dweigh
     w = _vector(weight, H, _CODES, dev, where)
     ld_dy, ld_dh = _row_stride(dy, shape, dtype, dev, where), _row_stride(dh, shape, dtype, dev, where)
     ld_h, ld_dx = _row_stride(h, shape, dtype, dev, where), _row_stride(dx, shape, dtype, dev, where)
-    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    ws, ws_bytes = _workspace(workspace, dev, where)
     code = lib().mrl_rmsnorm_residual_bwd(
         dy.data_ptr(), ld_dy, None if dh is None else dh.data_ptr(), ld_dh, h.data_ptr(), ld_h, code, w, _CODES[weight.dtype],
         _float_vector(rstd, N, dev, where), N, H, np, dx.data_ptr(), ld_dx, _float_vector(dweight, H, dev, where), ws, ws_bytes,
@@ -403,7 +412,7 @@ class TensorList:
 def mrl_grad_norm(tensors: TensorList, max_norm: float, norm=None, coef=None, workspace=None, stream=None):
     where, dev = "mrl_grad_norm", tensors.device
     st = _stream_of(dev, stream, where)
-    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    ws, ws_bytes = _workspace(workspace, dev, where)
     code = lib().mrl_grad_norm(tensors.address, tensors.n, max_norm, _float_vector(norm, 1, dev, where),
                                _float_vector(coef, 1, dev, where), ws, ws_bytes, st)
     if code != OK:
@@ -413,7 +422,7 @@ def mrl_grad_norm(tensors: TensorList, max_norm: float, norm=None, coef=None, wo
 def mrl_adamw_step(tensors: TensorList, ap: AdamwParams, grad_scale=None, status=None, workspace=None, stream=None):
     where, dev = "mrl_adamw_step", tensors.device
     st = _stream_of(dev, stream, where)
-    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    ws, ws_bytes = _workspace(workspace, dev, where)
     code = lib().mrl_adamw_step(tensors.address, tensors.n, ap, _float_vector(grad_scale, 1, dev, where),
                                 _vector(status, 1, (torch.int32,), dev, where), ws, ws_bytes, st)
     if code != OK:

@@ -144,8 +144,9 @@ __device__ __forceinline__ float2 unpack_e4m3x2(uint16_t codes) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"(codes));
   return __half22float2(*reinterpret_cast<const __half2*>(&h2));  // every e4m3 value is a half
 }
-// The scale of a group of e4m3 codes: its largest magnitude lands on 448.  Not below 2^-126, so that 1 / scale is finite.
-__device__ __forceinline__ float e4m3_scale(float amax) { return fmaxf(amax / 448.0f, 1.17549435e-38f); }
+// The scale of a group of e4m3 codes: its largest magnitude lands on 448 (the product with the rounded 1 / 448 is off by two
+// halves of a unit in the last place at most).  Not below 2^-126, so that 1 / scale is finite.
+__device__ __forceinline__ float e4m3_scale(float amax) { return fmaxf(amax * (1.0f / 448.0f), 1.17549435e-38f); }
 
 // Two floats in a register pair: Blackwell adds, multiplies and fuses them with one instruction (kernels that stream with
 // little arithmetic per byte still issue enough of it for this to show).

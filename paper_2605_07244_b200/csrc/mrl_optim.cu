@@ -75,6 +75,12 @@ __device__ __forceinline__ float rcp_approx(float x) {
 
 constexpr float kRootMin = 1e-25f, kRootMax = 1e37f;  // where newton_root holds: s^2 and the residual stay normal
 
+// a + b of two products: a packed sum of packed products is compiled to a fused multiply-add, a single one is not.
+__device__ __forceinline__ f2 add_apart(f2 a, f2 b) {
+  const float2 u = split_f2(a), v = split_f2(b);
+  return make_f2(__fadd_rn(u.x, v.x), __fadd_rn(u.y, v.y));
+}
+
 __device__ __forceinline__ f2 newton_root(f2 v) {
   const float2 u = split_f2(v);
   float a, b;
@@ -83,15 +89,6 @@ __device__ __forceinline__ f2 newton_root(f2 v) {
   const f2 y = make_f2(a, b), s = mul_f2(v, y), half = mul_f2(y, make_f2(-0.5f, -0.5f));
   return fma_f2(fma_f2(s, s, v ^ 0x8000000080000000ull), half, s);  // s + (v - s^2) / (2 s), the signs moved together
 }
-__device__ __forceinline__ float newton_over_448(float x) {
-  const float c = 1.0f / 448.0f, q = x * c;
-  return fmaf(fmaf(-448.0f, q, x), c, q);
-}
-__device__ __forceinline__ float newton_reciprocal(float x) {
-  const float y = rcp_approx(x);
-  return fmaf(y, fmaf(-x, y, 1.0f), y);
-}
-
 __device__ __forceinline__ double block_sum(double v, double* red) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -264,16 +261,6 @@ __device__ __forceinline__ void bounds8(const f2 (&x)[4], uint32_t* least, uint3
     *most = max(max(a, b), *most);
   }
 }
-// The scale of a block and its reciprocal as IEEE quotients, corrected on their fused residuals the same way.
-__device__ __forceinline__ void block_scale(float amax, float* scale, float* inv) {
-  *scale = newton_over_448(amax);
-  *inv = newton_reciprocal(*scale);
-  if (!(amax >= 1e-30f && amax <= 1e30f)) {
-    *scale = e4m3_scale(amax);
-    *inv = __frcp_rn(*scale);
-  }
-}
-
 // |y| (at most about 448, not NaN) with the part below an e4m3 step rounded up with probability remainder / step: the 16
 // bits are added below the last kept bit and the rest is cut.  Below 2^-6 the codes are 2^-9 apart, as they are from 2^-6
 // to 2^-5: the value is moved there and back.
@@ -317,7 +304,7 @@ __device__ __forceinline__ void encode(const f2 (&x)[4], float least, float inv,
 }
 
 // One block of MRL_STATE_BLOCK elements by a warp.  The moments are rounded operation by operation as the formula stands
-// (no fused multiply-add) and the 8-bit states take the IEEE root and quotients: the codes, which feed the next step, are
+// (no fused multiply-add) and the 8-bit states take the IEEE root and reciprocal: the codes, which feed the next step, are
 // then the same for every evaluation of the formula in float32, and a value on the border between two codes does not
 // depend on how an expression was contracted.
 // kKind: kind_of().
@@ -417,8 +404,8 @@ __device__ __forceinline__ void adamw_block(const AdamwArgs& a, const Hyper& hy,
   for (int j = 0; j < 4; ++j) {
     const f2 gj = mul_f2(in.g.pair(j), gs2);
     p[j] = in.p.pair(j);
-    m[j] = add_f2(mul_f2(b1, m[j]), mul_f2(o1, gj));
-    v[j] = add_f2(mul_f2(b2, v[j]), mul_f2(o2, mul_f2(gj, gj)));
+    m[j] = add_apart(mul_f2(b1, m[j]), mul_f2(o1, gj));
+    v[j] = add_apart(mul_f2(b2, v[j]), mul_f2(o2, mul_f2(gj, gj)));
   }
   uint32_t least_m = 0, most_m = 0, least_v = 0, most_v = 0;
   if constexpr (kCodes) {
@@ -479,18 +466,17 @@ __device__ __forceinline__ void adamw_block(const AdamwArgs& a, const Hyper& hy,
   if constexpr (kCodes) {
     most_m = __reduce_max_sync(0xffffffffu, most_m);
     most_v = __reduce_max_sync(0xffffffffu, most_v);
-    float sm, sv, inv_m, inv_v;
-    block_scale(__uint_as_float(most_m), &sm, &inv_m);
-    block_scale(__fsqrt_rn(__uint_as_float(most_v)), &sv, &inv_v);  // (the largest root is the root of the largest)
+    const float sm = e4m3_scale(__uint_as_float(most_m));
+    const float sv = e4m3_scale(__fsqrt_rn(__uint_as_float(most_v)));  // (the largest root is the root of the largest)
     if ((threadIdx.x & 31) == 0) {
       *c.ms = sm;
       *c.vs = sv;
     }
     uint32_t codes[2];
     const bool seeded = a.seeded && most_m < 0x7f800000u && most_v < 0x7f800000u;  // (the dither's arithmetic on bits is for numbers)
-    encode<false>(m, __uint_as_float(least_m), inv_m, seeded, bits, codes);
+    encode<false>(m, __uint_as_float(least_m), __frcp_rn(sm), seeded, bits, codes);
     store_codes(c.m, n, vec, codes);
-    encode<true>(root, sqrt_approx(__uint_as_float(least_v)) * 0.9999f, inv_v, seeded, bits, codes);
+    encode<true>(root, sqrt_approx(__uint_as_float(least_v)) * 0.9999f, __frcp_rn(sv), seeded, bits, codes);
     store_codes(c.v, n, vec, codes);
   } else {
     store8(c.m, n, vec, m);
