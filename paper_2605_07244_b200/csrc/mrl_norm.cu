@@ -15,8 +15,10 @@ using namespace mrl;
 constexpr int kSms = 148;
 constexpr int kLoopThreads = 512;
 constexpr int kWide = 32, kMiddle = 16, kNarrow = 8;      // columns of a thread of the row kernels
+constexpr int kNoCodes = 0, kRowCodes = 1, kGroupCodes = 2;
 constexpr int kRowMax = 16384;                            // the widest row that one CTA holds
-constexpr int kFwdRegs = 64, kBwdRegs = 64;               // registers of a thread of the row kernels
+constexpr int kBwdRegs = 64;                              // registers of a thread of the row kernels
+constexpr int fwd_regs(int cols) { return cols == kWide ? 80 : 64; }  // (wide: shared memory allows no more CTAs anyway)
 
 template <typename T>
 __device__ __forceinline__ float load_f(const T* p);
@@ -354,8 +356,9 @@ __host__ __device__ __forceinline__ int fwd_slots(const NormFwdArgs& a, bool odd
 // column after a barrier, and outputs go the same way back.
 // Columns: a warp owns 32 * kRowCols adjacent ones, unit u of a lane lies u * kStep behind its first.  A warp whose columns
 // all lie inside the row runs without tests (kFull).
-template <typename T, bool kOdd, int kRowCols>
-__global__ void __maxnreg__(kFwdRegs) rmsnorm_fwd_row_kernel(const __grid_constant__ NormFwdArgs a) {
+// kCodes: what of y8 there is (its code costs registers): nothing, one scale a row, one a group.
+template <typename T, bool kOdd, int kRowCols, int kCodes>
+__global__ void __maxnreg__(fwd_regs(kRowCols)) rmsnorm_fwd_row_kernel(const __grid_constant__ NormFwdArgs a) {
   using U = Unit<T, kOdd>;
   constexpr int kUnits = kRowCols / U::kCols, kStep = U::kStep, kPairs = U::kPairs, kHalf = kOdd ? 32 : 0;
   extern __shared__ __align__(16) char smem[];
@@ -369,7 +372,7 @@ __global__ void __maxnreg__(kFwdRegs) rmsnorm_fwd_row_kernel(const __grid_consta
   char* img_q = smem + a.stages * stage;
   const int group = a.group > 0 ? a.group : a.H, groups = (a.H + group - 1) / group;
   // lanes whose columns share a scale sit side by side; more than a warp of them meet in shared memory
-  const bool meet = a.y8 != nullptr && a.group > (kOdd ? 32 : kStep);
+  const bool meet = kCodes == kGroupCodes && a.group > (kOdd ? 32 : kStep);
   for (int k = tid; k < 256; k += nt) (&red[0][0][0])[k] = 0.f;
   __syncthreads();
 
@@ -500,10 +503,10 @@ __global__ void __maxnreg__(kFwdRegs) rmsnorm_fwd_row_kernel(const __grid_consta
       else write(std::false_type{}, static_cast<const float*>(a.w));
     }
 
-    if (a.y8 != nullptr) {
+    if constexpr (kCodes != kNoCodes) {
       const int shift = 31 - __clz(group);  // of a group that is a power of two
       float row_inv = 0.f;
-      if (a.group == 0) {
+      if constexpr (kCodes == kRowCodes) {
         float top = 0.f;
 #pragma unroll
         for (int u = 0; u < kUnits; ++u)
@@ -534,50 +537,19 @@ __global__ void __maxnreg__(kFwdRegs) rmsnorm_fwd_row_kernel(const __grid_consta
       float* scales = a.scales + row * groups;
       uint8_t* q = a.y8 + row * a.ld_y8 + c0;
       if (kOdd) q = reinterpret_cast<uint8_t*>(img_q) + image_of(a.y8, row * a.ld_y8, a.H).off + c0;
-      // the lanes that share a scale with this one
-      const int lanes = kOdd ? 32 : min(32, max(1, group / U::kCols));
-      const uint32_t beside = (lanes < 32 ? (1u << lanes) - 1u : 0xffffffffu) << ((tid & 31) & ~(lanes - 1));
-#pragma unroll
-      for (int u = 0; u < kUnits; ++u) {
+      // unit u as codes; inv0, inv1: 1 / scale of columns c on, and in odd rows of column c + 32
+      const auto put_codes = [&](int u, float inv0, float inv1) {
         const int c = c0 + u * kStep;
-        // the scale of columns c on, and in odd rows of column c + 32
-        float inv0 = row_inv, inv1 = row_inv;
-        if (a.group != 0) {
-          float m0 = 0.f, m1 = 0.f;
-          if (meet) {
-            if (c < a.H) m0 = __uint_as_float(peak[c >> shift]);
-            if (kOdd && c + 32 < a.H) m1 = __uint_as_float(peak[(c + 32) >> shift]);
-          } else if constexpr (kOdd) {
-            const float2 v = split_f2(h[u].p[0]);
-            m0 = __uint_as_float(__reduce_max_sync(0xffffffffu, peak_bits(v.x)));
-            m1 = __uint_as_float(__reduce_max_sync(0xffffffffu, peak_bits(v.y)));
-          } else {
-#pragma unroll
-            for (int k = 0; k < kPairs; ++k) m0 = abs_max(m0, h[u].p[k]);
-            // (one instruction per set of lanes: 65,536 x 4,096 bf16 with groups of 256, 128 and 32 columns 317, 332 and 379 us,
-            // by shuffles 365, 358 and 350)
-            if (lanes >= 16)
-              m0 = __uint_as_float(__reduce_max_sync(beside, __float_as_uint(m0)));
-            else
-              for (int o = lanes >> 1; o > 0; o >>= 1) m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, o));
-          }
-          m0 = e4m3_scale(m0);
-          m1 = e4m3_scale(m1);
-          if (c < a.H && (c & (group - 1)) == 0) scales[c >> shift] = m0;
-          if (kOdd && c + 32 < a.H && ((c + 32) & (group - 1)) == 0) scales[(c + 32) >> shift] = m1;
-          inv0 = __fdividef(1.f, m0);
-          inv1 = __fdividef(1.f, m1);
-        }
         if constexpr (kOdd) {
           const float2 v = split_f2(h[u].p[0]);
           const uint32_t code = pack_e4m3x2(v.x * inv0, v.y * inv1);
           if (c < a.H) q[u * kStep] = (uint8_t)code;
           if (c + 32 < a.H) q[u * kStep + 32] = (uint8_t)(code >> 8);
-        } else if (c < a.H) {
+        } else if (full || c < a.H) {
           uint32_t o[kPairs / 2];
+          const f2 i2 = make_f2(inv0, inv0);
 #pragma unroll
           for (int k = 0; k < kPairs / 2; ++k) {
-            const f2 i2 = make_f2(inv0, inv0);
             const float2 v = split_f2(mul_f2(h[u].p[2 * k], i2)), w = split_f2(mul_f2(h[u].p[2 * k + 1], i2));
             o[k] = pack_e4m3x2(v.x, v.y) | pack_e4m3x2(w.x, w.y) << 16;
           }
@@ -586,13 +558,51 @@ __global__ void __maxnreg__(kFwdRegs) rmsnorm_fwd_row_kernel(const __grid_consta
           else
             *reinterpret_cast<uint32_t*>(q + u * kStep) = o[0];
         }
+      };
+      // all units, from the maxima of their groups (of the lane's own columns in, of the group out)
+      const auto by_group = [&](auto peak_of) {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+          const int c = c0 + u * kStep;
+          float m0 = 0.f, m1 = 0.f;
+          if constexpr (kOdd) {
+            const float2 v = split_f2(h[u].p[0]);
+            m0 = fmaxf(fabsf(v.x), 0.f), m1 = fmaxf(fabsf(v.y), 0.f);
+          } else {
+#pragma unroll
+            for (int k = 0; k < kPairs; ++k) m0 = abs_max(m0, h[u].p[k]);
+          }
+          m0 = e4m3_scale(peak_of(m0, c));
+          if (kOdd) m1 = e4m3_scale(peak_of(m1, c + 32));
+          if (c < a.H && (c & (group - 1)) == 0) scales[c >> shift] = m0;
+          if (kOdd && c + 32 < a.H && ((c + 32) & (group - 1)) == 0) scales[(c + 32) >> shift] = m1;
+          put_codes(u, __fdividef(1.f, m0), kOdd ? __fdividef(1.f, m1) : 0.f);
+        }
+      };
+      // the lanes that share a scale with this one
+      const int lanes = kOdd ? 32 : min(32, max(1, group / U::kCols));
+      const uint32_t beside = (lanes < 32 ? (1u << lanes) - 1u : 0xffffffffu) << ((tid & 31) & ~(lanes - 1));
+      if constexpr (kCodes == kRowCodes) {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) put_codes(u, row_inv, row_inv);
+      } else if (meet) {
+        by_group([&](float, int c) { return c < a.H ? __uint_as_float(peak[c >> shift]) : 0.f; });
+      } else if (lanes >= 16) {
+        // one instruction per set of lanes (65,536 x 4,096 bf16 with groups of 256, 128 and 32 columns: 317, 332 and 379 us, by
+        // shuffles 365, 358 and 350)
+        by_group([&](float m, int) { return __uint_as_float(__reduce_max_sync(beside, __float_as_uint(m))); });
+      } else {
+        by_group([&](float m, int) {
+          for (int o = lanes >> 1; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+          return m;
+        });
       }
     }
     if constexpr (kOdd) {
       __syncthreads();
       if (a.h_out != nullptr) image_store<T>(here, image_of(static_cast<T*>(a.h_out), row * a.ld_h, a.H));
       if (a.y != nullptr) image_store<T>(here + y_at, image_of(static_cast<T*>(a.y), row * a.ld_y, a.H));
-      if (a.y8 != nullptr) image_store<uint8_t>(img_q, image_of(a.y8, row * a.ld_y8, a.H));
+      if (kCodes != kNoCodes) image_store<uint8_t>(img_q, image_of(a.y8, row * a.ld_y8, a.H));
     } else if (meet) {
       __syncthreads();  // the next row clears the peaks
     }
@@ -802,8 +812,9 @@ constexpr int kSmemPerSm = 227 * 1024, kSmemCta = 227 * 1024 - 4096;  // (4 KB: 
 RowPlan plan_rows(int threads, int regs, int stage_bytes, int out_bytes) {
   RowPlan p;
   p.threads = threads;
-  int c = 65536 / (regs * p.threads);
+  int c = 4 * (16384 / (regs * 32)) / (threads / 32);  // (each quarter of the SM holds whole warps)
   if (c > 32) c = 32;
+  if (c < 1) c = 1;
   const int own = 4096;
   while (c > 1 && c * (2 * stage_bytes + out_bytes + own) > kSmemPerSm) --c;
   const int s = stage_bytes > 0 ? (kSmemPerSm / c - own - out_bytes) / stage_bytes : 1;
@@ -825,21 +836,26 @@ int allow_smem(K kernel, std::atomic<uint64_t>& done) {
   return mrl_once_per_device(done, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemCta); });
 }
 // -1: the rows do not fit; the looping kernel takes them.
-template <typename T, bool kOdd, int kCols>
-int launch_fwd_rows(NormFwdArgs a, cudaStream_t st) {
+template <typename T, bool kOdd, int kCols, int kCodes>
+int launch_fwd_codes(NormFwdArgs a, cudaStream_t st) {
   const int threads = row_threads(a.H, kCols);
   const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : threads * kCols * (int)sizeof(T);
-  const RowPlan p = plan_rows(threads, kFwdRegs, fwd_slots(a, kOdd) * slot, kOdd && a.y8 != nullptr ? image_bytes(a.H, 1) : 0);
+  const RowPlan p = plan_rows(threads, fwd_regs(kCols), fwd_slots(a, kOdd) * slot, kOdd && a.y8 != nullptr ? image_bytes(a.H, 1) : 0);
   if (p.smem > kSmemCta) return -1;
   a.stages = p.stages;
   const long long most = (long long)kSms * p.ctas_per_sm;
   static std::atomic<uint64_t> done;
-  const int rc = allow_smem(rmsnorm_fwd_row_kernel<T, kOdd, kCols>, done);
+  const int rc = allow_smem(rmsnorm_fwd_row_kernel<T, kOdd, kCols, kCodes>, done);
   if (rc != MRL_OK) return rc;
   mrl_profile_before(st, "rmsnorm_fwd_row_kernel");
-  rmsnorm_fwd_row_kernel<T, kOdd, kCols><<<(unsigned)(a.N < most ? a.N : most), p.threads, p.smem, st>>>(a);
+  rmsnorm_fwd_row_kernel<T, kOdd, kCols, kCodes><<<(unsigned)(a.N < most ? a.N : most), p.threads, p.smem, st>>>(a);
   mrl_profile_after(st);
   return cudaGetLastError() == cudaSuccess ? MRL_OK : MRL_ERR_CUDA;
+}
+template <typename T, bool kOdd, int kCols>
+int launch_fwd_rows(const NormFwdArgs& a, cudaStream_t st) {
+  if (a.y8 == nullptr) return launch_fwd_codes<T, kOdd, kCols, kNoCodes>(a, st);
+  return a.group == 0 ? launch_fwd_codes<T, kOdd, kCols, kRowCodes>(a, st) : launch_fwd_codes<T, kOdd, kCols, kGroupCodes>(a, st);
 }
 template <typename T, bool kOdd, int kCols>
 int launch_bwd_rows(NormBwdArgs a, int* ctas, cudaStream_t st) {
