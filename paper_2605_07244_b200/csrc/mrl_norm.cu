@@ -17,7 +17,8 @@ constexpr int kLoopThreads = 512;
 constexpr int kWide = 32, kMiddle = 16, kNarrow = 8;      // columns of a thread of the row kernels
 constexpr int kNoCodes = 0, kRowCodes = 1, kGroupCodes = 2;
 constexpr int kRowMax = 16384;                            // the widest row that one CTA holds
-constexpr int kBwdRegs = 64;                              // registers of a thread of the row kernels
+// registers of a thread of the row kernels
+constexpr int kBwdRegs = 64, kBwdRegsMore = 80;
 constexpr int fwd_regs(int cols) { return cols == kWide ? 80 : 64; }  // (wide: shared memory allows no more CTAs anyway)
 
 template <typename T>
@@ -610,9 +611,10 @@ __global__ void __maxnreg__(fwd_regs(kRowCols)) rmsnorm_fwd_row_kernel(const __g
 }
 
 // Backward, with rows on their way as above.  Each thread keeps the dweight sums of its columns in registers over all of
-// the CTA's rows and writes them once; what a row needs after its sum is read from shared memory again.
-template <typename T, bool kOdd, int kRowCols>
-__global__ void __maxnreg__(kBwdRegs) rmsnorm_bwd_row_kernel(const __grid_constant__ NormBwdArgs a) {
+// the CTA's rows and writes them once; h and dh are read from shared memory again after the
+// row's sum.
+template <typename T, bool kOdd, int kRowCols, int kRegs>
+__global__ void __maxnreg__(kRegs) rmsnorm_bwd_row_kernel(const __grid_constant__ NormBwdArgs a) {
   using U = Unit<T, kOdd>;
   constexpr int kUnits = kRowCols / U::kCols, kStep = U::kStep, kPairs = U::kPairs, kHalf = kOdd ? 32 : 0;
   extern __shared__ __align__(16) char smem[];
@@ -681,7 +683,7 @@ __global__ void __maxnreg__(kBwdRegs) rmsnorm_bwd_row_kernel(const __grid_consta
     const int unit_bytes = kOdd ? kStep * (int)sizeof(T) : nt * 16;
 
     const f2 rstd2 = make_f2(rstd, rstd);
-    f2 acc[2] = {0ull, 0ull};
+    f2 gd[kUnits][kPairs], acc[2] = {0ull, 0ull};  // (w + o) dy
     const auto read = [&](auto all, auto w) {
       constexpr bool kFull = decltype(all)::value;
 #pragma unroll
@@ -693,9 +695,10 @@ __global__ void __maxnreg__(kBwdRegs) rmsnorm_bwd_row_kernel(const __grid_consta
         load_gain<U, kOdd>(w, a.offset, c0 + u * kStep, in0, in1, &g);
 #pragma unroll
         for (int k = 0; k < kPairs; ++k) {
-          const f2 v = mul_f2(d.p[k], mul_f2(x.p[k], rstd2));
-          dw[u][k] = add_f2(dw[u][k], v);
-          acc[k & 1] = fma_f2(v, g.p[k], acc[k & 1]);
+          const f2 xhat = mul_f2(x.p[k], rstd2);
+          gd[u][k] = mul_f2(d.p[k], g.p[k]);
+          dw[u][k] = fma_f2(d.p[k], xhat, dw[u][k]);
+          acc[k & 1] = fma_f2(gd[u][k], xhat, acc[k & 1]);
         }
       }
     };
@@ -712,17 +715,15 @@ __global__ void __maxnreg__(kBwdRegs) rmsnorm_bwd_row_kernel(const __grid_consta
     T* out = static_cast<T*>(a.dx) + row * a.ld_dx + c0;
     if (kOdd) out = reinterpret_cast<T*>(img + image_of(static_cast<T*>(a.dx), row * a.ld_dx, a.H).off) + c0;
     const f2 minus2 = make_f2(-rstd * mean, -rstd * mean);
-    const auto write = [&](auto all, auto w) {
+    const auto write = [&](auto all) {
       constexpr bool kFull = decltype(all)::value;
 #pragma unroll
       for (int u = 0; u < kUnits; ++u) {
         const bool in0 = kFull || c0 + u * kStep < a.H, in1 = kFull || c0 + u * kStep + kHalf < a.H;
-        U d, x, g;
-        d.load(in_d + u * unit_bytes, in0, in1);
+        U d, x;
         x.load(in_h + u * unit_bytes, in0, in1);
-        load_gain<U, kOdd>(w, a.offset, c0 + u * kStep, in0, in1, &g);  // again, from L1: cheaper than its registers
 #pragma unroll
-        for (int k = 0; k < kPairs; ++k) d.p[k] = fma_f2(x.p[k], minus2, mul_f2(d.p[k], g.p[k]));
+        for (int k = 0; k < kPairs; ++k) d.p[k] = fma_f2(x.p[k], minus2, gd[u][k]);
         if (a.dh != nullptr) {
           x.load(in_e + u * unit_bytes, in0, in1);
 #pragma unroll
@@ -734,13 +735,7 @@ __global__ void __maxnreg__(kBwdRegs) rmsnorm_bwd_row_kernel(const __grid_consta
         d.store(out + u * kStep, in0, in1);
       }
     };
-    if (a.w_bf16) {
-      if (full) write(std::true_type{}, static_cast<const __nv_bfloat16*>(a.w));
-      else write(std::false_type{}, static_cast<const __nv_bfloat16*>(a.w));
-    } else {
-      if (full) write(std::true_type{}, static_cast<const float*>(a.w));
-      else write(std::false_type{}, static_cast<const float*>(a.w));
-    }
+    if (full) write(std::true_type{}); else write(std::false_type{});
     if constexpr (kOdd) {
       __syncthreads();
       image_store<T>(img, image_of(static_cast<T*>(a.dx), row * a.ld_dx, a.H));
@@ -857,21 +852,29 @@ int launch_fwd_rows(const NormFwdArgs& a, cudaStream_t st) {
   if (a.y8 == nullptr) return launch_fwd_codes<T, kOdd, kCols, kNoCodes>(a, st);
   return a.group == 0 ? launch_fwd_codes<T, kOdd, kCols, kRowCodes>(a, st) : launch_fwd_codes<T, kOdd, kCols, kGroupCodes>(a, st);
 }
-template <typename T, bool kOdd, int kCols>
-int launch_bwd_rows(NormBwdArgs a, int* ctas, cudaStream_t st) {
+template <typename T, bool kOdd, int kCols, int kRegs>
+int launch_bwd_regs(NormBwdArgs a, int* ctas, cudaStream_t st) {
   const int threads = row_threads(a.H, kCols);
   const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : threads * kCols * (int)sizeof(T);
-  const RowPlan p = plan_rows(threads, kBwdRegs, (a.dh != nullptr ? 3 : 2) * slot, kOdd ? slot : 0);
+  const RowPlan p = plan_rows(threads, kRegs, (a.dh != nullptr ? 3 : 2) * slot, kOdd ? slot : 0);
   if (p.smem > kSmemCta) return -1;
   a.stages = p.stages;
   *ctas = bwd_ctas(a.N, p.ctas_per_sm);
   static std::atomic<uint64_t> done;
-  const int rc = allow_smem(rmsnorm_bwd_row_kernel<T, kOdd, kCols>, done);
+  const int rc = allow_smem(rmsnorm_bwd_row_kernel<T, kOdd, kCols, kRegs>, done);
   if (rc != MRL_OK) return rc;
   mrl_profile_before(st, "rmsnorm_bwd_row_kernel");
-  rmsnorm_bwd_row_kernel<T, kOdd, kCols><<<*ctas, p.threads, p.smem, st>>>(a);
+  rmsnorm_bwd_row_kernel<T, kOdd, kCols, kRegs><<<*ctas, p.threads, p.smem, st>>>(a);
   mrl_profile_after(st);
   return cudaGetLastError() == cudaSuccess ? MRL_OK : MRL_ERR_CUDA;
+}
+// 16 columns a thread: with up to 256 threads 80 registers leave room for 24 warps of an SM and spare the spills of 64
+// (65,536 x 4,096 bf16: 344 us, 370 with 64); beyond, too few CTAs would fit (32,768 x 8,192: 428, 375).
+template <typename T, bool kOdd, int kCols>
+int launch_bwd_rows(const NormBwdArgs& a, int* ctas, cudaStream_t st) {
+  if constexpr (kCols == kMiddle)
+    if (row_threads(a.H, kCols) <= 256) return launch_bwd_regs<T, kOdd, kCols, kBwdRegsMore>(a, ctas, st);
+  return launch_bwd_regs<T, kOdd, kCols, kBwdRegs>(a, ctas, st);
 }
 template <typename T>
 int launch_fwd(const NormFwdArgs& a, bool odd, cudaStream_t st) {

@@ -323,3 +323,67 @@ def test_seeded_rounding_keeps_small_updates_in_the_mean():
     c.b["param"][1].fill_(0.375)
     step_of([c], step=1, lr=1e-5)
     assert bool((c.b["param"][1] == 0.375).all())
+
+
+def _float32_step(state, grad, scale, step, seeded):
+    """The moments and their codes by torch's float32 operations, one after the other as the formula stands."""
+    block = lambda t: t.view(-1, B.STATE_BLOCK)  # noqa: E731
+    g = grad.float() * scale
+    m = (block(state["m"].view(E4M3).float()) * state["m_scale"][:, None]).view(-1)
+    v = (block(state["v"].view(E4M3).float()) * state["v_scale"][:, None]).view(-1)
+    v = v * v
+    m, v = B1 * m + (1.0 - B1) * g, B2 * v + (1.0 - B2) * (g * g)
+    out = {}
+    dither = S.dithers(64, seeded, step, 0) if seeded is not None else None      # (checked below for what it covers)
+    for k, (name, s) in enumerate((("m", m), ("v", v.sqrt()))):
+        sc = (block(s.abs()).amax(1) * torch.tensor(1.0 / 448.0, dtype=F32, device="cuda")).clamp_min(2.0 ** -126)
+        y = (block(s) * (1.0 / sc)[:, None]).view(-1)
+        if dither is None:
+            q = y.clamp(-448, 448).to(E4M3)
+        else:
+            y = y[:64]
+            a = y.abs()
+            up = torch.where(a < 2.0 ** -6, 2.0 ** -6, 0.0).float()
+            z = (((a + up).view(torch.int32) + (dither[k].int().cuda() << 4)) & ~0xFFFFF).view(F32) - up
+            q = torch.copysign(z.clamp(max=448.0), y).to(E4M3)
+        if name == "v":
+            q = torch.where((y > 0) & (q.float() == 0), 2.0 ** -9, q.float()).to(E4M3)
+        out[name], out[name + "_scale"] = q, sc
+    return out
+
+
+@pytest.mark.parametrize("seeded", [None, 31])
+def test_codes_are_those_of_the_float32_operations_bit_for_bit(seeded):
+    """A million elements over three steps: scales and codes equal those of single float32 operations in the formula's order
+    (with seeded rounding the first 64 codes, whose dithers are formed here one by one)."""
+    c = Case(1 << 20, F32, False, BF16, E4M3, seed=11)
+    for step in (4, 5, 6):
+        state = {k: c.b[k][1].clone() for k in ("m", "v", "m_scale", "v_scale")}
+        grad = torch.randn(c.n, generator=torch.Generator(device="cuda").manual_seed(step), device="cuda") * 10.0 ** -step
+        c.b["grad"][1].copy_(grad)
+        want = _float32_step(state, c.b["grad"][1], torch.tensor([0.37], device="cuda"), step, seeded)
+        step_of([c], step=step, seeded=seeded, scale=0.37)
+        for k in ("m", "v", "m_scale", "v_scale"):
+            n = want[k].numel()
+            assert torch.equal(c.b[k][1][:n].view(torch.uint8), want[k].view(torch.uint8)), (k, step)
+
+
+def test_a_state_that_is_not_finite_stays_in_its_block():
+    for kind in KINDS:
+        for seeded in (None, 3):
+            c, d = (Case(1024, *kind, seed=12) for _ in range(2))
+            c.b["grad"][1][300] = float("nan")
+            c.b["grad"][1][700] = float("inf")
+            for one in (c, d):
+                step_of([one], seeded=seeded)
+            name = "master" if "master" in c.b else "param"
+            p, q = c.b[name][1], d.b[name][1]
+            assert bool(torch.isnan(p[300])) and bool(torch.isnan(p[700]))        # inf / inf
+            rest = torch.ones(1024, dtype=torch.bool, device="cuda")
+            rest[[300, 700]] = False
+            assert torch.equal(p[rest], q[rest])
+            for k in ("m", "v"):
+                a, b = c.b[k][1], d.b[k][1]
+                assert torch.equal(a[:256], b[:256]) and torch.equal(a[768:], b[768:])
+                if kind[3] == E4M3:
+                    assert int(a.view(torch.uint8)[300]) & 0x7F == 0x7F

@@ -2,7 +2,7 @@
 
 Tolerances, derived.  u = 2^-24 is half a float32 step relative to the value.  A row's sum of squares is a sum of
 non-negative float32 terms: its relative error is at most (longest chain of additions) u; the longest chain of any
-kernel is 16 columns in a thread, 5 shuffles and 32 warps, or H / 512 columns in the looping kernel.  The square root
+kernel is 16 additions in a thread, 5 shuffles and 32 warps, or H / 512 columns in the looping kernel.  The square root
 halves it; the float reciprocal of H, the addition of eps, rsqrtf (2 units in the last place = 4 u), and the products
 and the sum that make h and y add at most 10 u.  So y before its rounding is off by at most (chain / 2 + 10) u of itself, and
 rounding to the row's type adds half a step, eps / 2 of the value."""
@@ -252,6 +252,64 @@ def test_backward_row_strides_and_addresses(dtype, pad, shift):
         out = run_bwd(dy, dh, h, w, rstd, dx=dx)
         check_bwd(dy, dh, h, w, rstd, out)
         assert bool(torch.isnan(dx.as_strided((N, H + pad), (H + pad, 1))[:, H:].float()).all())
+
+
+MANY = [(20000, 64), (9000, 320), (7000, 512), (3000, 1000), (3000, 1024), (2500, 1027), (2100, 4096), (2100, 4095), (700, 8192),
+        (450, 16384)]
+
+
+def random_rows(N, H, dtype, seed, pad=0, scale=1.0):
+    """As rows(), made on the device (the oracle reads back what it needs)."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    wide = torch.full((N, H + pad), float("nan"), dtype=dtype, device="cuda")
+    wide[:, :H] = torch.randn(N, H, generator=g, device="cuda") * scale
+    return wide[:, :H]
+
+
+@pytest.mark.parametrize("N,H", MANY)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_more_rows_than_run_at_once(N, H, dtype):
+    """Each CTA walks several rows, with later ones on their way: every row against the oracle, over the inputs and apart."""
+    for pad in (0, 3):
+        x, res = random_rows(N, H, dtype, 1, pad), random_rows(N, H, dtype, 2, pad, 2.0)
+        w = torch.randn(H, generator=torch.Generator().manual_seed(7)).to(dtype).cuda()
+        ref = S.rmsnorm_residual_fwd(x, res, w, 0.0, float(torch.tensor(1e-6, dtype=F32)))
+        plain = run_fwd(x, res, w, want=("h", "y", "rstd"))
+        check_fwd(x, res, w, plain, ref, 0.0, 0)
+        for group in (0, 128):
+            out = run_fwd(x, res, w, group=group, want=("y", "rstd", "q"))
+            assert torch.equal(out["y"], plain["y"]) and torch.equal(out["rstd"], plain["rstd"])
+            check_fwd(x, res, w, {k: out[k] for k in ("q", "scales")}, ref, 0.0, group)
+        over = run_fwd(x, res, w, want=("rstd",), place={"h": res, "y": x})
+        assert torch.equal(over["h"], plain["h"]) and torch.equal(over["y"], plain["y"]) and torch.equal(over["rstd"], plain["rstd"])
+
+
+@pytest.mark.parametrize("N,H", MANY)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_backward_of_more_rows_than_run_at_once(N, H, dtype):
+    for pad in (0, 3):
+        dy, dh, h = (random_rows(N, H, dtype, s, pad) for s in (1, 2, 3))
+        w = torch.randn(H, generator=torch.Generator().manual_seed(7)).cuda()
+        rstd = S.rmsnorm_residual_fwd(h, None, w, 0.0, 1e-6)[1].float().cuda()
+        out = run_bwd(dy, dh, h, w, rstd)
+        check_bwd(dy, dh, h, w, rstd, out)
+        check_bwd(dy, None, h, w, rstd, run_bwd(dy, None, h, w, rstd))
+        over = run_bwd(dy, dh, h, w, rstd, dx=dh)
+        assert torch.equal(over["dx"], out["dx"]) and torch.equal(over["dw"], out["dw"])
+
+
+@pytest.mark.parametrize("H", [8193, 10007, 12001, 16383])
+def test_wide_rows_of_odd_width(H):
+    """float32 rows that leave no room for a second row, or for one, in shared memory."""
+    for N in (5, 400):
+        x, res = random_rows(N, H, F32, 1), random_rows(N, H, F32, 2)
+        w = torch.randn(H, generator=torch.Generator().manual_seed(7)).cuda()
+        ref = S.rmsnorm_residual_fwd(x, res, w, 0.0, float(torch.tensor(1e-6, dtype=F32)))
+        out = run_fwd(x, res, w, group=256, want=("h", "y", "rstd", "q"))
+        check_fwd(x, res, w, out, ref, 0.0, 256)
+        dy, dh = random_rows(N, H, F32, 3), random_rows(N, H, F32, 4)
+        check_bwd(dy, dh, x, w, out["rstd"], run_bwd(dy, dh, x, w, out["rstd"]))
+        check_bwd(dy, None, x, w, out["rstd"], run_bwd(dy, None, x, w, out["rstd"]))
 
 
 def test_gradients_match_differences_of_the_forward_pass():
