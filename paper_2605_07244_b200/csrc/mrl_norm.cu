@@ -282,12 +282,12 @@ __device__ __forceinline__ Image image_of(P* base, long long element, int H) {
   const int off = (int)(reinterpret_cast<uintptr_t>(p) & 15);
   return Image{p - off, off, H * (int)sizeof(P)};
 }
-// Granules of a row into its copy.  Bytes of the row before it come along where it starts inside a granule, except before
-// the first row, which is none of the tensor's memory; nothing behind the row's end is read.
+// Granules of a row into its copy.  Bytes before the row come along where it starts inside a granule, but none from before
+// the tensor (the first row, or the first few of less than a granule); nothing behind the row's end is read.
 template <typename T>
-__device__ __forceinline__ void image_load(char* dst, const Image& im, bool first_row) {
+__device__ __forceinline__ void image_load(char* dst, const Image& im, const T* base) {
   const int end = im.off + im.len;
-  const bool by_element = first_row && im.off != 0;
+  const bool by_element = im.first < reinterpret_cast<const char*>(base);
   for (int k = threadIdx.x + by_element; 16 * k < end; k += blockDim.x) copy_async(dst + 16 * k, im.first + 16 * k, min(16, end - 16 * k));
   if (by_element) {
     const int b = im.off + (int)threadIdx.x * (int)sizeof(T);
@@ -383,8 +383,8 @@ __global__ void __maxnreg__(fwd_regs(kRowCols)) rmsnorm_fwd_row_kernel(const __g
       const T* x = static_cast<const T*>(a.x);
       const T* r = static_cast<const T*>(a.res);
       if constexpr (kOdd) {
-        image_load<T>(dst, image_of(x, row * a.ld_x, a.H), row == 0);
-        if (r != nullptr) image_load<T>(dst + slot, image_of(r, row * a.ld_res, a.H), row == 0);
+        image_load<T>(dst, image_of(x, row * a.ld_x, a.H), x);
+        if (r != nullptr) image_load<T>(dst + slot, image_of(r, row * a.ld_res, a.H), r);
       } else {
         dst += tid * 16;
         x += row * a.ld_x + c0;
@@ -611,8 +611,8 @@ __global__ void __maxnreg__(fwd_regs(kRowCols)) rmsnorm_fwd_row_kernel(const __g
 }
 
 // Backward, with rows on their way as above.  Each thread keeps the dweight sums of its columns in registers over all of
-// the CTA's rows and writes them once; h and dh are read from shared memory again after the
-// row's sum.
+// the CTA's rows and writes them once; (w + o) dy stays there from the row's sum on, h and dh are read from shared memory
+// after it.
 template <typename T, bool kOdd, int kRowCols, int kRegs>
 __global__ void __maxnreg__(kRegs) rmsnorm_bwd_row_kernel(const __grid_constant__ NormBwdArgs a) {
   using U = Unit<T, kOdd>;
@@ -638,7 +638,7 @@ __global__ void __maxnreg__(kRegs) rmsnorm_bwd_row_kernel(const __grid_constant_
         if (from[k] == nullptr) continue;
         const T* p = static_cast<const T*>(from[k]);
         if constexpr (kOdd) {
-          image_load<T>(dst + k * slot, image_of(p, row * ld[k], a.H), row == 0);
+          image_load<T>(dst + k * slot, image_of(p, row * ld[k], a.H), p);
         } else {
           p += row * ld[k] + c0;
 #pragma unroll
@@ -891,6 +891,8 @@ int launch_bwd(const NormBwdArgs& a, bool odd, int* ctas, cudaStream_t st) {
   return odd ? launch_bwd_rows<T, true, kMiddle>(a, ctas, st) : launch_bwd_rows<T, false, kMiddle>(a, ctas, st);
 }
 
+constexpr int kMaxCols = 1 << 30;
+bool on_element(const void* p, int elem) { return (reinterpret_cast<uintptr_t>(p) & (elem - 1)) == 0; }
 bool row_type_ok(int32_t dtype) { return dtype == MRL_BF16 || dtype == MRL_F32; }
 
 }  // namespace
@@ -906,6 +908,7 @@ extern "C" int mrl_rmsnorm_residual_fwd(const void* x, int64_t ld_x, const void*
                                         void* y8, int64_t ld_y8, float* scales, float* rstd, void* stream) {
   if (!row_type_ok(dtype) || !row_type_ok(w_dtype)) return MRL_ERR_UNSUPPORTED_DTYPE;
   if (np == nullptr || N < 0 || H < 1) return MRL_ERR_INVALID_ARG;
+  if (H > kMaxCols) return MRL_ERR_UNSUPPORTED_SHAPE;
   if (!(np->eps > 0.f) || np->eps > 3.4e38f || !(np->weight_offset - np->weight_offset == 0.f)) return MRL_ERR_INVALID_ARG;
   if (np->group != 0 && np->group != 32 && np->group != 64 && np->group != 128 && np->group != 256) return MRL_ERR_INVALID_ARG;
   if (N == 0) return MRL_OK;
@@ -915,11 +918,14 @@ extern "C" int mrl_rmsnorm_residual_fwd(const void* x, int64_t ld_x, const void*
     return MRL_ERR_INVALID_ARG;
   if (h_out != nullptr && h_out == y) return MRL_ERR_INVALID_ARG;
   if (x == nullptr || weight == nullptr) return MRL_ERR_INVALID_ARG;
+  const bool bf16 = dtype == MRL_BF16;
+  const int elem = bf16 ? 2 : 4;
+  if (!on_element(x, elem) || !on_element(residual, elem) || !on_element(h_out, elem) || !on_element(y, elem) ||
+      !on_element(weight, w_dtype == MRL_BF16 ? 2 : 4))
+    return MRL_ERR_INVALID_ARG;
   NormFwdArgs a{x, residual, weight, h_out, y, static_cast<uint8_t*>(y8), scales, rstd, ld_x, ld_res, ld_h, ld_y, ld_y8, N,
                 H, np->group, w_dtype == MRL_BF16, np->eps, np->weight_offset, 1.0f / (float)H, 0};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const bool bf16 = dtype == MRL_BF16;
-  const int elem = bf16 ? 2 : 4;
   int rc = -1;
   if (H <= kRowMax) {
     const bool whole = H % (16 / elem) == 0 && aligned(x, ld_x, elem, 16) && aligned(residual, ld_res, elem, 16) &&
@@ -945,6 +951,7 @@ extern "C" int mrl_rmsnorm_residual_bwd(const void* dy, int64_t ld_dy, const voi
                                         void* stream) {
   if (!row_type_ok(dtype) || !row_type_ok(w_dtype)) return MRL_ERR_UNSUPPORTED_DTYPE;
   if (np == nullptr || N < 0 || H < 1 || (np->flags & ~MRL_FLAG_ACCUMULATE_DW) != 0) return MRL_ERR_INVALID_ARG;
+  if (H > kMaxCols) return MRL_ERR_UNSUPPORTED_SHAPE;
   if (!(np->weight_offset - np->weight_offset == 0.f)) return MRL_ERR_INVALID_ARG;
   if (ld_dy < H || ld_h < H || ld_dx < H || (dh != nullptr && ld_dh < H)) return MRL_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -954,14 +961,17 @@ extern "C" int mrl_rmsnorm_residual_bwd(const void* dy, int64_t ld_dy, const voi
     return MRL_OK;
   }
   if (dy == nullptr || h == nullptr || weight == nullptr || rstd == nullptr || dx == nullptr) return MRL_ERR_INVALID_ARG;
+  const bool bf16 = dtype == MRL_BF16;
+  const int elem = bf16 ? 2 : 4;
+  if (!on_element(dy, elem) || !on_element(dh, elem) || !on_element(h, elem) || !on_element(dx, elem) ||
+      !on_element(weight, w_dtype == MRL_BF16 ? 2 : 4))
+    return MRL_ERR_INVALID_ARG;
   if (dweight != nullptr) {
     if (workspace == nullptr || workspace_bytes < mrl_rmsnorm_bwd_workspace_bytes(N, H)) return MRL_ERR_WORKSPACE_TOO_SMALL;
     if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return MRL_ERR_INVALID_ARG;
   }
   NormBwdArgs a{dy, dh, h, weight, rstd, dx, dweight != nullptr ? static_cast<float*>(workspace) : nullptr, ld_dy, ld_dh,
                 ld_h, ld_dx, N, H, w_dtype == MRL_BF16, np->weight_offset, 1.0f / (float)H, 0};
-  const bool bf16 = dtype == MRL_BF16;
-  const int elem = bf16 ? 2 : 4;
   int rc = -1, ctas = 0;
   if (H <= kRowMax) {
     const bool whole = H % (16 / elem) == 0 && aligned(dy, ld_dy, elem, 16) && aligned(dh, ld_dh, elem, 16) &&

@@ -37,8 +37,7 @@ struct Slot {
 
 // What changes from step to step.
 struct Hyper {
-  float lr, lr_c1, root_c2;  // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
-  int skip;
+  float lr, lr_c1, root_c2;  // lr, lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
   unsigned long long key;   // of the step's random words
 };
 
@@ -104,7 +103,7 @@ __device__ __forceinline__ void write_norm(double sum, float max_norm, float* no
   const double root = sqrt(sum);
   if (norm != nullptr) *norm = (float)root;
   if (coef != nullptr) {
-    const float c = max_norm > 0.f ? (float)((double)max_norm / fmax(root, (double)max_norm)) : 1.f;
+    const float c = max_norm > 0.f && max_norm < INFINITY ? (float)((double)max_norm / fmax(root, (double)max_norm)) : 1.f;
     *coef = root < INFINITY ? c : NAN;
   }
 }
@@ -122,10 +121,9 @@ __global__ void __launch_bounds__(kThreads) grad_norm_finish_kernel(const double
 __global__ void adamw_prepare_kernel(Hyper h, double lr, double beta1, double beta2, const float* lr_dev, int64_t* step_dev,
                                      int64_t step, unsigned long long seed, const float* grad_scale, Hyper* out) {
   const float gs = grad_scale != nullptr ? *grad_scale : 1.f;
-  h.skip = !(fabsf(gs) < INFINITY);
   if (step_dev != nullptr) {
     step = *step_dev + 1;
-    if (!h.skip) *step_dev = step;
+    if (fabsf(gs) < INFINITY) *step_dev = step;  // (the step is skipped otherwise)
   }
   if (lr_dev != nullptr) lr = (double)*lr_dev;
   h.lr = (float)lr;

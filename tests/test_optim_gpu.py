@@ -90,7 +90,8 @@ def test_grad_norm_range_and_non_finite_values():
             norm, coef = norm_of(grads)
             assert not norm < float("inf") and coef != coef
     grads = [torch.zeros(100, device="cuda")]
-    assert norm_of(grads) == (0.0, 1.0)
+    assert norm_of(grads) == (0.0, 1.0) and norm_of(grads, max_norm=float("inf")) == (0.0, 1.0)
+    assert norm_of([torch.full((100,), 2.0, device="cuda")], max_norm=float("inf")) == (20.0, 1.0)
 
 
 class Case:

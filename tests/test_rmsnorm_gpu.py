@@ -138,6 +138,22 @@ def test_row_strides_and_addresses(dtype, pad, shift):
         assert bool((between == 0x55).all())
 
 
+@pytest.mark.parametrize("H", [1, 2, 3, 5, 7, 8, 9, 17])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_of_less_than_a_granule_at_any_address(H, dtype):
+    w = torch.randn(H, generator=torch.Generator().manual_seed(7)).to(dtype).cuda()
+    for shift in range(9):
+        for pad in (0, 1, 3):
+            x, res = rows(21, H, dtype, 3, pad, shift), rows(21, H, dtype, 4, pad, shift)
+            ref = S.rmsnorm_residual_fwd(x, res, w, 0.0, float(torch.tensor(1e-6, dtype=F32)))
+            out = run_fwd(x, res, w, group=32, want=("h", "y", "rstd", "q"), pad=pad, shift=shift)
+            check_fwd(x, res, w, out, ref, 0.0, 32)
+            back = run_bwd(res, None, x, w, out["rstd"], dx=rows(21, H, dtype, 5, pad, shift))
+            check_bwd(res, None, x, w, out["rstd"], back)
+            for t in (out["h"], out["y"], back["dx"]):
+                assert bool(torch.isnan(t.as_strided((21, H + pad), (H + pad, 1))[:, H:].float()).all())
+
+
 @pytest.mark.parametrize("H", [256, 1001, 4096, 16400])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_outputs_over_inputs(H, dtype):

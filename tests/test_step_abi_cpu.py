@@ -39,6 +39,9 @@ def test_rmsnorm_fwd_refusals(lib):
     assert call(y8=FAKE) == 1 and call(y8=FAKE, scales=FAKE, ld8=7) == 1          # codes without scales; a short row
     assert call(y=None) == 1 and call(h=0x3000, y=0x3000) == 1                     # no output; one buffer for two
     assert call(x=None) == 1 and call(w=None) == 1
+    assert call(x=0x1001) == 1 and call(w=0x1002) == 1 and call(y=0x1001) == 1 and call(h=0x2001) == 1    # not on an element
+    big = (1 << 30) + 1
+    assert call(H=big, ld_x=big, ld_y=big) == 7
     assert call(x=None, N=0) == 0
 
 
@@ -54,6 +57,9 @@ def test_rmsnorm_bwd_refusals(lib):
     assert call(ld_dy=7) == 1 and call(ld_h=7) == 1 and call(ld_dx=7) == 1 and call(dh=FAKE, ld_dh=7) == 1
     assert call(dy=None) == 1 and call(h=None) == 1 and call(rstd=None) == 1 and call(dx=None) == 1 and call(w=None) == 1
     assert call(ws=None) == 4 and call(ws_bytes=16) == 4 and call(ws=0x1010) == 1
+    assert call(dy=0x1002) == 1 and call(dh=0x1001) == 1 and call(h=0x1003) == 1 and call(dx=0x1002) == 1
+    big = (1 << 30) + 1
+    assert call(H=big, ld_dy=big, ld_h=big, ld_dx=big) == 7
     assert call(N=0, dw=None) == 0
 
 
