@@ -152,7 +152,7 @@ typedef struct mrl_tensor_slot {
 } mrl_tensor_slot;
 
 typedef struct mrl_adamw_params {
-  double lr, beta1, beta2, eps;   /* 0 <= beta < 1, eps > 0 */
+  double lr, beta1, beta2, eps;   /* 0 <= beta < 1, eps >= 2^-126 */
   int64_t step;             /* number of this step, from 1 (bias corrections, seeded rounding); unused with step_dev */
   uint64_t seed;            /* MRL_ROUND_SEEDED */
   int32_t rounding;         /* MRL_ROUND_*: of 8-bit states, and of bf16 parameters without a master copy */

@@ -3,7 +3,9 @@
 //
 // Forward: h = x + r, rstd = 1 / sqrt(mean h^2 + eps), y = h rstd (w + o), optionally as e4m3 codes with a scale per group.
 // Backward: with g = (w + o) dy and xhat = h rstd, dx = dh + rstd (g - xhat mean(g xhat)), dw = sum over rows of dy xhat.
-// A few operations per element against 6 to 9 bytes: bound by HBM.
+// A few operations per element against 6 to 9 bytes: bound by HBM where rows are whole 16-byte granules (65,536 x 4,096 bf16:
+// forward with residual 343-350 us, backward 344-349 us, 6.1-6.3 TB/s of the bytes that have to move; e4m3 codes beside y, 33,880
+// rows: 208 us, 6.0 TB/s), by the instructions' issue where they are not (65,552 x 4,095: 561 and 547 us).
 #include <type_traits>
 
 #include "mrl_common.cuh"

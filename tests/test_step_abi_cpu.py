@@ -90,7 +90,7 @@ def test_adamw_refusals(lib):
 
     assert call(ap=0) == 1 and call(n=-1) == 1 and call(slots=None, n=1) == 1
     assert call(beta1=1.0) == 1 and call(beta1=-0.1) == 1 and call(beta2=float("nan")) == 1
-    assert call(eps=0.0) == 1 and call(eps=1e-60) == 1 and call(eps=float("inf")) == 1 and call(lr=float("nan")) == 1
+    assert call(eps=0.0) == 1 and call(eps=1e-60) == 1 and call(eps=1e-40) == 1 and call(eps=float("inf")) == 1 and call(lr=float("nan")) == 1
     assert call(step=0) == 1 and call(rounding=2) == 1 and call(flags=1) == 1
     for bad in (dict(grad=None), dict(param=None), dict(m=None), dict(v=None), dict(numel=-1), dict(master=FAKE),
                 dict(weight_decay=float("inf")), dict(state_dtype=B.E4M3), dict(state_dtype=B.E4M3, m_scale=FAKE)):
