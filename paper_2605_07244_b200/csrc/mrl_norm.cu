@@ -747,12 +747,17 @@ __global__ void __maxnreg__(kRegs) rmsnorm_bwd_row_kernel(const __grid_constant_
     float* to = a.partial + (size_t)blockIdx.x * a.H + c0;
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
+      const int c = c0 + u * kStep;
+      if constexpr (kOdd) {
+        const float2 v = split_f2(dw[u][0]);
+        if (c < a.H) to[u * kStep] = v.x;
+        if (c + 32 < a.H) to[u * kStep + 32] = v.y;
+      } else if (c < a.H) {
 #pragma unroll
-      for (int k = 0; k < kPairs; ++k) {
-        const float2 v = split_f2(dw[u][k]);
-        const int c = c0 + u * kStep + 2 * k;
-        if (c < a.H) to[u * kStep + 2 * k] = v.x;
-        if (c + (kOdd ? 32 : 1) < a.H) to[u * kStep + 2 * k + (kOdd ? 32 : 1)] = v.y;
+        for (int k = 0; k < kPairs; k += 2) {
+          const float2 v = split_f2(dw[u][k]), w = split_f2(dw[u][k + 1]);
+          *reinterpret_cast<float4*>(to + u * kStep + 2 * k) = make_float4(v.x, v.y, w.x, w.y);
+        }
       }
     }
   }
