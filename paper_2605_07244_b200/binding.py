@@ -380,18 +380,14 @@ class TensorSlot:
     def __init__(self, grad, param=None, master=None, m=None, v=None, m_scale=None, v_scale=None, weight_decay=0.0,
                  rng_first=0):
         n, dev, where = grad.numel(), grad.get_device(), "TensorSlot"
-        s = self.struct = TensorSlotStruct()
-        s.grad = _vector(grad, n, _CODES, dev, where)
-        s.grad_dtype = _CODES[grad.dtype]
-        s.param = _vector(param, n, _CODES, dev, where)
-        s.param_dtype = F32 if param is None else _CODES[param.dtype]
-        s.master = _vector(master, n, _F32_ONLY, dev, where)
-        s.state_dtype = E4M3 if m is not None and m.dtype in _CODE_TYPES else F32
-        kind = _CODE_TYPES if s.state_dtype == E4M3 else _F32_ONLY
-        s.m, s.v = _vector(m, n, kind, dev, where), _vector(v, n, kind, dev, where)
+        codes = m is not None and m.dtype in _CODE_TYPES
+        kind = _CODE_TYPES if codes else _F32_ONLY
         blocks = -(-n // STATE_BLOCK)
-        s.m_scale, s.v_scale = (_vector(t, blocks, _F32_ONLY, dev, where) for t in (m_scale, v_scale))
-        s.numel, s.rng_first, s.weight_decay = n, rng_first, weight_decay
+        self.struct = TensorSlotStruct(
+            _vector(grad, n, _CODES, dev, where), _vector(param, n, _CODES, dev, where), _float_vector(master, n, dev, where),
+            _vector(m, n, kind, dev, where), _vector(v, n, kind, dev, where), _float_vector(m_scale, blocks, dev, where),
+            _float_vector(v_scale, blocks, dev, where), n, rng_first, weight_decay, _CODES[grad.dtype],
+            F32 if param is None else _CODES[param.dtype], E4M3 if codes else F32)
         self.device = dev
         self.tensors = (grad, param, master, m, v, m_scale, v_scale)
 

@@ -16,7 +16,7 @@ constexpr int kThreads = 256;
 constexpr int kChunk = 8 * MRL_STATE_BLOCK;   // elements of a CTA at least: a state block per warp
 constexpr int kSlotsFew = 16, kSlots = 160;   // tensors per launch: the tables stay below the 32,764 bytes of kernel arguments
 constexpr int kSms = 148;
-constexpr int kNormCtas = kSms * 8;
+constexpr int kNormCtas = kSms * 5;           // as many as are resident (48 registers)
 constexpr uint32_t kSmallChunks = 16;
 constexpr int kCluster = 8;                   // CTAs of the gradient norm of few elements
 constexpr int kCodesCtas = 3;                 // per SM, of the update with 8-bit states
