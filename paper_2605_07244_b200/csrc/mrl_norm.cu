@@ -5,7 +5,7 @@
 // Backward: with g = (w + o) dy and xhat = h rstd, dx = dh + rstd (g - xhat mean(g xhat)), dw = sum over rows of dy xhat.
 // A few operations per element against 6 to 9 bytes: bound by HBM where rows are whole 16-byte granules (65,536 x 4,096 bf16:
 // forward with residual 343-350 us, backward 344-349 us, 6.1-6.3 TB/s of the bytes that have to move; e4m3 codes beside y, 33,880
-// rows: 208 us, 6.0 TB/s), by the instructions' issue where they are not (65,552 x 4,095: 561 and 547 us).
+// rows: 208 us, 6.0 TB/s), by the instructions' issue where they are not (65,552 x 4,095: 564 and 537 us).
 #include <type_traits>
 
 #include "mrl_common.cuh"
@@ -673,8 +673,8 @@ __global__ void __maxnreg__(kRegs) rmsnorm_bwd_row_kernel(const __grid_constant_
       fetch(row + (long long)(a.stages - 1) * gridDim.x, s == 0 ? a.stages - 1 : s - 1);
       copy_wait(a.stages - 1);
     }
-    char* img = smem + a.stages * stage;
-    const char* in_d = smem + s * stage + (kOdd ? c0 * (int)sizeof(T) : tid * 16);
+    char* img = smem + s * stage;  // odd rows: dx takes dy's place, which all have read before the row's sum is there
+    const char* in_d = img + (kOdd ? c0 * (int)sizeof(T) : tid * 16);
     const char *in_h = in_d + slot, *in_e = in_h + slot;
     if (kOdd) {
       in_d += image_of(static_cast<const T*>(a.dy), row * a.ld_dy, a.H).off;
@@ -863,7 +863,7 @@ template <typename T, bool kOdd, int kCols, int kRegs>
 int launch_bwd_regs(NormBwdArgs a, int* ctas, cudaStream_t st) {
   const int threads = row_threads(a.H, kCols);
   const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : threads * kCols * (int)sizeof(T);
-  const RowPlan p = plan_rows(threads, kRegs, (a.dh != nullptr ? 3 : 2) * slot, kOdd ? slot : 0);
+  const RowPlan p = plan_rows(threads, kRegs, (a.dh != nullptr ? 3 : 2) * slot, 0);
   if (p.smem > kSmemCta) return -1;
   a.stages = p.stages;
   *ctas = bwd_ctas(a.N, p.ctas_per_sm);
