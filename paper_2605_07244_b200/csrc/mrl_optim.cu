@@ -19,7 +19,12 @@ constexpr int kSms = 148;
 constexpr int kNormCtas = kSms * 5;           // as many as are resident (48 registers)
 constexpr uint32_t kSmallChunks = 16;
 constexpr int kCluster = 8;                   // CTAs of the gradient norm of few elements
-constexpr int kCodesCtas = 3;                 // per SM, of the update with 8-bit states
+// The update's threads and CTAs per SM (8: the kind's bit for 8-bit states), and the blocks of a warp in a large call.
+// 8-bit states, 525 M elements: 24 warps of 80 registers in 6 CTAs 1,231 us, in 3 CTAs 1,343; 28 of 72 registers 1,279, 32 of
+// 64 slower still; 8, 16, 32 and 128 blocks a warp 1,252, 1,249, 1,255 and 1,276.  float32 states, 622 M: 4 blocks 2,583, 8 2,624.
+__host__ __device__ constexpr int step_threads(int kind) { return kind & 8 ? 128 : 256; }
+__host__ __device__ constexpr int step_ctas(int kind) { return kind & 8 ? 6 : 4; }
+__host__ __device__ constexpr int step_blocks(int kind) { return kind & 8 ? 16 : 4; }
 
 struct Slot {
   const void* grad;
@@ -246,19 +251,22 @@ __device__ __forceinline__ void root8(const f2 (&v)[4], uint32_t least, uint32_t
     }
   }
 }
+// of magnitudes; a NaN among them is passed over by the minimum and is the maximum
+__device__ __forceinline__ float min3(float a, float b, float c) {
+  float r;
+  asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)), "f"(fabsf(c)));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)), "f"(fabsf(c)));
+  return r;
+}
 // The smallest and the largest magnitude of eight values as ordered integers; NaN lies above infinity.
-template <bool kSigned>
 __device__ __forceinline__ void bounds8(const f2 (&x)[4], uint32_t* least, uint32_t* most) {
-  *least = 0xffffffffu;
-  *most = 0;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float2 u = split_f2(x[j]);
-    uint32_t a = __float_as_uint(u.x), b = __float_as_uint(u.y);
-    if (kSigned) a &= 0x7fffffffu, b &= 0x7fffffffu;
-    *least = min(min(a, b), *least);
-    *most = max(max(a, b), *most);
-  }
+  const float2 a = split_f2(x[0]), b = split_f2(x[1]), c = split_f2(x[2]), d = split_f2(x[3]);
+  *least = __float_as_uint(min3(min3(a.x, a.y, b.x), min3(b.y, c.x, c.y), fminf(fabsf(d.x), fabsf(d.y))));
+  *most = __float_as_uint(max3(max3(max3(a.x, a.y, b.x), b.y, c.x), max3(c.y, d.x, d.y), 0.f));
 }
 // |y| (at most about 448, not NaN) with the part below an e4m3 step rounded up with probability remainder / step: the 16
 // bits are added below the last kept bit and the rest is cut.  Below 2^-6 the codes are 2^-9 apart, as they are from 2^-6
@@ -350,16 +358,19 @@ struct AdamwBlock {
       if constexpr (kMaster) low += e;
       if constexpr (kCodes) ms += blocks, vs += blocks;
     }
-    __device__ __forceinline__ int count() const { return min(8, max(0, left - (int)(threadIdx.x & 31) * 8)); }
-    __device__ __forceinline__ bool vec() const { return aligned && left >= MRL_STATE_BLOCK; }  // the same for the warp
+    // elements of the lane in the block `ahead` elements on; whether the block is whole and aligned (the same for the warp)
+    template <bool kWhole>
+    __device__ __forceinline__ int count(int ahead) const { return kWhole ? 8 : min(8, max(0, left - ahead - (int)(threadIdx.x & 31) * 8)); }
+    template <bool kWhole>
+    __device__ __forceinline__ bool vec(int ahead) const { return kWhole || (aligned && left - ahead >= MRL_STATE_BLOCK); }
   };
 
   // `ahead` blocks behind the cursor
+  template <bool kWhole>
   __device__ __forceinline__ void load(const Cursor& c, int ahead) {
     constexpr int kState = kCodes ? 1 : 4;
-    const int e = ahead * MRL_STATE_BLOCK, left = c.left - e;
-    const int n = min(8, max(0, left - (int)(threadIdx.x & 31) * 8));
-    const bool vec = c.aligned && left >= MRL_STATE_BLOCK;
+    const int e = ahead * MRL_STATE_BLOCK, n = c.template count<kWhole>(e);
+    const bool vec = c.template vec<kWhole>(e);
     g.load(c.g + e, n, vec);
     if constexpr (kCodes) {
       cm = load_codes(c.m + e, n, vec);
@@ -374,13 +385,14 @@ struct AdamwBlock {
   }
 };
 
-template <int kKind>
+// `in` is the block; where `next` blocks on there is another one, its loads take the registers once they are free.
+template <int kKind, bool kWhole>
 __device__ __forceinline__ void adamw_block(const AdamwArgs& a, const Hyper& hy, float gs, float decay, const typename AdamwBlock<kKind>::Cursor& c,
-                                            const AdamwBlock<kKind>& in) {
+                                            AdamwBlock<kKind>& in, bool more, int next) {
   using In = AdamwBlock<kKind>;
   constexpr bool kParamBf16 = In::kParamBf16, kMaster = In::kMaster, kCodes = In::kCodes;
-  const int n = c.count();
-  const bool vec = c.vec();
+  const int n = c.template count<kWhole>(0);
+  const bool vec = c.template vec<kWhole>(0);
   f2 m[4], v[4], p[4];
   if constexpr (kCodes) {
     decode(in.cm, in.sm, m);
@@ -394,22 +406,26 @@ __device__ __forceinline__ void adamw_block(const AdamwArgs& a, const Hyper& hy,
       v[j] = in.v.pair(j);
     }
   }
-  f2 root[4];
+  f2 root[4], g[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) g[j] = in.g.pair(j);
+  const Raw8<typename In::P> raw = in.p;
+  if (kCodes && more) in.template load<kWhole>(c, next);
   const f2 gs2 = make_f2(gs, gs), b1 = make_f2(a.beta1, a.beta1), o1 = make_f2(a.one_beta1, a.one_beta1);
   const f2 b2 = make_f2(a.beta2, a.beta2), o2 = make_f2(a.one_beta2, a.one_beta2);
   const f2 rc2 = make_f2(hy.root_c2, hy.root_c2), eps2 = make_f2(a.eps, a.eps), lr2 = make_f2(-hy.lr_c1, -hy.lr_c1);
   const f2 keep2 = make_f2(-hy.lr * decay, -hy.lr * decay);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const f2 gj = mul_f2(in.g.pair(j), gs2);
-    p[j] = in.p.pair(j);
+    const f2 gj = mul_f2(g[j], gs2);
+    p[j] = raw.pair(j);
     m[j] = add_apart(mul_f2(b1, m[j]), mul_f2(o1, gj));
     v[j] = add_apart(mul_f2(b2, v[j]), mul_f2(o2, mul_f2(gj, gj)));
   }
   uint32_t least_m = 0, most_m = 0, least_v = 0, most_v = 0;
   if constexpr (kCodes) {
-    bounds8<true>(m, &least_m, &most_m);
-    bounds8<false>(v, &least_v, &most_v);
+    bounds8(m, &least_m, &most_m);
+    bounds8(v, &least_v, &most_v);
     root8(v, least_v, most_v, root);
   }
 #pragma unroll
@@ -434,13 +450,11 @@ __device__ __forceinline__ void adamw_block(const AdamwArgs& a, const Hyper& hy,
   if constexpr (kMaster) store8(c.p, n, vec, p);
   if constexpr (kParamBf16) {
     uint32_t w[4];
-    f2 nothing = 0ull;  // 0, or NaN where a value is not finite
+    const bool cut = !kMaster && a.seeded;
+    if (cut) {  // the 16 bits that are cut decide against m's in reverse order
+      f2 nothing = 0ull;  // 0, or NaN where a value is not finite
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      w[j] = f2_to_bf16x2(p[j]);
-      if (!kMaster) nothing = fma_f2(p[j], 0ull, nothing);
-    }
-    if (!kMaster && a.seeded) {  // the 16 bits that are cut decide against m's in reverse order
+      for (int j = 0; j < 4; ++j) nothing = fma_f2(p[j], 0ull, nothing);
       const float2 none = split_f2(nothing);
       if (none.x + none.y == 0.f) {
 #pragma unroll
@@ -453,10 +467,15 @@ __device__ __forceinline__ void adamw_block(const AdamwArgs& a, const Hyper& hy,
         for (int j = 0; j < 4; ++j) {
           const float2 u = split_f2(p[j]);
           const uint32_t lo = __float_as_uint(u.x) + (__brev(bits[2 * j]) >> 16), hi = __float_as_uint(u.y) + (__brev(bits[2 * j + 1]) >> 16);
+          w[j] = f2_to_bf16x2(p[j]);
           if (fabsf(u.x) < INFINITY) w[j] = (w[j] & 0xffff0000u) | lo >> 16;
           if (fabsf(u.y) < INFINITY) w[j] = (w[j] & 0xffffu) | (hi & 0xffff0000u);
         }
       }
+    }
+    if (!cut) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = f2_to_bf16x2(p[j]);
     }
     store8_bf16(kMaster ? (void*)c.low : (void*)c.p, n, vec, w);
   } else {
@@ -563,13 +582,32 @@ __global__ void __cluster_dims__(kCluster) __launch_bounds__(kThreads) grad_norm
   }
 }
 
+// A chunk by its CTA.  kWhole: blocks of 256 aligned elements throughout, without tests.
+template <int kKind, bool kWhole>
+__device__ __forceinline__ void adamw_chunk(const AdamwArgs& a, const Hyper& hy, float gs, const Slot& s, long long lo, long long hi) {
+  constexpr int kNext = step_threads(kKind) / 32;
+  typename AdamwBlock<kKind>::Cursor c(s, lo + (threadIdx.x >> 5) * MRL_STATE_BLOCK, hi, hy.key);
+  if (c.left <= 0) return;
+  const float decay = s.decay;
+  AdamwBlock<kKind> in;
+  in.template load<kWhole>(c, 0);
+#pragma unroll 1
+  for (;;) {
+    const bool more = c.left > kNext * MRL_STATE_BLOCK;
+    adamw_block<kKind, kWhole>(a, hy, gs, decay, c, in, more, kNext);
+    if (!more) break;
+    c.advance(kNext);
+    if (!AdamwBlock<kKind>::kCodes) in.template load<kWhole>(c, 0);
+  }
+}
+
 // The tensors of one kind (types of gradient, parameter and states), which share the launch and its registers.
 // With float32 states bound by HBM: 622 M elements (28 bytes each) in 2,585 us, 6.7 TB/s.  With 8-bit states and seeded
-// rounding bound by the instructions' issue: a warp's 256 elements take some 550 of them (two 64-bit multiplications for
-// every two elements' random words, an IEEE root, codes both ways), 525 M elements (10 bytes each) 1,420 us, 3.7 TB/s; the
-// next block's loads are under way meanwhile, and 3 CTAs of 80 registers an SM measured faster than 4 of 64 (1,391, 1,527 us).
+// rounding bound by the instructions' issue: a warp's 256 elements take 480 of them (two 64-bit multiplications for
+// every two elements' random words, an IEEE root, codes both ways), 525 M elements (10 bytes each) 1,194 us, 4.4 TB/s.  The
+// next block's loads are under way meanwhile, into the registers that this block's have left.
 template <int kKind, int kN>
-__global__ void __launch_bounds__(kThreads, kKind & 8 ? kCodesCtas : 4) adamw_kernel(const __grid_constant__ Table<kN> t, const __grid_constant__ AdamwArgs a) {
+__global__ void __launch_bounds__(step_threads(kKind), step_ctas(kKind)) adamw_kernel(const __grid_constant__ Table<kN> t, const __grid_constant__ AdamwArgs a) {
   const float gs = a.grad_scale != nullptr ? *a.grad_scale : 1.f;
   if (!(fabsf(gs) < INFINITY)) {
     if (blockIdx.x == 0 && threadIdx.x == 0 && a.status != nullptr) atomicOr(a.status, MRL_DEV_NONFINITE_GRAD);
@@ -579,24 +617,10 @@ __global__ void __launch_bounds__(kThreads, kKind & 8 ? kCodesCtas : 4) adamw_ke
   const int k = slot_of(t, blockIdx.x);
   const Slot& s = t.slot[k];
   const long long lo = (long long)(blockIdx.x - t.first[k]) * t.chunk, hi = min(lo + t.chunk, s.numel);
-  constexpr bool kAhead = (kKind & 8) != 0;
-  constexpr int kNext = kThreads / 32;
-  typename AdamwBlock<kKind>::Cursor c(s, lo + (threadIdx.x >> 5) * MRL_STATE_BLOCK, hi, hy.key);
-  if (c.left <= 0) return;
-  const float decay = s.decay;
-  AdamwBlock<kKind> in;
-  in.load(c, 0);
-#pragma unroll 1
-  for (;;) {
-    // the next block is on its way while this one is worked on
-    AdamwBlock<kKind> next;
-    const bool more = c.left > kNext * MRL_STATE_BLOCK;
-    if (kAhead && more) next.load(c, kNext);
-    adamw_block<kKind>(a, hy, gs, decay, c, in);
-    if (!more) break;
-    c.advance(kNext);
-    if (kAhead) in = next; else in.load(c, 0);
-  }
+  if (s.aligned && ((hi - lo) & (MRL_STATE_BLOCK - 1)) == 0)
+    adamw_chunk<kKind, true>(a, hy, gs, s, lo, hi);
+  else
+    adamw_chunk<kKind, false>(a, hy, gs, s, lo, hi);
 }
 
 bool grad_type_ok(int32_t dtype) { return dtype == MRL_BF16 || dtype == MRL_F32; }
@@ -639,16 +663,16 @@ int fill_table(const mrl_tensor_slot* slots, int n, int at, int chunk, int only,
 }
 
 // Elements of a chunk: small ones while there are few, for the sake of parallel CTAs; `most` times as many otherwise.
-int chunk_of(const mrl_tensor_slot* slots, int n, int most) {
+int chunk_of(const mrl_tensor_slot* slots, int n, int threads, int most) {
   long long total = 0;
   for (int k = 0; k < n; ++k) total += slots[k].numel;
-  return total <= (long long)kSms * 8 * 4 * kChunk ? kChunk : most * kChunk;
+  return threads * 8 * (total <= (long long)kSms * 8 * 4 * kChunk ? 1 : most);
 }
 
 template <int kN>
 int launch_grad_norm(const mrl_tensor_slot* slots, int n, float max_norm, float* norm, float* coef, double* partial, cudaStream_t st) {
   Table<kN> t;
-  const int chunk = chunk_of(slots, n, 8);
+  const int chunk = chunk_of(slots, n, kThreads, 8);
   int ctas = 0;
   for (int at = 0; at < n || ctas == 0;) {
     at = fill_table(slots, n, at, chunk, -1, &t);
@@ -680,7 +704,7 @@ int launch_adamw_kind(const mrl_tensor_slot* slots, int n, int chunk, const Adam
     at = fill_table(slots, n, at, chunk, kKind, &t);
     if (t.n == 0) break;
     mrl_profile_before(st, "adamw_kernel");
-    adamw_kernel<kKind, kN><<<t.first[t.n], kThreads, 0, st>>>(t, a);
+    adamw_kernel<kKind, kN><<<t.first[t.n], step_threads(kKind), 0, st>>>(t, a);
     mrl_profile_after(st);
     MRL_CUDA_OK(cudaGetLastError());
   }
@@ -763,9 +787,7 @@ extern "C" int mrl_adamw_step(const mrl_tensor_slot* slots, int32_t n_slots, con
   }
   int count[16] = {0};
   for (int k = 0; k < n_slots; ++k) count[kind_of(slots[k])] += slots[k].numel > 0;
-  // (output layer, 622 M elements: 2,583 us with chunks of 4 and float32 states, 2,624 with 8; 8-bit, whose next block is on its
-  // way while one is worked on: 1,525 and 1,391)
-  const int chunk[2] = {chunk_of(slots, n_slots, 4), chunk_of(slots, n_slots, 8)};
+  const int chunk[2] = {chunk_of(slots, n_slots, step_threads(0), step_blocks(0)), chunk_of(slots, n_slots, step_threads(8), step_blocks(8))};
   int rc = MRL_OK;
   const auto run = [&](auto kind) {
     constexpr int kKind = decltype(kind)::value;

@@ -369,6 +369,37 @@ def test_codes_are_those_of_the_float32_operations_bit_for_bit(seeded):
             assert torch.equal(c.b[k][1][:n].view(torch.uint8), want[k].view(torch.uint8)), (k, step)
 
 
+@pytest.mark.parametrize("param,master,grad,state", KINDS)
+@pytest.mark.parametrize("tail", [0, 77])
+def test_large_calls_give_what_their_pieces_give_alone(param, master, grad, state, tail):
+    """A call of more than 9.7 M elements gives its CTAs longer runs: bit for bit the results of calls of fewer."""
+    n, cut = 256 * 40_000 + tail, 256 * 13_001
+    g = torch.Generator(device="cuda").manual_seed(5)
+    start = {"grad": torch.randn(n, generator=g, device="cuda").to(grad), "param": torch.randn(n, generator=g, device="cuda").to(param)}
+    if master:
+        start["master"] = start["param"].float()
+    if state == E4M3:
+        for name in ("m", "v"):
+            start[name] = torch.randint(0, 0x7F, (n,), generator=g, device="cuda", dtype=torch.uint8).view(E4M3)
+            start[name + "_scale"] = torch.rand(-(-n // 256), generator=g, device="cuda") * 1e-4
+    else:
+        start["m"], start["v"] = torch.randn(n, generator=g, device="cuda"), torch.rand(n, generator=g, device="cuda")
+    large, parts = ({k: t.clone() for k, t in start.items()} for _ in range(2))
+
+    def slot(tensors, lo, hi):
+        of = {k: t[lo // 256:-(-hi // 256)] if k.endswith("_scale") else t[lo:hi] for k, t in tensors.items()}
+        return B.TensorSlot(**of, weight_decay=0.01, rng_first=100 + lo // 2)
+
+    ap = B.AdamwParams(lr=LR, beta1=B1, beta2=B2, eps=EPS, step=3, seed=9, rounding=B.ROUND_SEEDED)
+    B.mrl_adamw_step(B.TensorList([slot(large, 0, n)]), ap)
+    for lo in range(0, n, cut):
+        B.mrl_adamw_step(B.TensorList([slot(parts, lo, min(n, lo + cut))]), ap)
+    torch.cuda.synchronize()
+    for k in start:
+        assert torch.equal(large[k].view(torch.uint8), parts[k].view(torch.uint8)), k
+        assert k == "grad" or not torch.equal(large[k].view(torch.uint8), start[k].view(torch.uint8)), k
+
+
 def test_a_state_that_is_not_finite_stays_in_its_block():
     for kind in KINDS:
         for seeded in (None, 3):
