@@ -4,8 +4,8 @@
 // Forward: h = x + r, rstd = 1 / sqrt(mean h^2 + eps), y = h rstd (w + o), optionally as e4m3 codes with a scale per group.
 // Backward: with g = (w + o) dy and xhat = h rstd, dx = dh + rstd (g - xhat mean(g xhat)), dw = sum over rows of dy xhat.
 // A few operations per element against 6 to 9 bytes: bound by HBM where rows are whole 16-byte granules (65,536 x 4,096 bf16:
-// forward with residual 343-350 us, backward 344-349 us, 6.1-6.3 TB/s of the bytes that have to move; e4m3 codes beside y, 33,880
-// rows: 208 us, 6.0 TB/s), by the instructions' issue where they are not (65,552 x 4,095: 564 and 537 us).
+// forward with residual 334-339 us, backward 340-349 us, 6.1-6.4 TB/s of the bytes that have to move; e4m3 codes beside y, 33,880
+// rows: 208 us, 6.0 TB/s), by the instructions' issue where they are not (65,552 x 4,095: 553 and 537 us).
 #include <type_traits>
 
 #include "mrl_common.cuh"
@@ -204,7 +204,7 @@ struct Unit {
       p[0] = make_f2(in0 ? load_f(e) : 0.f, in1 ? load_f(e + 32) : 0.f);
     }
   }
-  // to shared memory (odd rows: their copy) or global memory
+  // to the unit's place in a row
   __device__ __forceinline__ void store(T* to, bool in0, bool in1) const {
     if constexpr (!kOdd) {
       if (in0) *reinterpret_cast<uint4*>(to) = bits();
@@ -275,12 +275,12 @@ __device__ __forceinline__ void copy_wait(int newer) {
 
 // Where a row's bytes lie in a copy of the 16-byte granules that hold them (rows of any alignment).
 struct Image {
-  char* first;   // granule with the row's first byte
-  int off, len;  // first byte inside it; bytes of the row
+  const char* first;  // granule with the row's first byte
+  int off, len;       // first byte inside it; bytes of the row
 };
 template <typename P>
-__device__ __forceinline__ Image image_of(P* base, long long element, int H) {
-  char* p = const_cast<char*>(reinterpret_cast<const char*>(base + element));
+__device__ __forceinline__ Image image_of(const P* base, long long element, int H) {
+  const char* p = reinterpret_cast<const char*>(base + element);
   const int off = (int)(reinterpret_cast<uintptr_t>(p) & 15);
   return Image{p - off, off, H * (int)sizeof(P)};
 }
@@ -294,19 +294,6 @@ __device__ __forceinline__ void image_load(char* dst, const Image& im, const T* 
   if (by_element) {
     const int b = im.off + (int)threadIdx.x * (int)sizeof(T);
     if (b < min(16, end)) *reinterpret_cast<T*>(dst + b) = *reinterpret_cast<const T*>(im.first + b);
-  }
-}
-// The copy's granules to the row: whole ones at once, what the row has of its first and last one by element.
-template <typename P>
-__device__ __forceinline__ void image_store(const char* src, const Image& im) {
-  const int end = im.off + im.len, from = im.off != 0, to = end / 16;
-  for (int k = from + (int)threadIdx.x; k < to; k += blockDim.x)
-    *reinterpret_cast<uint4*>(im.first + 16 * k) = *reinterpret_cast<const uint4*>(src + 16 * k);
-  if (threadIdx.x < 32) {
-    const int j = (threadIdx.x & 15) * (int)sizeof(P), tail = max(to, from) * 16 + j, head = im.off + j;
-    const bool first = threadIdx.x < 16;
-    const int b = first ? head : tail;
-    if (first ? im.off != 0 && b < min(16, end) : b < end) *reinterpret_cast<P*>(im.first + b) = *reinterpret_cast<const P*>(src + b);
   }
 }
 // A magnitude as an ordered integer, 0 for NaN.
@@ -346,17 +333,12 @@ __device__ __forceinline__ float row_reduce(float v, float* red) {
   return kMax ? fmaxf(fmaxf(s.x, s.y), fmaxf(s.z, s.w)) : (s.x + s.y) + (s.z + s.w);
 }
 
-// Copies of a row that a stage holds.
-__host__ __device__ __forceinline__ int fwd_slots(const NormFwdArgs& a, bool odd) {
-  const int in = 1 + (a.res != nullptr), out = (a.h_out != nullptr) + (a.y != nullptr);
-  return odd && out > in ? out : in;
-}
-
 // Rows of up to kRowMax columns, each read once and written once.  A CTA walks rows blockIdx.x, + gridDim.x, ...; the rows to
 // come are under way into shared memory (`stages` of them, 16-byte asynchronous copies), so the bytes in flight do not
 // depend on registers.  kOdd = false: rows of 16-byte granules; a thread copies the granules whose columns it works on
 // and needs no barrier to read them.  kOdd = true: rows of any alignment; the granules are copied as they lie and read by
-// column after a barrier, and outputs go the same way back.
+// column after a barrier; outputs go from registers to their rows by element (32,776 x 4,095 float32: 429 us, through shared
+// memory 484; bf16 of 61, 4,095, 8,191 columns: 140, 553, 610 us, 189, 563, 592).
 // Columns: a warp owns 32 * kRowCols adjacent ones, unit u of a lane lies u * kStep behind its first.  A warp whose columns
 // all lie inside the row runs without tests (kFull).
 // kCodes: what of y8 there is (its code costs registers): nothing, one scale a row, one a group.
@@ -371,8 +353,7 @@ __global__ void __maxnreg__(fwd_regs(kRowCols)) rmsnorm_fwd_row_kernel(const __g
   const int c0 = (tid >> 5) * (kUnits * kStep) + (tid & 31) * (kOdd ? 1 : U::kCols);
   const bool full = ((tid >> 5) + 1) * (kUnits * kStep) <= a.H;
   const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : nt * kRowCols * (int)sizeof(T);
-  const int stage = fwd_slots(a, kOdd) * slot;
-  char* img_q = smem + a.stages * stage;
+  const int stage = a.res != nullptr ? 2 * slot : slot;
   const int group = a.group > 0 ? a.group : a.H, groups = (a.H + group - 1) / group;
   // lanes whose columns share a scale sit side by side; more than a warp of them meet in shared memory
   const bool meet = kCodes == kGroupCodes && a.group > (kOdd ? 32 : kStep);
@@ -478,13 +459,8 @@ __global__ void __maxnreg__(fwd_regs(kRowCols)) rmsnorm_fwd_row_kernel(const __g
     if (tid == 0 && a.rstd != nullptr) a.rstd[row] = rstd;
 
     const f2 rstd2 = make_f2(rstd, rstd);
-    const int y_at = a.h_out != nullptr ? slot : 0;  // odd rows: outputs take the place of the row's inputs, which have all been read
     T* to_h = static_cast<T*>(a.h_out) + row * a.ld_h + c0;
     T* to_y = static_cast<T*>(a.y) + row * a.ld_y + c0;
-    if (kOdd) {
-      to_h = reinterpret_cast<T*>(here + image_of(static_cast<T*>(a.h_out), row * a.ld_h, a.H).off) + c0;
-      to_y = reinterpret_cast<T*>(here + y_at + image_of(static_cast<T*>(a.y), row * a.ld_y, a.H).off) + c0;
-    }
     const auto write = [&](auto all, auto w) {
       constexpr bool kFull = decltype(all)::value;
 #pragma unroll
@@ -539,7 +515,6 @@ __global__ void __maxnreg__(fwd_regs(kRowCols)) rmsnorm_fwd_row_kernel(const __g
       }
       float* scales = a.scales + row * groups;
       uint8_t* q = a.y8 + row * a.ld_y8 + c0;
-      if (kOdd) q = reinterpret_cast<uint8_t*>(img_q) + image_of(a.y8, row * a.ld_y8, a.H).off + c0;
       // unit u as codes; inv0, inv1: 1 / scale of columns c on, and in odd rows of column c + 32
       const auto put_codes = [&](int u, float inv0, float inv1) {
         const int c = c0 + u * kStep;
@@ -601,12 +576,7 @@ __global__ void __maxnreg__(fwd_regs(kRowCols)) rmsnorm_fwd_row_kernel(const __g
         });
       }
     }
-    if constexpr (kOdd) {
-      __syncthreads();
-      if (a.h_out != nullptr) image_store<T>(here, image_of(static_cast<T*>(a.h_out), row * a.ld_h, a.H));
-      if (a.y != nullptr) image_store<T>(here + y_at, image_of(static_cast<T*>(a.y), row * a.ld_y, a.H));
-      if (kCodes != kNoCodes) image_store<uint8_t>(img_q, image_of(a.y8, row * a.ld_y8, a.H));
-    } else if (meet) {
+    if (!kOdd && meet) {
       __syncthreads();  // the next row clears the peaks
     }
   }
@@ -673,8 +643,7 @@ __global__ void __maxnreg__(kRegs) rmsnorm_bwd_row_kernel(const __grid_constant_
       fetch(row + (long long)(a.stages - 1) * gridDim.x, s == 0 ? a.stages - 1 : s - 1);
       copy_wait(a.stages - 1);
     }
-    char* img = smem + s * stage;  // odd rows: dx takes dy's place, which all have read before the row's sum is there
-    const char* in_d = img + (kOdd ? c0 * (int)sizeof(T) : tid * 16);
+    const char* in_d = smem + s * stage + (kOdd ? c0 * (int)sizeof(T) : tid * 16);
     const char *in_h = in_d + slot, *in_e = in_h + slot;
     if (kOdd) {
       in_d += image_of(static_cast<const T*>(a.dy), row * a.ld_dy, a.H).off;
@@ -715,7 +684,6 @@ __global__ void __maxnreg__(kRegs) rmsnorm_bwd_row_kernel(const __grid_constant_
     const float mean = row_reduce<false>(part.x + part.y, red[turn]) * a.inv_h;
 
     T* out = static_cast<T*>(a.dx) + row * a.ld_dx + c0;
-    if (kOdd) out = reinterpret_cast<T*>(img + image_of(static_cast<T*>(a.dx), row * a.ld_dx, a.H).off) + c0;
     const f2 minus2 = make_f2(-rstd * mean, -rstd * mean);
     const auto write = [&](auto all) {
       constexpr bool kFull = decltype(all)::value;
@@ -738,10 +706,6 @@ __global__ void __maxnreg__(kRegs) rmsnorm_bwd_row_kernel(const __grid_constant_
       }
     };
     if (full) write(std::true_type{}); else write(std::false_type{});
-    if constexpr (kOdd) {
-      __syncthreads();
-      image_store<T>(img, image_of(static_cast<T*>(a.dx), row * a.ld_dx, a.H));
-    }
   }
   if (a.partial != nullptr) {
     float* to = a.partial + (size_t)blockIdx.x * a.H + c0;
@@ -792,7 +756,7 @@ int row_threads(int H, int cols) { return (H + cols * 32 - 1) / (cols * 32) * 32
 // Columns of a thread.  Few rows, or short ones, are spread over more threads (one row of 4,096: 2.5 us with 8 columns, 3.4
 // with 32; 262,144 rows of 64: 93 us with 8, 133 with 16).  Forward, 32 columns are fastest for rows of 2 to 16 KB in 16-byte
 // granules once there are many (65,536 x 4,096 bf16: 341 us with 32, 374 with 16; 32,768 x 8,192: 338, 357), 16 for wider rows
-// (16,384 x 16,384: 356, 339), for fewer (1,024 x 4,096: 8.9, 7.6) and for odd ones (65,552 x 4,095: 727, 633).  Backward,
+// (16,384 x 16,384: 356, 339), for fewer (1,024 x 4,096: 8.9, 7.6) and for odd ones (65,552 x 4,095: 557 us, 624 with 8).  Backward,
 // whose sums take registers, 16 (65,536 x 4,096: 394 with 32, 367 with 16).
 bool few_or_short(long long N, int H) { return H <= 512 || (H <= 512 * kNarrow && N <= 2 * kSms); }
 int fwd_cols(long long N, int H, int elem, bool odd) {
@@ -805,24 +769,24 @@ bool aligned(const void* p, long long ld, int elem, int bytes) {
   return p == nullptr || ((reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0 && (ld * elem) % bytes == 0);
 }
 
-// How a row kernel is launched.  CTAs per SM: as many as their registers allow and as leave each at least two rows in shared
+// How a row kernel is launched.  CTAs per SM: as many as their registers allow and as leave each at least `rows` rows in shared
 // memory; stages: what fits then, 4 at most.
 struct RowPlan {
   int threads, ctas_per_sm, stages, smem;
 };
 constexpr int kSmemPerSm = 227 * 1024, kSmemCta = 227 * 1024 - 4096;  // (4 KB: the kernels' own arrays and the system's)
-RowPlan plan_rows(int threads, int regs, int stage_bytes, int out_bytes) {
+RowPlan plan_rows(int threads, int regs, int stage_bytes, int rows = 2) {
   RowPlan p;
   p.threads = threads;
   int c = 4 * (16384 / (regs * 32)) / (threads / 32);  // (each quarter of the SM holds whole warps)
   if (c > 32) c = 32;
   if (c < 1) c = 1;
   const int own = 4096;
-  while (c > 1 && c * (2 * stage_bytes + out_bytes + own) > kSmemPerSm) --c;
-  const int s = stage_bytes > 0 ? (kSmemPerSm / c - own - out_bytes) / stage_bytes : 1;
+  while (c > 1 && c * (rows * stage_bytes + own) > kSmemPerSm) --c;
+  const int s = stage_bytes > 0 ? (kSmemPerSm / c - own) / stage_bytes : 1;
   p.stages = s > 4 ? 4 : (s < 1 ? 1 : s);
   p.ctas_per_sm = c;
-  p.smem = p.stages * stage_bytes + out_bytes;
+  p.smem = p.stages * stage_bytes;
   return p;
 }
 // CTAs of the backward kernels, and rows of dweight partials; the most that any alignment and type of the rows leads to.
@@ -831,7 +795,14 @@ int bwd_ctas(long long N, int per_sm) {
   const long long most = (long long)kSms * per_sm, few = N / 4 > kSms ? N / 4 : kSms;
   return (int)(N < few ? N : (few < most ? few : most));
 }
-int bwd_ctas_most(long long N, int H) { return bwd_ctas(N, H <= kRowMax ? plan_rows(row_threads(H, kMiddle), kBwdRegs, 0, 0).ctas_per_sm : 2); }
+int bwd_ctas_most(long long N, int H) { return bwd_ctas(N, H <= kRowMax ? plan_rows(row_threads(H, kMiddle), kBwdRegs, 0).ctas_per_sm : 2); }
+
+// Forward, two tensors in and no codes out: where a tensor does not fit L2, fewer CTAs with three rows each are faster (65,536 x
+// 4,096 bf16: 352 us with two rows, 337 with three, 355 with four; 131,072 x 2,048: 364, 344, 357), but not where it does (8,192 x
+// 4,096: 45.2, 46.3), nor where three rows leave less than three CTAs (49,152 x 6,144: 384, 393), nor for the others (e4m3 codes
+// beside y: 335, 371; backward 343, 388).
+constexpr long long kFewerBytes = 100000000;
+constexpr int kFewerStage = 20480;
 
 template <typename K>
 int allow_smem(K kernel, std::atomic<uint64_t>& done) {
@@ -842,7 +813,9 @@ template <typename T, bool kOdd, int kCols, int kCodes>
 int launch_fwd_codes(NormFwdArgs a, cudaStream_t st) {
   const int threads = row_threads(a.H, kCols);
   const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : threads * kCols * (int)sizeof(T);
-  const RowPlan p = plan_rows(threads, fwd_regs(kCols), fwd_slots(a, kOdd) * slot, kOdd && a.y8 != nullptr ? image_bytes(a.H, 1) : 0);
+  const int stage = (a.res != nullptr ? 2 : 1) * slot;
+  const bool fewer = !kOdd && kCodes == kNoCodes && a.res != nullptr && stage <= kFewerStage && a.N * a.H >= kFewerBytes / (int)sizeof(T);
+  const RowPlan p = plan_rows(threads, fwd_regs(kCols), stage, fewer ? 3 : 2);
   if (p.smem > kSmemCta) return -1;
   a.stages = p.stages;
   const long long most = (long long)kSms * p.ctas_per_sm;
@@ -863,7 +836,7 @@ template <typename T, bool kOdd, int kCols, int kRegs>
 int launch_bwd_regs(NormBwdArgs a, int* ctas, cudaStream_t st) {
   const int threads = row_threads(a.H, kCols);
   const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : threads * kCols * (int)sizeof(T);
-  const RowPlan p = plan_rows(threads, kRegs, (a.dh != nullptr ? 3 : 2) * slot, 0);
+  const RowPlan p = plan_rows(threads, kRegs, (a.dh != nullptr ? 3 : 2) * slot);
   if (p.smem > kSmemCta) return -1;
   a.stages = p.stages;
   *ctas = bwd_ctas(a.N, p.ctas_per_sm);
