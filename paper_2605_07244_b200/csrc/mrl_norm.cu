@@ -5,7 +5,7 @@
 // Backward: with g = (w + o) dy and xhat = h rstd, dx = dh + rstd (g - xhat mean(g xhat)), dw = sum over rows of dy xhat.
 // A few operations per element against 6 to 9 bytes: bound by HBM where rows are whole 16-byte granules (65,536 x 4,096 bf16:
 // forward with residual 334-339 us, backward 340-349 us, 6.1-6.4 TB/s of the bytes that have to move; e4m3 codes beside y, 33,880
-// rows: 208 us, 6.0 TB/s), by the instructions' issue where they are not (65,552 x 4,095: 553 and 537 us).
+// rows: 204-209 us, 6.1 TB/s), by the instructions' issue where they are not (65,552 x 4,095: 553 and 537 us).
 #include <type_traits>
 
 #include "mrl_common.cuh"
@@ -21,7 +21,9 @@ constexpr int kNoCodes = 0, kRowCodes = 1, kGroupCodes = 2;
 constexpr int kRowMax = 16384;                            // the widest row that one CTA holds
 // registers of a thread of the row kernels
 constexpr int kBwdRegs = 64, kBwdRegsMore = 80;
-constexpr int fwd_regs(int cols) { return cols == kWide ? 80 : 64; }  // (wide: shared memory allows no more CTAs anyway)
+// (wide: shared memory allows no more CTAs anyway; codes by group spill below 96: 33,880 rows of 4,096 208 us, with 80 216; 65,536 of
+// 2,048 166 and 174, but without a residual 118 and 115, and with one scale a row 170 and 167)
+constexpr int fwd_regs(int cols, int codes) { return cols != kWide ? 64 : (codes == kGroupCodes ? 96 : 80); }
 
 template <typename T>
 __device__ __forceinline__ float load_f(const T* p);
@@ -343,7 +345,7 @@ __device__ __forceinline__ float row_reduce(float v, float* red) {
 // all lie inside the row runs without tests (kFull).
 // kCodes: what of y8 there is (its code costs registers): nothing, one scale a row, one a group.
 template <typename T, bool kOdd, int kRowCols, int kCodes>
-__global__ void __maxnreg__(fwd_regs(kRowCols)) rmsnorm_fwd_row_kernel(const __grid_constant__ NormFwdArgs a) {
+__global__ void __maxnreg__(fwd_regs(kRowCols, kCodes)) rmsnorm_fwd_row_kernel(const __grid_constant__ NormFwdArgs a) {
   using U = Unit<T, kOdd>;
   constexpr int kUnits = kRowCols / U::kCols, kStep = U::kStep, kPairs = U::kPairs, kHalf = kOdd ? 32 : 0;
   extern __shared__ __align__(16) char smem[];
@@ -815,7 +817,7 @@ int launch_fwd_codes(NormFwdArgs a, cudaStream_t st) {
   const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : threads * kCols * (int)sizeof(T);
   const int stage = (a.res != nullptr ? 2 : 1) * slot;
   const bool fewer = !kOdd && kCodes == kNoCodes && a.res != nullptr && stage <= kFewerStage && a.N * a.H >= kFewerBytes / (int)sizeof(T);
-  const RowPlan p = plan_rows(threads, fwd_regs(kCols), stage, fewer ? 3 : 2);
+  const RowPlan p = plan_rows(threads, fwd_regs(kCols, kCodes), stage, fewer ? 3 : 2);
   if (p.smem > kSmemCta) return -1;
   a.stages = p.stages;
   const long long most = (long long)kSms * p.ctas_per_sm;
