@@ -314,6 +314,28 @@ def test_backward_of_more_rows_than_run_at_once(N, H, dtype):
         assert torch.equal(over["dx"], out["dx"]) and torch.equal(over["dw"], out["dw"])
 
 
+@pytest.mark.parametrize("N,H,dtype", [(13000, 4096, BF16), (50000, 1024, BF16), (12500, 2048, F32), (10000, 5120, BF16), (13001, 4095, BF16)])
+def test_large_forward_calls_give_what_their_pieces_give_alone(N, H, dtype):
+    """Tensors above 100 MB run with fewer CTAs; pieces of more than 2,048 rows have the same sums, so the same bits."""
+    x, res = random_rows(N, H, dtype, 1), random_rows(N, H, dtype, 2, scale=2.0)
+    w = torch.randn(H, generator=torch.Generator().manual_seed(7)).to(dtype).cuda()
+    np = B.NormParams(1e-6, 1.0, 0, 0)
+    h, y, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(N, device="cuda")
+    B.mrl_rmsnorm_residual_fwd(x, res, w, np, h, y, rstd=rstd)
+    ph, py, prstd = torch.empty_like(x), torch.empty_like(x), torch.empty(N, device="cuda")
+    cuts = list(range(0, N, 2500))[:-1] + [N]
+    for lo, hi in zip(cuts, cuts[1:]):
+        B.mrl_rmsnorm_residual_fwd(x[lo:hi], res[lo:hi], w, np, ph[lo:hi], py[lo:hi], rstd=prstd[lo:hi])
+    torch.cuda.synchronize()
+    assert torch.equal(h, ph) and torch.equal(y, py) and torch.equal(rstd, prstd)
+    some = slice(N - 40, N)
+    ref = S.rmsnorm_residual_fwd(x[some], res[some], w, 1.0, float(torch.tensor(1e-6, dtype=F32)))
+    check_fwd(x[some], res[some], w, {"h": h[some], "y": y[some], "rstd": rstd[some]}, ref, 1.0, 0)
+    B.mrl_rmsnorm_residual_fwd(x, res, w, np, res, x, rstd=rstd)
+    torch.cuda.synchronize()
+    assert torch.equal(res, h) and torch.equal(x, y) and torch.equal(rstd, prstd)
+
+
 @pytest.mark.parametrize("H", [8193, 10007, 12001, 16383])
 def test_wide_rows_of_odd_width(H):
     """float32 rows that leave no room for a second row, or for one, in shared memory."""
