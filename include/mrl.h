@@ -132,7 +132,8 @@ typedef struct mrl_norm_params {
   uint32_t flags;           /* backward only: MRL_FLAG_ACCUMULATE_DW (dweight is added to, not overwritten) */
 } mrl_norm_params;
 
-/* One tensor of mrl_grad_norm / mrl_adamw_step.  Contiguous; every pointer [device]. */
+/* One tensor of mrl_grad_norm / mrl_adamw_step.  Contiguous; every pointer [device] and a multiple of its element (else
+ * MRL_ERR_INVALID_ARG). */
 typedef struct mrl_tensor_slot {
   const void* grad;         /* grad_dtype [numel] */
   void* param;              /* param_dtype [numel] */
@@ -477,8 +478,8 @@ int mrl_thl_word_align_logprobs(const float* src_logp, const int32_t* src_word, 
  * One output at least has to be given; outputs must not overlap one another, nor an input otherwise than said.
  * Bitwise reproducible.  One read of each input where H <= 16,384.  Any row stride and address that is a multiple of the
  * element; rows whose addresses and H are multiples of 16 bytes are about 1.6 times as fast as others.  N = 0 is a no-op.
- * H < 1, a row stride below H, a null required pointer, eps that is not finite and positive, an unknown group ->
- * MRL_ERR_INVALID_ARG; H > 2^30 -> MRL_ERR_UNSUPPORTED_SHAPE.
+ * H < 1, a row stride below H, a null required pointer, an address that is not a multiple of its element, eps that is not
+ * finite and positive, an unknown group -> MRL_ERR_INVALID_ARG; H > 2^30 -> MRL_ERR_UNSUPPORTED_SHAPE.
  */
 int mrl_rmsnorm_residual_fwd(const void* x, int64_t ld_x, const void* residual, int64_t ld_res, int32_t dtype,
                              const void* weight, int32_t w_dtype, int64_t N, int32_t H, const mrl_norm_params* np,
@@ -501,6 +502,7 @@ int mrl_rmsnorm_residual_fwd(const void* x, int64_t ld_x, const void* residual, 
  *   dweight [device] float32 [H], nullable; overwritten, or added to under MRL_FLAG_ACCUMULATE_DW
  *   workspace: mrl_workspace_bytes(MRL_WS_RMSNORM_BWD, N, 0, H, 0, 0); may be NULL where dweight is
  * float32 arithmetic and sums in a fixed order: bitwise reproducible.  N = 0: dweight is zeroed unless accumulated.
+ * Errors as in the forward pass.
  */
 int mrl_rmsnorm_residual_bwd(const void* dy, int64_t ld_dy, const void* dh, int64_t ld_dh, const void* h, int64_t ld_h,
                              int32_t dtype, const void* weight, int32_t w_dtype, const float* rstd, int64_t N, int32_t H,
@@ -544,6 +546,8 @@ int mrl_grad_norm(const mrl_tensor_slot* slots, int32_t n_slots, float max_norm,
  *   workspace: mrl_workspace_bytes(MRL_WS_ADAMW, 0, 0, 0, 0, 0); may be NULL unless lr_dev or step_dev is given
  * Bitwise reproducible.  A non-finite gradient that grad_scale does not announce spoils its element (8-bit
  * states: its block).  n_slots = 0 with step_dev still counts the step.
+ * A null required pointer, an address that is not a multiple of its element, parameters outside their ranges ->
+ * MRL_ERR_INVALID_ARG.
  */
 int mrl_adamw_step(const mrl_tensor_slot* slots, int32_t n_slots, const mrl_adamw_params* ap, const float* grad_scale,
                    int32_t* status, void* workspace, size_t workspace_bytes, void* stream);

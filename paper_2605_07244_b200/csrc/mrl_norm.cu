@@ -903,7 +903,7 @@ extern "C" int mrl_rmsnorm_residual_fwd(const void* x, int64_t ld_x, const void*
   const bool bf16 = dtype == MRL_BF16;
   const int elem = bf16 ? 2 : 4;
   if (!on_element(x, elem) || !on_element(residual, elem) || !on_element(h_out, elem) || !on_element(y, elem) ||
-      !on_element(weight, w_dtype == MRL_BF16 ? 2 : 4))
+      !on_element(weight, w_dtype == MRL_BF16 ? 2 : 4) || (y8 != nullptr && !on_element(scales, 4)) || !on_element(rstd, 4))
     return MRL_ERR_INVALID_ARG;
   NormFwdArgs a{x, residual, weight, h_out, y, static_cast<uint8_t*>(y8), scales, rstd, ld_x, ld_res, ld_h, ld_y, ld_y8, N,
                 H, np->group, w_dtype == MRL_BF16, np->eps, np->weight_offset, 1.0f / (float)H, 0};
@@ -946,7 +946,7 @@ extern "C" int mrl_rmsnorm_residual_bwd(const void* dy, int64_t ld_dy, const voi
   const bool bf16 = dtype == MRL_BF16;
   const int elem = bf16 ? 2 : 4;
   if (!on_element(dy, elem) || !on_element(dh, elem) || !on_element(h, elem) || !on_element(dx, elem) ||
-      !on_element(weight, w_dtype == MRL_BF16 ? 2 : 4))
+      !on_element(weight, w_dtype == MRL_BF16 ? 2 : 4) || !on_element(rstd, 4) || !on_element(dweight, 4))
     return MRL_ERR_INVALID_ARG;
   if (dweight != nullptr) {
     if (workspace == nullptr || workspace_bytes < mrl_rmsnorm_bwd_workspace_bytes(N, H)) return MRL_ERR_WORKSPACE_TOO_SMALL;

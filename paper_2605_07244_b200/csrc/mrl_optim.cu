@@ -627,6 +627,15 @@ bool grad_type_ok(int32_t dtype) { return dtype == MRL_BF16 || dtype == MRL_F32;
 
 bool aligned_to(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
+// Every pointer has to be a multiple of its element: a kernel's access anywhere else loses the context.  (Codes are bytes.)
+int elem_bytes(int32_t dtype) { return dtype == MRL_BF16 ? 2 : 4; }
+bool on_elements(const mrl_tensor_slot& s) {
+  const uintptr_t state = s.state_dtype == MRL_E4M3 ? 1 : 4;
+  return aligned_to(s.grad, elem_bytes(s.grad_dtype)) && aligned_to(s.param, elem_bytes(s.param_dtype)) && aligned_to(s.master, 4) &&
+         aligned_to(s.m, state) && aligned_to(s.v, state) &&
+         (s.state_dtype != MRL_E4M3 || (aligned_to(s.m_scale, 4) && aligned_to(s.v_scale, 4)));
+}
+
 // Groups of eight elements: 32 bytes of float32, 16 of bf16, 8 of codes.
 bool grad_aligned(const mrl_tensor_slot& s) { return aligned_to(s.grad, s.grad_dtype == MRL_BF16 ? 16 : 32); }
 bool all_aligned(const mrl_tensor_slot& s) {
@@ -726,11 +735,13 @@ size_t mrl_adamw_workspace_bytes() { return 256; }
 
 extern "C" int mrl_grad_norm(const mrl_tensor_slot* slots, int32_t n_slots, float max_norm, float* norm, float* coef,
                              void* workspace, size_t workspace_bytes, void* stream) {
-  if (n_slots < 0 || (n_slots > 0 && slots == nullptr) || max_norm != max_norm || (norm == nullptr && coef == nullptr))
+  if (n_slots < 0 || (n_slots > 0 && slots == nullptr) || max_norm != max_norm || (norm == nullptr && coef == nullptr) ||
+      !aligned_to(norm, 4) || !aligned_to(coef, 4))
     return MRL_ERR_INVALID_ARG;
   for (int k = 0; k < n_slots; ++k) {
     if (!grad_type_ok(slots[k].grad_dtype)) return MRL_ERR_UNSUPPORTED_DTYPE;
-    if (slots[k].numel < 0 || slots[k].numel > kMaxNumel || (slots[k].numel > 0 && slots[k].grad == nullptr))
+    if (slots[k].numel < 0 || slots[k].numel > kMaxNumel ||
+        (slots[k].numel > 0 && (slots[k].grad == nullptr || !aligned_to(slots[k].grad, elem_bytes(slots[k].grad_dtype)))))
       return MRL_ERR_INVALID_ARG;
   }
   if (workspace == nullptr || workspace_bytes < mrl_grad_norm_workspace_bytes()) return MRL_ERR_WORKSPACE_TOO_SMALL;
@@ -758,7 +769,10 @@ extern "C" int mrl_adamw_step(const mrl_tensor_slot* slots, int32_t n_slots, con
     if (s.grad == nullptr || s.param == nullptr || s.m == nullptr || s.v == nullptr) return MRL_ERR_INVALID_ARG;
     if (s.master != nullptr && s.param_dtype != MRL_BF16) return MRL_ERR_INVALID_ARG;
     if (s.state_dtype == MRL_E4M3 && (s.m_scale == nullptr || s.v_scale == nullptr)) return MRL_ERR_INVALID_ARG;
+    if (!on_elements(s)) return MRL_ERR_INVALID_ARG;
   }
+  if (!aligned_to(grad_scale, 4) || !aligned_to(status, 4) || !aligned_to(ap->lr_dev, 4) || !aligned_to(ap->step_dev, 8))
+    return MRL_ERR_INVALID_ARG;
   const bool on_device = ap->lr_dev != nullptr || ap->step_dev != nullptr;
   if (on_device) {
     if (workspace == nullptr || workspace_bytes < mrl_adamw_workspace_bytes()) return MRL_ERR_WORKSPACE_TOO_SMALL;
