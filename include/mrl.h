@@ -121,7 +121,8 @@ extern "C" {
 
 /* mrl_adamw_params.rounding: how what is kept in fewer bits than float32 is rounded */
 #define MRL_ROUND_NEAREST 0
-#define MRL_ROUND_SEEDED 1   /* up or down with the probability of the remainder, from the seed: equal in the mean */
+#define MRL_ROUND_SEEDED 1   /* up or down with the probability of the remainder, from the seed: what is
+                                rounded (m, sqrt(v), the bf16 parameter) is equal in the mean */
 
 #define MRL_STATE_BLOCK 256  /* elements of a tensor that share the scale of an 8-bit optimiser state */
 
@@ -535,9 +536,14 @@ int mrl_grad_norm(const mrl_tensor_slot* slots, int32_t n_slots, float max_norm,
  * above zero never gets the code of zero (its update would be unbounded).  States start as zeros (codes and scales).
  *
  * MRL_ROUND_SEEDED.  At lr 1e-6 nearest rounding loses every update of a bf16 weight, and an 8-bit moving average stands
- * still: its change per step is below half a code.  Seeded rounding keeps both equal to the exact value in the mean:
- * the remainder is compared with 16 bits of the word splitmix64(splitmix64(splitmix64(seed) + step) + rng_first + i / 2)
- * -- from bit 32 (i mod 2): 16 for m, then 16 for v; the parameter uses m's bits in reverse order.
+ * still: its change per step is below half a code.  Seeded rounding keeps m, sqrt(v) and the weight equal to the exact value in
+ * the mean of each step: the remainder is compared with 16 bits of the word
+ * splitmix64(splitmix64(splitmix64(seed) + step) + rng_first + i / 2) -- from bit 32 (i mod 2): 16 for m, then 16 for v; the
+ * parameter uses m's bits in reverse order.  v itself, the square of the stored root, gains the rounding's variance at every
+ * step and settles above the v of float32 states.  On stationary Gaussian gradients: by 5.8 % at beta2 0.999, 5.0 % at 0.99,
+ * 2.5 % at 0.95 (its root by 1.5, 1.3 and 0.5 %, and updates are that much shorter), by 1/16 of itself at most where the root is
+ * above 3.5e-5 of its block's largest (the normal codes); by 12 % at 3e-5 and 42 % at 1e-5 of it, and what is below 4.4e-6
+ * of it stands at the smallest code.  Nearest rounding: by 11 % at 0.999.
  *
  *   slots      [host] n_slots tensors; they must not overlap
  *   ap         [host]
