@@ -551,7 +551,7 @@ int mrl_grad_norm(const mrl_tensor_slot* slots, int32_t n_slots, float max_norm,
  *   status     [device] int32 [1], nullable
  *   workspace: mrl_workspace_bytes(MRL_WS_ADAMW, 0, 0, 0, 0, 0); may be NULL unless lr_dev or step_dev is given
  * Bitwise reproducible.  A non-finite gradient that grad_scale does not announce spoils its element (8-bit
- * states: its block).  n_slots = 0 with step_dev still counts the step.
+ * states: its block).  Without any elements the step is still counted and the status set.
  * A null required pointer, an address that is not a multiple of its element, parameters outside their ranges ->
  * MRL_ERR_INVALID_ARG.
  */

@@ -123,10 +123,13 @@ __global__ void __launch_bounds__(kThreads) grad_norm_finish_kernel(const double
   if (threadIdx.x == 0) write_norm(sum, max_norm, norm, coef);
 }
 
-// Reads the step's device-resident inputs (learning rate, step counter), once per call.
+// Reads the step's device-resident inputs (learning rate, step counter), once per call; out is null where there are none and the
+// call has no elements whose kernels would set the status.
 __global__ void adamw_prepare_kernel(Hyper h, double lr, double beta1, double beta2, const float* lr_dev, int64_t* step_dev,
-                                     int64_t step, unsigned long long seed, const float* grad_scale, Hyper* out) {
+                                     int64_t step, unsigned long long seed, const float* grad_scale, int32_t* status, Hyper* out) {
   const float gs = grad_scale != nullptr ? *grad_scale : 1.f;
+  if (!(fabsf(gs) < INFINITY) && status != nullptr) atomicOr(status, MRL_DEV_NONFINITE_GRAD);
+  if (out == nullptr) return;
   if (step_dev != nullptr) {
     step = *step_dev + 1;
     if (fabsf(gs) < INFINITY) *step_dev = step;  // (the step is skipped otherwise)
@@ -789,18 +792,20 @@ extern "C" int mrl_adamw_step(const mrl_tensor_slot* slots, int32_t n_slots, con
   a.one_beta2 = (float)(1.0 - ap->beta2);
   a.eps = (float)ap->eps;
   a.seeded = ap->rounding == MRL_ROUND_SEEDED;
-  if (on_device) {
+  int count[16] = {0}, tensors = 0;
+  for (int k = 0; k < n_slots; ++k)
+    if (slots[k].numel > 0) ++count[kind_of(slots[k])], ++tensors;
+  if (on_device || (tensors == 0 && grad_scale != nullptr && status != nullptr)) {
     adamw_prepare_kernel<<<1, 1, 0, st>>>(Hyper{}, ap->lr, ap->beta1, ap->beta2, ap->lr_dev, ap->step_dev, ap->step, ap->seed,
-                                          grad_scale, static_cast<Hyper*>(workspace));
+                                          grad_scale, status, on_device ? static_cast<Hyper*>(workspace) : nullptr);
     MRL_CUDA_OK(cudaGetLastError());
-  } else {
+  }
+  if (!on_device) {
     a.hyper.lr = (float)ap->lr;
     a.hyper.lr_c1 = (float)(ap->lr / (1.0 - pow(ap->beta1, (double)ap->step)));
     a.hyper.root_c2 = (float)(1.0 / sqrt(1.0 - pow(ap->beta2, (double)ap->step)));
     a.hyper.key = splitmix64(splitmix64(ap->seed) + (uint64_t)ap->step);
   }
-  int count[16] = {0};
-  for (int k = 0; k < n_slots; ++k) count[kind_of(slots[k])] += slots[k].numel > 0;
   const int chunk[2] = {chunk_of(slots, n_slots, step_threads(0), step_blocks(0)), chunk_of(slots, n_slots, step_threads(8), step_blocks(8))};
   int rc = MRL_OK;
   const auto run = [&](auto kind) {
