@@ -127,7 +127,7 @@ extern "C" {
 #define MRL_STATE_BLOCK 256  /* elements of a tensor that share the scale of an 8-bit optimiser state */
 
 typedef struct mrl_norm_params {
-  float eps;                /* added to the mean square; > 0 (forward only) */
+  float eps;                /* added to the mean square; >= 2^-126 (forward only) */
   float weight_offset;      /* the gain is weight + weight_offset: 0, or 1 where the weight is stored as its distance from 1 */
   int32_t group;            /* columns that share a scale of y8: 0 (the whole row), 32, 64, 128 or 256 (forward only) */
   uint32_t flags;           /* backward only: MRL_FLAG_ACCUMULATE_DW (dweight is added to, not overwritten) */
@@ -479,8 +479,8 @@ int mrl_thl_word_align_logprobs(const float* src_logp, const int32_t* src_word, 
  * One output at least has to be given; outputs must not overlap one another, nor an input otherwise than said.
  * Bitwise reproducible.  One read of each input where H <= 16,384.  Any row stride and address that is a multiple of the
  * element; rows whose addresses and H are multiples of 16 bytes are about 1.6 times as fast as others.  N = 0 is a no-op.
- * H < 1, a row stride below H, a null required pointer, an address that is not a multiple of its element, eps that is not
- * finite and positive, an unknown group -> MRL_ERR_INVALID_ARG; H > 2^30 -> MRL_ERR_UNSUPPORTED_SHAPE.
+ * H < 1, a row stride below H, a null required pointer, an address that is not a multiple of its element, eps below 2^-126 or
+ * not finite, an unknown group -> MRL_ERR_INVALID_ARG; H > 2^30 -> MRL_ERR_UNSUPPORTED_SHAPE.
  */
 int mrl_rmsnorm_residual_fwd(const void* x, int64_t ld_x, const void* residual, int64_t ld_res, int32_t dtype,
                              const void* weight, int32_t w_dtype, int64_t N, int32_t H, const mrl_norm_params* np,

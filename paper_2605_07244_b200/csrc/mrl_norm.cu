@@ -874,6 +874,8 @@ int launch_bwd(const NormBwdArgs& a, bool odd, int* ctas, cudaStream_t st) {
 }
 
 constexpr int kMaxCols = 1 << 30;
+// The smallest eps: a square below the normal range is off by 2^-150, the mean too, and 2^-126 beside it keeps that at half a step.
+constexpr float kEpsMin = 1.17549435e-38f;
 bool on_element(const void* p, int elem) { return (reinterpret_cast<uintptr_t>(p) & (elem - 1)) == 0; }
 bool row_type_ok(int32_t dtype) { return dtype == MRL_BF16 || dtype == MRL_F32; }
 
@@ -891,7 +893,7 @@ extern "C" int mrl_rmsnorm_residual_fwd(const void* x, int64_t ld_x, const void*
   if (!row_type_ok(dtype) || !row_type_ok(w_dtype)) return MRL_ERR_UNSUPPORTED_DTYPE;
   if (np == nullptr || N < 0 || H < 1) return MRL_ERR_INVALID_ARG;
   if (H > kMaxCols) return MRL_ERR_UNSUPPORTED_SHAPE;
-  if (!(np->eps > 0.f) || np->eps > 3.4e38f || !(np->weight_offset - np->weight_offset == 0.f)) return MRL_ERR_INVALID_ARG;
+  if (!(np->eps >= kEpsMin) || np->eps > 3.4e38f || !(np->weight_offset - np->weight_offset == 0.f)) return MRL_ERR_INVALID_ARG;
   if (np->group != 0 && np->group != 32 && np->group != 64 && np->group != 128 && np->group != 256) return MRL_ERR_INVALID_ARG;
   if (N == 0) return MRL_OK;
   if (h_out == nullptr && y == nullptr && y8 == nullptr && rstd == nullptr) return MRL_ERR_INVALID_ARG;
