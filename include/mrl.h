@@ -480,7 +480,8 @@ int mrl_thl_word_align_logprobs(const float* src_logp, const int32_t* src_word, 
  * Bitwise reproducible.  One read of each input where H <= 16,384.  Any row stride and address that is a multiple of the
  * element; rows whose addresses and H are multiples of 16 bytes are about 1.6 times as fast as others.  N = 0 is a no-op.
  * H < 1, a row stride below H, a null required pointer, an address that is not a multiple of its element, eps below 2^-126 or
- * not finite, an unknown group -> MRL_ERR_INVALID_ARG; H > 2^30 -> MRL_ERR_UNSUPPORTED_SHAPE.
+ * not finite, an unknown group, an output at another tensor's address otherwise than said -> MRL_ERR_INVALID_ARG;
+ * H > 2^30 -> MRL_ERR_UNSUPPORTED_SHAPE.
  */
 int mrl_rmsnorm_residual_fwd(const void* x, int64_t ld_x, const void* residual, int64_t ld_res, int32_t dtype,
                              const void* weight, int32_t w_dtype, int64_t N, int32_t H, const mrl_norm_params* np,

@@ -877,6 +877,10 @@ constexpr int kMaxCols = 1 << 30;
 // The smallest eps: a square below the normal range is off by 2^-150, the mean too, and 2^-126 beside it keeps that at half a step.
 constexpr float kEpsMin = 1.17549435e-38f;
 bool on_element(const void* p, int elem) { return (reinterpret_cast<uintptr_t>(p) & (elem - 1)) == 0; }
+// An output at an input's address has to have its row stride: it would lie over rows that are still to be read.
+bool over_other_rows(const void* out, long long ld_out, const void* in, long long ld_in, long long N) {
+  return out != nullptr && out == in && ld_out != ld_in && N > 1;
+}
 bool row_type_ok(int32_t dtype) { return dtype == MRL_BF16 || dtype == MRL_F32; }
 
 }  // namespace
@@ -901,6 +905,10 @@ extern "C" int mrl_rmsnorm_residual_fwd(const void* x, int64_t ld_x, const void*
       (y8 != nullptr && (ld_y8 < H || scales == nullptr)))
     return MRL_ERR_INVALID_ARG;
   if (h_out != nullptr && h_out == y) return MRL_ERR_INVALID_ARG;
+  if (y8 != nullptr && (y8 == x || y8 == residual || y8 == h_out || y8 == y)) return MRL_ERR_INVALID_ARG;
+  if (over_other_rows(h_out, ld_h, x, ld_x, N) || over_other_rows(h_out, ld_h, residual, ld_res, N) ||
+      over_other_rows(y, ld_y, x, ld_x, N) || over_other_rows(y, ld_y, residual, ld_res, N))
+    return MRL_ERR_INVALID_ARG;
   if (x == nullptr || weight == nullptr) return MRL_ERR_INVALID_ARG;
   const bool bf16 = dtype == MRL_BF16;
   const int elem = bf16 ? 2 : 4;
@@ -945,6 +953,8 @@ extern "C" int mrl_rmsnorm_residual_bwd(const void* dy, int64_t ld_dy, const voi
     return MRL_OK;
   }
   if (dy == nullptr || h == nullptr || weight == nullptr || rstd == nullptr || dx == nullptr) return MRL_ERR_INVALID_ARG;
+  if (over_other_rows(dx, ld_dx, dy, ld_dy, N) || over_other_rows(dx, ld_dx, dh, ld_dh, N) || over_other_rows(dx, ld_dx, h, ld_h, N))
+    return MRL_ERR_INVALID_ARG;
   const bool bf16 = dtype == MRL_BF16;
   const int elem = bf16 ? 2 : 4;
   if (!on_element(dy, elem) || !on_element(dh, elem) || !on_element(h, elem) || !on_element(dx, elem) ||
