@@ -375,7 +375,11 @@ def mrl_rmsnorm_residual_bwd(dy, dh, h, weight, rstd, np: NormParams, dx, dweigh
 
 class TensorSlot:
     """One tensor of mrl_grad_norm / mrl_adamw_step: contiguous CUDA tensors of one size.  A gradient norm needs `grad`
-    alone; 8-bit states are uint8 or float8_e4m3fn tensors with `m_scale`, `v_scale` of ceil(numel / STATE_BLOCK)."""
+    alone; 8-bit states are uint8 or float8_e4m3fn tensors with `m_scale`, `v_scale` of ceil(numel / STATE_BLOCK).
+
+    The addresses are those of now: a tensor that is allocated anew later on (a gradient that autograd makes again after
+    `p.grad = None`, a parameter whose `.data` is exchanged) needs a new slot.  Where `param` is a leaf and `grad` its `.grad`, a call
+    after that has become another tensor is refused; other gradients are the caller's to keep in place."""
 
     def __init__(self, grad, param=None, master=None, m=None, v=None, m_scale=None, v_scale=None, weight_decay=0.0,
                  rng_first=0):
@@ -390,10 +394,11 @@ class TensorSlot:
             F32 if param is None else _CODES[param.dtype], E4M3 if codes else F32)
         self.device = dev
         self.tensors = (grad, param, master, m, v, m_scale, v_scale)
+        self.watched = param is not None and param.requires_grad and param.is_leaf and param.grad is grad
 
 
 class TensorList:
-    """The table of a step's tensors, built once; it keeps them alive."""
+    """The table of a step's tensors: built once for tensors that stay where they are, which it keeps alive (see TensorSlot)."""
 
     def __init__(self, slots):
         self.slots = list(slots)
@@ -403,10 +408,19 @@ class TensorList:
         self.n = len(self.slots)
         self.table = (TensorSlotStruct * self.n)(*[s.struct for s in self.slots])
         self.address = C.addressof(self.table) if self.n else None
+        self.watched = [(s.tensors[1], s.tensors[0]) for s in self.slots if s.watched]
+
+    def check(self, where):
+        """Refuses a list whose parameters have got other gradients since it was built."""
+        for param, grad in self.watched:
+            if param.grad is not grad:
+                raise MrlError(1, f"{where}: a parameter's gradient is another tensor than in the list")
 
 
 def mrl_grad_norm(tensors: TensorList, max_norm: float, norm=None, coef=None, workspace=None, stream=None):
     where, dev = "mrl_grad_norm", tensors.device
+    if tensors.watched:
+        tensors.check(where)
     st = _stream_of(dev, stream, where)
     ws, ws_bytes = _workspace(workspace, dev, where)
     code = lib().mrl_grad_norm(tensors.address, tensors.n, max_norm, _float_vector(norm, 1, dev, where),
@@ -417,6 +431,8 @@ def mrl_grad_norm(tensors: TensorList, max_norm: float, norm=None, coef=None, wo
 
 def mrl_adamw_step(tensors: TensorList, ap: AdamwParams, grad_scale=None, status=None, workspace=None, stream=None):
     where, dev = "mrl_adamw_step", tensors.device
+    if tensors.watched:
+        tensors.check(where)
     st = _stream_of(dev, stream, where)
     ws, ws_bytes = _workspace(workspace, dev, where)
     code = lib().mrl_adamw_step(tensors.address, tensors.n, ap, _float_vector(grad_scale, 1, dev, where),
