@@ -322,7 +322,7 @@ def _workspace(t, device, where):
     """Address and bytes of a workspace."""
     if t is None:
         return None, 0
-    if t.get_device() != device:
+    if t.get_device() != device or not t.is_contiguous():
         raise MrlError(1, where)
     return t.data_ptr(), t.nbytes
 
