@@ -810,7 +810,8 @@ template <typename K>
 int allow_smem(K kernel, std::atomic<uint64_t>& done) {
   return mrl_once_per_device(done, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemCta); });
 }
-// -1: the rows do not fit; the looping kernel takes them.
+// One row of everything that is read fits a CTA, at most: three float32 rows of kRowMax columns off the granule (image_bytes).
+static_assert(3 * (kRowMax * 4 + 16) <= kSmemCta, "rows of the row kernels");
 template <typename T, bool kOdd, int kCols, int kCodes>
 int launch_fwd_codes(NormFwdArgs a, cudaStream_t st) {
   const int threads = row_threads(a.H, kCols);
@@ -818,7 +819,6 @@ int launch_fwd_codes(NormFwdArgs a, cudaStream_t st) {
   const int stage = (a.res != nullptr ? 2 : 1) * slot;
   const bool fewer = !kOdd && kCodes == kNoCodes && a.res != nullptr && stage <= kFewerStage && a.N * a.H >= kFewerBytes / (int)sizeof(T);
   const RowPlan p = plan_rows(threads, fwd_regs(kCols, kCodes), stage, fewer ? 3 : 2);
-  if (p.smem > kSmemCta) return -1;
   a.stages = p.stages;
   const long long most = (long long)kSms * p.ctas_per_sm;
   static std::atomic<uint64_t> done;
@@ -839,7 +839,6 @@ int launch_bwd_regs(NormBwdArgs a, int* ctas, cudaStream_t st) {
   const int threads = row_threads(a.H, kCols);
   const int slot = kOdd ? image_bytes(a.H, sizeof(T)) : threads * kCols * (int)sizeof(T);
   const RowPlan p = plan_rows(threads, kRegs, (a.dh != nullptr ? 3 : 2) * slot);
-  if (p.smem > kSmemCta) return -1;
   a.stages = p.stages;
   *ctas = bwd_ctas(a.N, p.ctas_per_sm);
   static std::atomic<uint64_t> done;
@@ -918,14 +917,12 @@ extern "C" int mrl_rmsnorm_residual_fwd(const void* x, int64_t ld_x, const void*
   NormFwdArgs a{x, residual, weight, h_out, y, static_cast<uint8_t*>(y8), scales, rstd, ld_x, ld_res, ld_h, ld_y, ld_y8, N,
                 H, np->group, w_dtype == MRL_BF16, np->eps, np->weight_offset, 1.0f / (float)H, 0};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  int rc = -1;
   if (H <= kRowMax) {
     const bool whole = H % (16 / elem) == 0 && aligned(x, ld_x, elem, 16) && aligned(residual, ld_res, elem, 16) &&
                        aligned(h_out, ld_h, elem, 16) && aligned(y, ld_y, elem, 16) && aligned(y8, ld_y8, 1, 16 / elem) &&
                        aligned(weight, 0, 1, 16);
-    rc = bf16 ? launch_fwd<__nv_bfloat16>(a, !whole, st) : launch_fwd<float>(a, !whole, st);
+    return bf16 ? launch_fwd<__nv_bfloat16>(a, !whole, st) : launch_fwd<float>(a, !whole, st);
   }
-  if (rc >= 0) return rc;
   const unsigned grid = (unsigned)(N < 0x7fffffffll ? N : 0x7fffffffll);
   mrl_profile_before(st, "rmsnorm_fwd_loop_kernel");
   if (bf16)
@@ -966,13 +963,12 @@ extern "C" int mrl_rmsnorm_residual_bwd(const void* dy, int64_t ld_dy, const voi
   }
   NormBwdArgs a{dy, dh, h, weight, rstd, dx, dweight != nullptr ? static_cast<float*>(workspace) : nullptr, ld_dy, ld_dh,
                 ld_h, ld_dx, N, H, w_dtype == MRL_BF16, np->weight_offset, 1.0f / (float)H, 0};
-  int rc = -1, ctas = 0;
+  int rc, ctas = 0;
   if (H <= kRowMax) {
     const bool whole = H % (16 / elem) == 0 && aligned(dy, ld_dy, elem, 16) && aligned(dh, ld_dh, elem, 16) &&
                        aligned(h, ld_h, elem, 16) && aligned(dx, ld_dx, elem, 16) && aligned(weight, 0, 1, 16);
     rc = bf16 ? launch_bwd<__nv_bfloat16>(a, !whole, &ctas, st) : launch_bwd<float>(a, !whole, &ctas, st);
-  }
-  if (rc < 0) {
+  } else {
     ctas = bwd_ctas_most(N, H);
     mrl_profile_before(st, "rmsnorm_bwd_loop_kernel");
     if (bf16)
