@@ -182,6 +182,18 @@ __device__ __forceinline__ uint32_t f2_to_bf16x2(f2 v) {
   return pack_bf16x2(u.x, u.y);
 }
 
+// IEEE square roots of two floats from kRootMin to kRootMax: v * rsqrt(v), brought to the nearest float by one Newton step on the
+// fused residual v - s^2 (Markstein 1990).  tests/test_newton_root_gpu.py compares every float of the range with sqrtf.
+constexpr float kRootMin = 1e-25f, kRootMax = 1e37f;  // where s^2 and the residual stay normal
+__device__ __forceinline__ f2 newton_root(f2 v) {
+  const float2 u = split_f2(v);
+  float a, b;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(u.x));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(u.y));
+  const f2 y = make_f2(a, b), s = mul_f2(v, y), half = mul_f2(y, make_f2(-0.5f, -0.5f));
+  return fma_f2(fma_f2(s, s, v ^ 0x8000000080000000ull), half, s);  // s + (v - s^2) / (2 s), the signs moved together
+}
+
 // SplitMix64 output function (Steele, Lea, Flood 2014).
 __host__ __device__ __forceinline__ uint64_t splitmix64(uint64_t x) {
   x += 0x9E3779B97F4A7C15ull;

@@ -77,21 +77,10 @@ __device__ __forceinline__ float rcp_approx(float x) {
   return y;
 }
 
-constexpr float kRootMin = 1e-25f, kRootMax = 1e37f;  // where newton_root holds: s^2 and the residual stay normal
-
 // a + b of two products: a packed sum of packed products is compiled to a fused multiply-add, a single one is not.
 __device__ __forceinline__ f2 add_apart(f2 a, f2 b) {
   const float2 u = split_f2(a), v = split_f2(b);
   return make_f2(__fadd_rn(u.x, v.x), __fadd_rn(u.y, v.y));
-}
-
-__device__ __forceinline__ f2 newton_root(f2 v) {
-  const float2 u = split_f2(v);
-  float a, b;
-  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(u.x));
-  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(u.y));
-  const f2 y = make_f2(a, b), s = mul_f2(v, y), half = mul_f2(y, make_f2(-0.5f, -0.5f));
-  return fma_f2(fma_f2(s, s, v ^ 0x8000000080000000ull), half, s);  // s + (v - s^2) / (2 s), the signs moved together
 }
 
 __device__ __forceinline__ double block_sum(double v, double* red) {
@@ -239,9 +228,8 @@ __device__ __forceinline__ void decode(uint2 codes, float scale, f2 (&x)[4]) {
   }
 }
 
-// IEEE square roots of eight values whose smallest and largest are given: v * rsqrt(v), brought to the nearest float by one
-// Newton step on the fused residual v - s^2 (Markstein 1990; all floats of its range were compared with sqrtf on B200: equal).
-// Values near zero, where the residual would leave float32, and infinities go through sqrtf.
+// IEEE square roots of eight values whose smallest and largest are given.  Values near zero, where newton_root's residual would
+// leave float32, and infinities go through sqrtf.
 __device__ __forceinline__ void root8(const f2 (&v)[4], uint32_t least, uint32_t most, f2 (&root)[4]) {
   if (least >= __float_as_uint(kRootMin) && most <= __float_as_uint(kRootMax)) {
 #pragma unroll
