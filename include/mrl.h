@@ -464,8 +464,10 @@ int mrl_thl_word_align_logprobs(const float* src_logp, const int32_t* src_word, 
  * and, for 8-bit rows, with the columns cut into groups (the last one may be short):
  *   scales[t, k] = max(max over group k of |y[t, i]| / 448, 2^-126),   y8[t, i] = e4m3(y[t, i] / scales[t, k])
  * h and y are held in float32 and rounded once, to nearest even: the norm is taken of the unrounded sum, y8 of the
- * unrounded y.  NaN and infinities propagate as the formulas say; the maxima pass over NaN.  A row whose sum of
- * squares leaves float32 (elements above about 1e18) is summed again after division by a power of two.
+ * unrounded y.  (Stock models round the sum to their bf16 residual before its norm is taken: for their bits add first and pass the
+ * rounded sum as x without a residual.)  Codes are formed with float32 reciprocals: where y / scales is within 2^-22 of itself of the
+ * border between two codes, either may come.  NaN and infinities propagate as the formulas say; the maxima pass over NaN.
+ * A row whose sum of squares leaves float32 (elements above about 1e18) is summed again after division by a power of two.
  *
  *   x, residual [device] dtype [N, ld_x], [N, ld_res]; residual nullable (h = x)
  *   dtype    MRL_BF16 or MRL_F32
@@ -477,7 +479,9 @@ int mrl_thl_word_align_logprobs(const float* src_logp, const int32_t* src_word, 
  *   scales   [device] float32 [N, ceil(H / group)] (group 0: [N, 1]), contiguous; required with y8
  *   rstd     [device] float32 [N], nullable; the backward pass reads it
  * One output at least has to be given; outputs must not overlap one another, nor an input otherwise than said.
- * Bitwise reproducible.  One read of each input where H <= 16,384.  Any row stride and address that is a multiple of the
+ * Bitwise reproducible for calls of the same N, H, types and alignment.  The order of a row's sum goes by the columns of a thread,
+ * which follow these (other at N <= 296 and N > 2,048, and for rows off 16 bytes): the last bits of the same row can differ between
+ * calls of other sizes.  One read of each input where H <= 16,384.  Any row stride and address that is a multiple of the
  * element; rows whose addresses and H are multiples of 16 bytes are about 1.6 times as fast as others.  N = 0 is a no-op.
  * H < 1, a row stride below H, a null required pointer, an address that is not a multiple of its element, eps below 2^-126 or
  * not finite, an unknown group, an output at another tensor's address otherwise than said -> MRL_ERR_INVALID_ARG;
@@ -503,7 +507,8 @@ int mrl_rmsnorm_residual_fwd(const void* x, int64_t ld_x, const void* residual, 
  *   dx      [device] dtype [N, ld_dx]; may equal dy, dh or h (with its row stride)
  *   dweight [device] float32 [H], nullable; overwritten, or added to under MRL_FLAG_ACCUMULATE_DW
  *   workspace: mrl_workspace_bytes(MRL_WS_RMSNORM_BWD, N, 0, H, 0, 0); may be NULL where dweight is
- * float32 arithmetic and sums in a fixed order: bitwise reproducible.  N = 0: dweight is zeroed unless accumulated.
+ * float32 arithmetic and sums in a fixed order: bitwise reproducible for calls of the same N, H, types and alignment.  h is taken
+ * as it was stored, rstd as that of the sum before its rounding.  N = 0: dweight is zeroed unless accumulated.
  * Errors as in the forward pass.
  */
 int mrl_rmsnorm_residual_bwd(const void* dy, int64_t ld_dy, const void* dh, int64_t ld_dh, const void* h, int64_t ld_h,
@@ -531,10 +536,10 @@ int mrl_grad_norm(const mrl_tensor_slot* slots, int32_t n_slots, float max_norm,
  * mrl_fused_lmhead_loss_fwd_bwd and the dweight of mrl_rmsnorm_residual_bwd.
  *   g = grad * grad_scale,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
  *   p = p - lr (weight_decay p + (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps))
- * float32 arithmetic, the moments rounded after every operation as the formula stands.  p is master where given, else param; bf16 param is rounded once.  8-bit states: per
- * MRL_STATE_BLOCK elements of the tensor, scale = max(max |s| / 448, 2^-126) (by the
- * rounded 1 / 448) and code = e4m3(s * (1 / scale)), s = m or sqrt(v); a v
- * above zero never gets the code of zero (its update would be unbounded).  States start as zeros (codes and scales).
+ * float32 arithmetic, the moments rounded after every operation as the formula stands.  p is master where given, else param;
+ * bf16 param is rounded once.  8-bit states: per MRL_STATE_BLOCK elements of the tensor, scale = max(max |s| / 448, 2^-126) (by
+ * the rounded 1 / 448) and code = e4m3(s * (1 / scale)), s = m or sqrt(v); a v above zero never gets the code of zero (its
+ * update would be unbounded).  States start as zeros (codes and scales).
  *
  * MRL_ROUND_SEEDED.  At lr 1e-6 nearest rounding loses every update of a bf16 weight, and an 8-bit moving average stands
  * still: its change per step is below half a code.  Seeded rounding keeps m, sqrt(v) and the weight equal to the exact value in

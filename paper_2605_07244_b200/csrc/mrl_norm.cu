@@ -21,7 +21,7 @@ constexpr int kNoCodes = 0, kRowCodes = 1, kGroupCodes = 2;
 constexpr int kRowMax = 16384;                            // the widest row that one CTA holds
 // registers of a thread of the row kernels
 constexpr int kBwdRegs = 64, kBwdRegsMore = 80;
-// (wide: shared memory allows no more CTAs anyway; codes by group spill below 96: 33,880 rows of 4,096 208 us, with 80 216; 65,536 of
+// (wide: shared memory allows no more CTAs anyway; codes by group spill 24 to 32 bytes at 80, 8 to 12 at 96: 33,880 rows of 4,096 208 us, with 80 216; 65,536 of
 // 2,048 166 and 174, but without a residual 118 and 115, and with one scale a row 170 and 167)
 constexpr int fwd_regs(int cols, int codes) { return cols != kWide ? 64 : (codes == kGroupCodes ? 96 : 80); }
 
@@ -391,7 +391,7 @@ __global__ void __maxnreg__(fwd_regs(kRowCols, kCodes)) rmsnorm_fwd_row_kernel(c
   int s = 0, turn = 0;
   for (long long row = blockIdx.x; row < a.N; row += gridDim.x, turn ^= 1) {
     if (kOdd) {
-      // the copies of this row are there for all, and those of the last row, outputs by now, have been read
+      // the copies of this row are there for all, and those of the last row have been read by all
       if (a.stages > 1) copy_wait(a.stages - 2);
       __syncthreads();
       fetch(row + (long long)(a.stages - 1) * gridDim.x, s == 0 ? a.stages - 1 : s - 1);
@@ -759,7 +759,7 @@ int row_threads(int H, int cols) { return (H + cols * 32 - 1) / (cols * 32) * 32
 // with 32; 262,144 rows of 64: 93 us with 8, 133 with 16).  Forward, 32 columns are fastest for rows of 2 to 16 KB in 16-byte
 // granules once there are many (65,536 x 4,096 bf16: 341 us with 32, 374 with 16; 32,768 x 8,192: 338, 357), 16 for wider rows
 // (16,384 x 16,384: 356, 339), for fewer (1,024 x 4,096: 8.9, 7.6) and for odd ones (65,552 x 4,095: 557 us, 624 with 8).  Backward,
-// whose sums take registers, 16 (65,536 x 4,096: 394 with 32, 367 with 16).
+// whose sums take registers, 16 (65,536 x 4,096, before the registers of launch_bwd_rows: 394 with 32, 367 with 16).
 bool few_or_short(long long N, int H) { return H <= 512 || (H <= 512 * kNarrow && N <= 2 * kSms); }
 int fwd_cols(long long N, int H, int elem, bool odd) {
   if (few_or_short(N, H)) return kNarrow;

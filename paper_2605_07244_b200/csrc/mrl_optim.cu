@@ -20,8 +20,10 @@ constexpr int kNormCtas = kSms * 5;           // as many as are resident (48 reg
 constexpr uint32_t kSmallChunks = 16;
 constexpr int kCluster = 8;                   // CTAs of the gradient norm of few elements
 // The update's threads and CTAs per SM (8: the kind's bit for 8-bit states), and the blocks of a warp in a large call.
-// 8-bit states, 525 M elements: 24 warps of 80 registers in 6 CTAs 1,231 us, in 3 CTAs 1,343; 28 of 72 registers 1,279, 32 of
-// 64 slower still; 8, 16, 32 and 128 blocks a warp 1,252, 1,249, 1,255 and 1,276.  float32 states, 622 M: 4 blocks 2,583, 8 2,624.
+// 8-bit states, 525 M elements, compared before the arithmetic's last steps (1,194 us with them): 24 warps of 80 registers in 6
+// CTAs 1,231 us, in 3 CTAs 1,343; 28 of 72 registers 1,279, 32 of 64 slower still; 8, 16, 32 and 128 blocks a warp 1,252, 1,249, 1,255
+// and 1,276.  That is the kind with bf16 weights and gradients and no master weights, which has no spills; the other 8-bit kinds spill
+// 40 to 64 bytes at 80 registers and were not compared.  float32 states, 622 M: 4 blocks 2,583, 8 2,624.
 __host__ __device__ constexpr int step_threads(int kind) { return kind & 8 ? 128 : 256; }
 __host__ __device__ constexpr int step_ctas(int kind) { return kind & 8 ? 6 : 4; }
 __host__ __device__ constexpr int step_blocks(int kind) { return kind & 8 ? 16 : 4; }
