@@ -551,15 +551,15 @@ int mrl_grad_norm(const mrl_tensor_slot* slots, int32_t n_slots, float max_norm,
  * above 3.5e-5 of its block's largest (the normal codes); by 12 % at 3e-5 and 42 % at 1e-5 of it, and what is below 4.4e-6
  * of it stands at the smallest code.  Nearest rounding: by 11 % at 0.999.
  *
- *   slots      [host] n_slots tensors; they must not overlap
+ *   slots      [host] n_slots tensors; neither they nor the buffers of one may overlap
  *   ap         [host]
  *   grad_scale [device] float32 [1], nullable = 1.  Not finite: nothing is written, MRL_DEV_NONFINITE_GRAD is set
  *   status     [device] int32 [1], nullable
  *   workspace: mrl_workspace_bytes(MRL_WS_ADAMW, 0, 0, 0, 0, 0); may be NULL unless lr_dev or step_dev is given
  * Bitwise reproducible.  A non-finite gradient that grad_scale does not announce spoils its element (8-bit
  * states: its block).  Without any elements the step is still counted and the status set.
- * A null required pointer, an address that is not a multiple of its element, parameters outside their ranges ->
- * MRL_ERR_INVALID_ARG.
+ * A null required pointer, an address that is not a multiple of its element, one address for two of a tensor's buffers, parameters
+ * outside their ranges -> MRL_ERR_INVALID_ARG.
  */
 int mrl_adamw_step(const mrl_tensor_slot* slots, int32_t n_slots, const mrl_adamw_params* ap, const float* grad_scale,
                    int32_t* status, void* workspace, size_t workspace_bytes, void* stream);

@@ -629,6 +629,15 @@ bool on_elements(const mrl_tensor_slot& s) {
          (s.state_dtype != MRL_E4M3 || (aligned_to(s.m_scale, 4) && aligned_to(s.v_scale, 4)));
 }
 
+// One buffer may not stand for two of a tensor's.
+bool apart(const mrl_tensor_slot& s) {
+  const void* const p[5] = {s.grad, s.param, s.m, s.v, s.master};
+  for (int i = 0; i < 5; ++i)
+    for (int j = 0; j < i; ++j)
+      if (p[i] == p[j]) return false;  // (the master alone may be null)
+  return s.state_dtype != MRL_E4M3 || s.m_scale != s.v_scale;
+}
+
 // Groups of eight elements: 32 bytes of float32, 16 of bf16, 8 of codes.
 bool grad_aligned(const mrl_tensor_slot& s) { return aligned_to(s.grad, s.grad_dtype == MRL_BF16 ? 16 : 32); }
 bool all_aligned(const mrl_tensor_slot& s) {
@@ -771,6 +780,8 @@ extern "C" int mrl_adamw_step(const mrl_tensor_slot* slots, int32_t n_slots, con
     if (workspace == nullptr || workspace_bytes < mrl_adamw_workspace_bytes()) return MRL_ERR_WORKSPACE_TOO_SMALL;
     if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return MRL_ERR_INVALID_ARG;
   }
+  for (int k = 0; k < n_slots; ++k)
+    if (slots[k].numel > 0 && !apart(slots[k])) return MRL_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   AdamwArgs a{};
   a.hyper_dev = on_device ? static_cast<const Hyper*>(workspace) : nullptr;

@@ -14,7 +14,7 @@ def lib():
 
 
 def slot(**kw):
-    base = dict(grad=FAKE, param=FAKE, master=None, m=FAKE, v=FAKE, m_scale=None, v_scale=None, numel=10, rng_first=0,
+    base = dict(grad=FAKE, param=0x2000, master=None, m=0x3000, v=0x4000, m_scale=None, v_scale=None, numel=10, rng_first=0,
                 weight_decay=0.0, grad_dtype=B.F32, param_dtype=B.F32, state_dtype=B.F32)
     return B.TensorSlotStruct(**(base | kw))
 
@@ -24,10 +24,10 @@ def table(*slots):
 
 
 @pytest.mark.parametrize("bad", [
-    dict(grad=FAKE + 2), dict(grad=FAKE + 1, grad_dtype=B.BF16), dict(param=FAKE + 2), dict(param=FAKE + 1, param_dtype=B.BF16),
-    dict(param_dtype=B.BF16, master=FAKE + 2), dict(m=FAKE + 1), dict(v=FAKE + 2),
-    dict(state_dtype=B.E4M3, m=FAKE + 1, v=FAKE + 3, m_scale=FAKE + 2, v_scale=FAKE),
-    dict(state_dtype=B.E4M3, m_scale=FAKE, v_scale=FAKE + 1)])
+    dict(grad=FAKE + 2), dict(grad=FAKE + 1, grad_dtype=B.BF16), dict(param=0x2002), dict(param=0x2001, param_dtype=B.BF16),
+    dict(param_dtype=B.BF16, master=0x5002), dict(m=0x3001), dict(v=0x4002),
+    dict(state_dtype=B.E4M3, m=0x3001, v=0x4003, m_scale=0x6002, v_scale=0x7000),
+    dict(state_dtype=B.E4M3, m_scale=0x6000, v_scale=0x7001)])
 def test_adamw_refuses_tensors_off_their_elements(lib, bad):
     ap = B.AdamwParams(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1)
     assert lib.mrl_adamw_step(table(slot(), slot(**bad)), 2, ap, None, None, None, 0, None) == 1
