@@ -394,6 +394,7 @@ class TensorSlot:
             F32 if param is None else _CODES[param.dtype], E4M3 if codes else F32)
         self.device = dev
         self.tensors = (grad, param, master, m, v, m_scale, v_scale)
+        self.updates = None if param is None or n == 0 else param.data_ptr()
         self.watched = param is not None and param.requires_grad and param.is_leaf and param.grad is grad
 
 
@@ -404,6 +405,9 @@ class TensorList:
         self.slots = list(slots)
         if any(s.device != self.slots[0].device for s in self.slots):
             raise MrlError(1, "TensorList: tensors on several devices")
+        params = [s.updates for s in self.slots if s.updates is not None]
+        if len(set(params)) != len(params):
+            raise MrlError(1, "TensorList: a parameter is there twice")
         self.device = self.slots[0].device if self.slots else torch.cuda.current_device()
         self.n = len(self.slots)
         self.table = (TensorSlotStruct * self.n)(*[s.struct for s in self.slots])
