@@ -622,20 +622,21 @@ bool aligned_to(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintp
 
 // Every pointer has to be a multiple of its element: a kernel's access anywhere else loses the context.  (Codes are bytes.)
 int elem_bytes(int32_t dtype) { return dtype == MRL_BF16 ? 2 : 4; }
+// (This and apart() avoid branches: for 154 tensors they take 0.1 and 0.3 us of an update's 8.)
+uintptr_t bits_of(const void* p) { return reinterpret_cast<uintptr_t>(p); }
 bool on_elements(const mrl_tensor_slot& s) {
-  const uintptr_t state = s.state_dtype == MRL_E4M3 ? 1 : 4;
-  return aligned_to(s.grad, elem_bytes(s.grad_dtype)) && aligned_to(s.param, elem_bytes(s.param_dtype)) && aligned_to(s.master, 4) &&
-         aligned_to(s.m, state) && aligned_to(s.v, state) &&
-         (s.state_dtype != MRL_E4M3 || (aligned_to(s.m_scale, 4) && aligned_to(s.v_scale, 4)));
+  const bool codes = s.state_dtype == MRL_E4M3;
+  const uintptr_t floats = bits_of(s.master) | bits_of(codes ? s.m_scale : s.m) | bits_of(codes ? s.v_scale : s.v);
+  const uintptr_t halves = bits_of(s.grad) | bits_of(s.param);
+  if (((floats & 3) | (halves & 1)) != 0) return false;
+  return (halves & 2) == 0 || (aligned_to(s.grad, elem_bytes(s.grad_dtype)) && aligned_to(s.param, elem_bytes(s.param_dtype)));
 }
 
 // One buffer may not stand for two of a tensor's.
 bool apart(const mrl_tensor_slot& s) {
-  const void* const p[5] = {s.grad, s.param, s.m, s.v, s.master};
-  for (int i = 0; i < 5; ++i)
-    for (int j = 0; j < i; ++j)
-      if (p[i] == p[j]) return false;  // (the master alone may be null)
-  return s.state_dtype != MRL_E4M3 || s.m_scale != s.v_scale;
+  const void *g = s.grad, *p = s.param, *c = s.master;  // (the master alone may be null)
+  return !((g == p) | (g == s.m) | (g == s.v) | (g == c) | (p == s.m) | (p == s.v) | (p == c) | (s.m == s.v) | (s.m == c) | (s.v == c) |
+           ((s.state_dtype == MRL_E4M3) & (s.m_scale == s.v_scale)));
 }
 
 // Groups of eight elements: 32 bytes of float32, 16 of bf16, 8 of codes.
@@ -673,17 +674,15 @@ int fill_table(const mrl_tensor_slot* slots, int n, int at, int chunk, int only,
   return at;
 }
 
-// Elements of a chunk: small ones while there are few, for the sake of parallel CTAs; `most` times as many otherwise.
-int chunk_of(const mrl_tensor_slot* slots, int n, int threads, int most) {
-  long long total = 0;
-  for (int k = 0; k < n; ++k) total += slots[k].numel;
+// Elements of a chunk: small ones while there are few in all, for the sake of parallel CTAs; `most` times as many otherwise.
+int chunk_of(long long total, int threads, int most) {
   return threads * 8 * (total <= (long long)kSms * 8 * 4 * kChunk ? 1 : most);
 }
 
 template <int kN>
-int launch_grad_norm(const mrl_tensor_slot* slots, int n, float max_norm, float* norm, float* coef, double* partial, cudaStream_t st) {
+int launch_grad_norm(const mrl_tensor_slot* slots, int n, long long total, float max_norm, float* norm, float* coef, double* partial, cudaStream_t st) {
   Table<kN> t;
-  const int chunk = chunk_of(slots, n, kThreads, 8);
+  const int chunk = chunk_of(total, kThreads, 8);
   int ctas = 0;
   for (int at = 0; at < n || ctas == 0;) {
     at = fill_table(slots, n, at, chunk, -1, &t);
@@ -740,18 +739,20 @@ extern "C" int mrl_grad_norm(const mrl_tensor_slot* slots, int32_t n_slots, floa
   if (n_slots < 0 || (n_slots > 0 && slots == nullptr) || max_norm != max_norm || (norm == nullptr && coef == nullptr) ||
       !aligned_to(norm, 4) || !aligned_to(coef, 4))
     return MRL_ERR_INVALID_ARG;
+  long long total = 0;
   for (int k = 0; k < n_slots; ++k) {
     if (!grad_type_ok(slots[k].grad_dtype)) return MRL_ERR_UNSUPPORTED_DTYPE;
     if (slots[k].numel < 0 || slots[k].numel > kMaxNumel ||
         (slots[k].numel > 0 && (slots[k].grad == nullptr || !aligned_to(slots[k].grad, elem_bytes(slots[k].grad_dtype)))))
       return MRL_ERR_INVALID_ARG;
+    total += slots[k].numel;
   }
   if (workspace == nullptr || workspace_bytes < mrl_grad_norm_workspace_bytes()) return MRL_ERR_WORKSPACE_TOO_SMALL;
   if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return MRL_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   double* partial = static_cast<double*>(workspace);
-  return n_slots <= kSlotsFew ? launch_grad_norm<kSlotsFew>(slots, n_slots, max_norm, norm, coef, partial, st)
-                              : launch_grad_norm<kSlots>(slots, n_slots, max_norm, norm, coef, partial, st);
+  return n_slots <= kSlotsFew ? launch_grad_norm<kSlotsFew>(slots, n_slots, total, max_norm, norm, coef, partial, st)
+                              : launch_grad_norm<kSlots>(slots, n_slots, total, max_norm, norm, coef, partial, st);
 }
 
 extern "C" int mrl_adamw_step(const mrl_tensor_slot* slots, int32_t n_slots, const mrl_adamw_params* ap,
@@ -762,6 +763,10 @@ extern "C" int mrl_adamw_step(const mrl_tensor_slot* slots, int32_t n_slots, con
       (float)ap->eps < 1.17549435e-38f || !(ap->eps < 3.4e38) || !(ap->lr - ap->lr == 0.0) || ap->flags != 0 ||
       (ap->step_dev == nullptr && ap->step < 1) || (ap->rounding != MRL_ROUND_NEAREST && ap->rounding != MRL_ROUND_SEEDED))
     return MRL_ERR_INVALID_ARG;
+  // (one pass for all that the host needs of the tensors)
+  bool all_apart = true;
+  int count[16] = {0}, tensors = 0;
+  long long total = 0;
   for (int k = 0; k < n_slots; ++k) {
     const mrl_tensor_slot& s = slots[k];
     if (!grad_type_ok(s.grad_dtype) || !grad_type_ok(s.param_dtype) || (s.state_dtype != MRL_F32 && s.state_dtype != MRL_E4M3))
@@ -772,6 +777,9 @@ extern "C" int mrl_adamw_step(const mrl_tensor_slot* slots, int32_t n_slots, con
     if (s.master != nullptr && s.param_dtype != MRL_BF16) return MRL_ERR_INVALID_ARG;
     if (s.state_dtype == MRL_E4M3 && (s.m_scale == nullptr || s.v_scale == nullptr)) return MRL_ERR_INVALID_ARG;
     if (!on_elements(s)) return MRL_ERR_INVALID_ARG;
+    all_apart &= apart(s);
+    total += s.numel;
+    ++count[kind_of(s)], ++tensors;
   }
   if (!aligned_to(grad_scale, 4) || !aligned_to(status, 4) || !aligned_to(ap->lr_dev, 4) || !aligned_to(ap->step_dev, 8))
     return MRL_ERR_INVALID_ARG;
@@ -780,8 +788,7 @@ extern "C" int mrl_adamw_step(const mrl_tensor_slot* slots, int32_t n_slots, con
     if (workspace == nullptr || workspace_bytes < mrl_adamw_workspace_bytes()) return MRL_ERR_WORKSPACE_TOO_SMALL;
     if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return MRL_ERR_INVALID_ARG;
   }
-  for (int k = 0; k < n_slots; ++k)
-    if (slots[k].numel > 0 && !apart(slots[k])) return MRL_ERR_INVALID_ARG;
+  if (!all_apart) return MRL_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   AdamwArgs a{};
   a.hyper_dev = on_device ? static_cast<const Hyper*>(workspace) : nullptr;
@@ -793,9 +800,6 @@ extern "C" int mrl_adamw_step(const mrl_tensor_slot* slots, int32_t n_slots, con
   a.one_beta2 = (float)(1.0 - ap->beta2);
   a.eps = (float)ap->eps;
   a.seeded = ap->rounding == MRL_ROUND_SEEDED;
-  int count[16] = {0}, tensors = 0;
-  for (int k = 0; k < n_slots; ++k)
-    if (slots[k].numel > 0) ++count[kind_of(slots[k])], ++tensors;
   if (on_device || (tensors == 0 && grad_scale != nullptr && status != nullptr)) {
     adamw_prepare_kernel<<<1, 1, 0, st>>>(Hyper{}, ap->lr, ap->beta1, ap->beta2, ap->lr_dev, ap->step_dev, ap->step, ap->seed,
                                           grad_scale, status, on_device ? static_cast<Hyper*>(workspace) : nullptr);
@@ -807,7 +811,7 @@ extern "C" int mrl_adamw_step(const mrl_tensor_slot* slots, int32_t n_slots, con
     a.hyper.root_c2 = (float)(1.0 / sqrt(1.0 - pow(ap->beta2, (double)ap->step)));
     a.hyper.key = splitmix64(splitmix64(ap->seed) + (uint64_t)ap->step);
   }
-  const int chunk[2] = {chunk_of(slots, n_slots, step_threads(0), step_blocks(0)), chunk_of(slots, n_slots, step_threads(8), step_blocks(8))};
+  const int chunk[2] = {chunk_of(total, step_threads(0), step_blocks(0)), chunk_of(total, step_threads(8), step_blocks(8))};
   int rc = MRL_OK;
   const auto run = [&](auto kind) {
     constexpr int kKind = decltype(kind)::value;
