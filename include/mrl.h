@@ -61,6 +61,7 @@ extern "C" {
 #define MRL_DEV_TIMEOUT 2
 #define MRL_DEV_BAD_WORD_MAP 4
 #define MRL_DEV_NONFINITE_GRAD 8     /* mrl_adamw_step: *grad_scale is not finite; the step was skipped */
+#define MRL_DEV_BAD_LIST 16          /* mrl_distill_loss_fwd_bwd: a list names a token twice, or a log-prob in it is NaN or +inf */
 
 /* element types of logits / dlogits, rows, weights, gradients */
 #define MRL_F32 0
@@ -118,6 +119,19 @@ extern "C" {
 #define MRL_WS_RMSNORM_BWD 4            /* N rows of H columns; V, dtype, S unused */
 #define MRL_WS_GRAD_NORM 5              /* a constant; the sizes are unused */
 #define MRL_WS_ADAMW 6                  /* a constant; the sizes are unused */
+#define MRL_WS_DISTILL 7                /* N rows; V, H, dtype, S unused */
+
+#define MRL_MAX_TOP 128      /* longest list of a row's top tokens */
+
+/* mrl_distill_params.direction */
+#define MRL_DISTILL_FORWARD 0  /* KL(teacher || learner): covers what the teacher gives mass to */
+#define MRL_DISTILL_REVERSE 1  /* KL(learner || teacher): keeps to what the teacher gives mass to */
+
+/* mrl_distill_params.rest: what becomes of the vocabulary outside a teacher's list */
+#define MRL_REST_EVENT 0       /* one more event, with the mass that the list leaves */
+#define MRL_REST_NONE 1        /* none: the list's mass is scaled to 1 (MRL_DISTILL_FORWARD only) */
+
+#define MRL_SCALE_BLOCK 128    /* columns that share a scale of the codes of mrl_e4m3_quantize / mrl_e4m3_product */
 
 /* mrl_adamw_params.rounding: how what is kept in fewer bits than float32 is rounded */
 #define MRL_ROUND_NEAREST 0
@@ -132,6 +146,17 @@ typedef struct mrl_norm_params {
   int32_t group;            /* columns that share a scale of y8: 0 (the whole row), 32, 64, 128 or 256 (forward only) */
   uint32_t flags;           /* backward only: MRL_FLAG_ACCUMULATE_DW (dweight is added to, not overwritten) */
 } mrl_norm_params;
+
+typedef struct mrl_distill_params {
+  float temperature;        /* T, 1e-6 to 1e6: the learner's softmax is that of z / T */
+  float coeff;              /* factor of the loss and of its gradient */
+  int32_t direction;        /* MRL_DISTILL_* */
+  int32_t rest;             /* MRL_REST_* */
+  float rest_floor;         /* MRL_REST_EVENT: least mass of the rest in the teacher's distribution; in [0, 1), with
+                               MRL_DISTILL_REVERSE at least 2^-126 (the learner's mass there is weighed against it) */
+  uint32_t flags;           /* MRL_FLAG_ACCUMULATE_LOSS */
+  double denominator;       /* D: number of valid rows of the whole step when it is fed in several calls; <= 0: of this call */
+} mrl_distill_params;
 
 /* One tensor of mrl_grad_norm / mrl_adamw_step.  Contiguous; every pointer [device] and a multiple of its element (else
  * MRL_ERR_INVALID_ARG). */
@@ -563,6 +588,111 @@ int mrl_grad_norm(const mrl_tensor_slot* slots, int32_t n_slots, float max_norm,
  */
 int mrl_adamw_step(const mrl_tensor_slot* slots, int32_t n_slots, const mrl_adamw_params* ap, const float* grad_scale,
                    int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Scoring a frozen model in 8 bits and learning from its top tokens: the sequential-distillation counterpart of peer
+ * rollouts (the paper compares with it and says nothing about its kernels), and the traces `logp_old` / `logp_ref` of models
+ * that are held in 8 bits.  hidden (8-bit rows of mrl_rmsnorm_residual_fwd, group 128) -> mrl_e4m3_product -> logits ->
+ * mrl_top_logprobs -> lists -> mrl_distill_loss_fwd_bwd on the learner's logits.
+ *
+ * mrl_e4m3_quantize -- a matrix as e4m3 codes with one float32 scale per block of block_rows x 128 elements:
+ *   scales[a, b] = max(max over the block of |x| / 448, 2^-126),   codes[t, i] = e4m3(x[t, i] / scales[a, b])
+ * to nearest even (where x / scale is within 2^-22 of itself of the border between two codes, either may come); the blocks at
+ * the ends may be short.  NaN gives the code of NaN, infinities 448; the maxima pass over NaN, an infinite one gives an infinite
+ * scale and codes of zero (NaN for the infinite elements).
+ *
+ *   x          [device] dtype [N, ld_x], MRL_BF16 or MRL_F32
+ *   block_rows 128 (weights of mrl_e4m3_product) or 1 (its rows)
+ *   codes      [device] uint8 [N, ld_codes]
+ *   scales     [device] float32 [ceil(N / block_rows), ceil(H / 128)], contiguous
+ * N = 0 is a no-op.  H < 1, a row stride below H, a null pointer, an address that is not a multiple of its element, another
+ * block_rows -> MRL_ERR_INVALID_ARG; H > 2^30 -> MRL_ERR_UNSUPPORTED_SHAPE.
+ */
+int mrl_e4m3_quantize(const void* x, int64_t ld_x, int32_t dtype, int64_t N, int32_t H, int32_t block_rows, void* codes,
+                      int64_t ld_codes, float* scales, void* stream);
+
+/*
+ * mrl_e4m3_product -- rows times weights, both in e4m3 codes with a scale for each block of 128 columns:
+ *   out[t, v] = sum over blocks b of  x_scales[t, b] w_scales[v / 128, b]  sum over i in b of  x8[t, i] w8[v, i]
+ * The inner sums are the tensor cores' (float32 accumulators), the outer one is float32, rounded once to the output's type.
+ *
+ *   x8        [device] uint8 [N, ld_x]   e4m3 codes: those of mrl_rmsnorm_residual_fwd (group 128) or of mrl_e4m3_quantize
+ *   x_scales  [device] float32 [N, ceil(H / 128)], contiguous
+ *   w8        [device] uint8 [V, ld_w]   e4m3 codes of mrl_e4m3_quantize (block_rows 128)
+ *   w_scales  [device] float32 [ceil(V / 128), ceil(H / 128)], contiguous
+ *   out       [device] out_dtype [N, ld_out], MRL_BF16 or MRL_F32
+ *   status    [device] int32 [1], nullable
+ * x8 and w8 have to start on 16 bytes, with row strides (of more than one row) that are multiples of 16 (else MRL_ERR_INVALID_ARG); what lies between
+ * column H and the stride is not read.  Any N, H <= 2^24, V.  Bitwise reproducible; a row's result does not depend on the other rows, but its
+ * last bits may on N.  N = 0 is a no-op.  No gradient: what is scored here is frozen.
+ */
+int mrl_e4m3_product(const void* x8, int64_t ld_x, const float* x_scales, const void* w8, int64_t ld_w,
+                     const float* w_scales, int64_t N, int32_t H, int32_t V, int32_t out_dtype, void* out, int64_t ld_out,
+                     int32_t* status, void* stream);
+
+/*
+ * mrl_top_logprobs -- mrl_token_logprobs at a temperature, with each row's entropy and its `top` likeliest tokens.  With
+ * x = z[t, :] / temperature:
+ *   lse_t = log sum_v exp x_v,   logp_t = x[ids_t] - lse_t,   entropy_t = - sum_v p_v log p_v,  p = softmax(x)
+ *   top_ids[t, 0 .. top), top_logp[t, k] = x[top_ids[t, k]] - lse_t: the largest logits first, equal ones by their index
+ *
+ *   logits   [device] dtype [N, ld], ld >= V (read once); any address and ld that are multiples of the element
+ *   ids      [device] int32 [N], nullable (then logp has to be)
+ *   mask     [device] uint8 [N], nullable = all ones; rows with mask 0 are not read
+ *   temperature  1e-6 to 1e6
+ *   top      0 to min(V, MRL_MAX_TOP)
+ *   logp, lse, entropy  [device] float32 [N], each nullable
+ *   top_ids  [device] int32 [N, top], top_logp [device] float32 [N, top]; both required where top > 0
+ * A masked row and one with a bad id: logp, lse, entropy and top_logp 0, top_ids -1.  Logits of -inf have probability 0 (and
+ * are listed after all others, by their index); a row of nothing else, one with NaN or with +inf: lse, logp, entropy and
+ * top_logp as the formulas give them (NaN).  NaN logits are never listed; where fewer than `top` tokens can be, top_ids ends in -1, with
+ * top_logp -inf.
+ * float32 sums; bitwise reproducible for calls of the same N, V, dtype and alignment (few rows are cut among several CTAs: the
+ * last bits of lse can differ from those of a larger call; ids never do).  Cost follows the bytes except on rows with
+ * more than 2,048 candidates for the list -- rising ones, or long runs of one value at the top -- which are read several times.
+ * One output at least has to be given.  N = 0 is a no-op.  MRL_ERR_INVALID_ARG as in mrl_token_logprobs, and for a temperature or top
+ * outside its range, an address that is not a multiple of its element, one address for two outputs.
+ */
+int mrl_top_logprobs(const void* logits, int32_t dtype, int64_t N, int32_t V, int64_t ld, const int32_t* ids,
+                     const uint8_t* mask, float temperature, int32_t top, float* logp, float* lse, float* entropy,
+                     int32_t* top_ids, float* top_logp, int32_t* status, void* stream);
+
+/*
+ * mrl_distill_loss_fwd_bwd -- distillation of a learner from lists of a teacher's top tokens, with the gradient.
+ * With S_t the tokens listed in row t, q_k = exp(top_logp_k), p = softmax(z[t, :] / T), p_r = sum over v outside S_t of p_v:
+ *  MRL_REST_EVENT: the rest of the vocabulary is one more event, q_r = max(1 - sum_k q_k, rest_floor) in the teacher
+ *   FORWARD  KL_t = sum_k q_k (ln q_k - ln p_k) + q_r (ln q_r - ln p_r)
+ *   REVERSE  KL_t = sum_k p_k (ln p_k - ln q_k) + p_r (ln p_r - ln q_r)
+ *  MRL_REST_NONE: q scaled so that sum_k q_k = 1 (top_logp may then be any logits), KL_t = sum_k q_k (ln q_k - ln p_k)
+ *   row_kl[t] = KL_t,   loss = coeff / D * sum_t weight_t KL_t,   D = denominator (<= 0: the valid rows of this call)
+ *   dlogits = d loss / d z (the teacher's lists and the weights are constants), held in float32 and rounded once
+ * The lists are taken as log-probs at the temperature they are compared at: mrl_top_logprobs of the teacher with the same T.
+ *
+ *   logits     [device] dtype [N, ld], ld >= V; any address and ld that are multiples of the element
+ *   top_ids    [device] int32 [N, top], a negative id: an unused place;  top_logp [device] float32 [N, top], -inf: likewise
+ *   top        1 to min(V, MRL_MAX_TOP)
+ *   mask       [device] uint8 [N], nullable = all ones
+ *   row_weight [device] float32 [N], nullable = 1; a row of weight 0 adds exactly 0 to the loss and gets a gradient of 0
+ *   dp         [host]
+ *   dlogits    [device] dtype [N, ld_out]; may equal `logits` with ld_out = ld (in place); nullable = forward only.  Every
+ *              row is written
+ *   row_kl     [device] float32 [N], nullable
+ *   loss       [device] float32 [1]
+ *   stats      [device] int64 [2], nullable: valid rows, refused rows (both added to under MRL_FLAG_ACCUMULATE_LOSS)
+ *   workspace: mrl_workspace_bytes(MRL_WS_DISTILL, N, 0, 0, 0, 0)
+ * A row is valid if its mask is on, its list has a used place and is not refused.  Refused (and flagged): an id >= V
+ * (MRL_DEV_BAD_TOKEN_ID), a token twice, a log-prob of NaN or +inf (MRL_DEV_BAD_LIST).  Rows that are not valid: row_kl 0, gradient 0.
+ * Where the learner leaves the rest nothing -- every token is listed, or the others are masked with -inf or the type's lowest
+ * value: ln p_r < -700 -- there is no rest: its term is left out (q_r = 0).  A listed token with z = -inf makes the forward KL infinite, its
+ * gradient is finite; NaN, +inf and rows of -inf alone give NaN.
+ * The rows' sums are float32, a row's KL and the sum over the rows float64 in a fixed order: bitwise reproducible for calls
+ * of the same N, V, dtype and alignment.  N = 0: loss (and stats) are zeroed unless accumulated.  V > 2^20 -> MRL_ERR_UNSUPPORTED_SHAPE; other
+ * errors as in mrl_policy_loss_fwd_bwd and mrl_top_logprobs.
+ */
+int mrl_distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64_t N, int32_t V, int64_t ld, const int32_t* top_ids,
+                             const float* top_logp, int32_t top, const uint8_t* mask, const float* row_weight,
+                             const mrl_distill_params* dp, void* dlogits, int64_t ld_out, float* row_kl, float* loss,
+                             int64_t* stats, int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * mrl_profile_dominant_kernel -- instrumentation for benchmarks; the paper has no counterpart.

@@ -21,16 +21,20 @@ RATIO_TOKEN, RATIO_SEQUENCE = 0, 1
 KL_K1, KL_K2, KL_K3 = 0, 1, 2
 FLAG_ACCUMULATE_LOSS, FLAG_SKIP_ZERO_ROWS, FLAG_ACCUMULATE_DW, FLAG_PAIR_TILES = 1, 2, 4, 8
 WS_TOKEN_LOGPROBS, WS_POLICY_LOSS, WS_FUSED_LMHEAD, WS_THL_WORD_ALIGN = 0, 1, 2, 3
-WS_RMSNORM_BWD, WS_GRAD_NORM, WS_ADAMW = 4, 5, 6
-DEV_BAD_TOKEN_ID, DEV_TIMEOUT, DEV_BAD_WORD_MAP, DEV_NONFINITE_GRAD = 1, 2, 4, 8
+WS_RMSNORM_BWD, WS_GRAD_NORM, WS_ADAMW, WS_DISTILL = 4, 5, 6, 7
+DEV_BAD_TOKEN_ID, DEV_TIMEOUT, DEV_BAD_WORD_MAP, DEV_NONFINITE_GRAD, DEV_BAD_LIST = 1, 2, 4, 8, 16
 ROUND_NEAREST, ROUND_SEEDED = 0, 1
 STATE_BLOCK = 256
+DISTILL_FORWARD, DISTILL_REVERSE = 0, 1
+REST_EVENT, REST_NONE = 0, 1
+MAX_TOP, SCALE_BLOCK = 128, 128
 
 EXPORTS = ("mrl_group_advantages", "mrl_token_logprobs", "mrl_policy_loss_fwd_bwd",
            "mrl_fused_lmhead_loss_fwd_bwd", "mrl_workspace_bytes", "mrl_status_string", "mrl_version",
            "mrl_profile_dominant_kernel", "mrl_policy_loss_fwd_bwd_static", "mrl_thl_word_align_logprobs",
            "mrl_policy_loss_fwd_bwd_host", "mrl_host_pipeline_workspace_bytes", "mrl_profile_last_kernel",
-           "mrl_rmsnorm_residual_fwd", "mrl_rmsnorm_residual_bwd", "mrl_grad_norm", "mrl_adamw_step")
+           "mrl_rmsnorm_residual_fwd", "mrl_rmsnorm_residual_bwd", "mrl_grad_norm", "mrl_adamw_step",
+           "mrl_e4m3_quantize", "mrl_e4m3_product", "mrl_top_logprobs", "mrl_distill_loss_fwd_bwd")
 STATIC_MAX_ROWS, STATIC_MAX_SEQS = 65536, 65536
 ERR_STATIC_SCRATCH_TOO_SMALL = 8
 
@@ -64,6 +68,11 @@ class AdamwParams(C.Structure):
     _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
                 ("step", C.c_int64), ("seed", C.c_uint64), ("rounding", C.c_int32), ("flags", C.c_uint32),
                 ("lr_dev", C.c_void_p), ("step_dev", C.c_void_p)]
+
+
+class DistillParams(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("coeff", C.c_float), ("direction", C.c_int32), ("rest", C.c_int32),
+                ("rest_floor", C.c_float), ("flags", C.c_uint32), ("denominator", C.c_double)]
 
 
 class MrlError(RuntimeError):
@@ -115,6 +124,15 @@ def lib() -> C.CDLL:
         L.mrl_grad_norm.restype = C.c_int
         L.mrl_adamw_step.argtypes = [vp, i32, C.POINTER(AdamwParams), vp, vp, vp, sz, vp]
         L.mrl_adamw_step.restype = C.c_int
+        L.mrl_e4m3_quantize.argtypes = [vp, i64, i32, i64, i32, i32, vp, i64, vp, vp]
+        L.mrl_e4m3_quantize.restype = C.c_int
+        L.mrl_e4m3_product.argtypes = [vp, i64, vp, vp, i64, vp, i64, i32, i32, i32, vp, i64, vp, vp]
+        L.mrl_e4m3_product.restype = C.c_int
+        L.mrl_top_logprobs.argtypes = [vp, i32, i64, i32, i64, vp, vp, C.c_float, i32, vp, vp, vp, vp, vp, vp, vp]
+        L.mrl_top_logprobs.restype = C.c_int
+        L.mrl_distill_loss_fwd_bwd.argtypes = [vp, i32, i64, i32, i64, vp, vp, i32, vp, vp, C.POINTER(DistillParams), vp, i64,
+                                               vp, vp, vp, vp, vp, sz, vp]
+        L.mrl_distill_loss_fwd_bwd.restype = C.c_int
         L.mrl_workspace_bytes.argtypes = [i32, i64, i32, i32, i32, i32]
         L.mrl_workspace_bytes.restype = sz
         L.mrl_status_string.argtypes = [C.c_int]
@@ -441,6 +459,81 @@ def mrl_adamw_step(tensors: TensorList, ap: AdamwParams, grad_scale=None, status
     ws, ws_bytes = _workspace(workspace, dev, where)
     code = lib().mrl_adamw_step(tensors.address, tensors.n, ap, _float_vector(grad_scale, 1, dev, where),
                                 _vector(status, 1, (torch.int32,), dev, where), ws, ws_bytes, st)
+    if code != OK:
+        raise MrlError(code, where)
+
+
+# ---- a frozen model scored in 8 bits, its top tokens, and the loss that learns from them
+
+_I32_ONLY, _U8_ONLY, _I64_ONLY = (torch.int32,), (torch.uint8,), (torch.int64,)
+
+
+def _row_code(t, where):
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise MrlError(3, where)
+    return code
+
+
+def mrl_e4m3_quantize(x, codes, scales, block_rows: int, stream=None):
+    """Codes uint8 or float8_e4m3fn like x, scales float32 of ceil(N / block_rows) x ceil(H / 128)."""
+    where, shape, dev = "mrl_e4m3_quantize", x.shape, x.get_device()
+    N, H = shape
+    code, st = _row_code(x, where), _stream_of(dev, stream, where)
+    n_scales = -(-N // block_rows) * -(-H // SCALE_BLOCK) if block_rows > 0 else 0
+    code = lib().mrl_e4m3_quantize(x.data_ptr(), _row_stride(x, shape, x.dtype, dev, where), code, N, H, block_rows,
+                                   codes.data_ptr(), _row_stride(codes, shape, None, dev, where),
+                                   _float_vector(scales, n_scales, dev, where), st)
+    if code != OK:
+        raise MrlError(code, where)
+
+
+def mrl_e4m3_product(x8, x_scales, w8, w_scales, out, status=None, stream=None):
+    """out[N, V] (bf16 or float32) of rows x8[N, H] and weights w8[V, H]; codes uint8 or float8_e4m3fn."""
+    where, dev = "mrl_e4m3_product", x8.get_device()
+    (N, H), V = x8.shape, w8.shape[0]
+    code, st = _row_code(out, where), _stream_of(dev, stream, where)
+    blocks = -(-H // SCALE_BLOCK)
+    code = lib().mrl_e4m3_product(
+        x8.data_ptr(), _row_stride(x8, x8.shape, None, dev, where), _float_vector(x_scales, N * blocks, dev, where),
+        w8.data_ptr(), _row_stride(w8, (V, H), None, dev, where),
+        _float_vector(w_scales, -(-V // SCALE_BLOCK) * blocks, dev, where), N, H, V, code, out.data_ptr(),
+        _row_stride(out, (N, V), out.dtype, dev, where), _vector(status, 1, _I32_ONLY, dev, where), st)
+    if code != OK:
+        raise MrlError(code, where)
+
+
+def mrl_top_logprobs(logits, ids, mask, temperature: float, logp=None, lse=None, entropy=None, top_ids=None, top_logp=None,
+                     status=None, stream=None):
+    """`top` is the number of columns of top_ids and top_logp (none: 0)."""
+    where, shape, dev = "mrl_top_logprobs", logits.shape, logits.get_device()
+    N, V = shape
+    code, st = _row_code(logits, where), _stream_of(dev, stream, where)
+    top = 0 if top_ids is None else top_ids.shape[-1]
+    code = lib().mrl_top_logprobs(
+        logits.data_ptr(), code, N, V, _row_stride(logits, shape, logits.dtype, dev, where),
+        _vector(ids, N, _I32_ONLY, dev, where), _vector(mask, N, _U8_ONLY, dev, where), temperature, top,
+        _float_vector(logp, N, dev, where), _float_vector(lse, N, dev, where), _float_vector(entropy, N, dev, where),
+        _vector(top_ids, N * top, _I32_ONLY, dev, where), _float_vector(top_logp, N * top, dev, where),
+        _vector(status, 1, _I32_ONLY, dev, where), st)
+    if code != OK:
+        raise MrlError(code, where)
+
+
+def mrl_distill_loss_fwd_bwd(logits, top_ids, top_logp, mask, row_weight, dp: DistillParams, dlogits, row_kl, loss, stats=None,
+                             status=None, workspace=None, stream=None):
+    where, shape, dev = "mrl_distill_loss_fwd_bwd", logits.shape, logits.get_device()
+    N, V = shape
+    code, st = _row_code(logits, where), _stream_of(dev, stream, where)
+    top = top_ids.shape[-1]
+    ld, ld_out = _row_stride(logits, shape, logits.dtype, dev, where), _row_stride(dlogits, shape, logits.dtype, dev, where)
+    ws, ws_bytes = _workspace(workspace, dev, where)
+    code = lib().mrl_distill_loss_fwd_bwd(
+        logits.data_ptr(), code, N, V, ld, _vector(top_ids, N * top, _I32_ONLY, dev, where),
+        _float_vector(top_logp, N * top, dev, where), top, _vector(mask, N, _U8_ONLY, dev, where),
+        _float_vector(row_weight, N, dev, where), dp, None if dlogits is None else dlogits.data_ptr(), ld_out or ld,
+        _float_vector(row_kl, N, dev, where), _float_vector(loss, 1, dev, where), _vector(stats, 2, _I64_ONLY, dev, where),
+        _vector(status, 1, _I32_ONLY, dev, where), ws, ws_bytes, st)
     if code != OK:
         raise MrlError(code, where)
 
