@@ -1,5 +1,5 @@
 // Scoring in 8 bits: mrl_e4m3_quantize and mrl_e4m3_product.
-#include "mrl_common.cuh"
+#include "mrl_tensor.cuh"
 
 namespace {
 
@@ -38,47 +38,244 @@ __global__ void __launch_bounds__(256) quantize_kernel(const T* __restrict__ x, 
       codes[(row0 + r) * ld_codes + col] = (uint8_t)pack_e4m3x2(load_f<T>(x + (row0 + r) * ld_x + col) * inv, 0.f);
 }
 
-// 64 x 64 outputs per CTA of 256 threads, one block of 128 columns at a time.
+// ------------------------------------------------------------------------------------------ product
+// One CTA per SM works through tiles of 128 rows x 256 weights.  Warp 0 brings K-blocks of 128 codes (one 128-byte swizzle row) into a
+// ring by TMA, one thread of warp 1 multiplies each into one of two accumulators in tensor memory -- never two blocks into the same,
+// for each block has its own scale -- and eight warps add scale * accumulator to sums in registers, 128 columns (so one scale) of one
+// row a thread, while the next block is multiplied: 512 cycles of tensor core a block against 256 of packed multiply-adds.
+constexpr int kBM = 128, kBN = 256;
+constexpr int kStages = 4, kEpiWarps = 8, kProductThreads = 64 + 32 * kEpiWarps;
+constexpr uint32_t kATile = kBM * kBlock, kBTile = kBN * kBlock, kStage = kATile + kBTile;
+// staging of a warp's outputs: 32 rows of 64 bytes, 16 bytes between them
+constexpr uint32_t kOutRow = 80, kOutWarp = 32 * kOutRow;
+constexpr size_t kProductSmem = (size_t)kStages * kStage + 1024 /* alignment */ + 256 /* barriers */ + kEpiWarps * kOutWarp;
+constexpr uint32_t kIdescE4m3 = (1u << 4) /* float32 sums */ | ((uint32_t)(kBN >> 3) << 17) | ((uint32_t)(kBM >> 4) << 24);
+
+struct ProductArgs {
+  const float *x_scales, *w_scales;
+  void* out;
+  long long N, ld_out;
+  int V, k_blocks, m_tiles, n_tiles, group_m;
+  bool vector_out;  // rows of out start on 16 bytes
+  int32_t* status;
+};
+
+// D[tmem] (+)= A[smem] * B[smem]^T, one 128 x 256 x 32 step on e4m3 codes
+__device__ __forceinline__ void tc_mma_e4m3(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t accum) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(kIdescE4m3), "r"(accum)
+      : "memory");
+}
+
 template <typename T>
-__global__ void __launch_bounds__(256) product_kernel(const uint8_t* __restrict__ x8, long long ld_x, const float* __restrict__ xs,
-                                                      const uint8_t* __restrict__ w8, long long ld_w, const float* __restrict__ ws,
-                                                      long long N, int H, int V, T* __restrict__ out, long long ld_out) {
-  __shared__ float a[64][33], b[64][33];
-  const long long row0 = (long long)blockIdx.y * 64;
-  const long long col0 = (long long)blockIdx.x * 64;
-  const int tr = threadIdx.x >> 4, tc = threadIdx.x & 15, blocks = (H + kBlock - 1) / kBlock;
-  float sum[4][4] = {};
-  for (int kb = 0; kb < blocks; ++kb) {
-    float part[4][4] = {};
-    for (int k0 = 0; k0 < kBlock; k0 += 32) {
-      __syncthreads();
-      for (int i = threadIdx.x; i < 64 * 32; i += 256) {
-        const int r = i >> 5, k = kb * kBlock + k0 + (i & 31);
-        a[r][i & 31] = row0 + r < N && k < H ? unpack_e4m3x2(x8[(row0 + r) * ld_x + k]).x : 0.f;
-        b[r][i & 31] = col0 + r < V && k < H ? unpack_e4m3x2(w8[(col0 + r) * ld_w + k]).x : 0.f;
-      }
-      __syncthreads();
-      for (int k = 0; k < 32; ++k)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) part[i][j] = fmaf(a[tr * 4 + i][k], b[tc * 4 + j][k], part[i][j]);
+__global__ void __launch_bounds__(kProductThreads, 1)
+product_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const ProductArgs p) {
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_addr(smem_raw), tiles = (raw + 1023u) & ~1023u;
+  unsigned char* after = smem_raw + (tiles - raw) + (size_t)kStages * kStage;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(after);
+  const uint32_t bar0 = smem_addr(bars);
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (kStages + s); };
+  auto tfull_bar = [&](int a) { return bar0 + 8u * (2 * kStages + a); };
+  auto tempty_bar = [&](int a) { return bar0 + 8u * (2 * kStages + 2 + a); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kStages + 4);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int total = p.m_tiles * p.n_tiles;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const long long r = row0 + tr * 4 + i, c = col0 + tc * 4 + j;
-        if (r < N && c < V) sum[i][j] = fmaf(xs[r * blocks + kb] * ws[(c / kBlock) * blocks + kb], part[i][j], sum[i][j]);
-      }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(tfull_bar(a), 1);
+      mbar_init(tempty_bar(a), kEpiWarps);
+    }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const long long r = row0 + tr * 4 + i, c = col0 + tc * 4 + j;
-      if (r < N && c < V) store_f(out + r * ld_out + c, sum[i][j]);
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int t = blockIdx.x; t < total && ok; t += gridDim.x) {
+        int m, n;
+        tile_coords(t, p.m_tiles, p.n_tiles, p.group_m, m, n);
+        for (int kb = 0; kb < p.k_blocks; ++kb) {
+          if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) { ok = false; break; }
+          const uint32_t dst = tiles + (uint32_t)stage * kStage;
+          mbar_expect_tx(full_bar(stage), kStage);
+          tma_load_2d(dst, &map_x, kb * kBlock, m * kBM, full_bar(stage));
+          tma_load_2d(dst + kATile, &map_w, kb * kBlock, n * kBN, full_bar(stage));
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        }
+      }
     }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      int stage = 0, acc = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      bool ok = true;
+      for (int t = blockIdx.x; t < total && ok; t += gridDim.x) {
+        for (int kb = 0; kb < p.k_blocks; ++kb) {
+          if (!mbar_wait(tempty_bar(acc), acc_phase ^ 1u, abort_flag) || !mbar_wait(full_bar(stage), phase, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t src = tiles + (uint32_t)stage * kStage;
+          const uint64_t a = smem_desc_k128(src), b = smem_desc_k128(src + kATile);
+#pragma unroll
+          for (int k = 0; k < kBlock / 32; ++k)  // 32 codes: 32 bytes along a swizzle row
+            tc_mma_e4m3(tmem + (uint32_t)acc * kBN, a + 2 * k, b + 2 * k, k != 0);
+          tc_commit(empty_bar(stage));
+          tc_commit(tfull_bar(acc));
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+          acc ^= 1;
+          if (acc == 0) acc_phase ^= 1u;
+        }
+      }
+    }
+  } else {
+    const int quad = warp & 3, half = (warp - 2) >> 2;  // lanes 32 quad .. + 31 of tensor memory, columns 128 half .. + 127 of the tile
+    const uint32_t staging = smem_addr(after + 256) + (uint32_t)(warp - 2) * kOutWarp;
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; t < total && ok; t += gridDim.x) {
+      int m, n;
+      tile_coords(t, p.m_tiles, p.n_tiles, p.group_m, m, n);
+      const long long row0 = (long long)m * kBM + quad * 32, row = row0 + lane;
+      const int col0 = n * kBN + half * kBlock;
+      const bool live = row < p.N && col0 < p.V;
+      const float* xs = p.x_scales + (live ? row * p.k_blocks : 0);
+      const float* ws = p.w_scales + (live ? (long long)(n * 2 + half) * p.k_blocks : 0);
+      f2 sum[kBlock / 2];
+#pragma unroll
+      for (int j = 0; j < kBlock / 2; ++j) sum[j] = 0;
+      float sx = live ? xs[0] : 0.f, sw = live ? ws[0] : 0.f;
+#pragma unroll 1
+      for (int kb = 0; kb < p.k_blocks; ++kb) {
+        const float s = sx * sw;
+        const f2 s2 = make_f2(s, s);
+        const int next = kb + 1 < p.k_blocks ? kb + 1 : kb;
+        if (live) {
+          sx = xs[next];
+          sw = ws[next];
+        }
+        if (!mbar_wait(tfull_bar(acc), acc_phase, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t src = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * kBN + half * kBlock);
+#pragma unroll
+        for (int c = 0; c < kBlock; c += 32) {
+          float v[32];
+          tc_ld32(src + (uint32_t)c, v);
+          if (c == kBlock - 32) {  // read: the accumulator may be written again
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(tempty_bar(acc));
+          }
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) sum[(c + j) / 2] = fma_f2(make_f2(v[j], v[j + 1]), s2, sum[(c + j) / 2]);
+        }
+        acc ^= 1;
+        if (acc == 0) acc_phase ^= 1u;
+      }
+      if (!ok) break;
+      // out through shared memory, 64 bytes of 32 rows at a time
+      constexpr int kCols = 64 / (int)sizeof(T);
+      T* out = static_cast<T*>(p.out) + row0 * p.ld_out + col0;
+      const int rows = (int)min((long long)32, p.N - row0), cols = p.V - col0;
+      if (rows > 0) {
+#pragma unroll
+        for (int c = 0; c < kBlock; c += kCols) {
+          if (c < cols) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              uint32_t w[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                if constexpr (sizeof(T) == 2) {
+                  w[j] = f2_to_bf16x2(sum[c / 2 + q * 4 + j]);
+                } else {
+                  const float2 u = split_f2(sum[c / 2 + q * 2 + j / 2]);
+                  w[j] = __float_as_uint(j & 1 ? u.y : u.x);
+                }
+              }
+              sts_v4(staging + (uint32_t)lane * kOutRow + 16u * q, w[0], w[1], w[2], w[3]);
+            }
+            __syncwarp();
+            if (p.vector_out && c + kCols <= cols) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int r = (lane >> 2) + 8 * i;
+                const uint4 u = lds_v4(staging + (uint32_t)r * kOutRow + (uint32_t)(lane & 3) * 16u);
+                if (r < rows) *reinterpret_cast<uint4*>(out + r * p.ld_out + c + (lane & 3) * (16 / sizeof(T))) = u;
+              }
+            } else {
+              const T* mine = reinterpret_cast<const T*>(after + 256 + (warp - 2) * kOutWarp);
+              for (int r = 0; r < rows; ++r)
+                if (lane < kCols && c + lane < cols) out[r * p.ld_out + c + lane] = mine[r * (kOutRow / sizeof(T)) + lane];
+            }
+            __syncwarp();
+          }
+        }
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {
+    if (threadIdx.x == 0 && p.status != nullptr) atomicOr(p.status, MRL_DEV_TIMEOUT);
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);  // let copies and MMAs still in flight land before the CTA goes
+    __syncthreads();
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  }
+}
+
+// Tensor map of a row-major matrix of codes [rows, cols], read in tiles of box_rows x 128; zeros beyond its ends.
+int make_code_map(CUtensorMap* map, const void* base, long long rows, int cols, long long ld, int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (fn == nullptr) return MRL_ERR_CUDA;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)(rows > 1 ? ld : (long long)mrl_align_up((size_t)cols, 16))};
+  const cuuint32_t box[2] = {(cuuint32_t)kBlock, (cuuint32_t)box_rows};
+  const cuuint32_t step[2] = {1, 1};
+  const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, step,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? MRL_OK : MRL_ERR_CUDA;
+}
+
+template <typename T>
+int launch_product(const CUtensorMap& mx, const CUtensorMap& mw, const ProductArgs& a, cudaStream_t st) {
+  static std::atomic<uint64_t> attr_done;
+  const int rc = mrl_once_per_device(attr_done, [] {
+    return cudaFuncSetAttribute(product_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kProductSmem);
+  });
+  if (rc != MRL_OK) return rc;
+  const long long total = (long long)a.m_tiles * a.n_tiles;
+  const int grid = (int)(total < sm_count() ? total : sm_count());
+  mrl_profile_before(st, "product_kernel");
+  product_kernel<T><<<grid, kProductThreads, kProductSmem, st>>>(mx, mw, a);
+  mrl_profile_after(st);
+  return cudaGetLastError() == cudaSuccess ? MRL_OK : MRL_ERR_CUDA;
 }
 
 bool row_type_ok(int32_t dtype) { return dtype == MRL_BF16 || dtype == MRL_F32; }
@@ -121,14 +318,24 @@ extern "C" int mrl_e4m3_product(const void* x8, int64_t ld_x, const float* x_sca
     return MRL_ERR_INVALID_ARG;
   if (out == x8 || out == w8 || out == x_scales || out == w_scales) return MRL_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const dim3 grid((unsigned)((V + 63) / 64), (unsigned)((N + 63) / 64));
-  mrl_profile_before(st, "product_kernel");
-  if (out_dtype == MRL_BF16)
-    product_kernel<<<grid, 256, 0, st>>>(static_cast<const uint8_t*>(x8), ld_x, x_scales, static_cast<const uint8_t*>(w8), ld_w,
-                                         w_scales, N, H, V, static_cast<__nv_bfloat16*>(out), ld_out);
-  else
-    product_kernel<<<grid, 256, 0, st>>>(static_cast<const uint8_t*>(x8), ld_x, x_scales, static_cast<const uint8_t*>(w8), ld_w,
-                                         w_scales, N, H, V, static_cast<float*>(out), ld_out);
-  mrl_profile_after(st);
-  return cudaGetLastError() == cudaSuccess ? MRL_OK : MRL_ERR_CUDA;
+  CUtensorMap mx, mw;
+  int rc = make_code_map(&mx, x8, N, H, ld_x, kBM);
+  if (rc == MRL_OK) rc = make_code_map(&mw, w8, V, H, ld_w, kBN);
+  if (rc != MRL_OK) return rc;
+  const int es = out_dtype == MRL_BF16 ? 2 : 4;
+  ProductArgs a{};
+  a.x_scales = x_scales;
+  a.w_scales = w_scales;
+  a.out = out;
+  a.N = N;
+  a.ld_out = ld_out;
+  a.V = V;
+  a.k_blocks = (H + kBlock - 1) / kBlock;
+  a.m_tiles = (int)((N + kBM - 1) / kBM);
+  a.n_tiles = (V + kBN - 1) / kBN;
+  a.group_m = 4096 / kBM;  // rows of x that stay in L2 while the weights pass by
+  a.vector_out = on_element(out, 16) && (N == 1 || ld_out * es % 16 == 0);
+  a.status = status;
+  if ((long long)a.m_tiles * a.n_tiles > 0x7fffffffll) return MRL_ERR_UNSUPPORTED_SHAPE;
+  return out_dtype == MRL_BF16 ? launch_product<__nv_bfloat16>(mx, mw, a, st) : launch_product<float>(mx, mw, a, st);
 }

@@ -58,7 +58,8 @@ def test_the_chain_against_the_oracle():
     assert int(a.status) == 0
     cpu = lambda t: t.cpu()  # noqa: E731
     want, size = S.product(cpu(a.x8).view(torch.float8_e4m3fn), cpu(a.xs), cpu(a.w8).view(torch.float8_e4m3fn), cpu(a.ws))
-    assert bool(((cpu(a.teacher).double() - want).abs() <= 2.0 ** -9 * want.abs() * 1.001 + size * 12 * 2.0 ** -23).all())
+    # bf16 keeps eight bits: a rounding is off by half a step, 2^-8 of the value (values just above a power of two)
+    assert bool(((cpu(a.teacher).double() - want).abs() <= 2.0 ** -8 * want.abs() + size * 12 * 2.0 ** -23).all())
     # e4m3 keeps three bits: each factor is off by at most 2^-4 of itself, their product by 2^-3 + 2^-8
     y = torch.nn.functional.rms_norm(a.x.double(), (H,), a.gain.double(), 1e-6).cpu()
     exact, bound = y @ a.W.double().cpu().T, y.abs() @ a.W.double().abs().cpu().T
