@@ -13,8 +13,6 @@ template <>
 __device__ __forceinline__ float load_f<float>(const float* p) { return *p; }
 template <>
 __device__ __forceinline__ float load_f<__nv_bfloat16>(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-__device__ __forceinline__ void store_f(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store_f(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
 // One CTA per block of `rows` x 128 elements.
 template <typename T>
@@ -44,7 +42,9 @@ __global__ void __launch_bounds__(256) quantize_kernel(const T* __restrict__ x, 
 // for each block has its own scale -- and eight warps add scale * accumulator to sums in registers, 128 columns (so one scale) of one
 // row a thread, while the next block is multiplied: 512 cycles of tensor core a block against 256 of packed multiply-adds.
 constexpr int kBM = 128, kBN = 256;
-constexpr int kStages = 4, kEpiWarps = 8, kProductThreads = 64 + 32 * kEpiWarps;
+constexpr int kStages = 4, kEpiWarps = 8, kProductThreads = 128 + 32 * kEpiWarps;
+// registers of a thread: 168 at launch, moved from the first warpgroup (copies, issue) to the two that hold sums (128 x 40 + 256 x 232)
+constexpr int kIssueRegs = 40, kSumRegs = 232;
 constexpr uint32_t kATile = kBM * kBlock, kBTile = kBN * kBlock, kStage = kATile + kBTile;
 // staging of a warp's outputs: 32 rows of 64 bytes, 16 bytes between them
 constexpr uint32_t kOutRow = 80, kOutWarp = 32 * kOutRow;
@@ -56,9 +56,14 @@ struct ProductArgs {
   void* out;
   long long N, ld_out;
   int V, k_blocks, m_tiles, n_tiles, group_m;
-  bool vector_out;  // rows of out start on 16 bytes
+  bool vector_out, vector_scales;  // rows of out, and of both scales, start on 16 bytes
   int32_t* status;
 };
+
+// sum += a * b, where it stands among the loads (left to itself the compiler gathers the additions behind the last load)
+__device__ __forceinline__ void fma_f2_here(f2& sum, f2 a, f2 b) {
+  asm volatile("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(sum) : "l"(a), "l"(b));
+}
 
 // D[tmem] (+)= A[smem] * B[smem]^T, one 128 x 256 x 32 step on e4m3 codes
 __device__ __forceinline__ void tc_mma_e4m3(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t accum) {
@@ -108,6 +113,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
 
+  if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
   if (warp == 0) {
     if (lane == 0) {
       int stage = 0;
@@ -127,30 +133,34 @@ product_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      int stage = 0, acc = 0;
-      uint32_t phase = 0, acc_phase = 0;
-      bool ok = true;
-      for (int t = blockIdx.x; t < total && ok; t += gridDim.x) {
-        for (int kb = 0; kb < p.k_blocks; ++kb) {
-          if (!mbar_wait(tempty_bar(acc), acc_phase ^ 1u, abort_flag) || !mbar_wait(full_bar(stage), phase, abort_flag)) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t src = tiles + (uint32_t)stage * kStage;
-          const uint64_t a = smem_desc_k128(src), b = smem_desc_k128(src + kATile);
+    // (the whole warp goes through the loop, so that addresses and descriptors stay in uniform registers; one lane issues)
+    const bool issuer = elect_one();
+    int stage = 0, acc = 0;
+    uint32_t phase = 0, acc_phase = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; t < total && ok; t += gridDim.x) {
+      for (int kb = 0; kb < p.k_blocks; ++kb) {
+        if (!mbar_wait2(tempty_bar(acc), acc_phase ^ 1u, full_bar(stage), phase, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t src = tiles + (uint32_t)stage * kStage;
+        const uint64_t a = smem_desc_k128(src), b = smem_desc_k128(src + kATile);
+        if (issuer) {
 #pragma unroll
           for (int k = 0; k < kBlock / 32; ++k)  // 32 codes: 32 bytes along a swizzle row
             tc_mma_e4m3(tmem + (uint32_t)acc * kBN, a + 2 * k, b + 2 * k, k != 0);
           tc_commit(empty_bar(stage));
           tc_commit(tfull_bar(acc));
-          if (++stage == kStages) { stage = 0; phase ^= 1u; }
-          acc ^= 1;
-          if (acc == 0) acc_phase ^= 1u;
         }
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        acc ^= 1;
+        if (acc == 0) acc_phase ^= 1u;
       }
     }
-  } else {
-    const int quad = warp & 3, half = (warp - 2) >> 2;  // lanes 32 quad .. + 31 of tensor memory, columns 128 half .. + 127 of the tile
-    const uint32_t staging = smem_addr(after + 256) + (uint32_t)(warp - 2) * kOutWarp;
+  } else if (warp >= 4) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSumRegs));
+    const int quad = warp & 3, half = (warp - 4) >> 2;  // lanes 32 quad .. + 31 of tensor memory, columns 128 half .. + 127 of the tile
+    const uint32_t staging = smem_addr(after + 256) + (uint32_t)(warp - 4) * kOutWarp;
+    const uint32_t mine = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * kBlock);
     int acc = 0;
     uint32_t acc_phase = 0;
     bool ok = true;
@@ -165,33 +175,64 @@ product_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
       f2 sum[kBlock / 2];
 #pragma unroll
       for (int j = 0; j < kBlock / 2; ++j) sum[j] = 0;
-      float sx = live ? xs[0] : 0.f, sw = live ? ws[0] : 0.f;
+      // scales of four K-blocks at a time, the next four on their way (a row's scales lie in one or two lines: four single loads
+      // of them cost as much of L1 as one of 16 bytes)
+      float sx[4], sw[4], s4[4];
+      auto load_scales = [&](int kb) {
+        if (p.vector_scales) {
+          const float4 x = live && kb < p.k_blocks ? *reinterpret_cast<const float4*>(xs + kb) : make_float4(0.f, 0.f, 0.f, 0.f);
+          const float4 w = live && kb < p.k_blocks ? *reinterpret_cast<const float4*>(ws + kb) : make_float4(0.f, 0.f, 0.f, 0.f);
+          sx[0] = x.x, sx[1] = x.y, sx[2] = x.z, sx[3] = x.w;
+          sw[0] = w.x, sw[1] = w.y, sw[2] = w.z, sw[3] = w.w;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            sx[j] = live && kb + j < p.k_blocks ? xs[kb + j] : 0.f;
+            sw[j] = live && kb + j < p.k_blocks ? ws[kb + j] : 0.f;
+          }
+        }
+      };
+      load_scales(0);
+      if (!mbar_wait(tfull_bar(acc), acc_phase, abort_flag)) { ok = false; break; }
+      __syncwarp();
+      tc_fence_after();
+      uint32_t v[2][32];  // the 32 columns that are added and the 32 on their way
+      tc_ld32_start(mine + (uint32_t)(acc * kBN), v[0]);
 #pragma unroll 1
       for (int kb = 0; kb < p.k_blocks; ++kb) {
-        const float s = sx * sw;
-        const f2 s2 = make_f2(s, s);
-        const int next = kb + 1 < p.k_blocks ? kb + 1 : kb;
-        if (live) {
-          sx = xs[next];
-          sw = ws[next];
-        }
-        if (!mbar_wait(tfull_bar(acc), acc_phase, abort_flag)) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t src = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * kBN + half * kBlock);
+        if ((kb & 3) == 0) {
 #pragma unroll
-        for (int c = 0; c < kBlock; c += 32) {
-          float v[32];
-          tc_ld32(src + (uint32_t)c, v);
-          if (c == kBlock - 32) {  // read: the accumulator may be written again
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(tempty_bar(acc));
-          }
-#pragma unroll
-          for (int j = 0; j < 32; j += 2) sum[(c + j) / 2] = fma_f2(make_f2(v[j], v[j + 1]), s2, sum[(c + j) / 2]);
+          for (int j = 0; j < 4; ++j) s4[j] = sx[j] * sw[j];
+          load_scales(kb + 4);
         }
+        const f2 s2 = make_f2(s4[0], s4[0]);
+        s4[0] = s4[1], s4[1] = s4[2], s4[2] = s4[3];
+        const uint32_t src = mine + (uint32_t)(acc * kBN), last = tempty_bar(acc);
         acc ^= 1;
         if (acc == 0) acc_phase ^= 1u;
+        bool ready = false;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          tc_ld32_wait(v[c & 1]);
+          if (c < 3) {
+            tc_ld32_start(src + (uint32_t)(32 * (c + 1)), v[(c & 1) ^ 1]);
+            if (c == 2) ready = mbar_test(tfull_bar(acc), acc_phase);
+          } else {  // read: the accumulator may be written again
+            tc_fence_before();
+            if (lane == 0) mbar_arrive(last);
+            if (kb + 1 < p.k_blocks) {
+              if (!ready) ok = mbar_wait(tfull_bar(acc), acc_phase, abort_flag);
+              __syncwarp();
+              if (!ok) break;
+              tc_fence_after();
+              tc_ld32_start(mine + (uint32_t)(acc * kBN), v[0]);
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 32; j += 2)
+            fma_f2_here(sum[c * 16 + j / 2], make_f2(__uint_as_float(v[c & 1][j]), __uint_as_float(v[c & 1][j + 1])), s2);
+        }
+        if (!ok) break;
       }
       if (!ok) break;
       // out through shared memory, 64 bytes of 32 rows at a time
@@ -225,9 +266,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                 if (r < rows) *reinterpret_cast<uint4*>(out + r * p.ld_out + c + (lane & 3) * (16 / sizeof(T))) = u;
               }
             } else {
-              const T* mine = reinterpret_cast<const T*>(after + 256 + (warp - 2) * kOutWarp);
+              const T* staged = reinterpret_cast<const T*>(after + 256 + (warp - 4) * kOutWarp);
               for (int r = 0; r < rows; ++r)
-                if (lane < kCols && c + lane < cols) out[r * p.ld_out + c + lane] = mine[r * (kOutRow / sizeof(T)) + lane];
+                if (lane < kCols && c + lane < cols) out[r * p.ld_out + c + lane] = staged[r * (kOutRow / sizeof(T)) + lane];
             }
             __syncwarp();
           }
@@ -335,6 +376,7 @@ extern "C" int mrl_e4m3_product(const void* x8, int64_t ld_x, const float* x_sca
   a.n_tiles = (V + kBN - 1) / kBN;
   a.group_m = 4096 / kBM;  // rows of x that stay in L2 while the weights pass by
   a.vector_out = on_element(out, 16) && (N == 1 || ld_out * es % 16 == 0);
+  a.vector_scales = a.k_blocks % 4 == 0 && on_element(x_scales, 16) && on_element(w_scales, 16);
   a.status = status;
   if ((long long)a.m_tiles * a.n_tiles > 0x7fffffffll) return MRL_ERR_UNSUPPORTED_SHAPE;
   return out_dtype == MRL_BF16 ? launch_product<__nv_bfloat16>(mx, mw, a, st) : launch_product<float>(mx, mw, a, st);
