@@ -650,7 +650,7 @@ int mrl_e4m3_product(const void* x8, int64_t ld_x, const float* x_scales, const 
  * float32 sums; bitwise reproducible for calls of the same N, V, dtype and alignment (few rows are cut among several CTAs: the
  * last bits of lse can differ from those of a larger call; ids never do).  Cost follows the bytes except on rows with
  * more than 2,048 candidates for the list -- rising ones, or long runs of one value at the top -- which are read several times.
- * One output at least has to be given.  N = 0 is a no-op.  MRL_ERR_INVALID_ARG as in mrl_token_logprobs, and for a temperature or top
+ * One output at least has to be given.  N = 0 is a no-op.  V > 2^30 -> MRL_ERR_UNSUPPORTED_SHAPE.  MRL_ERR_INVALID_ARG as in mrl_token_logprobs, and for a temperature or top
  * outside its range, an address that is not a multiple of its element, one address for two outputs.
  */
 int mrl_top_logprobs(const void* logits, int32_t dtype, int64_t N, int32_t V, int64_t ld, const int32_t* ids,

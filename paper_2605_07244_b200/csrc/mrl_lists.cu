@@ -11,8 +11,9 @@ namespace {
 
 using namespace mrl;
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 512, kWarps = kThreads / 32;  // of the row kernels: two CTAs an SM
 constexpr int kTop = MRL_MAX_TOP;
+constexpr int kMaxParts = 8;                            // CTAs that share a row
 
 template <typename T>
 __device__ __forceinline__ float load_f(const T* p);
@@ -22,6 +23,102 @@ template <>
 __device__ __forceinline__ float load_f<__nv_bfloat16>(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ void store_f(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_f(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// 32 bytes of a row: eight floats, or sixteen bf16
+constexpr int kVecBytes = 32;
+template <typename T>
+constexpr int kVecElems = kVecBytes / (int)sizeof(T);
+struct Vec {
+  uint32_t w[8];
+};
+__device__ __forceinline__ Vec load_vec(const void* p) {
+  Vec v;
+  asm volatile("ld.global.L1::no_allocate.L2::evict_first.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]), "=r"(v.w[4]), "=r"(v.w[5]), "=r"(v.w[6]), "=r"(v.w[7])
+               : "l"(p));
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ Vec no_vec() {  // -inf throughout
+  Vec v;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v.w[j] = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+  return v;
+}
+// The two floats of word j, or (float32) of words j and j + 1
+template <typename T>
+__device__ __forceinline__ f2 pair_of(const Vec& v, int j) {
+  return sizeof(T) == 2 ? bf16x2_to_f2(v.w[j]) : make_f2(__uint_as_float(v.w[j]), __uint_as_float(v.w[j + 1]));
+}
+template <typename T>
+constexpr int kPairStep = sizeof(T) == 2 ? 1 : 2;
+template <typename T>
+__device__ __forceinline__ float vec_max(const Vec& v) {  // passes over NaN
+  if constexpr (sizeof(T) == 2) {
+    uint32_t m = v.w[0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v.w[j]));
+    return fmaxf(bf16lo_to_f32(m), bf16hi_to_f32(m));
+  } else {
+    float m = __uint_as_float(v.w[0]);
+#pragma unroll
+    for (int j = 1; j < 8; ++j) m = fmaxf(m, __uint_as_float(v.w[j]));
+    return m;
+  }
+}
+
+// A CTA's part of a row: `head` elements up to the first address that is a multiple of 32 bytes, `vecs` vectors, `tail` elements.  So rows
+// of any address and stride are read with the same wide loads.
+template <typename T>
+struct Part {
+  const T* z;
+  int first, n, head, vecs, tail;  // `first`: index in the row of the part's first element
+  __device__ Part(const T* row, int V, int parts, int rank) {
+    const int step = ((V + parts - 1) / parts + 15) & ~15;  // (V <= 2^31 - 1 where parts = 1: no addition passes it)
+    first = parts == 1 ? 0 : min(V, rank * step);
+    n = parts == 1 ? V : min(V - first, step);
+    z = row + first;
+    head = min(n, (int)((0u - (uint32_t)reinterpret_cast<uintptr_t>(z)) & (kVecBytes - 1)) / (int)sizeof(T));
+    vecs = (n - head) / kVecElems<T>;
+    tail = n - head - vecs * kVecElems<T>;
+  }
+  __device__ __forceinline__ const char* body() const { return reinterpret_cast<const char*>(z + head); }
+};
+
+// How many CTAs share a row: as many as keep two CTAs an SM busy, with 16 KB of it at least.
+int parts_of(long long N, long long row_bytes) {
+  int parts = 1;
+  while (parts < kMaxParts && N * parts * 2 <= 2 * 148 && row_bytes / (parts * 2) >= 16 * 1024) parts *= 2;
+  return parts;
+}
+
+template <typename... Params>
+int launch_rows(void (*kernel)(Params...), long long N, int parts, size_t smem, bool behind, cudaStream_t st, Params... args) {
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)parts;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(N * parts));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = behind ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? MRL_OK : MRL_ERR_CUDA;
+}
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+// `p` of this CTA's shared memory, in CTA `rank` of the cluster
+template <typename U>
+__device__ __forceinline__ U* in_cta(U* p, int rank) {
+  U* q;
+  asm("mapa.u64 %0, %1, %2;" : "=l"(q) : "l"(p), "r"(rank));
+  return q;
+}
 
 struct Sums {
   float zm, s, u;  // u = sum_v 2^(t_v) t_v, t_v = (z_v - zm) c
@@ -39,6 +136,25 @@ __device__ __forceinline__ Sums sums_merge(Sums a, Sums b, float c) {
   a = sums_raise(a, zm, c);
   b = sums_raise(b, zm, c);
   return Sums{zm, a.s + b.s, a.u + b.u};
+}
+// adds kU vectors whose largest element is `high`
+template <typename T, bool kEnt, int kU>
+__device__ __forceinline__ void sums_add(Sums& a, const Vec (&v)[kU], float high, float c) {
+  if (high > a.zm) a = sums_raise(a, high, c);
+  const f2 c2 = make_f2(c, c), low = make_f2(-a.zm, -a.zm);
+  f2 s = 0, u = 0;
+#pragma unroll
+  for (int i = 0; i < kU; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; j += kPairStep<T>) {
+      const float2 t = split_f2(mul_f2(add_f2(pair_of<T>(v[i], j), low), c2));
+      const f2 e = make_f2(ex2_approx(t.x), ex2_approx(t.y));
+      s = add_f2(s, e);
+      if (kEnt) u = fma_f2(e, make_f2(fmaxf(t.x, -1000.f), fmaxf(t.y, -1000.f)), u);  // (2^-1000 = 0, and no 0 * inf)
+    }
+  const float2 sum = split_f2(s), more = split_f2(u);
+  a.s += sum.x + sum.y;
+  if (kEnt) a.u += more.x + more.y;
 }
 __device__ __forceinline__ void sums_add(Sums& a, float z, float c) {
   if (z > a.zm) a = sums_raise(a, z, c);
@@ -84,115 +200,261 @@ struct TopArgs {
   int32_t *top_ids, *status;
 };
 
+// ------------------------------------------------------------------------------------------ top tokens
+// A token's key: its logit's ordinal above its reversed index, so that larger keys come first in a list, and no two are alike.
+typedef unsigned long long Key;
+__device__ __forceinline__ Key key_of(float z, int index) { return ((Key)ordinal(z) << 32) | (uint32_t)(0x7fffffff - index); }
+
+constexpr int kUnroll = 4;       // vectors of a thread and group
+constexpr int kCap = 2048;       // candidates of a CTA
+constexpr int kFew = 256;        // keys that are put in order by counting
+struct TopShared {
+  Key cand[kCap];                // candidates of this CTA
+  Key pool[kCap];                // (CTA 0) what is left of those of all CTAs of the row: kMaxParts * kFew at most
+  Sums part[kMaxParts], red[kWarps];
+  uint32_t hist[256], pick[4], n_cand, n_pool;
+};
+
 // The largest digit d (of 256) such that at least `want` counts lie at or above it; `want` becomes what is wanted of d itself.
-// Called by all threads; counts in shared memory.
-__device__ __forceinline__ int pick_digit(const uint32_t* hist, uint32_t& want, uint32_t* out) {
+__device__ __forceinline__ int pick_digit(TopShared& sh, uint32_t& want) {
   __syncthreads();
   if (threadIdx.x == 0) {
     uint32_t above = 0;
     int d = 255;
-    for (; d > 0 && above + hist[d] < want; --d) above += hist[d];
-    out[0] = (uint32_t)d;
-    out[1] = want - above;
+    for (; d > 0 && above + sh.hist[d] < want; --d) above += sh.hist[d];
+    sh.pick[0] = (uint32_t)d;
+    sh.pick[1] = want - above;
   }
   __syncthreads();
-  want = out[1];
-  return (int)out[0];
+  want = sh.pick[1];
+  return (int)sh.pick[0];
+}
+__device__ __forceinline__ void count_digit(uint32_t* hist, bool on, uint32_t digit) {
+  const unsigned who = __ballot_sync(0xffffffffu, on);
+  if (who == 0) return;
+  int same;
+  const uint32_t d = __shfl_sync(0xffffffffu, digit, __ffs(who) - 1);
+  same = __all_sync(0xffffffffu, !on || digit == d);  // (long runs of one value: one addition a warp)
+  if (same) {
+    if ((threadIdx.x & 31) == __ffs(who) - 1) atomicAdd(&hist[d], (uint32_t)__popc(who));
+  } else if (on) {
+    atomicAdd(&hist[digit], 1u);
+  }
 }
 
-// The `top` likeliest tokens of a row by 256-way counting: four passes find the value of the last of them, up to four more the index up
-// to which tokens of that value are listed, one collects.  Right for every row; the row is read nine times.  Returns their number.
+// The `top` largest keys of a part by 256-way counting: four passes find the value of the last of them, four more the index up to which
+// tokens of that value are listed, one collects.  Right for every row, and reads it nine times: taken where the candidates do not fit, or too
+// few logits are above -inf.  Returns their number.
 template <typename T>
-__device__ int select_top(const T* z, int V, int top, uint32_t* hist, uint32_t* pick, unsigned long long* keys) {
-  uint32_t value = 0, want = (uint32_t)top;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = threadIdx.x; i < 256; i += blockDim.x) hist[i] = 0;
+__device__ __noinline__ int select_top(const Part<T> part, int top, TopShared& sh) {
+  const int rounds = (part.n + kThreads - 1) / kThreads;
+  Key last = 0;
+  uint32_t want = (uint32_t)top;
+  int listed = top;
+#pragma unroll 1
+  for (int shift = 56; shift >= 0; shift -= 8) {
+    for (int i = threadIdx.x; i < 256; i += kThreads) sh.hist[i] = 0;
     __syncthreads();
-    for (int v = threadIdx.x; v < V; v += blockDim.x) {
-      const uint32_t o = ordinal(load_f<T>(z + v));
-      if (o != 0 && (shift == 24 || (o >> (shift + 8)) == (value >> (shift + 8)))) atomicAdd(&hist[(o >> shift) & 255u], 1u);
+#pragma unroll 4
+    for (int r = 0; r < rounds; ++r) {
+      const int i = r * kThreads + threadIdx.x;
+      const Key key = i < part.n ? key_of(load_f<T>(part.z + i), part.first + i) : 0;
+      count_digit(sh.hist, (key >> 32) != 0 && (shift == 56 || (key >> (shift + 8)) == (last >> (shift + 8))), (uint32_t)(key >> shift) & 255u);
     }
-    if (shift == 24) {  // (fewer numbers than places: all of them)
+    if (shift == 56) {  // (fewer numbers than places: all of them)
       __syncthreads();
-      if (threadIdx.x == 0) {
+      if (threadIdx.x < 32) {
         uint32_t n = 0;
-        for (int i = 0; i < 256; ++i) n += hist[i];
-        pick[2] = n;
+        for (int i = threadIdx.x; i < 256; i += 32) n += sh.hist[i];
+        n = __reduce_add_sync(0xffffffffu, n);
+        if (threadIdx.x == 0) sh.pick[2] = n;
       }
       __syncthreads();
-      want = min(want, pick[2]);
-      if (want == 0) return 0;
+      want = min(want, sh.pick[2]);
+      listed = (int)want;
+      if (listed == 0) return 0;
     }
-    value |= (uint32_t)pick_digit(hist, want, pick) << shift;
+    last |= (Key)pick_digit(sh, want) << shift;
   }
-  const int listed = (int)min((uint32_t)top, pick[2]);
-  // of the tokens of this value the first `want`: the largest bound that keeps that many of the reversed indices
-  uint32_t rev = 0;  // 2^31 - 1 - index
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = threadIdx.x; i < 256; i += blockDim.x) hist[i] = 0;
-    __syncthreads();
-    for (int v = threadIdx.x; v < V; v += blockDim.x) {
-      const uint32_t r = 0x7fffffffu - (uint32_t)v;
-      if (ordinal(load_f<T>(z + v)) == value && (shift == 24 || (r >> (shift + 8)) == (rev >> (shift + 8))))
-        atomicAdd(&hist[(r >> shift) & 255u], 1u);
-    }
-    rev |= (uint32_t)pick_digit(hist, want, pick) << shift;
-  }
-  const unsigned long long last = ((unsigned long long)value << 32) | rev;
-  if (threadIdx.x == 0) pick[3] = 0;
+  if (threadIdx.x == 0) sh.n_cand = 0;
   __syncthreads();
-  for (int v = threadIdx.x; v < V; v += blockDim.x) {
-    const unsigned long long key = ((unsigned long long)ordinal(load_f<T>(z + v)) << 32) | (0x7fffffffu - (uint32_t)v);
-    if (key >= last) keys[min(atomicAdd(&pick[3], 1u), (uint32_t)(kTop - 1))] = key;
+  for (int i = threadIdx.x; i < part.n; i += kThreads) {
+    const Key key = key_of(load_f<T>(part.z + i), part.first + i);
+    if (key >= last) sh.cand[min(atomicAdd(&sh.n_cand, 1u), (uint32_t)(kCap - 1))] = key;
   }
   __syncthreads();
   return listed;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) top_kernel(const TopArgs p) {
-  __shared__ Sums red[kWarps];
-  __shared__ uint32_t hist[256], pick[4];
-  __shared__ unsigned long long keys[kTop];
-  const long long row = blockIdx.x;
-  const T* z = static_cast<const T*>(p.logits) + row * p.ld;
+// Copies the keys that can be among the `top` largest of `from` to `to` (of CTA `rank`, behind what its counter says is there): at most kFew,
+// and all of the `top` largest among them.  Bits are settled from above until few enough are left.
+__device__ void keep_largest(const Key* from, int n, int top, Key* to, uint32_t* n_to) {
+  Key mine[kCap / kThreads];
+#pragma unroll
+  for (int i = 0; i < kCap / kThreads; ++i) mine[i] = i * kThreads + threadIdx.x < n ? from[i * kThreads + threadIdx.x] : 0;
+  const int few = min(kFew, 2 * top + 32);
+  Key least = 1;
+  if (n > few) {
+    least = 0;
+    for (int bit = 63; bit >= 0; --bit) {
+      const Key next = least | ((Key)1 << bit);
+      int total = __syncthreads_count(mine[0] >= next);
+      if (n > kThreads) {
+#pragma unroll
+        for (int i = 1; i < kCap / kThreads; ++i) total += __syncthreads_count(mine[i] >= next);
+      }
+      if (total >= top) least = next;
+      if (total >= top && total <= few) break;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kCap / kThreads; ++i)
+    if (mine[i] >= least) to[atomicAdd(n_to, 1u)] = mine[i];
+}
+
+template <typename T, bool kEnt>
+__global__ void __launch_bounds__(kThreads, 2) top_kernel(const TopArgs p) {
+  __shared__ TopShared sh;
+  const int tid = threadIdx.x;
+  int parts, rank;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const long long row = blockIdx.x / (unsigned)parts;
+  const T* zrow = static_cast<const T*>(p.logits) + row * p.ld;
   const int id = p.ids != nullptr ? p.ids[row] : 0;
   const bool on = p.mask == nullptr || p.mask[row] != 0, good = id >= 0 && id < p.V;
-  if (!on || !good) {
-    if (threadIdx.x == 0) {
+  if (!on || !good) {  // (all CTAs of the row)
+    if (rank != 0) return;
+    if (tid == 0) {
       if (on && p.status != nullptr) atomicOr(p.status, MRL_DEV_BAD_TOKEN_ID);
       if (p.logp != nullptr) p.logp[row] = 0.f;
       if (p.lse != nullptr) p.lse[row] = 0.f;
-      if (p.entropy != nullptr) p.entropy[row] = 0.f;
+      if (kEnt) p.entropy[row] = 0.f;
     }
-    for (int k = threadIdx.x; k < p.top; k += kThreads) {
-      p.top_ids[row * p.top + k] = -1;
-      p.top_logp[row * p.top + k] = 0.f;
+    if (tid < p.top) {
+      p.top_ids[row * p.top + tid] = -1;
+      p.top_logp[row * p.top + tid] = 0.f;
     }
     return;
   }
+  if (tid == 0) sh.n_cand = sh.n_pool = 0;
+  __syncthreads();
+  if (parts > 1) cluster_arrive();  // "my counters are set"
+  const Part<T> part(zrow, p.V, parts, rank);
+  const char* body = part.body() + (size_t)tid * kVecBytes;
+  const float z_head = tid < part.head ? load_f<T>(part.z + tid) : -INFINITY;
+  const float z_tail = tid < part.tail ? load_f<T>(part.z + part.n - part.tail + tid) : -INFINITY;
   Sums a = sums_empty();
-  for (int v = threadIdx.x; v < p.V; v += kThreads) sums_add(a, load_f<T>(z + v), p.c);
-  a = block_sums(a, p.c, red);
-  const float ln_s = a.s == 0.f ? NAN : logf(a.s);
-  if (threadIdx.x == 0) {
-    if (p.lse != nullptr) p.lse[row] = a.zm / p.temperature + ln_s;
-    if (p.logp != nullptr) p.logp[row] = (load_f<T>(z + id) - a.zm) / p.temperature - ln_s;
-    if (p.entropy != nullptr) p.entropy[row] = ln_s - a.u / a.s * MRL_NAT_HI;
-  }
-  if (p.top == 0) return;
-  const int n = select_top<T>(z, p.V, p.top, hist, pick, keys);
-  for (int k = threadIdx.x; k < p.top; k += kThreads) {
-    if (k < n) {  // its place is the number of larger keys
-      const unsigned long long key = keys[k];
-      int at = 0;
-      for (int j = 0; j < n; ++j) at += keys[j] > key;
-      p.top_ids[row * p.top + at] = (int32_t)(0x7fffffffu - (uint32_t)key);
-      p.top_logp[row * p.top + at] = (from_ordinal((uint32_t)(key >> 32)) - a.zm) / p.temperature - ln_s;
-    } else {
-      p.top_ids[row * p.top + k] = -1;
-      p.top_logp[row * p.top + k] = -INFINITY;
+  if (tid < part.head) sums_add(a, z_head, p.c);
+  if (tid < part.tail) sums_add(a, z_tail, p.c);
+  auto push = [&](float z, int index) {
+    const uint32_t at = atomicAdd(&sh.n_cand, 1u);
+    if (at < kCap) sh.cand[at] = key_of(z, part.first + index);
+  };
+  // Candidates are what is above `floor`.  In the first group it is set so that `top` threads at least have an element there (each at least one, so
+  // the list's last token is not below it); logits that equal it come in from this group alone, for later ones stand behind `top` others.
+  float floor = -INFINITY;
+  const int groups = max(1, (part.vecs + kThreads * kUnroll - 1) / (kThreads * kUnroll));
+#pragma unroll 1
+  for (int g = 0; g < groups; ++g) {
+    const int v0 = g * kThreads * kUnroll;
+    Vec v[kUnroll];
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i)
+      v[i] = v0 + i * kThreads + tid < part.vecs ? load_vec(body + (size_t)(v0 + i * kThreads) * kVecBytes) : no_vec<T>();
+    float high[kUnroll];
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i) high[i] = vec_max<T>(v[i]);
+    float most = high[0];
+#pragma unroll
+    for (int i = 1; i < kUnroll; ++i) most = fmaxf(most, high[i]);
+    if (v0 + tid < part.vecs) sums_add<T, kEnt>(a, v, most, p.c);
+    if (p.top == 0) continue;
+    float above = floor;
+    if (g == 0) {
+      const uint32_t mine = ordinal(fmaxf(most, z_head));
+      uint32_t least = 0;
+      for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t next = least | (1u << bit);
+        const int n = __syncthreads_count(mine >= next);
+        if (n >= p.top) least = next;
+        if (n >= p.top && n <= p.top + p.top / 4 + 4) break;
+      }
+      constexpr uint32_t kOrdinalMinusInf = 0x007fffffu, kOrdinalZero = 0x80000000u;
+      if (least > kOrdinalMinusInf) {
+        floor = from_ordinal(least);
+        above = from_ordinal(least == kOrdinalZero ? least - 2 : least - 1);  // (between -0 and +0 lies nothing)
+      }
+      if (z_head > above) push(z_head, tid);
     }
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i)
+      if (high[i] > above) {
+        const int index = part.head + (v0 + i * kThreads + tid) * kVecElems<T>;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if constexpr (sizeof(T) == 2) {
+            const float lo = bf16lo_to_f32(v[i].w[j]), hi = bf16hi_to_f32(v[i].w[j]);
+            if (lo > above) push(lo, index + 2 * j);
+            if (hi > above) push(hi, index + 2 * j + 1);
+          } else {
+            const float z = __uint_as_float(v[i].w[j]);
+            if (z > above) push(z, index + j);
+          }
+        }
+      }
+  }
+  if (p.top > 0 && z_tail > floor) push(z_tail, part.n - part.tail + tid);
+  a = block_sums(a, p.c, sh.red);  // (a barrier: the candidates are there)
+  int n = 0;
+  if (p.top > 0) {
+    n = (int)sh.n_cand;
+    const int places = min(p.top, part.n);
+    if (n > kCap || n < places) n = select_top<T>(part, places, sh);
+  }
+  if (parts > 1) {
+    cluster_wait();
+    if (tid == 0) *in_cta(&sh.part[rank], 0) = a;
+    if (n > 0) keep_largest(sh.cand, n, p.top, in_cta(sh.pool, 0), in_cta(&sh.n_pool, 0));
+    cluster_arrive();
+    cluster_wait();
+    if (rank != 0) return;
+    a = sh.part[0];
+    for (int k = 1; k < parts; ++k) a = sums_merge(a, sh.part[k], p.c);
+    n = (int)sh.n_pool;
+    if (tid == 0) sh.n_cand = 0;
+    __syncthreads();
+    if (n > 0) keep_largest(sh.pool, n, p.top, sh.cand, &sh.n_cand);
+    __syncthreads();
+    n = (int)sh.n_cand;
+  } else if (n > 0) {
+    keep_largest(sh.cand, n, p.top, sh.pool, &sh.n_pool);
+    __syncthreads();
+    n = (int)sh.n_pool;
+  }
+  const Key* keys = parts > 1 ? sh.cand : sh.pool;
+  const float ln_s = a.s == 0.f ? NAN : logf(a.s);
+  if (tid == 0) {
+    if (p.lse != nullptr) p.lse[row] = a.zm / p.temperature + ln_s;
+    if (p.logp != nullptr) p.logp[row] = (load_f<T>(zrow + id) - a.zm) / p.temperature - ln_s;
+    if (kEnt) p.entropy[row] = ln_s - a.u / a.s * MRL_NAT_HI;
+  }
+  // in order: a key's place is the number of larger ones, counted by four threads a key
+  for (int k0 = 0; k0 < n; k0 += kThreads / 4) {
+    const int k = k0 + (tid >> 2);
+    const Key key = k < n ? keys[k] : 0;
+    int at = 0;
+    for (int j = tid & 3; j < n; j += 4) at += keys[j] > key;
+    at += __shfl_xor_sync(0xffffffffu, at, 1);
+    at += __shfl_xor_sync(0xffffffffu, at, 2);
+    if (k < n && at < p.top && (tid & 3) == 0) {
+      p.top_ids[row * p.top + at] = 0x7fffffff - (int32_t)(uint32_t)key;
+      p.top_logp[row * p.top + at] = (from_ordinal((uint32_t)(key >> 32)) - a.zm) / p.temperature - ln_s;
+    }
+  }
+  for (int k = n + tid; k < p.top; k += kThreads) {
+    p.top_ids[row * p.top + k] = -1;
+    p.top_logp[row * p.top + k] = -INFINITY;
   }
 }
 
@@ -469,7 +731,7 @@ extern "C" int mrl_top_logprobs(const void* logits, int32_t dtype, int64_t N, in
                                 int32_t* top_ids, float* top_logp, int32_t* status, void* stream) {
   if (!row_type_ok(dtype)) return MRL_ERR_UNSUPPORTED_DTYPE;
   if (N < 0 || V < 1 || ld < V || !temperature_ok(temperature) || top < 0 || top > V) return MRL_ERR_INVALID_ARG;
-  if (top > kTop || N > 0x7fffffffll) return MRL_ERR_UNSUPPORTED_SHAPE;
+  if (top > kTop || N > 0x7fffffffll || V > (1 << 30)) return MRL_ERR_UNSUPPORTED_SHAPE;
   if (N == 0) return MRL_OK;
   if (top > 0 && (top_ids == nullptr || top_logp == nullptr)) return MRL_ERR_INVALID_ARG;
   if (top == 0) top_ids = nullptr, top_logp = nullptr;
@@ -485,13 +747,13 @@ extern "C" int mrl_top_logprobs(const void* logits, int32_t dtype, int64_t N, in
   if (!on_element(logits, dtype == MRL_BF16 ? 2 : 4) || !on_element(ids, 4) || !on_element(status, 4)) return MRL_ERR_INVALID_ARG;
   const TopArgs a{logits, ld, V, ids, mask, temperature, scale_of(temperature), top, logp, lse, entropy, top_logp, top_ids, status};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool bf16 = dtype == MRL_BF16, ent = entropy != nullptr;
+  const int parts = parts_of(N, (long long)V * (bf16 ? 2 : 4));
   mrl_profile_before(st, "top_kernel");
-  if (dtype == MRL_BF16)
-    top_kernel<__nv_bfloat16><<<(unsigned)N, kThreads, 0, st>>>(a);
-  else
-    top_kernel<float><<<(unsigned)N, kThreads, 0, st>>>(a);
+  const int rc = launch_rows(bf16 ? (ent ? top_kernel<__nv_bfloat16, true> : top_kernel<__nv_bfloat16, false>)
+                                  : (ent ? top_kernel<float, true> : top_kernel<float, false>), N, parts, 0, false, st, a);
   mrl_profile_after(st);
-  return cudaGetLastError() == cudaSuccess ? MRL_OK : MRL_ERR_CUDA;
+  return rc;
 }
 
 extern "C" int mrl_distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64_t N, int32_t V, int64_t ld, const int32_t* top_ids,
