@@ -1,8 +1,8 @@
 // Top tokens and learning from them: mrl_top_logprobs and mrl_distill_loss_fwd_bwd.
 //
-// Both read rows of logits against a running (zm, s): zm the largest logit, s = sum_v 2^((z_v - zm) c) with c = log2(e) / T.  The
-// difference is taken before the product, so that rows of the type's lowest value keep their softmax; zm starts at the lowest
-// float, not at -inf, so that -inf - zm stays -inf and a NaN always reaches the sum.  s = 0: nothing but -inf.
+// Both read rows of logits against a running (m, s): m the largest of z c, c = log2(e) / T, and s = sum_v 2^(z_v c - m).  m starts at the
+// lowest float, not at -inf, so that -inf - m stays -inf and a NaN always reaches the sum.  s = 0: nothing but -inf, or logits so low that z c
+// leaves float32 (rows masked throughout with the type's lowest value): those are summed again against their largest logit itself.
 #include <float.h>
 
 #include "mrl_common.cuh"
@@ -45,13 +45,6 @@ __device__ __forceinline__ Vec no_vec() {  // -inf throughout
   for (int j = 0; j < 8; ++j) v.w[j] = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
   return v;
 }
-// The two floats of word j, or (float32) of words j and j + 1
-template <typename T>
-__device__ __forceinline__ f2 pair_of(const Vec& v, int j) {
-  return sizeof(T) == 2 ? bf16x2_to_f2(v.w[j]) : make_f2(__uint_as_float(v.w[j]), __uint_as_float(v.w[j + 1]));
-}
-template <typename T>
-constexpr int kPairStep = sizeof(T) == 2 ? 1 : 2;
 template <typename T>
 __device__ __forceinline__ float vec_max(const Vec& v) {  // passes over NaN
   if constexpr (sizeof(T) == 2) {
@@ -121,63 +114,97 @@ __device__ __forceinline__ U* in_cta(U* p, int rank) {
 }
 
 struct Sums {
-  float zm, s, u;  // u = sum_v 2^(t_v) t_v, t_v = (z_v - zm) c
+  float m, s, u;  // u = sum_v 2^(t_v) t_v, t_v = z_v c - m
 };
 __device__ __forceinline__ Sums sums_empty() { return Sums{-FLT_MAX, 0.f, 0.f}; }
-// s and u over a higher maximum: u' = sum 2^(t + d) (t + d) with d = (zm - zm') c
-__device__ __forceinline__ Sums sums_raise(Sums a, float zm, float c) {
-  if (zm == a.zm) return a;
-  const float d = fmaxf((a.zm - zm) * c, -1000.f);  // 2^-1000 = 0, and no 0 * inf
-  const float f = ex2_approx((a.zm - zm) * c);      // (NaN for two infinities)
-  return Sums{zm, a.s * f, fmaf(a.s, d, a.u) * f};
+// s and u over a higher maximum: u' = sum 2^(t + d) (t + d) with d = m - m'
+__device__ __forceinline__ Sums sums_raise(Sums a, float m) {
+  const float d = a.m - m, f = ex2_approx(d);                       // (NaN for two infinities)
+  return Sums{m, a.s * f, fmaf(a.s, fmaxf(d, -1000.f), a.u) * f};  // 2^-1000 = 0, and no 0 * inf
 }
-__device__ __forceinline__ Sums sums_merge(Sums a, Sums b, float c) {
-  const float zm = fmaxf(a.zm, b.zm);
-  a = sums_raise(a, zm, c);
-  b = sums_raise(b, zm, c);
-  return Sums{zm, a.s + b.s, a.u + b.u};
+__device__ __forceinline__ Sums sums_merge(Sums a, Sums b) {
+  const float m = fmaxf(a.m, b.m);
+  a = sums_raise(a, m);
+  b = sums_raise(b, m);
+  return Sums{m, a.s + b.s, a.u + b.u};
 }
-// adds kU vectors whose largest element is `high`
-template <typename T, bool kEnt, int kU>
-__device__ __forceinline__ void sums_add(Sums& a, const Vec (&v)[kU], float high, float c) {
-  if (high > a.zm) a = sums_raise(a, high, c);
-  const f2 c2 = make_f2(c, c), low = make_f2(-a.zm, -a.zm);
-  f2 s = 0, u = 0;
+template <bool kEnt>
+__device__ __forceinline__ void sums_term(float z, float c, float m, float& s, float& u) {
+  const float t = fmaf(z, c, -m), e = ex2_approx(t);
+  s += e;
+  if (kEnt) u = fmaf(e, fmaxf(t, -1000.f), u);
+}
+// adds the elements of a vector, none of which is above a.m
+template <typename T, bool kEnt>
+__device__ __forceinline__ void sums_add(Sums& a, const Vec& v, float c) {
+  float s0 = 0.f, s1 = 0.f, u0 = 0.f, u1 = 0.f;
 #pragma unroll
-  for (int i = 0; i < kU; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; j += kPairStep<T>) {
-      const float2 t = split_f2(mul_f2(add_f2(pair_of<T>(v[i], j), low), c2));
-      const f2 e = make_f2(ex2_approx(t.x), ex2_approx(t.y));
-      s = add_f2(s, e);
-      if (kEnt) u = fma_f2(e, make_f2(fmaxf(t.x, -1000.f), fmaxf(t.y, -1000.f)), u);  // (2^-1000 = 0, and no 0 * inf)
+  for (int j = 0; j < 8; ++j) {
+    if constexpr (sizeof(T) == 2) {
+      sums_term<kEnt>(bf16lo_to_f32(v.w[j]), c, a.m, s0, u0);
+      sums_term<kEnt>(bf16hi_to_f32(v.w[j]), c, a.m, s1, u1);
+    } else {
+      sums_term<kEnt>(__uint_as_float(v.w[j]), c, a.m, j & 1 ? s1 : s0, j & 1 ? u1 : u0);
     }
-  const float2 sum = split_f2(s), more = split_f2(u);
-  a.s += sum.x + sum.y;
-  if (kEnt) a.u += more.x + more.y;
+  }
+  a.s += s0 + s1;
+  a.u += u0 + u1;
 }
 __device__ __forceinline__ void sums_add(Sums& a, float z, float c) {
-  if (z > a.zm) a = sums_raise(a, z, c);
-  const float t = (z - a.zm) * c, e = ex2_approx(t);
-  a.s += e;
-  a.u = fmaf(e, fmaxf(t, -1000.f), a.u);
+  const float m = fmaxf(a.m, z * c);
+  if (m > a.m) a = sums_raise(a, m);
+  sums_term<true>(z, c, a.m, a.s, a.u);
 }
-// over the block, in a fixed order; every thread gets the result
-__device__ __forceinline__ Sums block_sums(Sums a, float c, Sums* red) {
+// Over the block, in a fixed order; every thread gets the result.  The maximum first, so that each thread rescales once.
+__device__ __forceinline__ Sums block_sums(Sums a, Sums* red) {
+  float m = a.m;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (lane == 0) red[warp].m = m;
+  __syncthreads();
+  m = lane < kWarps ? red[lane].m : -FLT_MAX;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  a = sums_raise(a, m);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    Sums b;
-    b.zm = __shfl_xor_sync(0xffffffffu, a.zm, o);
-    b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
-    b.u = __shfl_xor_sync(0xffffffffu, a.u, o);
-    a = (threadIdx.x & o) ? sums_merge(b, a, c) : sums_merge(a, b, c);
+    a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+    a.u += __shfl_xor_sync(0xffffffffu, a.u, o);
   }
+  if (lane == 0) red[warp].s = a.s, red[warp].u = a.u;
   __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = a;
-  __syncthreads();
-  a = red[0];
-  for (int k = 1; k < (int)(blockDim.x >> 5); ++k) a = sums_merge(a, red[k], c);
+  a.s = lane < kWarps ? red[lane].s : 0.f;
+  a.u = lane < kWarps ? red[lane].u : 0.f;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+    a.u += __shfl_xor_sync(0xffffffffu, a.u, o);
+  }
   return a;
+}
+
+// A row's sums against their offset x0 = m, in float64: x = z c, ln p = (x - x0) nat - ln s, nat = 1 / (c T).
+struct Totals {
+  double x0;
+  float s, u;
+};
+// The sums of a row whose s above is 0, against its largest logit: 2^((z - zm) c).  `keep` says which elements count.  Called by the block;
+// slow, and hardly ever needed.
+template <typename T, typename Keep>
+__device__ __noinline__ Totals low_sums(const T* z, int V, float c, Sums* red, Keep keep) {
+  float zm = -FLT_MAX;
+  for (int v = threadIdx.x; v < V; v += kThreads)
+    if (keep(v)) zm = fmaxf(zm, load_f<T>(z + v));
+  Sums a{zm, 0.f, 0.f};
+  __syncthreads();
+  zm = block_sums(a, red).m;
+  a = Sums{0.f, 0.f, 0.f};
+  for (int v = threadIdx.x; v < V; v += kThreads)
+    if (keep(v)) sums_term<true>(load_f<T>(z + v) - zm, c, 0.f, a.s, a.u);
+  __syncthreads();
+  a = block_sums(a, red);
+  return Totals{(double)zm * (double)c, a.s, a.u};
 }
 
 // Whole numbers in the order of floats; 0: NaN.  -0 and +0 are one value.
@@ -212,7 +239,8 @@ struct TopShared {
   Key cand[kCap];                // candidates of this CTA
   Key pool[kCap];                // (CTA 0) what is left of those of all CTAs of the row: kMaxParts * kFew at most
   Sums part[kMaxParts], red[kWarps];
-  uint32_t hist[256], pick[4], n_cand, n_pool;
+  int vec[kCap];                 // vectors noted
+  uint32_t hist[256], pick[4], pick2[2 * kWarps], n_vec, n_cand, n_pool;
 };
 
 // The largest digit d (of 256) such that at least `want` counts lie at or above it; `want` becomes what is wanted of d itself.
@@ -292,9 +320,8 @@ __device__ void keep_largest(const Key* from, int n, int top, Key* to, uint32_t*
   Key mine[kCap / kThreads];
 #pragma unroll
   for (int i = 0; i < kCap / kThreads; ++i) mine[i] = i * kThreads + threadIdx.x < n ? from[i * kThreads + threadIdx.x] : 0;
-  const int few = min(kFew, 2 * top + 32);
   Key least = 1;
-  if (n > few) {
+  if (n > kFew) {
     least = 0;
     for (int bit = 63; bit >= 0; --bit) {
       const Key next = least | ((Key)1 << bit);
@@ -304,12 +331,69 @@ __device__ void keep_largest(const Key* from, int n, int top, Key* to, uint32_t*
         for (int i = 1; i < kCap / kThreads; ++i) total += __syncthreads_count(mine[i] >= next);
       }
       if (total >= top) least = next;
-      if (total >= top && total <= few) break;
+      if (total >= top && total <= kFew) break;
     }
   }
 #pragma unroll
   for (int i = 0; i < kCap / kThreads; ++i)
     if (mine[i] >= least) to[atomicAdd(n_to, 1u)] = mine[i];
+}
+
+constexpr uint32_t kLowest = 0x00800000u;  // the ordinal above that of -inf
+// An ordinal, kLowest at least, that `want` threads at least do not fall below with theirs, and hardly more of them.  Bits are settled from above, from
+// the first that the threads differ in.
+template <typename T>
+__device__ __forceinline__ uint32_t kth_ordinal(uint32_t mine, int want, uint32_t* red) {
+  uint32_t high = __reduce_max_sync(0xffffffffu, mine), low = __reduce_min_sync(0xffffffffu, mine);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (lane == 0) red[warp] = high, red[kWarps + warp] = low;
+  __syncthreads();
+  high = __reduce_max_sync(0xffffffffu, red[lane % kWarps]);
+  low = __reduce_min_sync(0xffffffffu, red[kWarps + lane % kWarps]);
+  if (high == low) {
+    __syncthreads();  // (`red` may be used again)
+    return max(low, kLowest);
+  }
+  const int first = 31 - __clz(high ^ low);
+  uint32_t found = high & ~(first == 31 ? ~0u : (2u << first) - 1);
+  for (int bit = first; bit >= (sizeof(T) == 2 ? 16 : 0); --bit) {
+    const uint32_t next = found | (1u << bit);
+    const int n = __syncthreads_count(mine >= next);
+    if (n >= want) found = next;
+    if (n >= want && n <= want + want / 8 + 2) break;
+  }
+  return max(found, kLowest);
+}
+// bits 0 .. 7 to the even places
+__device__ __forceinline__ uint32_t spread_bits(uint32_t b) {
+  b = (b | b << 4) & 0x0f0fu;
+  b = (b | b << 2) & 0x3333u;
+  return (b | b << 1) & 0x5555u;
+}
+// The least T whose ordinal is not below `o`.  (A bf16 has the ordinal of the float it is: sixteen zeros below, or ones if negative.)
+template <typename T>
+__device__ __forceinline__ float floor_of(uint32_t o) {
+  const float z = from_ordinal(o);
+  return sizeof(T) == 2 ? __uint_as_float(__float_as_uint(z) & 0xffff0000u) : z;
+}
+// Bit e: element e of the vector is not below `floor`, a T
+template <typename T>
+__device__ __forceinline__ uint32_t not_below(const Vec& v, float floor) {
+  uint32_t bits = 0;
+  if constexpr (sizeof(T) == 2) {
+    const uint32_t f = __float_as_uint(floor) >> 16 | (__float_as_uint(floor) & 0xffff0000u);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      uint32_t m;
+      asm("set.ge.u32.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(v.w[j]), "r"(f));
+      bits |= m & (0x10001u << j);
+    }
+    bits = spread_bits(bits & 0xffu) | spread_bits(bits >> 16) << 1;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) bits |= __uint_as_float(v.w[j]) >= floor ? 1u << j : 0u;
+  }
+  return bits;
 }
 
 template <typename T, bool kEnt>
@@ -337,7 +421,7 @@ __global__ void __launch_bounds__(kThreads, 2) top_kernel(const TopArgs p) {
     }
     return;
   }
-  if (tid == 0) sh.n_cand = sh.n_pool = 0;
+  if (tid == 0) sh.n_vec = sh.n_cand = sh.n_pool = 0;
   __syncthreads();
   if (parts > 1) cluster_arrive();  // "my counters are set"
   const Part<T> part(zrow, p.V, parts, rank);
@@ -347,70 +431,66 @@ __global__ void __launch_bounds__(kThreads, 2) top_kernel(const TopArgs p) {
   Sums a = sums_empty();
   if (tid < part.head) sums_add(a, z_head, p.c);
   if (tid < part.tail) sums_add(a, z_tail, p.c);
-  auto push = [&](float z, int index) {
-    const uint32_t at = atomicAdd(&sh.n_cand, 1u);
-    if (at < kCap) sh.cand[at] = key_of(z, part.first + index);
-  };
-  // Candidates are what is above `floor`.  In the first group it is set so that `top` threads at least have an element there (each at least one, so
-  // the list's last token is not below it); logits that equal it come in from this group alone, for later ones stand behind `top` others.
-  float floor = -INFINITY;
+  // Vectors that can hold a listed token are noted, by their place: those with an element that is not below a floor, which the first group sets
+  // so that `top` threads at least have an element there, each at least one.  The largest element of each thread sets the last floor behind the last
+  // group in the same way, a tight one, and what is not below it is read again from the vectors noted.
+  float best = z_head, floor = floor_of<T>(kLowest);
   const int groups = max(1, (part.vecs + kThreads * kUnroll - 1) / (kThreads * kUnroll));
 #pragma unroll 1
   for (int g = 0; g < groups; ++g) {
-    const int v0 = g * kThreads * kUnroll;
+    const int v0 = g * kThreads * kUnroll + tid;
     Vec v[kUnroll];
 #pragma unroll
-    for (int i = 0; i < kUnroll; ++i)
-      v[i] = v0 + i * kThreads + tid < part.vecs ? load_vec(body + (size_t)(v0 + i * kThreads) * kVecBytes) : no_vec<T>();
-    float high[kUnroll];
+    for (int i = 0; i < kUnroll; ++i) v[i] = v0 + i * kThreads < part.vecs ? load_vec(body + (size_t)(v0 - tid + i * kThreads) * kVecBytes) : no_vec<T>();
+    float high[kUnroll], most = best;
 #pragma unroll
-    for (int i = 0; i < kUnroll; ++i) high[i] = vec_max<T>(v[i]);
-    float most = high[0];
-#pragma unroll
-    for (int i = 1; i < kUnroll; ++i) most = fmaxf(most, high[i]);
-    if (v0 + tid < part.vecs) sums_add<T, kEnt>(a, v, most, p.c);
-    if (p.top == 0) continue;
-    float above = floor;
-    if (g == 0) {
-      const uint32_t mine = ordinal(fmaxf(most, z_head));
-      uint32_t least = 0;
-      for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t next = least | (1u << bit);
-        const int n = __syncthreads_count(mine >= next);
-        if (n >= p.top) least = next;
-        if (n >= p.top && n <= p.top + p.top / 4 + 4) break;
-      }
-      constexpr uint32_t kOrdinalMinusInf = 0x007fffffu, kOrdinalZero = 0x80000000u;
-      if (least > kOrdinalMinusInf) {
-        floor = from_ordinal(least);
-        above = from_ordinal(least == kOrdinalZero ? least - 2 : least - 1);  // (between -0 and +0 lies nothing)
-      }
-      if (z_head > above) push(z_head, tid);
+    for (int i = 0; i < kUnroll; ++i) {
+      high[i] = vec_max<T>(v[i]);
+      most = fmaxf(most, high[i]);
     }
+    best = most;
+    const float m = fmaxf(a.m, most * p.c);
+    if (m > a.m) a = sums_raise(a, m);
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i)
-      if (high[i] > above) {
-        const int index = part.head + (v0 + i * kThreads + tid) * kVecElems<T>;
+      if (v0 + i * kThreads < part.vecs) sums_add<T, kEnt>(a, v[i], p.c);
+    if (p.top == 0) continue;
+    if (g == 0) floor = floor_of<T>(kth_ordinal<T>(ordinal(best), p.top, sh.pick2));
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if constexpr (sizeof(T) == 2) {
-            const float lo = bf16lo_to_f32(v[i].w[j]), hi = bf16hi_to_f32(v[i].w[j]);
-            if (lo > above) push(lo, index + 2 * j);
-            if (hi > above) push(hi, index + 2 * j + 1);
-          } else {
-            const float z = __uint_as_float(v[i].w[j]);
-            if (z > above) push(z, index + j);
-          }
-        }
+    for (int i = 0; i < kUnroll; ++i)
+      if (high[i] >= floor) {
+        const uint32_t at = atomicAdd(&sh.n_vec, 1u);
+        if (at < kCap) sh.vec[at] = v0 + i * kThreads;
       }
   }
-  if (p.top > 0 && z_tail > floor) push(z_tail, part.n - part.tail + tid);
-  a = block_sums(a, p.c, sh.red);  // (a barrier: the candidates are there)
   int n = 0;
+  if (p.top > 0) {
+    best = fmaxf(best, z_tail);
+    floor = floor_of<T>(kth_ordinal<T>(ordinal(best), p.top, sh.pick2));  // (barriers: the vectors are noted)
+    auto push = [&](float z, int index) {
+      if (z >= floor) {
+        const uint32_t at = atomicAdd(&sh.n_cand, 1u);
+        if (at < kCap) sh.cand[at] = key_of(z, part.first + index);
+      }
+    };
+    if (tid < part.head) push(z_head, tid);
+    if (tid < part.tail) push(z_tail, part.n - part.tail + tid);
+    for (int k = tid; k < min(kCap, (int)sh.n_vec); k += kThreads) {
+      const int at = sh.vec[k];
+      const Vec v = load_vec(part.body() + (size_t)at * kVecBytes);
+      uint32_t bits = not_below<T>(v, floor);
+#pragma unroll 1
+      for (; bits != 0; bits &= bits - 1) {
+        const int index = part.head + at * kVecElems<T> + __ffs(bits) - 1;
+        push(load_f<T>(part.z + index), index);
+      }
+    }
+  }
+  a = block_sums(a, sh.red);  // (a barrier: the candidates are there)
   if (p.top > 0) {
     n = (int)sh.n_cand;
     const int places = min(p.top, part.n);
-    if (n > kCap || n < places) n = select_top<T>(part, places, sh);
+    if (n > kCap || n < places || sh.n_vec > kCap) n = select_top<T>(part, places, sh);
   }
   if (parts > 1) {
     cluster_wait();
@@ -420,7 +500,7 @@ __global__ void __launch_bounds__(kThreads, 2) top_kernel(const TopArgs p) {
     cluster_wait();
     if (rank != 0) return;
     a = sh.part[0];
-    for (int k = 1; k < parts; ++k) a = sums_merge(a, sh.part[k], p.c);
+    for (int k = 1; k < parts; ++k) a = sums_merge(a, sh.part[k]);
     n = (int)sh.n_pool;
     if (tid == 0) sh.n_cand = 0;
     __syncthreads();
@@ -433,23 +513,27 @@ __global__ void __launch_bounds__(kThreads, 2) top_kernel(const TopArgs p) {
     n = (int)sh.n_pool;
   }
   const Key* keys = parts > 1 ? sh.cand : sh.pool;
-  const float ln_s = a.s == 0.f ? NAN : logf(a.s);
+  Totals t{(double)a.m, a.s, a.u};
+  if (t.s == 0.f) t = low_sums<T>(zrow, p.V, p.c, sh.red, [](int) { return true; });
+  const double nat = 1.0 / ((double)p.c * (double)p.temperature), ln_s = t.s == 0.f ? NAN : log((double)t.s);
+  auto ln_p = [&](float z) { return (float)(((double)z * (double)p.c - t.x0) * nat - ln_s); };
   if (tid == 0) {
-    if (p.lse != nullptr) p.lse[row] = a.zm / p.temperature + ln_s;
-    if (p.logp != nullptr) p.logp[row] = (load_f<T>(zrow + id) - a.zm) / p.temperature - ln_s;
-    if (kEnt) p.entropy[row] = ln_s - a.u / a.s * MRL_NAT_HI;
+    if (p.lse != nullptr) p.lse[row] = (float)(t.x0 * nat + ln_s);
+    if (p.logp != nullptr) p.logp[row] = ln_p(load_f<T>(zrow + id));
+    if (kEnt) p.entropy[row] = (float)(ln_s - (double)t.u / (double)t.s * nat);
   }
   // in order: a key's place is the number of larger ones, counted by four threads a key
   for (int k0 = 0; k0 < n; k0 += kThreads / 4) {
     const int k = k0 + (tid >> 2);
     const Key key = k < n ? keys[k] : 0;
     int at = 0;
+#pragma unroll 4
     for (int j = tid & 3; j < n; j += 4) at += keys[j] > key;
     at += __shfl_xor_sync(0xffffffffu, at, 1);
     at += __shfl_xor_sync(0xffffffffu, at, 2);
     if (k < n && at < p.top && (tid & 3) == 0) {
       p.top_ids[row * p.top + at] = 0x7fffffff - (int32_t)(uint32_t)key;
-      p.top_logp[row * p.top + at] = (from_ordinal((uint32_t)(key >> 32)) - a.zm) / p.temperature - ln_s;
+      p.top_logp[row * p.top + at] = ln_p(from_ordinal((uint32_t)(key >> 32)));
     }
   }
   for (int k = n + tid; k < p.top; k += kThreads) {
@@ -580,8 +664,8 @@ struct RowResult {
 };
 
 // A row's KL and gradient factors from its list (thread k holds place k) and the sums over the rest, in float64.  Called by the block.
-__device__ RowResult distill_row(bool used, float z, float l, Sums rest, const mrl_distill_params& dp, double* red) {
-  const double T = dp.temperature;
+__device__ RowResult distill_row(bool used, float z, float l, Totals rest, float c, const mrl_distill_params& dp, double* red) {
+  const double nat = 1.0 / ((double)c * (double)dp.temperature);
   float zs = used ? fmaxf(z, -FLT_MAX) : -FLT_MAX;
   if (used && z != z) zs = INFINITY;  // (NaN: inf - inf below)
   __shared__ float zred[32];
@@ -591,14 +675,15 @@ __device__ RowResult distill_row(bool used, float z, float l, Sums rest, const m
   if ((threadIdx.x & 31) == 0) zred[threadIdx.x >> 5] = zs;
   __syncthreads();
   const bool any_rest = rest.s != 0.f;
-  float m = any_rest ? rest.zm : -FLT_MAX;
-  for (int k = 0; k < (int)(blockDim.x >> 5); ++k) m = fmaxf(m, zred[k]);
-  const double x = used ? ((double)z - (double)m) / T : 0.0;
-  const double in_rest = any_rest ? (double)rest.s * exp(((double)rest.zm - (double)m) / T) : 0.0;
+  for (int k = 0; k < (int)(blockDim.x >> 5); ++k) zs = fmaxf(zs, zred[k]);
+  double m = (double)zs * (double)c;  // (NaN and +inf stay what they are)
+  if (any_rest) m = fmax(m, rest.x0);
+  const double x = used ? ((double)z * (double)c - m) * nat : 0.0;
+  const double in_rest = any_rest ? (double)rest.s * exp((rest.x0 - m) * nat) : 0.0;
   const double total = block_sum(used ? exp(x) : 0.0, red) + in_rest;
   const double ln_total = total > 0.0 ? log(total) : NAN;
   const double ln_p = x - ln_total, p = used ? exp(ln_p) : 0.0;
-  const double ln_p_rest = any_rest ? log((double)rest.s) + ((double)rest.zm - (double)m) / T - ln_total : -INFINITY;
+  const double ln_p_rest = any_rest ? log((double)rest.s) + (rest.x0 - m) * nat - ln_total : -INFINITY;
   const bool has_rest = !(ln_p_rest < kNoRest);
   const double p_rest = has_rest ? exp(ln_p_rest) : 0.0;
   RowResult r;
@@ -661,11 +746,14 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const DistillArgs p) 
   const float mine = id >= 0 ? load_f<T>(z + id) : 0.f;
   if (id >= 0) atomicOr(&listed[id >> 5], 1u << (id & 31));
   __syncthreads();
-  Sums rest = sums_empty();
+  Sums sums = sums_empty();
   for (int v = threadIdx.x; v < p.V; v += kThreads)
-    if (!((listed[v >> 5] >> (v & 31)) & 1u)) sums_add(rest, load_f<T>(z + v), p.c);
-  rest = block_sums(rest, p.c, red);
-  const RowResult r = distill_row(id >= 0, mine, l, rest, p.dp, red64);
+    if (!((listed[v >> 5] >> (v & 31)) & 1u)) sums_add(sums, load_f<T>(z + v), p.c);
+  sums = block_sums(sums, red);
+  Totals rest{(double)sums.m, sums.s, 0.f};
+  const bool low = rest.s == 0.f;
+  if (low) rest = low_sums<T>(z, p.V, p.c, red, [](int v) { return !((listed[v >> 5] >> (v & 31)) & 1u); });
+  const RowResult r = distill_row(id >= 0, mine, l, rest, p.c, p.dp, red64);
   const float w = p.weight != nullptr ? p.weight[row] : 1.f;
   if (threadIdx.x == 0) {
     p.term[row] = w != 0.f ? (double)w * r.kl : 0.0;
@@ -676,8 +764,10 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const DistillArgs p) 
   const double scale = (double)p.dp.coeff * w / (denominator * p.dp.temperature);
   const float of_rest = scale != 0.0 && rest.s != 0.f ? (float)(r.of_rest * scale / rest.s) : 0.f;
   for (int v = threadIdx.x; v < p.V; v += kThreads)
-    if (!((listed[v >> 5] >> (v & 31)) & 1u))
-      store_f(dz + v, scale != 0.0 ? ex2_approx((load_f<T>(z + v) - rest.zm) * p.c) * of_rest : 0.f);
+    if (!((listed[v >> 5] >> (v & 31)) & 1u)) {
+      const float e = low ? ex2_approx((float)((double)load_f<T>(z + v) * (double)p.c - rest.x0)) : ex2_approx(fmaf(load_f<T>(z + v), p.c, -sums.m));
+      store_f(dz + v, scale != 0.0 && of_rest != 0.f ? e * of_rest : 0.f);
+    }
   if (id >= 0) store_f(dz + id, scale != 0.0 ? (float)(r.at * scale) : 0.f);
 }
 
