@@ -11,7 +11,8 @@ namespace {
 
 using namespace mrl;
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;  // of the row kernels: two CTAs an SM
+constexpr int kTopThreads = 256;                        // four CTAs an SM
+constexpr int kThreads = 512, kWarps = kThreads / 32;  // two CTAs an SM
 constexpr int kTop = MRL_MAX_TOP;
 constexpr int kMaxParts = 8;                            // CTAs that share a row
 
@@ -78,15 +79,15 @@ struct Part {
   __device__ __forceinline__ const char* body() const { return reinterpret_cast<const char*>(z + head); }
 };
 
-// How many CTAs share a row: as many as keep two CTAs an SM busy, with 16 KB of it at least.
-int parts_of(long long N, long long row_bytes) {
+// How many CTAs share a row: as many as there is room for on 148 SMs, with 16 KB of it at least.
+int parts_of(long long N, long long row_bytes, int ctas_per_sm) {
   int parts = 1;
-  while (parts < kMaxParts && N * parts * 2 <= 2 * 148 && row_bytes / (parts * 2) >= 16 * 1024) parts *= 2;
+  while (parts < kMaxParts && N * parts * 2 <= ctas_per_sm * 148 && row_bytes / (parts * 2) >= 16 * 1024) parts *= 2;
   return parts;
 }
 
 template <typename... Params>
-int launch_rows(void (*kernel)(Params...), long long N, int parts, size_t smem, bool behind, cudaStream_t st, Params... args) {
+int launch_rows(void (*kernel)(Params...), long long N, int parts, int threads, size_t smem, bool behind, cudaStream_t st, Params... args) {
   cudaLaunchAttribute attr[2]{};
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)parts;
@@ -95,7 +96,7 @@ int launch_rows(void (*kernel)(Params...), long long N, int parts, size_t smem, 
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(N * parts));
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cfg.attrs = attr;
@@ -128,23 +129,24 @@ __device__ __forceinline__ Sums sums_merge(Sums a, Sums b) {
   b = sums_raise(b, m);
   return Sums{m, a.s + b.s, a.u + b.u};
 }
-template <bool kEnt>
+// kGuard: right for z = -inf too, where 2^t t is 0
+template <bool kEnt, bool kGuard>
 __device__ __forceinline__ void sums_term(float z, float c, float m, float& s, float& u) {
   const float t = fmaf(z, c, -m), e = ex2_approx(t);
   s += e;
-  if (kEnt) u = fmaf(e, fmaxf(t, -1000.f), u);
+  if (kEnt) u = fmaf(e, kGuard ? fmaxf(t, -1000.f) : t, u);
 }
 // adds the elements of a vector, none of which is above a.m
-template <typename T, bool kEnt>
+template <typename T, bool kEnt, bool kGuard>
 __device__ __forceinline__ void sums_add(Sums& a, const Vec& v, float c) {
   float s0 = 0.f, s1 = 0.f, u0 = 0.f, u1 = 0.f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     if constexpr (sizeof(T) == 2) {
-      sums_term<kEnt>(bf16lo_to_f32(v.w[j]), c, a.m, s0, u0);
-      sums_term<kEnt>(bf16hi_to_f32(v.w[j]), c, a.m, s1, u1);
+      sums_term<kEnt, kGuard>(bf16lo_to_f32(v.w[j]), c, a.m, s0, u0);
+      sums_term<kEnt, kGuard>(bf16hi_to_f32(v.w[j]), c, a.m, s1, u1);
     } else {
-      sums_term<kEnt>(__uint_as_float(v.w[j]), c, a.m, j & 1 ? s1 : s0, j & 1 ? u1 : u0);
+      sums_term<kEnt, kGuard>(__uint_as_float(v.w[j]), c, a.m, j & 1 ? s1 : s0, j & 1 ? u1 : u0);
     }
   }
   a.s += s0 + s1;
@@ -153,10 +155,12 @@ __device__ __forceinline__ void sums_add(Sums& a, const Vec& v, float c) {
 __device__ __forceinline__ void sums_add(Sums& a, float z, float c) {
   const float m = fmaxf(a.m, z * c);
   if (m > a.m) a = sums_raise(a, m);
-  sums_term<true>(z, c, a.m, a.s, a.u);
+  sums_term<true, true>(z, c, a.m, a.s, a.u);
 }
 // Over the block, in a fixed order; every thread gets the result.  The maximum first, so that each thread rescales once.
+template <int kT>
 __device__ __forceinline__ Sums block_sums(Sums a, Sums* red) {
+  constexpr int kWarps = kT / 32;
   float m = a.m;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -191,19 +195,19 @@ struct Totals {
 };
 // The sums of a row whose s above is 0, against its largest logit: 2^((z - zm) c).  `keep` says which elements count.  Called by the block;
 // slow, and hardly ever needed.
-template <typename T, typename Keep>
+template <typename T, int kT, typename Keep>
 __device__ __noinline__ Totals low_sums(const T* z, int V, float c, Sums* red, Keep keep) {
   float zm = -FLT_MAX;
-  for (int v = threadIdx.x; v < V; v += kThreads)
+  for (int v = threadIdx.x; v < V; v += kT)
     if (keep(v)) zm = fmaxf(zm, load_f<T>(z + v));
   Sums a{zm, 0.f, 0.f};
   __syncthreads();
-  zm = block_sums(a, red).m;
+  zm = block_sums<kT>(a, red).m;
   a = Sums{0.f, 0.f, 0.f};
-  for (int v = threadIdx.x; v < V; v += kThreads)
-    if (keep(v)) sums_term<true>(load_f<T>(z + v) - zm, c, 0.f, a.s, a.u);
+  for (int v = threadIdx.x; v < V; v += kT)
+    if (keep(v)) sums_term<true, true>(load_f<T>(z + v) - zm, c, 0.f, a.s, a.u);
   __syncthreads();
-  a = block_sums(a, red);
+  a = block_sums<kT>(a, red);
   return Totals{(double)zm * (double)c, a.s, a.u};
 }
 
@@ -233,15 +237,18 @@ typedef unsigned long long Key;
 __device__ __forceinline__ Key key_of(float z, int index) { return ((Key)ordinal(z) << 32) | (uint32_t)(0x7fffffff - index); }
 
 constexpr int kUnroll = 4;       // vectors of a thread and group
-constexpr int kCap = 2048;       // candidates of a CTA
+constexpr int kTopWarps = kTopThreads / 32;
+constexpr int kCap = 1024;       // vectors noted, and candidates, of a CTA
 constexpr int kFew = 256;        // keys that are put in order by counting
 struct TopShared {
   Key cand[kCap];                // candidates of this CTA
-  Key pool[kCap];                // (CTA 0) what is left of those of all CTAs of the row: kMaxParts * kFew at most
-  Sums part[kMaxParts], red[kWarps];
+  Key list[kFew];                // what is left of them, or (CTA 0) of the pool
+  Sums part[kMaxParts], red[kTopWarps];
   int vec[kCap];                 // vectors noted
-  uint32_t hist[256], pick[4], pick2[2 * kWarps], n_vec, n_cand, n_pool;
+  uint32_t hist[256], pick[4], pick2[2 * kTopWarps], n_vec, n_cand, n_list, n_pool;
 };
+// (CTA 0 of a row that several share) what is left of the candidates of all
+constexpr int kPool = kMaxParts * kFew;
 
 // The largest digit d (of 256) such that at least `want` counts lie at or above it; `want` becomes what is wanted of d itself.
 __device__ __forceinline__ int pick_digit(TopShared& sh, uint32_t& want) {
@@ -275,17 +282,17 @@ __device__ __forceinline__ void count_digit(uint32_t* hist, bool on, uint32_t di
 // few logits are above -inf.  Returns their number.
 template <typename T>
 __device__ __noinline__ int select_top(const Part<T> part, int top, TopShared& sh) {
-  const int rounds = (part.n + kThreads - 1) / kThreads;
+  const int rounds = (part.n + kTopThreads - 1) / kTopThreads;
   Key last = 0;
   uint32_t want = (uint32_t)top;
   int listed = top;
 #pragma unroll 1
   for (int shift = 56; shift >= 0; shift -= 8) {
-    for (int i = threadIdx.x; i < 256; i += kThreads) sh.hist[i] = 0;
+    for (int i = threadIdx.x; i < 256; i += kTopThreads) sh.hist[i] = 0;
     __syncthreads();
 #pragma unroll 4
     for (int r = 0; r < rounds; ++r) {
-      const int i = r * kThreads + threadIdx.x;
+      const int i = r * kTopThreads + threadIdx.x;
       const Key key = i < part.n ? key_of(load_f<T>(part.z + i), part.first + i) : 0;
       count_digit(sh.hist, (key >> 32) != 0 && (shift == 56 || (key >> (shift + 8)) == (last >> (shift + 8))), (uint32_t)(key >> shift) & 255u);
     }
@@ -306,7 +313,7 @@ __device__ __noinline__ int select_top(const Part<T> part, int top, TopShared& s
   }
   if (threadIdx.x == 0) sh.n_cand = 0;
   __syncthreads();
-  for (int i = threadIdx.x; i < part.n; i += kThreads) {
+  for (int i = threadIdx.x; i < part.n; i += kTopThreads) {
     const Key key = key_of(load_f<T>(part.z + i), part.first + i);
     if (key >= last) sh.cand[min(atomicAdd(&sh.n_cand, 1u), (uint32_t)(kCap - 1))] = key;
   }
@@ -316,26 +323,28 @@ __device__ __noinline__ int select_top(const Part<T> part, int top, TopShared& s
 
 // Copies the keys that can be among the `top` largest of `from` to `to` (of CTA `rank`, behind what its counter says is there): at most kFew,
 // and all of the `top` largest among them.  Bits are settled from above until few enough are left.
-__device__ void keep_largest(const Key* from, int n, int top, Key* to, uint32_t* n_to) {
-  Key mine[kCap / kThreads];
+template <int kMost>
+__device__ __noinline__ void keep_largest(const Key* from, int n, int top, Key* to, uint32_t* n_to) {
+  constexpr int kEach = kMost / kTopThreads;
+  Key mine[kEach];
 #pragma unroll
-  for (int i = 0; i < kCap / kThreads; ++i) mine[i] = i * kThreads + threadIdx.x < n ? from[i * kThreads + threadIdx.x] : 0;
+  for (int i = 0; i < kEach; ++i) mine[i] = i * kTopThreads + threadIdx.x < n ? from[i * kTopThreads + threadIdx.x] : 0;
   Key least = 1;
   if (n > kFew) {
     least = 0;
     for (int bit = 63; bit >= 0; --bit) {
       const Key next = least | ((Key)1 << bit);
       int total = __syncthreads_count(mine[0] >= next);
-      if (n > kThreads) {
+      if (n > kTopThreads) {
 #pragma unroll
-        for (int i = 1; i < kCap / kThreads; ++i) total += __syncthreads_count(mine[i] >= next);
+        for (int i = 1; i < kEach; ++i) total += __syncthreads_count(mine[i] >= next);
       }
       if (total >= top) least = next;
       if (total >= top && total <= kFew) break;
     }
   }
 #pragma unroll
-  for (int i = 0; i < kCap / kThreads; ++i)
+  for (int i = 0; i < kEach; ++i)
     if (mine[i] >= least) to[atomicAdd(n_to, 1u)] = mine[i];
 }
 
@@ -346,10 +355,10 @@ template <typename T>
 __device__ __forceinline__ uint32_t kth_ordinal(uint32_t mine, int want, uint32_t* red) {
   uint32_t high = __reduce_max_sync(0xffffffffu, mine), low = __reduce_min_sync(0xffffffffu, mine);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (lane == 0) red[warp] = high, red[kWarps + warp] = low;
+  if (lane == 0) red[warp] = high, red[kTopWarps + warp] = low;
   __syncthreads();
-  high = __reduce_max_sync(0xffffffffu, red[lane % kWarps]);
-  low = __reduce_min_sync(0xffffffffu, red[kWarps + lane % kWarps]);
+  high = __reduce_max_sync(0xffffffffu, red[lane % kTopWarps]);
+  low = __reduce_min_sync(0xffffffffu, red[kTopWarps + lane % kTopWarps]);
   if (high == low) {
     __syncthreads();  // (`red` may be used again)
     return max(low, kLowest);
@@ -397,7 +406,7 @@ __device__ __forceinline__ uint32_t not_below(const Vec& v, float floor) {
 }
 
 template <typename T, bool kEnt>
-__global__ void __launch_bounds__(kThreads, 2) top_kernel(const TopArgs p) {
+__global__ void __launch_bounds__(kTopThreads, 1024 / kTopThreads) top_kernel(const TopArgs p) {
   __shared__ TopShared sh;
   const int tid = threadIdx.x;
   int parts, rank;
@@ -421,8 +430,9 @@ __global__ void __launch_bounds__(kThreads, 2) top_kernel(const TopArgs p) {
     }
     return;
   }
-  if (tid == 0) sh.n_vec = sh.n_cand = sh.n_pool = 0;
+  if (tid == 0) sh.n_vec = sh.n_cand = sh.n_list = sh.n_pool = 0;
   __syncthreads();
+  extern __shared__ Key pool[];  // [kPool] where parts > 1
   if (parts > 1) cluster_arrive();  // "my counters are set"
   const Part<T> part(zrow, p.V, parts, rank);
   const char* body = part.body() + (size_t)tid * kVecBytes;
@@ -435,13 +445,13 @@ __global__ void __launch_bounds__(kThreads, 2) top_kernel(const TopArgs p) {
   // so that `top` threads at least have an element there, each at least one.  The largest element of each thread sets the last floor behind the last
   // group in the same way, a tight one, and what is not below it is read again from the vectors noted.
   float best = z_head, floor = floor_of<T>(kLowest);
-  const int groups = max(1, (part.vecs + kThreads * kUnroll - 1) / (kThreads * kUnroll));
+  const int groups = max(1, (part.vecs + kTopThreads * kUnroll - 1) / (kTopThreads * kUnroll));
 #pragma unroll 1
   for (int g = 0; g < groups; ++g) {
-    const int v0 = g * kThreads * kUnroll + tid;
+    const int v0 = g * kTopThreads * kUnroll + tid;
     Vec v[kUnroll];
 #pragma unroll
-    for (int i = 0; i < kUnroll; ++i) v[i] = v0 + i * kThreads < part.vecs ? load_vec(body + (size_t)(v0 - tid + i * kThreads) * kVecBytes) : no_vec<T>();
+    for (int i = 0; i < kUnroll; ++i) v[i] = v0 + i * kTopThreads < part.vecs ? load_vec(body + (size_t)(v0 - tid + i * kTopThreads) * kVecBytes) : no_vec<T>();
     float high[kUnroll], most = best;
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i) {
@@ -451,16 +461,24 @@ __global__ void __launch_bounds__(kThreads, 2) top_kernel(const TopArgs p) {
     best = most;
     const float m = fmaxf(a.m, most * p.c);
     if (m > a.m) a = sums_raise(a, m);
+    Sums more{a.m, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i)
-      if (v0 + i * kThreads < part.vecs) sums_add<T, kEnt>(a, v[i], p.c);
+      if (v0 + i * kTopThreads < part.vecs) sums_add<T, kEnt, false>(more, v[i], p.c);
+    if (kEnt && more.u != more.u) {  // 0 * inf: masked logits among them (or NaN, which it stays)
+      more = Sums{a.m, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < kUnroll; ++i) sums_add<T, kEnt, true>(more, v[i], p.c);
+    }
+    a.s += more.s;
+    a.u += more.u;
     if (p.top == 0) continue;
-    if (g == 0) floor = floor_of<T>(kth_ordinal<T>(ordinal(best), p.top, sh.pick2));
+    if ((g & (g + 1)) == 0 && (g == 0 || g + 1 < groups)) floor = floor_of<T>(kth_ordinal<T>(ordinal(best), p.top, sh.pick2));
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i)
       if (high[i] >= floor) {
         const uint32_t at = atomicAdd(&sh.n_vec, 1u);
-        if (at < kCap) sh.vec[at] = v0 + i * kThreads;
+        if (at < kCap) sh.vec[at] = v0 + i * kTopThreads;
       }
   }
   int n = 0;
@@ -475,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, 2) top_kernel(const TopArgs p) {
     };
     if (tid < part.head) push(z_head, tid);
     if (tid < part.tail) push(z_tail, part.n - part.tail + tid);
-    for (int k = tid; k < min(kCap, (int)sh.n_vec); k += kThreads) {
+    for (int k = tid; k < min(kCap, (int)sh.n_vec); k += kTopThreads) {
       const int at = sh.vec[k];
       const Vec v = load_vec(part.body() + (size_t)at * kVecBytes);
       uint32_t bits = not_below<T>(v, floor);
@@ -486,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, 2) top_kernel(const TopArgs p) {
       }
     }
   }
-  a = block_sums(a, sh.red);  // (a barrier: the candidates are there)
+  a = block_sums<kTopThreads>(a, sh.red);  // (a barrier: the candidates are there)
   if (p.top > 0) {
     n = (int)sh.n_cand;
     const int places = min(p.top, part.n);
@@ -495,26 +513,22 @@ __global__ void __launch_bounds__(kThreads, 2) top_kernel(const TopArgs p) {
   if (parts > 1) {
     cluster_wait();
     if (tid == 0) *in_cta(&sh.part[rank], 0) = a;
-    if (n > 0) keep_largest(sh.cand, n, p.top, in_cta(sh.pool, 0), in_cta(&sh.n_pool, 0));
+    if (n > 0) keep_largest<kCap>(sh.cand, n, p.top, in_cta(pool, 0), in_cta(&sh.n_pool, 0));
     cluster_arrive();
     cluster_wait();
     if (rank != 0) return;
     a = sh.part[0];
     for (int k = 1; k < parts; ++k) a = sums_merge(a, sh.part[k]);
     n = (int)sh.n_pool;
-    if (tid == 0) sh.n_cand = 0;
-    __syncthreads();
-    if (n > 0) keep_largest(sh.pool, n, p.top, sh.cand, &sh.n_cand);
-    __syncthreads();
-    n = (int)sh.n_cand;
+    if (n > 0) keep_largest<kPool>(pool, n, p.top, sh.list, &sh.n_list);
   } else if (n > 0) {
-    keep_largest(sh.cand, n, p.top, sh.pool, &sh.n_pool);
-    __syncthreads();
-    n = (int)sh.n_pool;
+    keep_largest<kCap>(sh.cand, n, p.top, sh.list, &sh.n_list);
   }
-  const Key* keys = parts > 1 ? sh.cand : sh.pool;
+  __syncthreads();
+  n = (int)sh.n_list;
+  const Key* keys = sh.list;
   Totals t{(double)a.m, a.s, a.u};
-  if (t.s == 0.f) t = low_sums<T>(zrow, p.V, p.c, sh.red, [](int) { return true; });
+  if (t.s == 0.f) t = low_sums<T, kTopThreads>(zrow, p.V, p.c, sh.red, [](int) { return true; });
   const double nat = 1.0 / ((double)p.c * (double)p.temperature), ln_s = t.s == 0.f ? NAN : log((double)t.s);
   auto ln_p = [&](float z) { return (float)(((double)z * (double)p.c - t.x0) * nat - ln_s); };
   if (tid == 0) {
@@ -523,7 +537,7 @@ __global__ void __launch_bounds__(kThreads, 2) top_kernel(const TopArgs p) {
     if (kEnt) p.entropy[row] = (float)(ln_s - (double)t.u / (double)t.s * nat);
   }
   // in order: a key's place is the number of larger ones, counted by four threads a key
-  for (int k0 = 0; k0 < n; k0 += kThreads / 4) {
+  for (int k0 = 0; k0 < n; k0 += kTopThreads / 4) {
     const int k = k0 + (tid >> 2);
     const Key key = k < n ? keys[k] : 0;
     int at = 0;
@@ -536,7 +550,7 @@ __global__ void __launch_bounds__(kThreads, 2) top_kernel(const TopArgs p) {
       p.top_logp[row * p.top + at] = ln_p(from_ordinal((uint32_t)(key >> 32)));
     }
   }
-  for (int k = n + tid; k < p.top; k += kThreads) {
+  for (int k = n + tid; k < p.top; k += kTopThreads) {
     p.top_ids[row * p.top + k] = -1;
     p.top_logp[row * p.top + k] = -INFINITY;
   }
@@ -749,10 +763,10 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const DistillArgs p) 
   Sums sums = sums_empty();
   for (int v = threadIdx.x; v < p.V; v += kThreads)
     if (!((listed[v >> 5] >> (v & 31)) & 1u)) sums_add(sums, load_f<T>(z + v), p.c);
-  sums = block_sums(sums, red);
+  sums = block_sums<kThreads>(sums, red);
   Totals rest{(double)sums.m, sums.s, 0.f};
   const bool low = rest.s == 0.f;
-  if (low) rest = low_sums<T>(z, p.V, p.c, red, [](int v) { return !((listed[v >> 5] >> (v & 31)) & 1u); });
+  if (low) rest = low_sums<T, kThreads>(z, p.V, p.c, red, [](int v) { return !((listed[v >> 5] >> (v & 31)) & 1u); });
   const RowResult r = distill_row(id >= 0, mine, l, rest, p.c, p.dp, red64);
   const float w = p.weight != nullptr ? p.weight[row] : 1.f;
   if (threadIdx.x == 0) {
@@ -838,10 +852,11 @@ extern "C" int mrl_top_logprobs(const void* logits, int32_t dtype, int64_t N, in
   const TopArgs a{logits, ld, V, ids, mask, temperature, scale_of(temperature), top, logp, lse, entropy, top_logp, top_ids, status};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool bf16 = dtype == MRL_BF16, ent = entropy != nullptr;
-  const int parts = parts_of(N, (long long)V * (bf16 ? 2 : 4));
+  const int parts = parts_of(N, (long long)V * (bf16 ? 2 : 4), 1024 / kTopThreads);
   mrl_profile_before(st, "top_kernel");
   const int rc = launch_rows(bf16 ? (ent ? top_kernel<__nv_bfloat16, true> : top_kernel<__nv_bfloat16, false>)
-                                  : (ent ? top_kernel<float, true> : top_kernel<float, false>), N, parts, 0, false, st, a);
+                                  : (ent ? top_kernel<float, true> : top_kernel<float, false>), N, parts, kTopThreads,
+                             parts > 1 ? kPool * sizeof(Key) : 0, false, st, a);
   mrl_profile_after(st);
   return rc;
 }
