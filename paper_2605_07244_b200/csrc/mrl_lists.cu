@@ -11,7 +11,7 @@ namespace {
 
 using namespace mrl;
 
-constexpr int kTopThreads = 256;                        // four CTAs an SM
+constexpr int kTopThreads = 256, kTopCtas = 5;          // threads, and CTAs an SM, of the top tokens
 constexpr int kThreads = 512, kWarps = kThreads / 32;  // two CTAs an SM
 constexpr int kTop = MRL_MAX_TOP;
 constexpr int kMaxParts = 8;                            // CTAs that share a row
@@ -136,21 +136,23 @@ __device__ __forceinline__ void sums_term(float z, float c, float m, float& s, f
   s += e;
   if (kEnt) u = fmaf(e, kGuard ? fmaxf(t, -1000.f) : t, u);
 }
-// adds the elements of a vector, none of which is above a.m
+// The sums of vectors in pairs: even and odd elements
+struct Sums2 {
+  f2 s, u;
+};
+// adds the elements of a vector, none of which is above m; c2 = (c, c), m2 = (-m, -m)
 template <typename T, bool kEnt, bool kGuard>
-__device__ __forceinline__ void sums_add(Sums& a, const Vec& v, float c) {
-  float s0 = 0.f, s1 = 0.f, u0 = 0.f, u1 = 0.f;
+__device__ __forceinline__ void sums_add(Sums2& a, const Vec& v, f2 c2, f2 m2) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    if constexpr (sizeof(T) == 2) {
-      sums_term<kEnt, kGuard>(bf16lo_to_f32(v.w[j]), c, a.m, s0, u0);
-      sums_term<kEnt, kGuard>(bf16hi_to_f32(v.w[j]), c, a.m, s1, u1);
-    } else {
-      sums_term<kEnt, kGuard>(__uint_as_float(v.w[j]), c, a.m, j & 1 ? s1 : s0, j & 1 ? u1 : u0);
-    }
+  for (int j = 0; j < 8; j += sizeof(T) == 2 ? 1 : 2) {
+    const f2 z = sizeof(T) == 2 ? bf16x2_to_f2(v.w[j]) : make_f2(__uint_as_float(v.w[j]), __uint_as_float(v.w[(j + 1) & 7]));
+    f2 t = fma_f2(z, c2, m2);
+    float2 x = split_f2(t);
+    const f2 e = make_f2(ex2_approx(x.x), ex2_approx(x.y));
+    a.s = add_f2(a.s, e);
+    if (kEnt && kGuard) t = make_f2(fmaxf(x.x, -1000.f), fmaxf(x.y, -1000.f));
+    if (kEnt) a.u = fma_f2(e, t, a.u);
   }
-  a.s += s0 + s1;
-  a.u += u0 + u1;
 }
 __device__ __forceinline__ void sums_add(Sums& a, float z, float c) {
   const float m = fmaxf(a.m, z * c);
@@ -236,15 +238,16 @@ struct TopArgs {
 typedef unsigned long long Key;
 __device__ __forceinline__ Key key_of(float z, int index) { return ((Key)ordinal(z) << 32) | (uint32_t)(0x7fffffff - index); }
 
-constexpr int kUnroll = 4;       // vectors of a thread and group
+constexpr int kUnroll = 3;       // vectors of a thread and group
+constexpr int kSecondFloor = 3;  // the group behind which the floor is set again
 constexpr int kTopWarps = kTopThreads / 32;
-constexpr int kCap = 1024;       // vectors noted, and candidates, of a CTA
+constexpr int kNoted = 2048, kCap = 1024;  // vectors noted, and candidates, of a CTA
 constexpr int kFew = 256;        // keys that are put in order by counting
 struct TopShared {
   Key cand[kCap];                // candidates of this CTA
   Key list[kFew];                // what is left of them, or (CTA 0) of the pool
   Sums part[kMaxParts], red[kTopWarps];
-  int vec[kCap];                 // vectors noted
+  int vec[kNoted];               // vectors noted
   uint32_t hist[256], pick[4], pick2[2 * kTopWarps], n_vec, n_cand, n_list, n_pool;
 };
 // (CTA 0 of a row that several share) what is left of the candidates of all
@@ -277,48 +280,79 @@ __device__ __forceinline__ void count_digit(uint32_t* hist, bool on, uint32_t di
   }
 }
 
-// The `top` largest keys of a part by 256-way counting: four passes find the value of the last of them, four more the index up to which
-// tokens of that value are listed, one collects.  Right for every row, and reads it nine times: taken where the candidates do not fit, or too
-// few logits are above -inf.  Returns their number.
+// Calls f(z, index in the part) for every element of a part, with all threads of a warp together; z is NaN where a thread has none.
+template <typename T, typename F>
+__device__ __forceinline__ void each_element(const Part<T>& part, F f) {
+  const int tid = threadIdx.x;
+  f(tid < part.head ? load_f<T>(part.z + tid) : NAN, tid);
+  f(tid < part.tail ? load_f<T>(part.z + part.n - part.tail + tid) : NAN, part.n - part.tail + tid);
+#pragma unroll 1
+  for (int r = 0; r < part.vecs; r += kTopThreads) {
+    const bool on = r + tid < part.vecs;
+    const int at = part.head + (r + tid) * kVecElems<T>;
+    const Vec v = on ? load_vec(part.z + at) : no_vec<T>();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (sizeof(T) == 2) {
+        f(on ? bf16lo_to_f32(v.w[j]) : NAN, at + 2 * j);
+        f(on ? bf16hi_to_f32(v.w[j]) : NAN, at + 2 * j + 1);
+      } else {
+        f(on ? __uint_as_float(v.w[j]) : NAN, at + j);
+      }
+    }
+  }
+}
+
+// The `top` largest keys of a part by 256-way counting: a pass for each eight bits of the last one's value, then of its index up to which tokens of that
+// value are listed, and one that collects.  For rows with more than kCap tokens that are not below the last floor: long runs of one value at the top.  Reads
+// the row six (bf16) to eight times.
 template <typename T>
-__device__ __noinline__ int select_top(const Part<T> part, int top, TopShared& sh) {
-  const int rounds = (part.n + kTopThreads - 1) / kTopThreads;
+__device__ void select_top(const Part<T> part, int top, TopShared& sh) {
   Key last = 0;
   uint32_t want = (uint32_t)top;
-  int listed = top;
 #pragma unroll 1
   for (int shift = 56; shift >= 0; shift -= 8) {
+    if (sizeof(T) == 2 && (shift == 40 || shift == 32)) {  // a bf16's ordinal ends in sixteen zeros, or ones
+      if (!(last >> 63)) last |= (Key)0xff << shift;
+      continue;
+    }
     for (int i = threadIdx.x; i < 256; i += kTopThreads) sh.hist[i] = 0;
     __syncthreads();
-#pragma unroll 4
-    for (int r = 0; r < rounds; ++r) {
-      const int i = r * kTopThreads + threadIdx.x;
-      const Key key = i < part.n ? key_of(load_f<T>(part.z + i), part.first + i) : 0;
+    each_element<T>(part, [&](float z, int i) {
+      const Key key = key_of(z, part.first + i);
       count_digit(sh.hist, (key >> 32) != 0 && (shift == 56 || (key >> (shift + 8)) == (last >> (shift + 8))), (uint32_t)(key >> shift) & 255u);
-    }
-    if (shift == 56) {  // (fewer numbers than places: all of them)
-      __syncthreads();
-      if (threadIdx.x < 32) {
-        uint32_t n = 0;
-        for (int i = threadIdx.x; i < 256; i += 32) n += sh.hist[i];
-        n = __reduce_add_sync(0xffffffffu, n);
-        if (threadIdx.x == 0) sh.pick[2] = n;
-      }
-      __syncthreads();
-      want = min(want, sh.pick[2]);
-      listed = (int)want;
-      if (listed == 0) return 0;
-    }
+    });
     last |= (Key)pick_digit(sh, want) << shift;
   }
   if (threadIdx.x == 0) sh.n_cand = 0;
   __syncthreads();
-  for (int i = threadIdx.x; i < part.n; i += kTopThreads) {
-    const Key key = key_of(load_f<T>(part.z + i), part.first + i);
+  each_element<T>(part, [&](float z, int i) {
+    const Key key = key_of(z, part.first + i);
     if (key >= last) sh.cand[min(atomicAdd(&sh.n_cand, 1u), (uint32_t)(kCap - 1))] = key;
-  }
+  });
   __syncthreads();
-  return listed;
+}
+
+// Adds the first `want` tokens of -inf of a part to its candidates (all others are there).
+template <typename T>
+__device__ __noinline__ void add_masked(const Part<T> part, int want, TopShared& sh) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int r = 0; r < part.n && want > 0; r += kTopThreads) {
+    const int i = r + threadIdx.x;
+    const bool masked = i < part.n && load_f<T>(part.z + i) == -INFINITY;
+    const unsigned who = __ballot_sync(0xffffffffu, masked);
+    if (lane == 0) sh.hist[warp] = (uint32_t)__popc(who);
+    __syncthreads();
+    int before = __popc(who & ((1u << lane) - 1)), all = 0;
+    for (int w = 0; w < kTopWarps; ++w) {
+      before += w < warp ? (int)sh.hist[w] : 0;
+      all += (int)sh.hist[w];
+    }
+    if (masked && before < want) sh.cand[atomicAdd(&sh.n_cand, 1u)] = key_of(-INFINITY, part.first + i);
+    want -= all;
+    __syncthreads();
+  }
 }
 
 // Copies the keys that can be among the `top` largest of `from` to `to` (of CTA `rank`, behind what its counter says is there): at most kFew,
@@ -349,10 +383,10 @@ __device__ __noinline__ void keep_largest(const Key* from, int n, int top, Key* 
 }
 
 constexpr uint32_t kLowest = 0x00800000u;  // the ordinal above that of -inf
-// An ordinal, kLowest at least, that `want` threads at least do not fall below with theirs, and hardly more of them.  Bits are settled from above, from
+// An ordinal, kLowest at least, that `want` threads at least do not fall below with theirs, and `more` + 2 others if that can be.  Bits are settled from above, from
 // the first that the threads differ in.
 template <typename T>
-__device__ __forceinline__ uint32_t kth_ordinal(uint32_t mine, int want, uint32_t* red) {
+__device__ __forceinline__ uint32_t kth_ordinal(uint32_t mine, int want, int more, uint32_t* red) {
   uint32_t high = __reduce_max_sync(0xffffffffu, mine), low = __reduce_min_sync(0xffffffffu, mine);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (lane == 0) red[warp] = high, red[kTopWarps + warp] = low;
@@ -369,7 +403,7 @@ __device__ __forceinline__ uint32_t kth_ordinal(uint32_t mine, int want, uint32_
     const uint32_t next = found | (1u << bit);
     const int n = __syncthreads_count(mine >= next);
     if (n >= want) found = next;
-    if (n >= want && n <= want + want / 8 + 2) break;
+    if (n >= want && n <= want + more + 2) break;
   }
   return max(found, kLowest);
 }
@@ -406,7 +440,7 @@ __device__ __forceinline__ uint32_t not_below(const Vec& v, float floor) {
 }
 
 template <typename T, bool kEnt>
-__global__ void __launch_bounds__(kTopThreads, 1024 / kTopThreads) top_kernel(const TopArgs p) {
+__global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArgs p) {
   __shared__ TopShared sh;
   const int tid = threadIdx.x;
   int parts, rank;
@@ -461,30 +495,33 @@ __global__ void __launch_bounds__(kTopThreads, 1024 / kTopThreads) top_kernel(co
     best = most;
     const float m = fmaxf(a.m, most * p.c);
     if (m > a.m) a = sums_raise(a, m);
-    Sums more{a.m, 0.f, 0.f};
+    const f2 c2 = make_f2(p.c, p.c), m2 = make_f2(-a.m, -a.m);
+    Sums2 more{0, 0};
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i)
-      if (v0 + i * kTopThreads < part.vecs) sums_add<T, kEnt, false>(more, v[i], p.c);
-    if (kEnt && more.u != more.u) {  // 0 * inf: masked logits among them (or NaN, which it stays)
-      more = Sums{a.m, 0.f, 0.f};
+      if (v0 + i * kTopThreads < part.vecs) sums_add<T, kEnt, false>(more, v[i], c2, m2);
+    float2 s = split_f2(more.s), u = split_f2(more.u);
+    if (kEnt && !(u.x + u.y == u.x + u.y)) {  // 0 * inf: masked logits among them (or NaN, which it stays)
+      more = Sums2{0, 0};
 #pragma unroll
-      for (int i = 0; i < kUnroll; ++i) sums_add<T, kEnt, true>(more, v[i], p.c);
+      for (int i = 0; i < kUnroll; ++i) sums_add<T, kEnt, true>(more, v[i], c2, m2);
+      u = split_f2(more.u);
     }
-    a.s += more.s;
-    a.u += more.u;
+    a.s += s.x + s.y;
+    a.u += u.x + u.y;
     if (p.top == 0) continue;
-    if ((g & (g + 1)) == 0 && (g == 0 || g + 1 < groups)) floor = floor_of<T>(kth_ordinal<T>(ordinal(best), p.top, sh.pick2));
+    if (g == 0 || (g == kSecondFloor && g + 1 < groups)) floor = floor_of<T>(kth_ordinal<T>(ordinal(best), p.top, p.top / 4, sh.pick2));
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i)
       if (high[i] >= floor) {
         const uint32_t at = atomicAdd(&sh.n_vec, 1u);
-        if (at < kCap) sh.vec[at] = v0 + i * kTopThreads;
+        if (at < kNoted) sh.vec[at] = v0 + i * kTopThreads;
       }
   }
   int n = 0;
   if (p.top > 0) {
     best = fmaxf(best, z_tail);
-    floor = floor_of<T>(kth_ordinal<T>(ordinal(best), p.top, sh.pick2));  // (barriers: the vectors are noted)
+    floor = floor_of<T>(kth_ordinal<T>(ordinal(best), p.top, p.top / 4, sh.pick2));  // (barriers: the vectors are noted)
     auto push = [&](float z, int index) {
       if (z >= floor) {
         const uint32_t at = atomicAdd(&sh.n_cand, 1u);
@@ -493,8 +530,11 @@ __global__ void __launch_bounds__(kTopThreads, 1024 / kTopThreads) top_kernel(co
     };
     if (tid < part.head) push(z_head, tid);
     if (tid < part.tail) push(z_tail, part.n - part.tail + tid);
-    for (int k = tid; k < min(kCap, (int)sh.n_vec); k += kTopThreads) {
-      const int at = sh.vec[k];
+    // (too many noted -- a row that rises: all vectors, once more)
+    const bool all = sh.n_vec > kNoted;
+    const int noted = all ? part.vecs : (int)sh.n_vec;
+    for (int k = tid; k < noted; k += kTopThreads) {
+      const int at = all ? k : sh.vec[k];
       const Vec v = load_vec(part.body() + (size_t)at * kVecBytes);
       uint32_t bits = not_below<T>(v, floor);
 #pragma unroll 1
@@ -506,9 +546,13 @@ __global__ void __launch_bounds__(kTopThreads, 1024 / kTopThreads) top_kernel(co
   }
   a = block_sums<kTopThreads>(a, sh.red);  // (a barrier: the candidates are there)
   if (p.top > 0) {
+    const int found = (int)sh.n_cand;
+    if (found > kCap) select_top<T>(part, p.top, sh);
+    if (found < min(p.top, part.n)) {
+      __syncthreads();  // (all have read the number)
+      add_masked<T>(part, p.top - found, sh);
+    }
     n = (int)sh.n_cand;
-    const int places = min(p.top, part.n);
-    if (n > kCap || n < places || sh.n_vec > kCap) n = select_top<T>(part, places, sh);
   }
   if (parts > 1) {
     cluster_wait();
@@ -852,7 +896,7 @@ extern "C" int mrl_top_logprobs(const void* logits, int32_t dtype, int64_t N, in
   const TopArgs a{logits, ld, V, ids, mask, temperature, scale_of(temperature), top, logp, lse, entropy, top_logp, top_ids, status};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool bf16 = dtype == MRL_BF16, ent = entropy != nullptr;
-  const int parts = parts_of(N, (long long)V * (bf16 ? 2 : 4), 1024 / kTopThreads);
+  const int parts = parts_of(N, (long long)V * (bf16 ? 2 : 4), kTopCtas);
   mrl_profile_before(st, "top_kernel");
   const int rc = launch_rows(bf16 ? (ent ? top_kernel<__nv_bfloat16, true> : top_kernel<__nv_bfloat16, false>)
                                   : (ent ? top_kernel<float, true> : top_kernel<float, false>), N, parts, kTopThreads,
