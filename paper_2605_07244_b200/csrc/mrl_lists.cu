@@ -5,6 +5,8 @@
 // leaves float32 (rows masked throughout with the type's lowest value): those are summed again against their largest logit itself.
 #include <float.h>
 
+#include <type_traits>
+
 #include "mrl_common.cuh"
 
 namespace {
@@ -87,7 +89,7 @@ int parts_of(long long N, long long row_bytes, int ctas_per_sm) {
 }
 
 template <typename... Params>
-int launch_rows(void (*kernel)(Params...), long long N, int parts, int threads, size_t smem, bool behind, cudaStream_t st, Params... args) {
+int launch_rows(void (*kernel)(Params...), long long N, int parts, int threads, size_t smem, bool behind, cudaStream_t st, const Params&... args) {
   cudaLaunchAttribute attr[2]{};
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)parts;
@@ -620,8 +622,9 @@ struct DistillArgs {
   int32_t* status;
   uint8_t* rowstat;     // [N] kRow*
   int2* counts;         // [n_counts] valid and refused rows
-  int n_counts;
+  int n_counts;         // of `counts` as the row kernel reads them: sums of up to 32 CTAs of the check each
   double* term;         // [N] weight_t KL_t
+  int bit_words, park_slots;  // shared memory of the row kernel
 };
 
 // A warp per row: is its list one to learn from?  The entries stay in registers, four a lane; a token twice shows when every entry
@@ -629,6 +632,7 @@ struct DistillArgs {
 __global__ void __launch_bounds__(kListThreads) list_check_kernel(const DistillArgs p) {
   __shared__ int2 part[kListThreads / 32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  let_next_start();
   int2 n{0, 0};
   for (int r = warp; r < kListRows; r += kListThreads / 32) {
     const long long row = (long long)blockIdx.x * kListRows + r;
@@ -682,7 +686,7 @@ __global__ void __launch_bounds__(kListThreads) list_check_kernel(const DistillA
   }
 }
 
-// Valid rows of the call, for the denominator: the counts of all CTAs of the check, summed by a block (or one count, summed before).
+// Valid and refused rows of the call
 __device__ __forceinline__ int2 sum_counts(const int2* counts, int n, int2* red) {
   int2 a{0, 0};
   for (int i = threadIdx.x; i < n; i += blockDim.x) {
@@ -702,6 +706,22 @@ __device__ __forceinline__ int2 sum_counts(const int2* counts, int n, int2* red)
   return a;
 }
 
+// The counts of kListRows rows each added up to kCounts at most, so that the CTAs of the rows have few to read
+constexpr int kCounts = 32;
+__global__ void __launch_bounds__(1024) counts_kernel(const int2* __restrict__ from, int n, int each, int2* __restrict__ to) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  let_next_start();
+  wait_for_previous();
+  int2 a{0, 0};
+  for (int i = warp * each + lane; i < min(n, (warp + 1) * each); i += 32) {
+    a.x += from[i].x;
+    a.y += from[i].y;
+  }
+  a.x = __reduce_add_sync(0xffffffffu, a.x);
+  a.y = __reduce_add_sync(0xffffffffu, a.y);
+  if (lane == 0) to[warp] = a;
+}
+
 // Sum over the block in a fixed order.
 __device__ __forceinline__ double block_sum(double v, double* red) {
 #pragma unroll
@@ -714,125 +734,368 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
   return v;
 }
 
+// Listed tokens and rest of a row are told apart by a bit for each element in shared memory: a vector's bits are one word, hardly ever other than 0.  Pass 1
+// sums the rest (the listed tokens' logits are at hand from the start), thread k < 128 then works on place k of the list in float64, and pass 2 writes
+// of_rest * 2^(z c - m) everywhere but at the listed tokens, which come last.  As in the policy loss's kernel the row is read from HBM once: pass 1 walks it from
+// its end, the group read last stays in registers, the first ones are parked in shared memory, the rest comes from L2.
+constexpr int kDistillUnroll = 4;
+// Shared memory of a CTA: bits, parked vectors, staging of outputs that start off 16 bytes from their inputs.  What it leaves is L1, which holds the
+// loads in flight.
+constexpr size_t kDistillSmem = 68 * 1024;
+constexpr uint32_t kStageRow = kVecBytes * 32, kStageBytes = kWarps * kStageRow;
 constexpr double kNoRest = -700.0;  // ln p_r below which the learner gives the rest nothing: masks, of -inf or of the type's lowest value
+
+struct DistillShared {
+  Sums part[kMaxParts], red[kWarps];
+  double sum[3][2][kTop / 32];
+  float high[2][kTop / 32];
+  float of_rest, m;
+  int low;
+  uint32_t head_bits, tail_bits;
+  int ids[kTop];
+};
+
+// Two sums over the 128 threads of a list, in a fixed order
+__device__ __forceinline__ void list_barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void list_sums(double& a, double& b, double (*red)[kTop / 32]) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    a += __shfl_xor_sync(0xffffffffu, a, o);
+    b += __shfl_xor_sync(0xffffffffu, b, o);
+  }
+  if ((threadIdx.x & 31) == 0) red[0][threadIdx.x >> 5] = a, red[1][threadIdx.x >> 5] = b;
+  list_barrier();
+  a = (red[0][0] + red[0][1]) + (red[0][2] + red[0][3]);
+  b = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+}
 
 struct RowResult {
   double kl, at;    // KL_t; T dKL/dz of this thread's listed token
   double of_rest;   // T dKL/dz_v = of_rest * softmax over the rest (v)
 };
 
-// A row's KL and gradient factors from its list (thread k holds place k) and the sums over the rest, in float64.  Called by the block.
-__device__ RowResult distill_row(bool used, float z, float l, Totals rest, float c, const mrl_distill_params& dp, double* red) {
+// A row's KL and gradient factors from its list (thread k < 128 holds place k) and the sums over the rest, in float64
+__device__ RowResult distill_row(bool used, float z, float l, Totals rest, float c, const mrl_distill_params& dp, DistillShared& sh) {
   const double nat = 1.0 / ((double)c * (double)dp.temperature);
-  float zs = used ? fmaxf(z, -FLT_MAX) : -FLT_MAX;
+  float zs = used ? fmaxf(z, -FLT_MAX) : -FLT_MAX, ls = used ? l : -FLT_MAX;
   if (used && z != z) zs = INFINITY;  // (NaN: inf - inf below)
-  __shared__ float zred[32];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) zs = fmaxf(zs, __shfl_xor_sync(0xffffffffu, zs, o));
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) zred[threadIdx.x >> 5] = zs;
-  __syncthreads();
-  const bool any_rest = rest.s != 0.f;
-  for (int k = 0; k < (int)(blockDim.x >> 5); ++k) zs = fmaxf(zs, zred[k]);
-  double m = (double)zs * (double)c;  // (NaN and +inf stay what they are)
+  for (int o = 16; o > 0; o >>= 1) {
+    zs = fmaxf(zs, __shfl_xor_sync(0xffffffffu, zs, o));
+    ls = fmaxf(ls, __shfl_xor_sync(0xffffffffu, ls, o));
+  }
+  if ((threadIdx.x & 31) == 0) sh.high[0][threadIdx.x >> 5] = zs, sh.high[1][threadIdx.x >> 5] = ls;
+  list_barrier();
+#pragma unroll
+  for (int k = 0; k < kTop / 32; ++k) {
+    zs = fmaxf(zs, sh.high[0][k]);
+    ls = fmaxf(ls, sh.high[1][k]);
+  }
+  const bool event = dp.rest == MRL_REST_EVENT, any_rest = rest.s != 0.f;
+  double m = (double)zs * (double)c;  // (+inf stays what it is)
   if (any_rest) m = fmax(m, rest.x0);
   const double x = used ? ((double)z * (double)c - m) * nat : 0.0;
   const double in_rest = any_rest ? (double)rest.s * exp((rest.x0 - m) * nat) : 0.0;
-  const double total = block_sum(used ? exp(x) : 0.0, red) + in_rest;
+  const double d = event ? (double)l : (double)l - (double)ls;  // (without a rest any logits will do: from the largest)
+  double q = used ? exp(d) : 0.0, total = used ? exp(x) : 0.0, mass = q;
+  list_sums(total, mass, sh.sum[0]);
+  total += in_rest;
   const double ln_total = total > 0.0 ? log(total) : NAN;
   const double ln_p = x - ln_total, p = used ? exp(ln_p) : 0.0;
   const double ln_p_rest = any_rest ? log((double)rest.s) + (rest.x0 - m) * nat - ln_total : -INFINITY;
   const bool has_rest = !(ln_p_rest < kNoRest);
   const double p_rest = has_rest ? exp(ln_p_rest) : 0.0;
-  RowResult r;
-  if (dp.rest == MRL_REST_EVENT) {
-    const double q = used ? exp((double)l) : 0.0, mass = block_sum(q, red);
-    const double q_rest = has_rest ? fmax(1.0 - mass, (double)dp.rest_floor) : 0.0;
-    if (dp.direction == MRL_DISTILL_FORWARD) {
-      r.kl = block_sum(q > 0.0 ? q * ((double)l - ln_p) : 0.0, red) + (q_rest > 0.0 ? q_rest * (log(q_rest) - ln_p_rest) : 0.0);
-      r.at = (mass + q_rest) * p - q;
-      r.of_rest = has_rest ? (mass + q_rest) * p_rest - q_rest : 0.0;
-    } else {
-      const double ratio = ln_p - (double)l, ratio_rest = has_rest ? ln_p_rest - log(q_rest) : 0.0;
-      r.kl = block_sum(used && p != 0.0 ? p * ratio : 0.0, red) + (p_rest != 0.0 ? p_rest * ratio_rest : 0.0);
-      r.at = p != 0.0 ? p * (ratio - r.kl) : 0.0;
-      r.of_rest = p_rest != 0.0 ? p_rest * (ratio_rest - r.kl) : 0.0;
-    }
+  double term = 0.0, none = 0.0, q_rest = 0.0, ratio = 0.0;
+  if (!event) {
+    const double ln_q = d - log(mass);
+    q = used ? exp(ln_q) : 0.0;
+    term = q > 0.0 ? q * (ln_q - ln_p) : 0.0;
   } else {
-    __syncthreads();
-    float lm = used ? l : -FLT_MAX;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) lm = fmaxf(lm, __shfl_xor_sync(0xffffffffu, lm, o));
-    if ((threadIdx.x & 31) == 0) zred[threadIdx.x >> 5] = lm;
-    __syncthreads();
-    for (int k = 0; k < (int)(blockDim.x >> 5); ++k) lm = fmaxf(lm, zred[k]);
-    const double d = (double)l - (double)lm, mass = block_sum(used ? exp(d) : 0.0, red);
-    const double ln_q = d - log(mass), q = used ? exp(ln_q) : 0.0;
-    r.kl = block_sum(q > 0.0 ? q * (ln_q - ln_p) : 0.0, red);
+    q_rest = has_rest ? fmax(1.0 - mass, (double)dp.rest_floor) : 0.0;
+    ratio = ln_p - (double)l;
+    if (dp.direction == MRL_DISTILL_FORWARD) term = q > 0.0 ? -q * ratio : 0.0;
+    else term = used && p != 0.0 ? p * ratio : 0.0;
+  }
+  list_sums(term, none, sh.sum[1]);
+  RowResult r;
+  r.kl = term;
+  if (!event) {
     r.at = p - q;
     r.of_rest = p_rest;
+  } else if (dp.direction == MRL_DISTILL_FORWARD) {
+    r.kl += q_rest > 0.0 ? q_rest * (log(q_rest) - ln_p_rest) : 0.0;
+    r.at = (mass + q_rest) * p - q;
+    r.of_rest = has_rest ? (mass + q_rest) * p_rest - q_rest : 0.0;
+  } else {
+    const double ratio_rest = has_rest ? ln_p_rest - log(q_rest) : 0.0;
+    r.kl += p_rest != 0.0 ? p_rest * ratio_rest : 0.0;
+    r.at = p != 0.0 ? p * (ratio - r.kl) : 0.0;
+    r.of_rest = p_rest != 0.0 ? p_rest * (ratio_rest - r.kl) : 0.0;
   }
   return r;
 }
 
-// One CTA per row; a bit for each listed token in shared memory.
+// a vector that pass 2 wants again, if L2 can keep it
+__device__ __forceinline__ Vec load_vec_keep(const void* p) {
+  Vec v;
+  asm volatile("ld.global.L1::no_allocate.L2::evict_last.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]), "=r"(v.w[4]), "=r"(v.w[5]), "=r"(v.w[6]), "=r"(v.w[7])
+               : "l"(p));
+  return v;
+}
+__device__ __forceinline__ void store_vec(void* p, const Vec& v) {  // 32 bytes on 32
+  asm volatile("st.global.L2::evict_first.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v.w[0]), "r"(v.w[1]), "r"(v.w[2]),
+               "r"(v.w[3]), "r"(v.w[4]), "r"(v.w[5]), "r"(v.w[6]), "r"(v.w[7])
+               : "memory");
+}
+// A thread's own vectors in shared memory, as two planes of 16-byte halves
+__device__ __forceinline__ void park(uint4* planes, int slots, int slot, const Vec& v) {
+  planes[slot] = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+  planes[slots + slot] = make_uint4(v.w[4], v.w[5], v.w[6], v.w[7]);
+}
+__device__ __forceinline__ Vec parked(const uint4* planes, int slots, int slot) {
+  const uint4 a = planes[slot], b = planes[slots + slot];
+  return Vec{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+}
+// -inf in place of the elements whose bits are set
 template <typename T>
-__global__ void __launch_bounds__(kThreads) distill_kernel(const DistillArgs p) {
-  extern __shared__ uint32_t listed[];
-  __shared__ Sums red[kWarps];
-  __shared__ double red64[kWarps];
-  __shared__ int2 redc[kWarps];
-  const long long row = blockIdx.x;
-  const T* z = static_cast<const T*>(p.logits) + row * p.ld;
-  T* dz = p.dlogits != nullptr ? static_cast<T*>(p.dlogits) + row * p.ld_out : nullptr;
-  const int valid = p.dp.denominator > 0.0 ? 1 : sum_counts(p.counts, p.n_counts, redc).x;
-  if (p.rowstat[row] != kRowValid) {
-    if (dz != nullptr)
-      for (int v = threadIdx.x; v < p.V; v += kThreads) store_f(dz + v, 0.f);
-    if (threadIdx.x == 0) {
+__device__ __forceinline__ void strike_out(Vec& v, uint32_t bits) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    if constexpr (sizeof(T) == 2) {
+      if (bits & (1u << (2 * j))) v.w[j] = (v.w[j] & 0xffff0000u) | 0xff80u;
+      if (bits & (2u << (2 * j))) v.w[j] = (v.w[j] & 0xffffu) | 0xff800000u;
+    } else {
+      if (bits & (1u << j)) v.w[j] = 0xff800000u;
+    }
+  }
+}
+
+// The 32 vectors of a warp -- `count` of them -- to an address that is a multiple of the element only: through shared memory, in words as they lie in the output
+template <typename T>
+__device__ __forceinline__ void store_shifted(char* out, const Vec& v, int count, uint32_t* stage) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
+  uint4* mine = reinterpret_cast<uint4*>(stage) + 2 * lane;
+  mine[0] = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+  mine[1] = make_uint4(v.w[4], v.w[5], v.w[6], v.w[7]);
+  __syncwarp();
+  const int words = count * 8;
+  if (sizeof(T) == 4 || (reinterpret_cast<uintptr_t>(out) & 3) == 0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i * 32 + lane < words) __stcs(reinterpret_cast<uint32_t*>(out) + i * 32 + lane, stage[i * 32 + lane]);
+  } else {  // odd elements of bf16: word i of the output is the upper half of word i and the lower one of word i + 1
+    uint32_t* odd = reinterpret_cast<uint32_t*>(out + 2);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int at = i * 32 + lane;
+      if (at + 1 < words) __stcs(odd + at, __funnelshift_r(stage[at], stage[at + 1], 16));
+    }
+    if (lane == 0 && words > 0) {
+      reinterpret_cast<uint16_t*>(out)[0] = (uint16_t)stage[0];
+      reinterpret_cast<uint16_t*>(out)[2 * words - 1] = (uint16_t)(stage[words - 1] >> 16);
+    }
+  }
+}
+
+template <typename T>
+__device__ void zero_part(T* out, int n) {
+  const int head = min(n, (int)((0u - (uint32_t)reinterpret_cast<uintptr_t>(out)) & 15) / (int)sizeof(T));
+  const int pieces = (n - head) / (16 / (int)sizeof(T)), tail0 = head + pieces * (16 / (int)sizeof(T));
+  for (int i = threadIdx.x; i < pieces; i += kThreads) __stcs(reinterpret_cast<uint4*>(out + head) + i, make_uint4(0, 0, 0, 0));
+  if ((int)threadIdx.x < head) store_f(out + threadIdx.x, 0.f);
+  if (tail0 + (int)threadIdx.x < n) store_f(out + tail0 + threadIdx.x, 0.f);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillArgs p) {
+  extern __shared__ uint4 dyn[];
+  __shared__ DistillShared sh;
+  const int tid = threadIdx.x;
+  int parts, rank;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const long long row = blockIdx.x / (unsigned)parts;
+  const T* zrow = static_cast<const T*>(p.logits) + row * p.ld;
+  const Part<T> part(zrow, p.V, parts, rank);
+  T* out = p.dlogits != nullptr ? static_cast<T*>(p.dlogits) + row * p.ld_out + part.first : nullptr;
+  let_next_start();
+  wait_for_previous();
+  if (p.rowstat[row] != kRowValid) {  // (all CTAs of the row)
+    if (out != nullptr) zero_part(out, part.n);
+    if (tid == 0 && rank == 0) {
       p.term[row] = 0.0;
       if (p.row_kl != nullptr) p.row_kl[row] = 0.f;
     }
     return;
   }
-  for (int i = threadIdx.x; i < (p.V + 31) / 32; i += kThreads) listed[i] = 0;
-  __syncthreads();
-  const int k = threadIdx.x;
-  int id = k < p.top ? p.top_ids[row * p.top + k] : -1;
-  const float l = id >= 0 ? p.top_logp[row * p.top + k] : -INFINITY;
+  // shared memory: bits of the body's vectors | parked vectors | staging
+  using Bits = typename std::conditional<sizeof(T) == 2, uint16_t, uint8_t>::type;
+  Bits* bits = reinterpret_cast<Bits*>(dyn);
+  uint4* planes = dyn + p.bit_words / 4;
+  uint32_t* stage = reinterpret_cast<uint32_t*>(planes + 2 * p.park_slots) + (tid >> 5) * (kStageRow / 4);
+  for (int i = tid; i < p.bit_words / 4; i += kThreads) dyn[i] = make_uint4(0, 0, 0, 0);
+  if (tid == 0) sh.head_bits = sh.tail_bits = 0;
+  int id = tid < p.top ? p.top_ids[row * p.top + tid] : -1;
+  const float l = id >= 0 ? p.top_logp[row * p.top + tid] : -INFINITY;
   if (l == -INFINITY) id = -1;
-  const float mine = id >= 0 ? load_f<T>(z + id) : 0.f;
-  if (id >= 0) atomicOr(&listed[id >> 5], 1u << (id & 31));
+  const float mine = id >= 0 ? load_f<T>(zrow + id) : 0.f;
+  const float z_head = tid < part.head ? load_f<T>(part.z + tid) : -INFINITY;
+  const float z_tail = tid < part.tail ? load_f<T>(part.z + part.n - part.tail + tid) : -INFINITY;
+  if (tid < kTop) sh.ids[tid] = id;
   __syncthreads();
-  Sums sums = sums_empty();
-  for (int v = threadIdx.x; v < p.V; v += kThreads)
-    if (!((listed[v >> 5] >> (v & 31)) & 1u)) sums_add(sums, load_f<T>(z + v), p.c);
-  sums = block_sums<kThreads>(sums, red);
-  Totals rest{(double)sums.m, sums.s, 0.f};
-  const bool low = rest.s == 0.f;
-  if (low) rest = low_sums<T, kThreads>(z, p.V, p.c, red, [](int v) { return !((listed[v >> 5] >> (v & 31)) & 1u); });
-  const RowResult r = distill_row(id >= 0, mine, l, rest, p.c, p.dp, red64);
-  const float w = p.weight != nullptr ? p.weight[row] : 1.f;
-  if (threadIdx.x == 0) {
-    p.term[row] = w != 0.f ? (double)w * r.kl : 0.0;
-    if (p.row_kl != nullptr) p.row_kl[row] = (float)r.kl;
+  if (parts > 1) cluster_arrive();  // "here": its shared memory may be written to
+  const int rel = id - part.first;  // the listed token in this part
+  const bool owner = id >= 0 && rel >= 0 && rel < part.n;
+  if (owner) {
+    const int at = rel - part.head;
+    if (at < 0) atomicOr(&sh.head_bits, 1u << rel);
+    else if (at >= part.vecs * kVecElems<T>) atomicOr(&sh.tail_bits, 1u << (at - part.vecs * kVecElems<T>));
+    else atomicOr(reinterpret_cast<uint32_t*>(dyn) + (at >> 5), 1u << (at & 31));
   }
-  if (dz == nullptr) return;
-  const double denominator = p.dp.denominator > 0.0 ? p.dp.denominator : (double)valid;
-  const double scale = (double)p.dp.coeff * w / (denominator * p.dp.temperature);
-  const float of_rest = scale != 0.0 && rest.s != 0.f ? (float)(r.of_rest * scale / rest.s) : 0.f;
-  for (int v = threadIdx.x; v < p.V; v += kThreads)
-    if (!((listed[v >> 5] >> (v & 31)) & 1u)) {
-      const float e = low ? ex2_approx((float)((double)load_f<T>(z + v) * (double)p.c - rest.x0)) : ex2_approx(fmaf(load_f<T>(z + v), p.c, -sums.m));
-      store_f(dz + v, scale != 0.0 && of_rest != 0.f ? e * of_rest : 0.f);
+  __syncthreads();
+  const bool head_on = tid < part.head && !((sh.head_bits >> tid) & 1u), tail_on = tid < part.tail && !((sh.tail_bits >> tid) & 1u);
+  Sums a = sums_empty();
+  if (head_on) sums_add(a, z_head, p.c);
+  if (tail_on) sums_add(a, z_tail, p.c);
+
+  // ---- pass 1, from the last group (the ragged one) to the first, which is a full one wherever there are two
+  constexpr int kGroup = kThreads * kDistillUnroll;
+  const char* in = part.body() + (size_t)tid * kVecBytes;
+  const int last = part.vecs > 0 ? (part.vecs - 1) / kGroup * kGroup : -kGroup;
+  Vec v[kDistillUnroll];
+#pragma unroll 1
+  for (int base = last; base >= 0; base -= kGroup) {
+    const int slot0 = (last - base) / kDistillUnroll;  // of the parked vectors: kThreads a step of the unrolled loop
+#pragma unroll
+    for (int i = 0; i < kDistillUnroll; ++i) {
+      const int at = base + i * kThreads;
+      v[i] = at + tid < part.vecs ? load_vec_keep(in + (size_t)at * kVecBytes) : no_vec<T>();
     }
-  if (id >= 0) store_f(dz + id, scale != 0.0 ? (float)(r.at * scale) : 0.f);
+#pragma unroll
+    for (int i = 0; i < kDistillUnroll; ++i) {
+      const int at = base + i * kThreads + tid;
+      if (at < part.vecs) {
+        const uint32_t some = bits[at];
+        if (some != 0) strike_out<T>(v[i], some);
+        const int slot = slot0 * kDistillUnroll + i * kThreads + tid;
+        if (slot < p.park_slots) park(planes, p.park_slots, slot, v[i]);
+      }
+    }
+    float high = vec_max<T>(v[0]);
+#pragma unroll
+    for (int i = 1; i < kDistillUnroll; ++i) high = fmaxf(high, vec_max<T>(v[i]));
+    const float m = fmaxf(a.m, high * p.c);
+    if (m > a.m) a = sums_raise(a, m);
+    const f2 c2 = make_f2(p.c, p.c), m2 = make_f2(-a.m, -a.m);
+    Sums2 more{0, 0};
+#pragma unroll
+    for (int i = 0; i < kDistillUnroll; ++i)
+      if (base + i * kThreads + tid < part.vecs) sums_add<T, false, false>(more, v[i], c2, m2);
+    const float2 s = split_f2(more.s);
+    a.s += s.x + s.y;
+  }
+  a = block_sums<kThreads>(a, sh.red);
+  if (parts > 1) {
+    cluster_wait();
+    if (tid < parts) *in_cta(&sh.part[rank], tid) = a;
+    cluster_arrive();
+    cluster_wait();
+    a = sh.part[0];
+    for (int k = 1; k < parts; ++k) a = sums_merge(a, sh.part[k]);
+  }
+  Totals rest{(double)a.m, a.s, 0.f};
+  const bool low = a.s == 0.f;
+  if (low) {
+    rest = low_sums<T, kThreads>(zrow, p.V, p.c, sh.red, [&](int v) {
+      bool keep = true;
+      for (int k = 0; k < p.top; ++k) keep &= sh.ids[k] != v;
+      return keep;
+    });
+  }
+
+  // ---- the list
+  double scale = 0.0, at_listed = 0.0;
+  if (tid < kTop) {
+    const RowResult r = distill_row(id >= 0, mine, l, rest, p.c, p.dp, sh);
+    const float w = p.weight != nullptr ? p.weight[row] : 1.f;
+    double denominator = p.dp.denominator;
+    if (!(denominator > 0.0)) {
+      int n = 0;
+      for (int i = tid & 31; i < p.n_counts; i += 32) n += p.counts[i].x;
+      denominator = (double)__reduce_add_sync(0xffffffffu, n);
+    }
+    scale = (double)p.dp.coeff * w / (denominator * p.dp.temperature);
+    at_listed = scale != 0.0 ? r.at * scale : 0.0;
+    if (tid == 0) {
+      sh.of_rest = scale != 0.0 && rest.s != 0.f ? (float)(r.of_rest * scale / rest.s) : 0.f;
+      if (rank == 0) {
+        p.term[row] = w != 0.f ? (double)w * r.kl : 0.0;
+        if (p.row_kl != nullptr) p.row_kl[row] = (float)r.kl;
+      }
+    }
+  }
+  if (out == nullptr) return;
+  __syncthreads();
+  const float of_rest = sh.of_rest;
+  if (of_rest == 0.f) {
+    zero_part(out, part.n);
+  } else if (low) {
+    for (int i = tid; i < part.n; i += kThreads)
+      store_f(out + i, ex2_approx((float)((double)load_f<T>(part.z + i) * (double)p.c - rest.x0)) * of_rest);
+  } else {
+    // ---- pass 2: the first group from registers, the others as pass 1 read them last to first
+    const float m = -a.m;
+    char* body_out = reinterpret_cast<char*>(out + part.head);
+    const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(body_out) & (kVecBytes - 1);
+#pragma unroll 1
+    for (int base = 0; base <= last; base += kGroup) {
+      if (base != 0) {
+        const int slot0 = (last - base) / kDistillUnroll;
+#pragma unroll
+        for (int i = 0; i < kDistillUnroll; ++i) {
+          const int at = base + i * kThreads, slot = slot0 * kDistillUnroll + i * kThreads + tid;
+          v[i] = at + tid >= part.vecs ? no_vec<T>() : slot < p.park_slots ? parked(planes, p.park_slots, slot) : load_vec(in + (size_t)at * kVecBytes);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kDistillUnroll; ++i) {
+        Vec r;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if constexpr (sizeof(T) == 2)
+            r.w[j] = pack_bf16x2(ex2_approx(fmaf(bf16lo_to_f32(v[i].w[j]), p.c, m)) * of_rest, ex2_approx(fmaf(bf16hi_to_f32(v[i].w[j]), p.c, m)) * of_rest);
+          else
+            r.w[j] = __float_as_uint(ex2_approx(fmaf(__uint_as_float(v[i].w[j]), p.c, m)) * of_rest);
+        }
+        const int at = base + i * kThreads + tid;
+        char* dst = body_out + (size_t)at * kVecBytes;
+        if (off == 0) {
+          if (at < part.vecs) store_vec(dst, r);
+        } else if (off == 16) {
+          if (at < part.vecs) {
+            __stcs(reinterpret_cast<uint4*>(dst), make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]));
+            __stcs(reinterpret_cast<uint4*>(dst) + 1, make_uint4(r.w[4], r.w[5], r.w[6], r.w[7]));
+          }
+        } else {
+          const int count = max(0, min(32, part.vecs - (at - (tid & 31))));
+          store_shifted<T>(dst - (size_t)(tid & 31) * kVecBytes, r, count, stage);
+        }
+      }
+    }
+    if (tid < part.head) store_f(out + tid, ex2_approx(fmaf(z_head, p.c, m)) * of_rest);
+    if (tid < part.tail) store_f(out + part.n - part.tail + tid, ex2_approx(fmaf(z_tail, p.c, m)) * of_rest);
+  }
+  __syncthreads();  // the listed tokens over what stands in their places
+  if (owner) store_f(out + rel, (float)at_listed);
 }
 
 // Sums of the rows' terms and counts, one CTA, in a fixed order.
 __global__ void __launch_bounds__(1024) distill_finish_kernel(const DistillArgs p) {
   __shared__ double red[32];
   __shared__ int2 redc[32];
+  wait_for_previous();
   double v = 0.0;
   for (long long i = threadIdx.x; i < p.N; i += 1024) v += p.term[i];
   v = block_sum(v, red);
@@ -851,7 +1114,7 @@ __global__ void __launch_bounds__(1024) distill_finish_kernel(const DistillArgs 
 
 struct DistillWs {
   uint8_t* rowstat;
-  int2* counts;
+  int2 *counts, *sums;
   double* term;
   size_t bytes;
 };
@@ -860,6 +1123,7 @@ DistillWs carve(void* ws, long long N) {
   DistillWs w;
   w.term = c.take<double>((size_t)N);
   w.counts = c.take<int2>((size_t)((N + kListRows - 1) / kListRows));
+  w.sums = c.take<int2>(kCounts);
   w.rowstat = c.take<uint8_t>((size_t)N);
   w.bytes = c.off;
   return w;
@@ -938,24 +1202,41 @@ extern "C" int mrl_distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64
   const DistillWs w = carve(workspace, N);
   const int blocks = (int)((N + kListRows - 1) / kListRows);
   DistillArgs a{logits, dlogits, ld, ld_out, N, V, top, top_ids, top_logp, mask, row_weight, *dp, scale_of(dp->temperature), row_kl,
-                loss, reinterpret_cast<long long*>(stats), status, w.rowstat, w.counts, blocks, w.term};
+                loss, reinterpret_cast<long long*>(stats), status, w.rowstat, w.counts, blocks, w.term, 0, 0};
   list_check_kernel<<<blocks, kListThreads, 0, st>>>(a);
   MRL_CUDA_OK(cudaGetLastError());
-  const size_t smem = (size_t)(V + 31) / 32 * 4;
+  if (blocks > kCounts) {
+    MRL_CUDA_OK(mrl_launch_behind(counts_kernel, 1, 1024, st, w.counts, blocks, (blocks + kCounts - 1) / kCounts, w.sums));
+    a.counts = w.sums;
+    a.n_counts = kCounts;
+  }
+  // Rows of 512 KB or more are shared by two CTAs, so that the rows in flight still fit L2 between the passes.
+  int parts = parts_of(N, (long long)V * elem, 2);
+  if (parts == 1 && (long long)V * elem >= 512 * 1024) parts = 2;
+  const long long off = static_cast<const char*>(dlogits) - static_cast<const char*>(logits);
+  const bool shifted = dlogits != nullptr && (off % 16 != 0 || (N > 1 && (ld_out - ld) * elem % 16 != 0));
+  a.bit_words = (int)mrl_align_up((size_t)((V + parts - 1) / parts + 16 + 31) / 32, 4);
+  const size_t fixed = (size_t)a.bit_words * 4 + (shifted ? kStageBytes : 0);
+  if (dlogits != nullptr && fixed < kDistillSmem) a.park_slots = (int)((kDistillSmem - fixed) / (kThreads * kVecBytes)) * kThreads;
+  const size_t smem = fixed + (size_t)a.park_slots * kVecBytes;
+  using Kernel = void (*)(const DistillArgs);
+  const Kernel kernel = dtype == MRL_BF16 ? distill_kernel<__nv_bfloat16> : distill_kernel<float>;
   static std::atomic<uint64_t> attr_done;
-  const int rc = mrl_once_per_device(attr_done, [] {
-    const cudaError_t e = cudaFuncSetAttribute(distill_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, 1 << 17);
-    return e != cudaSuccess ? e : cudaFuncSetAttribute(distill_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, 1 << 17);
+  int rc = mrl_once_per_device(attr_done, [] {
+    // the carve-out that two CTAs an SM need, as a percentage of the 228 KB it can give: the rest stays L1
+    constexpr int kCarve = (int)((2 * (kDistillSmem + 4096) * 100 + 228 * 1024 - 1) / (228 * 1024));
+    for (const Kernel k : {static_cast<Kernel>(distill_kernel<__nv_bfloat16>), static_cast<Kernel>(distill_kernel<float>)}) {
+      cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+      if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, kCarve);
+      if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
   });
   if (rc != MRL_OK) return rc;
   mrl_profile_before(st, "distill_kernel");
-  if (dtype == MRL_BF16)
-    distill_kernel<__nv_bfloat16><<<(unsigned)N, kThreads, smem, st>>>(a);
-  else
-    distill_kernel<float><<<(unsigned)N, kThreads, smem, st>>>(a);
+  rc = launch_rows(kernel, N, parts, kThreads, smem, true, st, a);
   mrl_profile_after(st);
-  MRL_CUDA_OK(cudaGetLastError());
-  distill_finish_kernel<<<1, 1024, 0, st>>>(a);
-  MRL_CUDA_OK(cudaGetLastError());
+  if (rc != MRL_OK) return rc;
+  MRL_CUDA_OK(mrl_launch_behind(distill_finish_kernel, 1, 1024, st, a));
   return MRL_OK;
 }

@@ -216,7 +216,24 @@ def test_slabs_with_one_denominator_are_the_whole_step():
         parts.append(run(cut, cut.view(-1), ids[a:b], logq[a:b], None, None, p, loss=loss, stats=stats))
     assert stats.tolist() == whole["stats"]
     assert abs(float(loss) - whole["loss"]) <= 4 * HALF * abs(whole["loss"])
-    # (few rows: the same number of CTAs a row in each call, so the same sums)
+    # Rows of 3,001 floats start on another address in a slab than in the whole, and a row's sum is taken in an order that goes by its address: either is
+    # within chain of the exact sum, as `check` has it, so the two are within twice that of one another (and of its rounding, and the slope's).
+    e = 2 * (chain(3001) + 8 * HALF) * kl_slack(z, ids, logq, 1.0, FLOOR)
+    kl = torch.cat([p["row_kl"] for p in parts])
+    assert bool(((kl - whole["row_kl"]).abs() <= e + 2 * HALF * kl.abs()).all())
+    ref = S.distill_loss(z.float(), ids, logq, None, None, 1.0, 1.0, True, True, FLOOR, 0.0)
+    off = (torch.cat([p["dz"] for p in parts]).double() - whole["dz"].double()).abs()
+    assert bool((off <= 4 * e[:, None] * ref["parts"] + 4 * HALF * ref["dlogits"].abs()).all())
+
+
+def test_slabs_of_aligned_rows_are_the_whole_step_bit_for_bit():
+    z, flat = rows(50, 3008, torch.float32, 2)
+    ids, logq = lists(z, 10, 1)
+    whole = run(z, flat, ids, logq, None, None, params("reverse"))
+    parts = []
+    for a, b in ((0, 17), (17, 18), (18, 50)):
+        cut = z[a:b].clone()
+        parts.append(run(cut, cut.view(-1), ids[a:b], logq[a:b], None, None, params("reverse", denominator=float(whole["stats"][0]))))
     assert torch.equal(torch.cat([p["row_kl"] for p in parts]), whole["row_kl"])
     assert torch.equal(torch.cat([p["dz"] for p in parts]), whole["dz"])
 
