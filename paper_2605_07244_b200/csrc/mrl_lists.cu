@@ -603,8 +603,34 @@ __global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArg
 }
 
 // ------------------------------------------------------------------------------------------ distillation
+// Three kernels.  list_kernel: which rows count, and what a row's list gives by itself.  distill_kernel: the rows of logits, the bulk of the work.  finish_kernel: the
+// gradient of the listed tokens, and the loss.
 constexpr int kRowOff = 0, kRowValid = 1, kRowRefused = 2;
-constexpr int kListThreads = 1024, kListRows = 64;  // rows of a CTA of the list check
+constexpr int kListThreads = 512, kListRows = kListThreads / 32;  // of a CTA of list_kernel: a warp per row
+constexpr int kPlaces = kTop / 32;                 // places of a lane
+
+// Of a row's list.  With x_k = z_k / T, xs the largest of them, e_k = exp(x_k - xs), q_k the teacher's probabilities:
+struct ListRecord {
+  double xs;      // in units of z c
+  double sum_e;   // sum e_k
+  double mass;    // sum q_k
+  double mixed;   // forward: sum q_k (ln q_k - (x_k - xs)); reverse: sum e_k ((x_k - xs) - ln q_k)
+  double q_rest, ln_q_rest;
+  double ln_one;  // ln q_k = top_logp_k - ln_one
+  // what the gradient of the rest needs, in float32, so that it is there soon
+  float zs;              // the largest listed logit
+  float sum_e_f, mass_f, q_rest_f;
+  float against, against_lo;  // reverse: ln q_rest + mixed / sum_e, in two floats
+  float weight;
+  int stat;       // kRow*
+};
+// Of a row, for its listed tokens: p_k = p_of_e e_k, ln p_k = (x_k - xs) + shift
+struct RowFactors {
+  double shift, kl;
+  double mass;    // forward: sum q_k + q_rest
+  double scale;   // coeff weight / (D T)
+  float p_of_e, of_rest;  // T dKL/dz_v = of_rest * softmax over the rest (v); rest_factor gives it sooner
+};
 
 struct DistillArgs {
   const void* logits;
@@ -617,19 +643,29 @@ struct DistillArgs {
   const float* weight;
   mrl_distill_params dp;
   float c;
+  double nat;            // 1 / (c T)
   float *row_kl, *loss;
   long long* stats;
   int32_t* status;
-  uint8_t* rowstat;     // [N] kRow*
-  int2* counts;         // [n_counts] valid and refused rows
-  int n_counts;         // of `counts` as the row kernel reads them: sums of up to 32 CTAs of the check each
-  double* term;         // [N] weight_t KL_t
-  int bit_words, park_slots;  // shared memory of the row kernel
+  ListRecord* records;   // [N]
+  float* z;              // [N, top] the listed tokens' logits (the gradient may be written over them)
+  RowFactors* factors;   // [N]
+  double* term;          // [N] weight_t KL_t
+  int2* counts;          // valid and refused rows: of kListRows rows each, or sums of those, kCounts at most
+  int n_counts;
+  int bit_words, park_slots;  // shared memory of distill_kernel
 };
 
-// A warp per row: is its list one to learn from?  The entries stay in registers, four a lane; a token twice shows when every entry
-// is compared with those of the other places, carried round the warp.
-__global__ void __launch_bounds__(kListThreads) list_check_kernel(const DistillArgs p) {
+__device__ __forceinline__ double warp_sum(double a) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+  return a;
+}
+
+// A row's list: is it one to learn from, and its sums?  The entries stay in registers, kPlaces a lane; a token twice shows when every entry is compared
+// with those of the other places, carried round the warp.
+template <typename T>
+__global__ void __launch_bounds__(kListThreads) list_kernel(const DistillArgs p) {
   __shared__ int2 part[kListThreads / 32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   let_next_start();
@@ -638,31 +674,37 @@ __global__ void __launch_bounds__(kListThreads) list_check_kernel(const DistillA
     const long long row = (long long)blockIdx.x * kListRows + r;
     if (row >= p.N) break;
     if (p.mask != nullptr && p.mask[row] == 0) {
-      if (lane == 0) p.rowstat[row] = kRowOff;
+      if (lane == 0) p.records[row].stat = kRowOff;
       continue;
     }
-    int id[kTop / 32];
+    int id[kPlaces];
+    float l[kPlaces], z[kPlaces];
     int bad = 0;
     bool any = false;
 #pragma unroll
-    for (int q = 0; q < kTop / 32; ++q) {
+    for (int q = 0; q < kPlaces; ++q) {
       const int k = q * 32 + lane;
       id[q] = k < p.top ? p.top_ids[row * p.top + k] : -1;
-      const float l = k < p.top && id[q] >= 0 ? p.top_logp[row * p.top + k] : -INFINITY;
-      if (!(l < INFINITY)) bad |= MRL_DEV_BAD_LIST;  // (NaN too)
-      if (l == -INFINITY) id[q] = -1;
+      l[q] = k < p.top ? p.top_logp[row * p.top + k] : -INFINITY;
+    }
+#pragma unroll
+    for (int q = 0; q < kPlaces; ++q) {
+      if (id[q] < 0) l[q] = -INFINITY;
+      if (!(l[q] < INFINITY)) bad |= MRL_DEV_BAD_LIST;  // (NaN too)
+      if (l[q] == -INFINITY) id[q] = -1;
       if (id[q] >= p.V) bad |= MRL_DEV_BAD_TOKEN_ID;
       any |= id[q] >= 0;
+      z[q] = id[q] >= 0 && id[q] < p.V ? load_f<T>(static_cast<const T*>(p.logits) + row * p.ld + id[q]) : 0.f;
     }
     const int used = (p.top + 31) / 32;
 #pragma unroll 1
     for (int o = 0; o < 32; ++o) {
 #pragma unroll
-      for (int q = 0; q < kTop / 32; ++q) {
+      for (int q = 0; q < kPlaces; ++q) {
         if (q >= used) break;
         const int other = __shfl_sync(0xffffffffu, id[q], (lane + o) & 31);
 #pragma unroll
-        for (int j = 0; j < kTop / 32; ++j)
+        for (int j = 0; j < kPlaces; ++j)
           if (other >= 0 && other == id[j] && !(o == 0 && j == q)) bad |= MRL_DEV_BAD_LIST;
       }
     }
@@ -671,39 +713,77 @@ __global__ void __launch_bounds__(kListThreads) list_check_kernel(const DistillA
     const int stat = bad != 0 ? kRowRefused : any ? kRowValid : kRowOff;
     n.x += stat == kRowValid;
     n.y += stat == kRowRefused;
-    if (lane == 0) {
-      p.rowstat[row] = (uint8_t)stat;
-      if (bad != 0 && p.status != nullptr) atomicOr(p.status, bad);
+    if (stat != kRowValid) {
+      if (lane == 0) {
+        p.records[row].stat = stat;
+        if (bad != 0 && p.status != nullptr) atomicOr(p.status, bad);
+      }
+      continue;
     }
+    float zs = -FLT_MAX, ls = -FLT_MAX;
+#pragma unroll
+    for (int q = 0; q < kPlaces; ++q)
+      if (id[q] >= 0) {
+        zs = z[q] == z[q] ? fmaxf(zs, z[q]) : INFINITY;  // (NaN: inf - inf below)
+        ls = fmaxf(ls, l[q]);
+      }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      zs = fmaxf(zs, __shfl_xor_sync(0xffffffffu, zs, o));
+      ls = fmaxf(ls, __shfl_xor_sync(0xffffffffu, ls, o));
+    }
+    const bool event = p.dp.rest == MRL_REST_EVENT, forward = p.dp.direction == MRL_DISTILL_FORWARD;
+    ListRecord rec{};
+    rec.xs = (double)zs * (double)p.c;
+    double x[kPlaces], e[kPlaces], q[kPlaces];
+#pragma unroll
+    for (int i = 0; i < kPlaces; ++i) {
+      x[i] = e[i] = q[i] = 0.0;
+      if (id[i] >= 0) {
+        x[i] = ((double)z[i] * (double)p.c - rec.xs) * p.nat;
+        e[i] = exp(x[i]);
+        q[i] = exp(event ? (double)l[i] : (double)l[i] - (double)ls);  // (without a rest any logits will do: from the largest)
+      }
+      rec.sum_e += e[i];
+      rec.mass += q[i];
+      if (i * 32 + lane < p.top) p.z[row * p.top + i * 32 + lane] = z[i];
+    }
+    rec.sum_e = warp_sum(rec.sum_e);
+    rec.mass = warp_sum(rec.mass);
+    rec.ln_one = event ? 0.0 : (double)ls + log(rec.mass);  // (scaled to 1)
+    const double to_one = event ? 1.0 : 1.0 / rec.mass;
+#pragma unroll
+    for (int i = 0; i < kPlaces; ++i) {
+      const double ratio = x[i] - ((double)l[i] - rec.ln_one);
+      if (id[i] >= 0 && forward && q[i] > 0.0) rec.mixed -= q[i] * to_one * ratio;
+      if (id[i] >= 0 && !forward && e[i] != 0.0) rec.mixed += e[i] * ratio;
+    }
+    rec.mixed = warp_sum(rec.mixed);
+    if (event) {
+      rec.q_rest = fmax(1.0 - rec.mass, (double)p.dp.rest_floor);
+      rec.ln_q_rest = rec.q_rest > 0.0 ? log(rec.q_rest) : 0.0;
+    } else {
+      rec.mass = 1.0;
+    }
+    rec.zs = zs;
+    rec.sum_e_f = (float)rec.sum_e;
+    rec.mass_f = (float)rec.mass;
+    rec.q_rest_f = (float)rec.q_rest;
+    const double against = rec.ln_q_rest + rec.mixed / rec.sum_e;
+    rec.against = (float)against;
+    rec.against_lo = (float)(against - (double)rec.against);
+    rec.weight = p.weight != nullptr ? p.weight[row] : 1.f;
+    rec.stat = kRowValid;
+    if (lane == 0) p.records[row] = rec;
   }
   if (lane == 0) part[warp] = n;
   __syncthreads();
   if (warp == 0) {
-    n = part[lane];
+    n = lane < kListThreads / 32 ? part[lane] : int2{0, 0};
     n.x = __reduce_add_sync(0xffffffffu, n.x);
     n.y = __reduce_add_sync(0xffffffffu, n.y);
     if (lane == 0) p.counts[blockIdx.x] = n;
   }
-}
-
-// Valid and refused rows of the call
-__device__ __forceinline__ int2 sum_counts(const int2* counts, int n, int2* red) {
-  int2 a{0, 0};
-  for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    a.x += counts[i].x;
-    a.y += counts[i].y;
-  }
-  a.x = __reduce_add_sync(0xffffffffu, a.x);
-  a.y = __reduce_add_sync(0xffffffffu, a.y);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = a;
-  __syncthreads();
-  a = red[0];
-  for (int k = 1; k < (int)(blockDim.x >> 5); ++k) {
-    a.x += red[k].x;
-    a.y += red[k].y;
-  }
-  return a;
 }
 
 // The counts of kListRows rows each added up to kCounts at most, so that the CTAs of the rows have few to read
@@ -722,23 +802,13 @@ __global__ void __launch_bounds__(1024) counts_kernel(const int2* __restrict__ f
   if (lane == 0) to[warp] = a;
 }
 
-// Sum over the block in a fixed order.
-__device__ __forceinline__ double block_sum(double v, double* red) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = red[0];
-  for (int k = 1; k < (int)(blockDim.x >> 5); ++k) v += red[k];
-  return v;
-}
-
 // Listed tokens and rest of a row are told apart by a bit for each element in shared memory: a vector's bits are one word, hardly ever other than 0.  Pass 1
-// sums the rest (the listed tokens' logits are at hand from the start), thread k < 128 then works on place k of the list in float64, and pass 2 writes
-// of_rest * 2^(z c - m) everywhere but at the listed tokens, which come last.  As in the policy loss's kernel the row is read from HBM once: pass 1 walks it from
-// its end, the group read last stays in registers, the first ones are parked in shared memory, the rest comes from L2.
+// sums the rest, a few steps join it with the list's record, and pass 2 writes of_rest * 2^(z c - m), and 0 for the listed tokens, whose gradient comes behind
+// the last row.  As in the policy loss's kernel the row is read from HBM once: pass 1 walks it from its end, the group read last stays in registers, the first ones
+// are parked in shared memory, the rest comes from L2.  (A small load takes some 3 us while all others stream: what a row needs besides its logits is asked for
+// together with its first vectors.)
 constexpr int kDistillUnroll = 4;
+constexpr int kStream = kThreads - 32;  // threads that work on the logits; the last warp works on the list (in float64: with vectors in its registers too it would spill)
 // Shared memory of a CTA: bits, parked vectors, staging of outputs that start off 16 bytes from their inputs.  What it leaves is L1, which holds the
 // loads in flight.
 constexpr size_t kDistillSmem = 68 * 1024;
@@ -747,90 +817,80 @@ constexpr double kNoRest = -700.0;  // ln p_r below which the learner gives the 
 
 struct DistillShared {
   Sums part[kMaxParts], red[kWarps];
-  double sum[3][2][kTop / 32];
-  float high[2][kTop / 32];
-  float of_rest, m;
-  int low;
+  float of_rest;
   uint32_t head_bits, tail_bits;
   int ids[kTop];
 };
 
-// Two sums over the 128 threads of a list, in a fixed order
-__device__ __forceinline__ void list_barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
-__device__ __forceinline__ void list_sums(double& a, double& b, double (*red)[kTop / 32]) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    a += __shfl_xor_sync(0xffffffffu, a, o);
-    b += __shfl_xor_sync(0xffffffffu, b, o);
-  }
-  if ((threadIdx.x & 31) == 0) red[0][threadIdx.x >> 5] = a, red[1][threadIdx.x >> 5] = b;
-  list_barrier();
-  a = (red[0][0] + red[0][1]) + (red[0][2] + red[0][3]);
-  b = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+// exp(d), d <= 0 in units of z c (so 2^d but for the rounding of c), and ln of a float, their arguments split so that float32 functions are off by some
+// 1e-7 of the first and 3e-8 in the second, whatever the size: as exact as the sums that they are applied to, at a fraction of float64's latency.
+__device__ __forceinline__ float exp_of(double d, double nat) {
+  if (!(d > -1000.0)) return d == d && d < 0.0 ? 0.f : NAN;
+  const int whole = (int)rint(d);
+  return ldexpf(expf((float)((d - (double)whole) * nat)), max(whole, -200));
+}
+__device__ __forceinline__ double ln_of(float v) {  // v > 0 and normal, or +inf, NaN
+  if (!(v <= FLT_MAX)) return (double)v;
+  int whole = (int)(__float_as_uint(v) >> 23) - 127;
+  float part = __uint_as_float((__float_as_uint(v) & 0x007fffffu) | 0x3f800000u);
+  if (part > 1.41421356f) part *= 0.5f, ++whole;
+  return (double)whole * 0.69314718055994530942 + (double)logf(part);
 }
 
-struct RowResult {
-  double kl, at;    // KL_t; T dKL/dz of this thread's listed token
-  double of_rest;   // T dKL/dz_v = of_rest * softmax over the rest (v)
-};
+// The rest's gradient from a list's record and the sums over the rest: T dKL/dz_v = rest_factor * softmax over the rest (v).  In float32, for all other warps
+// wait for it (float64 took 4,000 cycles here).  With p_r and P the learner's mass on the rest and on the list:
+//   forward  (sum q_k + q_r) p_r - q_r;   no rest in the teacher  p_r
+//   reverse  p_r (ln p_r - ln q_r - KL) = p_r P (ln s - d - (ln q_r + mixed / sum_e)), where the difference is taken in two floats a term
+__device__ __forceinline__ float rest_factor(const ListRecord& list, Sums a, float c, float nat_hi, float nat_lo, const mrl_distill_params& dp) {
+  const float d = fmaf(list.zs, c, -a.m);  // from the largest of the rest to the largest of the list, in units of z c
+  const float of_list = d < 0.f ? exp2f(d) : 1.f, of_rest = d < 0.f ? 1.f : exp2f(-d);
+  const float in_list = list.sum_e_f * of_list, in_rest = a.s * of_rest, total = in_list + in_rest;
+  const float p_rest = in_rest / total;
+  if (dp.rest != MRL_REST_EVENT) return p_rest;
+  if (!(p_rest >= 1e-30f) && p_rest == p_rest) {  // is there a rest?  ln p_r below kNoRest
+    const double ln_p_rest = (double)logf(a.s / total) - (d > 0.f ? (double)d * (double)nat_hi : 0.0);
+    if (ln_p_rest < kNoRest) return 0.f;
+  }
+  if (dp.direction == MRL_DISTILL_FORWARD) return fmaf(list.mass_f + list.q_rest_f, p_rest, -list.q_rest_f);
+  if (in_list == 0.f) return 0.f;  // (a list masked away: d may be -inf)
+  int whole = (int)(__float_as_uint(a.s) >> 23) - 127;  // ln s = whole ln 2 + ln part
+  float part = __uint_as_float((__float_as_uint(a.s) & 0x007fffffu) | 0x3f800000u);
+  if (part > 1.41421356f) part *= 0.5f, ++whole;
+  constexpr float kLn2Hi = 0.693145751953125f, kLn2Lo = 1.42860677e-6f;  // ln 2; products of the first and of small whole numbers are exact
+  const float u = (float)whole * kLn2Hi, w = d * nat_hi, v = u - w, v_err = (u - v) - w;
+  const float x = v - list.against, x_err = (v - x) - list.against;
+  const float rest = (logf(part) + (float)whole * kLn2Lo) - fmaf(d, nat_lo, fmaf(d, nat_hi, -w)) - list.against_lo;
+  return p_rest * (in_list / total) * (x + (x_err + v_err + rest));
+}
 
-// A row's KL and gradient factors from its list (thread k < 128 holds place k) and the sums over the rest, in float64
-__device__ RowResult distill_row(bool used, float z, float l, Totals rest, float c, const mrl_distill_params& dp, DistillShared& sh) {
-  const double nat = 1.0 / ((double)c * (double)dp.temperature);
-  float zs = used ? fmaxf(z, -FLT_MAX) : -FLT_MAX, ls = used ? l : -FLT_MAX;
-  if (used && z != z) zs = INFINITY;  // (NaN: inf - inf below)
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    zs = fmaxf(zs, __shfl_xor_sync(0xffffffffu, zs, o));
-    ls = fmaxf(ls, __shfl_xor_sync(0xffffffffu, ls, o));
-  }
-  if ((threadIdx.x & 31) == 0) sh.high[0][threadIdx.x >> 5] = zs, sh.high[1][threadIdx.x >> 5] = ls;
-  list_barrier();
-#pragma unroll
-  for (int k = 0; k < kTop / 32; ++k) {
-    zs = fmaxf(zs, sh.high[0][k]);
-    ls = fmaxf(ls, sh.high[1][k]);
-  }
+// A row's KL, and what its listed tokens' gradient takes
+__device__ __forceinline__ RowFactors distill_row(const ListRecord& list, Totals rest, double nat, const mrl_distill_params& dp) {
   const bool event = dp.rest == MRL_REST_EVENT, any_rest = rest.s != 0.f;
-  double m = (double)zs * (double)c;  // (+inf stays what it is)
-  if (any_rest) m = fmax(m, rest.x0);
-  const double x = used ? ((double)z * (double)c - m) * nat : 0.0;
-  const double in_rest = any_rest ? (double)rest.s * exp((rest.x0 - m) * nat) : 0.0;
-  const double d = event ? (double)l : (double)l - (double)ls;  // (without a rest any logits will do: from the largest)
-  double q = used ? exp(d) : 0.0, total = used ? exp(x) : 0.0, mass = q;
-  list_sums(total, mass, sh.sum[0]);
-  total += in_rest;
-  const double ln_total = total > 0.0 ? log(total) : NAN;
-  const double ln_p = x - ln_total, p = used ? exp(ln_p) : 0.0;
-  const double ln_p_rest = any_rest ? log((double)rest.s) + (rest.x0 - m) * nat - ln_total : -INFINITY;
+  const double m = any_rest ? fmax(list.xs, rest.x0) : list.xs, below = list.xs - m, below_rest = rest.x0 - m;
+  const float of_list = exp_of(below, nat), in_rest = any_rest ? rest.s * exp_of(below_rest, nat) : 0.f;
+  const float total = fmaf((float)list.sum_e, of_list, in_rest);
+  const double ln_total = total > 0.f ? ln_of(total) : NAN;
+  RowFactors r;
+  r.shift = below * nat - ln_total;
+  r.p_of_e = of_list / total;
+  const double ln_p_rest = any_rest ? ln_of(rest.s) + below_rest * nat - ln_total : -INFINITY;
   const bool has_rest = !(ln_p_rest < kNoRest);
-  const double p_rest = has_rest ? exp(ln_p_rest) : 0.0;
-  double term = 0.0, none = 0.0, q_rest = 0.0, ratio = 0.0;
-  if (!event) {
-    const double ln_q = d - log(mass);
-    q = used ? exp(ln_q) : 0.0;
-    term = q > 0.0 ? q * (ln_q - ln_p) : 0.0;
+  r.mass = list.mass;
+  const float p_rest = has_rest ? in_rest / total : 0.f;
+  r.of_rest = p_rest;
+  if (!event || dp.direction == MRL_DISTILL_FORWARD) {
+    r.kl = list.mixed - list.mass * r.shift;
+    if (event && has_rest) {
+      r.mass += list.q_rest;
+      if (list.q_rest > 0.0) r.kl += list.q_rest * (list.ln_q_rest - ln_p_rest);
+      r.of_rest = (float)(r.mass * (double)p_rest - list.q_rest);
+    }
   } else {
-    q_rest = has_rest ? fmax(1.0 - mass, (double)dp.rest_floor) : 0.0;
-    ratio = ln_p - (double)l;
-    if (dp.direction == MRL_DISTILL_FORWARD) term = q > 0.0 ? -q * ratio : 0.0;
-    else term = used && p != 0.0 ? p * ratio : 0.0;
-  }
-  list_sums(term, none, sh.sum[1]);
-  RowResult r;
-  r.kl = term;
-  if (!event) {
-    r.at = p - q;
-    r.of_rest = p_rest;
-  } else if (dp.direction == MRL_DISTILL_FORWARD) {
-    r.kl += q_rest > 0.0 ? q_rest * (log(q_rest) - ln_p_rest) : 0.0;
-    r.at = (mass + q_rest) * p - q;
-    r.of_rest = has_rest ? (mass + q_rest) * p_rest - q_rest : 0.0;
-  } else {
-    const double ratio_rest = has_rest ? ln_p_rest - log(q_rest) : 0.0;
-    r.kl += p_rest != 0.0 ? p_rest * ratio_rest : 0.0;
-    r.at = p != 0.0 ? p * (ratio - r.kl) : 0.0;
-    r.of_rest = p_rest != 0.0 ? p_rest * (ratio_rest - r.kl) : 0.0;
+    r.kl = r.p_of_e != 0.f ? (double)r.p_of_e * (list.mixed + r.shift * list.sum_e) : 0.0;
+    if (p_rest != 0.f) {
+      r.kl += (double)p_rest * (ln_p_rest - list.ln_q_rest);
+      r.of_rest = (float)((double)p_rest * (ln_p_rest - list.ln_q_rest - r.kl));
+    }
   }
   return r;
 }
@@ -847,6 +907,10 @@ __device__ __forceinline__ void store_vec(void* p, const Vec& v) {  // 32 bytes 
   asm volatile("st.global.L2::evict_first.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v.w[0]), "r"(v.w[1]), "r"(v.w[2]),
                "r"(v.w[3]), "r"(v.w[4]), "r"(v.w[5]), "r"(v.w[6]), "r"(v.w[7])
                : "memory");
+}
+// asks L2 for `bytes` (a multiple of 16) from `p` (on 16 bytes)
+__device__ __forceinline__ void prefetch_l2(const void* p, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
 }
 // A thread's own vectors in shared memory, as two planes of 16-byte halves
 __device__ __forceinline__ void park(uint4* planes, int slots, int slot, const Vec& v) {
@@ -903,16 +967,37 @@ template <typename T>
 __device__ void zero_part(T* out, int n) {
   const int head = min(n, (int)((0u - (uint32_t)reinterpret_cast<uintptr_t>(out)) & 15) / (int)sizeof(T));
   const int pieces = (n - head) / (16 / (int)sizeof(T)), tail0 = head + pieces * (16 / (int)sizeof(T));
-  for (int i = threadIdx.x; i < pieces; i += kThreads) __stcs(reinterpret_cast<uint4*>(out + head) + i, make_uint4(0, 0, 0, 0));
+  for (int i = threadIdx.x; i < pieces; i += kStream) __stcs(reinterpret_cast<uint4*>(out + head) + i, make_uint4(0, 0, 0, 0));
   if ((int)threadIdx.x < head) store_f(out + threadIdx.x, 0.f);
   if (tail0 + (int)threadIdx.x < n) store_f(out + tail0 + threadIdx.x, 0.f);
+}
+
+// The sums over the rest of a row from those of this thread, over all CTAs of the row; `low`: their offset is not a.m.  Called by all threads.
+template <typename T>
+__device__ __forceinline__ Totals rest_of_row(Sums& a, bool& low, const DistillArgs& p, const T* zrow, int parts, int rank, DistillShared& sh) {
+  a = block_sums<kThreads>(a, sh.red);
+  if (parts > 1) {
+    cluster_wait();
+    if ((int)threadIdx.x < parts) *in_cta(&sh.part[rank], threadIdx.x) = a;
+    cluster_arrive();
+    cluster_wait();
+    a = sh.part[0];
+    for (int k = 1; k < parts; ++k) a = sums_merge(a, sh.part[k]);
+  }
+  low = a.s == 0.f;
+  if (!low) return Totals{(double)a.m, a.s, 0.f};
+  return low_sums<T, kThreads>(zrow, p.V, p.c, sh.red, [&](int v) {
+    bool keep = true;
+    for (int k = 0; k < p.top; ++k) keep &= sh.ids[k] != v;
+    return keep;
+  });
 }
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillArgs p) {
   extern __shared__ uint4 dyn[];
   __shared__ DistillShared sh;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31;
   int parts, rank;
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -920,66 +1005,120 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillArgs 
   const T* zrow = static_cast<const T*>(p.logits) + row * p.ld;
   const Part<T> part(zrow, p.V, parts, rank);
   T* out = p.dlogits != nullptr ? static_cast<T*>(p.dlogits) + row * p.ld_out + part.first : nullptr;
-  let_next_start();
-  wait_for_previous();
-  if (p.rowstat[row] != kRowValid) {  // (all CTAs of the row)
-    if (out != nullptr) zero_part(out, part.n);
-    if (tid == 0 && rank == 0) {
-      p.term[row] = 0.0;
-      if (p.row_kl != nullptr) p.row_kl[row] = 0.f;
-    }
-    return;
-  }
   // shared memory: bits of the body's vectors | parked vectors | staging
   using Bits = typename std::conditional<sizeof(T) == 2, uint16_t, uint8_t>::type;
   Bits* bits = reinterpret_cast<Bits*>(dyn);
-  uint4* planes = dyn + p.bit_words / 4;
-  uint32_t* stage = reinterpret_cast<uint32_t*>(planes + 2 * p.park_slots) + (tid >> 5) * (kStageRow / 4);
-  for (int i = tid; i < p.bit_words / 4; i += kThreads) dyn[i] = make_uint4(0, 0, 0, 0);
-  if (tid == 0) sh.head_bits = sh.tail_bits = 0;
-  int id = tid < p.top ? p.top_ids[row * p.top + tid] : -1;
-  const float l = id >= 0 ? p.top_logp[row * p.top + tid] : -INFINITY;
-  if (l == -INFINITY) id = -1;
-  const float mine = id >= 0 ? load_f<T>(zrow + id) : 0.f;
-  const float z_head = tid < part.head ? load_f<T>(part.z + tid) : -INFINITY;
-  const float z_tail = tid < part.tail ? load_f<T>(part.z + part.n - part.tail + tid) : -INFINITY;
-  if (tid < kTop) sh.ids[tid] = id;
-  __syncthreads();
-  if (parts > 1) cluster_arrive();  // "here": its shared memory may be written to
-  const int rel = id - part.first;  // the listed token in this part
-  const bool owner = id >= 0 && rel >= 0 && rel < part.n;
-  if (owner) {
-    const int at = rel - part.head;
-    if (at < 0) atomicOr(&sh.head_bits, 1u << rel);
-    else if (at >= part.vecs * kVecElems<T>) atomicOr(&sh.tail_bits, 1u << (at - part.vecs * kVecElems<T>));
-    else atomicOr(reinterpret_cast<uint32_t*>(dyn) + (at >> 5), 1u << (at & 31));
-  }
-  __syncthreads();
-  const bool head_on = tid < part.head && !((sh.head_bits >> tid) & 1u), tail_on = tid < part.tail && !((sh.tail_bits >> tid) & 1u);
-  Sums a = sums_empty();
-  if (head_on) sums_add(a, z_head, p.c);
-  if (tail_on) sums_add(a, z_tail, p.c);
+  let_next_start();
 
-  // ---- pass 1, from the last group (the ragged one) to the first, which is a full one wherever there are two
-  constexpr int kGroup = kThreads * kDistillUnroll;
+  if (tid >= kStream) {
+    // ---- the last warp: the list
+    int id[kPlaces];
+    float l[kPlaces];
+#pragma unroll
+    for (int i = 0; i < kPlaces; ++i) {
+      const int k = lane + 32 * i;
+      id[i] = k < p.top ? p.top_ids[row * p.top + k] : -1;
+      l[i] = k < p.top ? p.top_logp[row * p.top + k] : -INFINITY;
+    }
+    wait_for_previous();
+    // (a word of the record a lane, and the counts: they come together)
+    constexpr int kRecordWords = (int)sizeof(ListRecord) / 4;
+    const int stat = p.records[row].stat, word = reinterpret_cast<const int*>(p.records + row)[lane % kRecordWords];
+    int valid = lane < p.n_counts ? p.counts[lane].x : 0;
+    if (stat != kRowValid) {
+      if (lane == 0 && rank == 0) {
+        p.term[row] = 0.0;
+        if (p.row_kl != nullptr) p.row_kl[row] = 0.f;
+      }
+      return;
+    }
+    __syncthreads();  // the bits are zero
+    if (parts > 1) cluster_arrive();  // "here": its shared memory may be written to
+#pragma unroll
+    for (int i = 0; i < kPlaces; ++i) {
+      if (l[i] == -INFINITY) id[i] = -1;
+      sh.ids[lane + 32 * i] = id[i];
+      const int rel = id[i] - part.first, at = rel - part.head;  // the listed token in this part
+      if (id[i] < 0 || rel < 0 || rel >= part.n) continue;
+      if (at < 0) atomicOr(&sh.head_bits, 1u << rel);
+      else if (at >= part.vecs * kVecElems<T>) atomicOr(&sh.tail_bits, 1u << (at - part.vecs * kVecElems<T>));
+      else atomicOr(reinterpret_cast<uint32_t*>(dyn) + (at >> 5), 1u << (at & 31));
+    }
+    __syncthreads();  // the bits are set
+    union {
+      ListRecord list;
+      int words[kRecordWords];
+    } rec;
+#pragma unroll
+    for (int k = 0; k < kRecordWords; ++k) rec.words[k] = __shfl_sync(0xffffffffu, word, k);
+    const double denominator = p.dp.denominator > 0.0 ? p.dp.denominator : (double)__reduce_add_sync(0xffffffffu, valid);
+    const double scale = (double)p.dp.coeff * rec.list.weight / (denominator * p.dp.temperature);
+    const float scale_f = (float)scale, nat_hi = (float)p.nat, nat_lo = (float)(p.nat - (double)nat_hi);
+    Sums a = sums_empty();
+    bool low;
+    const Totals rest = rest_of_row<T>(a, low, p, zrow, parts, rank, sh);
+    if (lane == 0) {
+      float f = 0.f;
+      if (scale != 0.0 && rest.s != 0.f)
+        f = (low ? distill_row(rec.list, rest, p.nat, p.dp).of_rest : rest_factor(rec.list, a, p.c, nat_hi, nat_lo, p.dp)) / rest.s * scale_f;
+      sh.of_rest = f;
+    }
+    __syncwarp();
+    if (out != nullptr) asm volatile("bar.arrive 1, %0;" ::"n"(kThreads) : "memory");
+    RowFactors r = distill_row(rec.list, rest, p.nat, p.dp);
+    r.scale = scale;
+    if (lane == 0 && rank == 0) {
+      p.factors[row] = r;
+      p.term[row] = rec.list.weight != 0.f ? (double)rec.list.weight * r.kl : 0.0;
+      if (p.row_kl != nullptr) p.row_kl[row] = (float)r.kl;
+    }
+    return;
+  }
+
+  // ---- the other warps: the logits.  The first loads wait for nothing: the logits were there before list_kernel began.  (A row that is not valid reads
+  // them in vain.)
+  constexpr int kGroup = kStream * kDistillUnroll;
   const char* in = part.body() + (size_t)tid * kVecBytes;
   const int last = part.vecs > 0 ? (part.vecs - 1) / kGroup * kGroup : -kGroup;
   Vec v[kDistillUnroll];
-#pragma unroll 1
-  for (int base = last; base >= 0; base -= kGroup) {
-    const int slot0 = (last - base) / kDistillUnroll;  // of the parked vectors: kThreads a step of the unrolled loop
+  auto load_group = [&](int base) {
 #pragma unroll
     for (int i = 0; i < kDistillUnroll; ++i) {
-      const int at = base + i * kThreads;
+      const int at = base + i * kStream;
       v[i] = at + tid < part.vecs ? load_vec_keep(in + (size_t)at * kVecBytes) : no_vec<T>();
     }
+  };
+  load_group(max(last, 0));
+  const float z_head = tid < part.head ? load_f<T>(part.z + tid) : -INFINITY;
+  const float z_tail = tid < part.tail ? load_f<T>(part.z + part.n - part.tail + tid) : -INFINITY;
+  wait_for_previous();
+  const int stat = p.records[row].stat;
+  uint4* planes = dyn + p.bit_words / 4;
+  for (int i = tid; i < p.bit_words / 4; i += kStream) dyn[i] = make_uint4(0, 0, 0, 0);
+  if (tid == 0) sh.head_bits = sh.tail_bits = 0;
+  if (stat != kRowValid) {  // (all CTAs of the row)
+    if (out != nullptr) zero_part(out, part.n);
+    return;
+  }
+  __syncthreads();
+  if (parts > 1) cluster_arrive();
+  __syncthreads();
+  Sums a = sums_empty();
+  if (tid < part.head && !((sh.head_bits >> tid) & 1u)) sums_add(a, z_head, p.c);
+  if (tid < part.tail && !((sh.tail_bits >> tid) & 1u)) sums_add(a, z_tail, p.c);
+
+  // pass 1, from the last group (the ragged one) to the first, which is a full one wherever there are two
+#pragma unroll 1
+  for (int base = last; base >= 0; base -= kGroup) {
+    if (base != last) load_group(base);
+    if (tid == 0 && base > 0) prefetch_l2(part.body() + (size_t)(base - kGroup) * kVecBytes, kGroup * kVecBytes);
 #pragma unroll
     for (int i = 0; i < kDistillUnroll; ++i) {
-      const int at = base + i * kThreads + tid;
+      const int at = base + i * kStream + tid;
       if (at < part.vecs) {
         const uint32_t some = bits[at];
         if (some != 0) strike_out<T>(v[i], some);
-        const int slot = slot0 * kDistillUnroll + i * kThreads + tid;
+        const int slot = last - base + i * kStream + tid;
         if (slot < p.park_slots) park(planes, p.park_slots, slot, v[i]);
       }
     }
@@ -992,115 +1131,110 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillArgs 
     Sums2 more{0, 0};
 #pragma unroll
     for (int i = 0; i < kDistillUnroll; ++i)
-      if (base + i * kThreads + tid < part.vecs) sums_add<T, false, false>(more, v[i], c2, m2);
+      if (base + i * kStream + tid < part.vecs) sums_add<T, false, false>(more, v[i], c2, m2);
     const float2 s = split_f2(more.s);
     a.s += s.x + s.y;
   }
-  a = block_sums<kThreads>(a, sh.red);
-  if (parts > 1) {
-    cluster_wait();
-    if (tid < parts) *in_cta(&sh.part[rank], tid) = a;
-    cluster_arrive();
-    cluster_wait();
-    a = sh.part[0];
-    for (int k = 1; k < parts; ++k) a = sums_merge(a, sh.part[k]);
-  }
-  Totals rest{(double)a.m, a.s, 0.f};
-  const bool low = a.s == 0.f;
-  if (low) {
-    rest = low_sums<T, kThreads>(zrow, p.V, p.c, sh.red, [&](int v) {
-      bool keep = true;
-      for (int k = 0; k < p.top; ++k) keep &= sh.ids[k] != v;
-      return keep;
-    });
-  }
-
-  // ---- the list
-  double scale = 0.0, at_listed = 0.0;
-  if (tid < kTop) {
-    const RowResult r = distill_row(id >= 0, mine, l, rest, p.c, p.dp, sh);
-    const float w = p.weight != nullptr ? p.weight[row] : 1.f;
-    double denominator = p.dp.denominator;
-    if (!(denominator > 0.0)) {
-      int n = 0;
-      for (int i = tid & 31; i < p.n_counts; i += 32) n += p.counts[i].x;
-      denominator = (double)__reduce_add_sync(0xffffffffu, n);
-    }
-    scale = (double)p.dp.coeff * w / (denominator * p.dp.temperature);
-    at_listed = scale != 0.0 ? r.at * scale : 0.0;
-    if (tid == 0) {
-      sh.of_rest = scale != 0.0 && rest.s != 0.f ? (float)(r.of_rest * scale / rest.s) : 0.f;
-      if (rank == 0) {
-        p.term[row] = w != 0.f ? (double)w * r.kl : 0.0;
-        if (p.row_kl != nullptr) p.row_kl[row] = (float)r.kl;
-      }
-    }
-  }
+  bool low;
+  const double x0 = rest_of_row<T>(a, low, p, zrow, parts, rank, sh).x0;
   if (out == nullptr) return;
-  __syncthreads();
+  asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");  // the list warp has the factor
   const float of_rest = sh.of_rest;
   if (of_rest == 0.f) {
     zero_part(out, part.n);
-  } else if (low) {
-    for (int i = tid; i < part.n; i += kThreads)
-      store_f(out + i, ex2_approx((float)((double)load_f<T>(part.z + i) * (double)p.c - rest.x0)) * of_rest);
-  } else {
-    // ---- pass 2: the first group from registers, the others as pass 1 read them last to first
-    const float m = -a.m;
-    char* body_out = reinterpret_cast<char*>(out + part.head);
-    const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(body_out) & (kVecBytes - 1);
+    return;
+  }
+  if (low) {
+    for (int i = tid; i < part.n; i += kStream) store_f(out + i, ex2_approx((float)((double)load_f<T>(part.z + i) * (double)p.c - x0)) * of_rest);
+    return;
+  }
+
+  // pass 2: the first group from registers, the others as pass 1 read them last to first
+  const float m = -a.m;
+  char* body_out = reinterpret_cast<char*>(out + part.head);
+  const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(body_out) & (kVecBytes - 1);
+  uint32_t* stage = reinterpret_cast<uint32_t*>(planes + 2 * p.park_slots) + (tid >> 5) * (kStageRow / 4);
 #pragma unroll 1
-    for (int base = 0; base <= last; base += kGroup) {
-      if (base != 0) {
-        const int slot0 = (last - base) / kDistillUnroll;
-#pragma unroll
-        for (int i = 0; i < kDistillUnroll; ++i) {
-          const int at = base + i * kThreads, slot = slot0 * kDistillUnroll + i * kThreads + tid;
-          v[i] = at + tid >= part.vecs ? no_vec<T>() : slot < p.park_slots ? parked(planes, p.park_slots, slot) : load_vec(in + (size_t)at * kVecBytes);
-        }
-      }
+  for (int base = 0; base <= last; base += kGroup) {
+    if (base != 0) {
 #pragma unroll
       for (int i = 0; i < kDistillUnroll; ++i) {
-        Vec r;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if constexpr (sizeof(T) == 2)
-            r.w[j] = pack_bf16x2(ex2_approx(fmaf(bf16lo_to_f32(v[i].w[j]), p.c, m)) * of_rest, ex2_approx(fmaf(bf16hi_to_f32(v[i].w[j]), p.c, m)) * of_rest);
-          else
-            r.w[j] = __float_as_uint(ex2_approx(fmaf(__uint_as_float(v[i].w[j]), p.c, m)) * of_rest);
-        }
-        const int at = base + i * kThreads + tid;
-        char* dst = body_out + (size_t)at * kVecBytes;
-        if (off == 0) {
-          if (at < part.vecs) store_vec(dst, r);
-        } else if (off == 16) {
-          if (at < part.vecs) {
-            __stcs(reinterpret_cast<uint4*>(dst), make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]));
-            __stcs(reinterpret_cast<uint4*>(dst) + 1, make_uint4(r.w[4], r.w[5], r.w[6], r.w[7]));
-          }
-        } else {
-          const int count = max(0, min(32, part.vecs - (at - (tid & 31))));
-          store_shifted<T>(dst - (size_t)(tid & 31) * kVecBytes, r, count, stage);
-        }
+        const int at = base + i * kStream, slot = last - base + i * kStream + tid;
+        v[i] = at + tid >= part.vecs ? no_vec<T>() : slot < p.park_slots ? parked(planes, p.park_slots, slot) : load_vec(in + (size_t)at * kVecBytes);
       }
     }
-    if (tid < part.head) store_f(out + tid, ex2_approx(fmaf(z_head, p.c, m)) * of_rest);
-    if (tid < part.tail) store_f(out + part.n - part.tail + tid, ex2_approx(fmaf(z_tail, p.c, m)) * of_rest);
+#pragma unroll
+    for (int i = 0; i < kDistillUnroll; ++i) {
+      Vec r;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (sizeof(T) == 2)
+          r.w[j] = pack_bf16x2(ex2_approx(fmaf(bf16lo_to_f32(v[i].w[j]), p.c, m)) * of_rest, ex2_approx(fmaf(bf16hi_to_f32(v[i].w[j]), p.c, m)) * of_rest);
+        else
+          r.w[j] = __float_as_uint(ex2_approx(fmaf(__uint_as_float(v[i].w[j]), p.c, m)) * of_rest);
+      }
+      const int at = base + i * kStream + tid;
+      char* dst = body_out + (size_t)at * kVecBytes;
+      if (off == 0) {
+        if (at < part.vecs) store_vec(dst, r);
+      } else if (off == 16) {
+        if (at < part.vecs) {
+          __stcs(reinterpret_cast<uint4*>(dst), make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]));
+          __stcs(reinterpret_cast<uint4*>(dst) + 1, make_uint4(r.w[4], r.w[5], r.w[6], r.w[7]));
+        }
+      } else {
+        const int count = max(0, min(32, part.vecs - (at - lane)));
+        store_shifted<T>(dst - (size_t)lane * kVecBytes, r, count, stage);
+      }
+    }
   }
-  __syncthreads();  // the listed tokens over what stands in their places
-  if (owner) store_f(out + rel, (float)at_listed);
+  if (tid < part.head) store_f(out + tid, ex2_approx(fmaf(z_head, p.c, m)) * of_rest);
+  if (tid < part.tail) store_f(out + part.n - part.tail + tid, ex2_approx(fmaf(z_tail, p.c, m)) * of_rest);
 }
 
-// Sums of the rows' terms and counts, one CTA, in a fixed order.
-__global__ void __launch_bounds__(1024) distill_finish_kernel(const DistillArgs p) {
+// The gradient of the listed tokens, a warp per row, over what stands in their places; the first CTA sums the rows' terms and counts in a fixed order.
+template <typename T>
+__global__ void __launch_bounds__(1024) finish_kernel(const DistillArgs p) {
   __shared__ double red[32];
   __shared__ int2 redc[32];
   wait_for_previous();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (blockIdx.x > 0) {
+    const long long row = (long long)(blockIdx.x - 1) * 32 + warp;
+    if (row >= p.N || p.records[row].stat != kRowValid) return;
+    const RowFactors r = p.factors[row];
+    const double xs = p.records[row].xs, ln_one = p.records[row].ln_one;
+    T* out = static_cast<T*>(p.dlogits) + row * p.ld_out;
+    for (int k = lane; k < p.top; k += 32) {
+      const int id = p.top_ids[row * p.top + k];
+      const float l = p.top_logp[row * p.top + k];
+      if (id < 0 || l == -INFINITY) continue;
+      const double x = ((double)p.z[row * p.top + k] * (double)p.c - xs) * p.nat, ln_q = (double)l - ln_one, pk = exp(x) * (double)r.p_of_e;
+      double g;
+      if (p.dp.direction == MRL_DISTILL_REVERSE) g = pk != 0.0 ? pk * (x - ln_q + r.shift - r.kl) : 0.0;
+      else g = r.mass * pk - exp(ln_q);
+      store_f(out + id, r.scale != 0.0 ? (float)(g * r.scale) : 0.f);
+    }
+    return;
+  }
   double v = 0.0;
   for (long long i = threadIdx.x; i < p.N; i += 1024) v += p.term[i];
-  v = block_sum(v, red);
-  const int2 n = sum_counts(p.counts, p.n_counts, redc);
+  v = warp_sum(v);
+  int2 n{0, 0};
+  for (int i = threadIdx.x; i < p.n_counts; i += 1024) {
+    n.x += p.counts[i].x;
+    n.y += p.counts[i].y;
+  }
+  n.x = __reduce_add_sync(0xffffffffu, n.x);
+  n.y = __reduce_add_sync(0xffffffffu, n.y);
+  if (lane == 0) red[warp] = v, redc[warp] = n;
+  __syncthreads();
   if (threadIdx.x == 0) {
+    for (int k = 1; k < 32; ++k) {
+      v += red[k];
+      n.x += redc[k].x;
+      n.y += redc[k].y;
+    }
     const bool more = (p.dp.flags & MRL_FLAG_ACCUMULATE_LOSS) != 0;
     const double d = p.dp.denominator > 0.0 ? p.dp.denominator : (double)n.x;
     const double loss = d > 0.0 && p.dp.coeff != 0.f ? v * (double)p.dp.coeff / d : 0.0;
@@ -1113,18 +1247,22 @@ __global__ void __launch_bounds__(1024) distill_finish_kernel(const DistillArgs 
 }
 
 struct DistillWs {
-  uint8_t* rowstat;
-  int2 *counts, *sums;
+  ListRecord* records;
+  RowFactors* factors;
+  float* z;
   double* term;
+  int2 *counts, *sums;
   size_t bytes;
 };
 DistillWs carve(void* ws, long long N) {
   MrlCarver c(ws);
   DistillWs w;
+  w.records = c.take<ListRecord>((size_t)N);
+  w.factors = c.take<RowFactors>((size_t)N);
+  w.z = c.take<float>((size_t)N * kTop);
   w.term = c.take<double>((size_t)N);
   w.counts = c.take<int2>((size_t)((N + kListRows - 1) / kListRows));
   w.sums = c.take<int2>(kCounts);
-  w.rowstat = c.take<uint8_t>((size_t)N);
   w.bytes = c.off;
   return w;
 }
@@ -1201,9 +1339,14 @@ extern "C" int mrl_distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64
   if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return MRL_ERR_INVALID_ARG;
   const DistillWs w = carve(workspace, N);
   const int blocks = (int)((N + kListRows - 1) / kListRows);
-  DistillArgs a{logits, dlogits, ld, ld_out, N, V, top, top_ids, top_logp, mask, row_weight, *dp, scale_of(dp->temperature), row_kl,
-                loss, reinterpret_cast<long long*>(stats), status, w.rowstat, w.counts, blocks, w.term, 0, 0};
-  list_check_kernel<<<blocks, kListThreads, 0, st>>>(a);
+  const bool bf16 = dtype == MRL_BF16;
+  DistillArgs a{logits, dlogits, ld, ld_out, N, V, top, top_ids, top_logp, mask, row_weight, *dp, scale_of(dp->temperature), 0.0, row_kl,
+                loss, reinterpret_cast<long long*>(stats), status, w.records, w.z, w.factors, w.term, w.counts, blocks, 0, 0};
+  a.nat = 1.0 / ((double)a.c * (double)dp->temperature);
+  if (bf16)
+    list_kernel<__nv_bfloat16><<<blocks, kListThreads, 0, st>>>(a);
+  else
+    list_kernel<float><<<blocks, kListThreads, 0, st>>>(a);
   MRL_CUDA_OK(cudaGetLastError());
   if (blocks > kCounts) {
     MRL_CUDA_OK(mrl_launch_behind(counts_kernel, 1, 1024, st, w.counts, blocks, (blocks + kCounts - 1) / kCounts, w.sums));
@@ -1217,10 +1360,10 @@ extern "C" int mrl_distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64
   const bool shifted = dlogits != nullptr && (off % 16 != 0 || (N > 1 && (ld_out - ld) * elem % 16 != 0));
   a.bit_words = (int)mrl_align_up((size_t)((V + parts - 1) / parts + 16 + 31) / 32, 4);
   const size_t fixed = (size_t)a.bit_words * 4 + (shifted ? kStageBytes : 0);
-  if (dlogits != nullptr && fixed < kDistillSmem) a.park_slots = (int)((kDistillSmem - fixed) / (kThreads * kVecBytes)) * kThreads;
+  if (dlogits != nullptr && fixed < kDistillSmem) a.park_slots = (int)((kDistillSmem - fixed) / (kStream * kVecBytes)) * kStream;
   const size_t smem = fixed + (size_t)a.park_slots * kVecBytes;
   using Kernel = void (*)(const DistillArgs);
-  const Kernel kernel = dtype == MRL_BF16 ? distill_kernel<__nv_bfloat16> : distill_kernel<float>;
+  const Kernel kernel = bf16 ? distill_kernel<__nv_bfloat16> : distill_kernel<float>;
   static std::atomic<uint64_t> attr_done;
   int rc = mrl_once_per_device(attr_done, [] {
     // the carve-out that two CTAs an SM need, as a percentage of the 228 KB it can give: the rest stays L1
@@ -1237,6 +1380,7 @@ extern "C" int mrl_distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64
   rc = launch_rows(kernel, N, parts, kThreads, smem, true, st, a);
   mrl_profile_after(st);
   if (rc != MRL_OK) return rc;
-  MRL_CUDA_OK(mrl_launch_behind(distill_finish_kernel, 1, 1024, st, a));
+  const unsigned ctas = dlogits != nullptr ? 1 + (unsigned)((N + 31) / 32) : 1;
+  MRL_CUDA_OK(mrl_launch_behind(bf16 ? finish_kernel<__nv_bfloat16> : finish_kernel<float>, ctas, 1024, st, a));
   return MRL_OK;
 }
