@@ -197,19 +197,24 @@ struct Totals {
   double x0;
   float s, u;
 };
-// The sums of a row whose s above is 0, against its largest logit: 2^((z - zm) c).  `keep` says which elements count.  Called by the block;
-// slow, and hardly ever needed.
-template <typename T, int kT, typename Keep>
-__device__ __noinline__ Totals low_sums(const T* z, int V, float c, Sums* red, Keep keep) {
+// The sums of a row whose s above is 0, against its largest logit: 2^((z - zm) c); without the `n` tokens of `ids`.  Called by the block; slow, and hardly
+// ever needed.  (Plain arguments: what a lambda takes by reference is copied to every thread's stack before the kernel begins, 250 MB for 1,480 rows.)
+template <typename T, int kT>
+__device__ __noinline__ Totals low_sums(const T* z, int V, float c, Sums* red, const int* ids, int n) {
+  auto listed = [&](int v) {
+    bool found = false;
+    for (int k = 0; k < n; ++k) found |= ids[k] == v;
+    return found;
+  };
   float zm = -FLT_MAX;
   for (int v = threadIdx.x; v < V; v += kT)
-    if (keep(v)) zm = fmaxf(zm, load_f<T>(z + v));
+    if (!listed(v)) zm = fmaxf(zm, load_f<T>(z + v));
   Sums a{zm, 0.f, 0.f};
   __syncthreads();
   zm = block_sums<kT>(a, red).m;
   a = Sums{0.f, 0.f, 0.f};
   for (int v = threadIdx.x; v < V; v += kT)
-    if (keep(v)) sums_term<true, true>(load_f<T>(z + v) - zm, c, 0.f, a.s, a.u);
+    if (!listed(v)) sums_term<true, true>(load_f<T>(z + v) - zm, c, 0.f, a.s, a.u);
   __syncthreads();
   a = block_sums<kT>(a, red);
   return Totals{(double)zm * (double)c, a.s, a.u};
@@ -574,7 +579,7 @@ __global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArg
   n = (int)sh.n_list;
   const Key* keys = sh.list;
   Totals t{(double)a.m, a.s, a.u};
-  if (t.s == 0.f) t = low_sums<T, kTopThreads>(zrow, p.V, p.c, sh.red, [](int) { return true; });
+  if (t.s == 0.f) t = low_sums<T, kTopThreads>(zrow, p.V, p.c, sh.red, nullptr, 0);
   const double nat = 1.0 / ((double)p.c * (double)p.temperature), ln_s = t.s == 0.f ? NAN : log((double)t.s);
   auto ln_p = [&](float z) { return (float)(((double)z * (double)p.c - t.x0) * nat - ln_s); };
   if (tid == 0) {
@@ -986,14 +991,12 @@ __device__ __forceinline__ Totals rest_of_row(Sums& a, bool& low, const DistillA
   }
   low = a.s == 0.f;
   if (!low) return Totals{(double)a.m, a.s, 0.f};
-  return low_sums<T, kThreads>(zrow, p.V, p.c, sh.red, [&](int v) {
-    bool keep = true;
-    for (int k = 0; k < p.top; ++k) keep &= sh.ids[k] != v;
-    return keep;
-  });
+  return low_sums<T, kThreads>(zrow, p.V, p.c, sh.red, sh.ids, p.top);
 }
 
-template <typename T>
+// kShifted: outputs need not start on the same bytes of 32 as their inputs.  (A kernel of its own: code that a row runs through once comes from far, some 30 cycles
+// an instruction, if the loops leave no room for it near the SM.)
+template <typename T, bool kShifted>
 __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillArgs p) {
   extern __shared__ uint4 dyn[];
   __shared__ DistillShared sh;
@@ -1152,7 +1155,7 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillArgs 
   // pass 2: the first group from registers, the others as pass 1 read them last to first
   const float m = -a.m;
   char* body_out = reinterpret_cast<char*>(out + part.head);
-  const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(body_out) & (kVecBytes - 1);
+  const bool aligned = (reinterpret_cast<uintptr_t>(body_out) & (kVecBytes - 1)) == 0;
   uint32_t* stage = reinterpret_cast<uint32_t*>(planes + 2 * p.park_slots) + (tid >> 5) * (kStageRow / 4);
 #pragma unroll 1
   for (int base = 0; base <= last; base += kGroup) {
@@ -1175,13 +1178,8 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillArgs 
       }
       const int at = base + i * kStream + tid;
       char* dst = body_out + (size_t)at * kVecBytes;
-      if (off == 0) {
+      if (!kShifted || aligned) {
         if (at < part.vecs) store_vec(dst, r);
-      } else if (off == 16) {
-        if (at < part.vecs) {
-          __stcs(reinterpret_cast<uint4*>(dst), make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]));
-          __stcs(reinterpret_cast<uint4*>(dst) + 1, make_uint4(r.w[4], r.w[5], r.w[6], r.w[7]));
-        }
       } else {
         const int count = max(0, min(32, part.vecs - (at - lane)));
         store_shifted<T>(dst - (size_t)lane * kVecBytes, r, count, stage);
@@ -1357,18 +1355,19 @@ extern "C" int mrl_distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64
   int parts = parts_of(N, (long long)V * elem, 2);
   if (parts == 1 && (long long)V * elem >= 512 * 1024) parts = 2;
   const long long off = static_cast<const char*>(dlogits) - static_cast<const char*>(logits);
-  const bool shifted = dlogits != nullptr && (off % 16 != 0 || (N > 1 && (ld_out - ld) * elem % 16 != 0));
+  const bool shifted = dlogits != nullptr && (off % kVecBytes != 0 || (N > 1 && (ld_out - ld) * elem % kVecBytes != 0));
   a.bit_words = (int)mrl_align_up((size_t)((V + parts - 1) / parts + 16 + 31) / 32, 4);
   const size_t fixed = (size_t)a.bit_words * 4 + (shifted ? kStageBytes : 0);
   if (dlogits != nullptr && fixed < kDistillSmem) a.park_slots = (int)((kDistillSmem - fixed) / (kStream * kVecBytes)) * kStream;
   const size_t smem = fixed + (size_t)a.park_slots * kVecBytes;
   using Kernel = void (*)(const DistillArgs);
-  const Kernel kernel = bf16 ? distill_kernel<__nv_bfloat16> : distill_kernel<float>;
+  const Kernel kernels[4] = {distill_kernel<__nv_bfloat16, false>, distill_kernel<__nv_bfloat16, true>, distill_kernel<float, false>,
+                             distill_kernel<float, true>};
   static std::atomic<uint64_t> attr_done;
-  int rc = mrl_once_per_device(attr_done, [] {
+  int rc = mrl_once_per_device(attr_done, [&] {
     // the carve-out that two CTAs an SM need, as a percentage of the 228 KB it can give: the rest stays L1
     constexpr int kCarve = (int)((2 * (kDistillSmem + 4096) * 100 + 228 * 1024 - 1) / (228 * 1024));
-    for (const Kernel k : {static_cast<Kernel>(distill_kernel<__nv_bfloat16>), static_cast<Kernel>(distill_kernel<float>)}) {
+    for (const Kernel k : kernels) {
       cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
       if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, kCarve);
       if (e != cudaSuccess) return e;
@@ -1377,7 +1376,7 @@ extern "C" int mrl_distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64
   });
   if (rc != MRL_OK) return rc;
   mrl_profile_before(st, "distill_kernel");
-  rc = launch_rows(kernel, N, parts, kThreads, smem, true, st, a);
+  rc = launch_rows(kernels[(bf16 ? 0 : 2) + shifted], N, parts, kThreads, smem, true, st, a);
   mrl_profile_after(st);
   if (rc != MRL_OK) return rc;
   const unsigned ctas = dlogits != nullptr ? 1 + (unsigned)((N + 31) / 32) : 1;
