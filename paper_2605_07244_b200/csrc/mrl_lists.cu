@@ -63,6 +63,14 @@ __device__ __forceinline__ float vec_max(const Vec& v) {  // passes over NaN
   }
 }
 
+template <typename T>
+__device__ __forceinline__ float element(const Vec& v, int e) {
+  const int j = sizeof(T) == 2 ? e >> 1 : e;
+  const uint32_t a = j & 1 ? v.w[1] : v.w[0], b = j & 1 ? v.w[3] : v.w[2], c = j & 1 ? v.w[5] : v.w[4], d = j & 1 ? v.w[7] : v.w[6];
+  const uint32_t w = j & 4 ? (j & 2 ? d : c) : (j & 2 ? b : a);
+  return sizeof(T) == 4 ? __uint_as_float(w) : e & 1 ? bf16hi_to_f32(w) : bf16lo_to_f32(w);
+}
+
 // A CTA's part of a row: `head` elements up to the first address that is a multiple of 32 bytes, `vecs` vectors, `tail` elements.  So rows
 // of any address and stride are read with the same wide loads.
 template <typename T>
@@ -234,7 +242,8 @@ struct TopArgs {
   int V;
   const int32_t* ids;
   const uint8_t* mask;
-  float temperature, c;
+  float c;
+  double nat;  // 1 / (c T)
   int top;
   float *logp, *lse, *entropy, *top_logp;
   int32_t *top_ids, *status;
@@ -248,12 +257,13 @@ __device__ __forceinline__ Key key_of(float z, int index) { return ((Key)ordinal
 constexpr int kUnroll = 3;       // vectors of a thread and group
 constexpr int kSecondFloor = 3;  // the group behind which the floor is set again
 constexpr int kTopWarps = kTopThreads / 32;
-constexpr int kNoted = 2048, kCap = 1024;  // vectors noted, and candidates, of a CTA
+constexpr int kNoted = 2048, kHeld = 320, kCap = 1024;  // vectors noted, those of them whose elements are held, and candidates, of a CTA
 constexpr int kFew = 256;        // keys that are put in order by counting
 struct TopShared {
   Key cand[kCap];                // candidates of this CTA
   Key list[kFew];                // what is left of them, or (CTA 0) of the pool
   Sums part[kMaxParts], red[kTopWarps];
+  uint4 held[2 * kHeld];         // the first of them
   int vec[kNoted];               // vectors noted
   uint32_t hist[256], pick[4], pick2[2 * kTopWarps], n_vec, n_cand, n_list, n_pool;
 };
@@ -484,7 +494,7 @@ __global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArg
   if (tid < part.tail) sums_add(a, z_tail, p.c);
   // Vectors that can hold a listed token are noted, by their place: those with an element that is not below a floor, which the first group sets
   // so that `top` threads at least have an element there, each at least one.  The largest element of each thread sets the last floor behind the last
-  // group in the same way, a tight one, and what is not below it is read again from the vectors noted.
+  // group in the same way, a tight one, and what is not below it is taken from the vectors noted: the first are held in shared memory, others read again.
   float best = z_head, floor = floor_of<T>(kLowest);
   const int groups = max(1, (part.vecs + kTopThreads * kUnroll - 1) / (kTopThreads * kUnroll));
 #pragma unroll 1
@@ -523,6 +533,10 @@ __global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArg
       if (high[i] >= floor) {
         const uint32_t at = atomicAdd(&sh.n_vec, 1u);
         if (at < kNoted) sh.vec[at] = v0 + i * kTopThreads;
+        if (at < kHeld) {
+          sh.held[at] = make_uint4(v[i].w[0], v[i].w[1], v[i].w[2], v[i].w[3]);
+          sh.held[kHeld + at] = make_uint4(v[i].w[4], v[i].w[5], v[i].w[6], v[i].w[7]);
+        }
       }
   }
   int n = 0;
@@ -542,12 +556,18 @@ __global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArg
     const int noted = all ? part.vecs : (int)sh.n_vec;
     for (int k = tid; k < noted; k += kTopThreads) {
       const int at = all ? k : sh.vec[k];
-      const Vec v = load_vec(part.body() + (size_t)at * kVecBytes);
+      Vec v;
+      if (!all && k < kHeld) {
+        const uint4 a = sh.held[k], b = sh.held[kHeld + k];
+        v = Vec{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+      } else {
+        v = load_vec(part.body() + (size_t)at * kVecBytes);
+      }
       uint32_t bits = not_below<T>(v, floor);
 #pragma unroll 1
       for (; bits != 0; bits &= bits - 1) {
-        const int index = part.head + at * kVecElems<T> + __ffs(bits) - 1;
-        push(load_f<T>(part.z + index), index);
+        const int e = __ffs(bits) - 1;
+        push(element<T>(v, e), part.head + at * kVecElems<T> + e);
       }
     }
   }
@@ -579,14 +599,9 @@ __global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArg
   n = (int)sh.n_list;
   const Key* keys = sh.list;
   Totals t{(double)a.m, a.s, a.u};
-  if (t.s == 0.f) t = low_sums<T, kTopThreads>(zrow, p.V, p.c, sh.red, nullptr, 0);
-  const double nat = 1.0 / ((double)p.c * (double)p.temperature), ln_s = t.s == 0.f ? NAN : log((double)t.s);
-  auto ln_p = [&](float z) { return (float)(((double)z * (double)p.c - t.x0) * nat - ln_s); };
-  if (tid == 0) {
-    if (p.lse != nullptr) p.lse[row] = (float)(t.x0 * nat + ln_s);
-    if (p.logp != nullptr) p.logp[row] = ln_p(load_f<T>(zrow + id));
-    if (kEnt) p.entropy[row] = (float)(ln_s - (double)t.u / (double)t.s * nat);
-  }
+  const bool low = t.s == 0.f;
+  if (low) t = low_sums<T, kTopThreads>(zrow, p.V, p.c, sh.red, nullptr, 0);
+  const float ln_s = t.s == 0.f ? NAN : logf(t.s), nat = (float)p.nat;
   // in order: a key's place is the number of larger ones, counted by four threads a key
   for (int k0 = 0; k0 < n; k0 += kTopThreads / 4) {
     const int k = k0 + (tid >> 2);
@@ -597,9 +612,18 @@ __global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArg
     at += __shfl_xor_sync(0xffffffffu, at, 1);
     at += __shfl_xor_sync(0xffffffffu, at, 2);
     if (k < n && at < p.top && (tid & 3) == 0) {
+      const float z = from_ordinal((uint32_t)(key >> 32));
+      const float x = fmaf(z, p.c, -a.m);
       p.top_ids[row * p.top + at] = 0x7fffffff - (int32_t)(uint32_t)key;
-      p.top_logp[row * p.top + at] = ln_p(from_ordinal((uint32_t)(key >> 32)));
+      // (float64 where z c leaves float32)
+      p.top_logp[row * p.top + at] = low || x < -FLT_MAX ? (float)(((double)z * (double)p.c - t.x0) * p.nat - (double)ln_s) : fmaf(x, nat, -ln_s);
     }
+  }
+  if (tid == kTopThreads - 32) {  // (a warp that has hardly any keys)
+    const double ln_s64 = t.s == 0.f ? NAN : log((double)t.s);
+    if (p.lse != nullptr) p.lse[row] = (float)(t.x0 * p.nat + ln_s64);
+    if (p.logp != nullptr) p.logp[row] = (float)(((double)load_f<T>(zrow + id) * (double)p.c - t.x0) * p.nat - ln_s64);
+    if (kEnt) p.entropy[row] = (float)(ln_s64 - (double)t.u / (double)t.s * p.nat);
   }
   for (int k = n + tid; k < p.top; k += kTopThreads) {
     p.top_ids[row * p.top + k] = -1;
@@ -1293,7 +1317,8 @@ extern "C" int mrl_top_logprobs(const void* logits, int32_t dtype, int64_t N, in
       if (outs[i] == outs[j]) return MRL_ERR_INVALID_ARG;
   }
   if (!on_element(logits, dtype == MRL_BF16 ? 2 : 4) || !on_element(ids, 4) || !on_element(status, 4)) return MRL_ERR_INVALID_ARG;
-  const TopArgs a{logits, ld, V, ids, mask, temperature, scale_of(temperature), top, logp, lse, entropy, top_logp, top_ids, status};
+  const float c = scale_of(temperature);
+  const TopArgs a{logits, ld, V, ids, mask, c, 1.0 / ((double)c * (double)temperature), top, logp, lse, entropy, top_logp, top_ids, status};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool bf16 = dtype == MRL_BF16, ent = entropy != nullptr;
   const int parts = parts_of(N, (long long)V * (bf16 ? 2 : 4), kTopCtas);
