@@ -7,6 +7,9 @@ using namespace mrl;
 
 constexpr int kBlock = MRL_SCALE_BLOCK;
 
+__device__ __forceinline__ void store_f(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_f(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
 // ------------------------------------------------------------------------------------------ quantizer
 // A block's elements stay in registers between its maximum and its codes: one read, one write.  Bound by HBM (151,936 x 4,096 bf16 300 us, 6.2 TB/s).
 // kWide: 16 bytes of a row by one load, and their codes by one store.  Otherwise (rows off 16 bytes) four elements by single loads, and four codes by
@@ -175,13 +178,13 @@ __device__ __forceinline__ void fma_f2_here(f2& sum, f2 a, f2 b) {
   asm volatile("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(sum) : "l"(a), "l"(b));
 }
 
-// D[tmem] (+)= A[smem] * B[smem]^T, one 128 x 256 x 32 step on e4m3 codes
-__device__ __forceinline__ void tc_mma_e4m3(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t accum) {
+// D[tmem] (+)= A[smem] * B[smem]^T, one step of 32 on e4m3 codes
+__device__ __forceinline__ void tc_mma_e4m3(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accum) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(kIdescE4m3), "r"(accum)
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accum)
       : "memory");
 }
 
@@ -257,7 +260,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         if (issuer) {
 #pragma unroll
           for (int k = 0; k < kBlock / 32; ++k)  // 32 codes: 32 bytes along a swizzle row
-            tc_mma_e4m3(tmem + (uint32_t)acc * kBN, a + 2 * k, b + 2 * k, k != 0);
+            tc_mma_e4m3(tmem + (uint32_t)acc * kBN, a + 2 * k, b + 2 * k, kIdescE4m3, k != 0);
           tc_commit(empty_bar(stage));
           tc_commit(tfull_bar(acc));
         }
@@ -400,6 +403,173 @@ product_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
   }
 }
 
+// ------------------------------------------------------------------------------------------ product of few rows
+// Up to 16 rows of x: bound by the weights' bytes.  The weights take the tensor core's 128 lanes here and the rows of x its columns, so that a CTA keeps a deep
+// ring of weights alone on its way; a thread sums one weight row's outputs.  Tiles are as high as makes all CTAs work on the same number of
+// them (151,936 rows: 9 of 115 on each of 148 SMs instead of 8 or 9 of 128).
+constexpr int kFewThreads = 192, kFewAccs = 8;  // warps: copies, issue, four that sum; accumulators, one K-block each
+constexpr int kFew = 16;                        // (of 17 rows 129 us against 126 with the tiles above, of 64, with as many columns, 154 against 130)
+constexpr uint32_t kFewStage = kATile + kFew * kBlock;
+constexpr int kFewStages = (int)(200 * 1024 / kFewStage);
+constexpr size_t kFewSmem = (size_t)kFewStages * kFewStage + 1024 /* alignment */ + 512 /* barriers */ + 4 * 4 * kFew * 4 /* scales of x */;
+
+struct FewArgs {
+  const float *x_scales, *w_scales;
+  void* out;
+  long long ld_out;
+  int N, V, k_blocks, tiles, height;  // height: weight rows of a tile
+  int32_t* status;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kFewThreads, 1)
+product_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const FewArgs p) {
+  constexpr uint32_t kIdesc = (1u << 4) | ((uint32_t)(kFew >> 3) << 17) | ((uint32_t)(kBM >> 4) << 24);
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_addr(smem_raw), tiles = (raw + 1023u) & ~1023u;
+  unsigned char* after = smem_raw + (tiles - raw) + (size_t)kFewStages * kFewStage;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(after);
+  const uint32_t bar0 = smem_addr(bars);
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (kFewStages + s); };
+  auto tfull_bar = [&](int a) { return bar0 + 8u * (2 * kFewStages + a); };
+  auto tempty_bar = [&](int a) { return bar0 + 8u * (2 * kFewStages + kFewAccs + a); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kFewStages + 2 * kFewAccs);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kFewStages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    for (int a = 0; a < kFewAccs; ++a) {
+      mbar_init(tfull_bar(a), 1);
+      mbar_init(tempty_bar(a), 4);
+    }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int t = blockIdx.x; t < p.tiles && ok; t += gridDim.x)
+        for (int kb = 0; kb < p.k_blocks; ++kb) {
+          if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) { ok = false; break; }
+          const uint32_t dst = tiles + (uint32_t)stage * kFewStage;
+          mbar_expect_tx(full_bar(stage), (uint32_t)(p.height + kFew) * kBlock);
+          tma_load_2d(dst, &map_w, kb * kBlock, t * p.height, full_bar(stage));
+          tma_load_2d(dst + kATile, &map_x, kb * kBlock, 0, full_bar(stage));
+          if (++stage == kFewStages) { stage = 0; phase ^= 1u; }
+        }
+    }
+  } else if (warp == 1) {
+    const bool issuer = elect_one();
+    int stage = 0, acc = 0;
+    uint32_t phase = 0, acc_phase = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; t < p.tiles && ok; t += gridDim.x)
+      for (int kb = 0; kb < p.k_blocks; ++kb) {
+        if (!mbar_wait2(tempty_bar(acc), acc_phase ^ 1u, full_bar(stage), phase, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t src = tiles + (uint32_t)stage * kFewStage;
+        const uint64_t a = smem_desc_k128(src), b = smem_desc_k128(src + kATile);
+        if (issuer) {
+#pragma unroll
+          for (int k = 0; k < kBlock / 32; ++k) tc_mma_e4m3(tmem + (uint32_t)(acc * kFew), a + 2 * k, b + 2 * k, kIdesc, k != 0);
+          tc_commit(empty_bar(stage));
+          tc_commit(tfull_bar(acc));
+        }
+        if (++stage == kFewStages) { stage = 0; phase ^= 1u; }
+        if (++acc == kFewAccs) { acc = 0; acc_phase ^= 1u; }
+      }
+  } else {
+    const int quad = warp & 3;
+    float* sx = reinterpret_cast<float*>(after + 512) + (warp - 2) * 4 * kFew;  // [4 K-blocks][kFew], this warp's own
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; t < p.tiles && ok; t += gridDim.x) {
+      const int within = quad * 32 + lane, v = t * p.height + within;
+      const bool live = within < p.height && v < p.V;
+      const float* ws = p.w_scales + (live ? (long long)(v / kBlock) * p.k_blocks : 0);
+      float sum[kFew];
+#pragma unroll
+      for (int j = 0; j < kFew; ++j) sum[j] = 0.f;
+#pragma unroll 1
+      for (int kb0 = 0; kb0 < p.k_blocks && ok; kb0 += 4) {
+        float sw[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sw[q] = live && kb0 + q < p.k_blocks ? ws[kb0 + q] : 0.f;
+        __syncwarp();
+#pragma unroll
+        for (int r = lane; r < kFew; r += 32)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) sx[q * kFew + r] = r < p.N && kb0 + q < p.k_blocks ? p.x_scales[(long long)r * p.k_blocks + kb0 + q] : 0.f;
+        __syncwarp();
+#pragma unroll 1
+        for (int q = 0; q < 4 && kb0 + q < p.k_blocks; ++q) {
+          ok = mbar_wait(tfull_bar(acc), acc_phase, abort_flag);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+          const float w = q == 0 ? sw[0] : q == 1 ? sw[1] : q == 2 ? sw[2] : sw[3];
+          const uint32_t src = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * kFew);
+          const float4* s4 = reinterpret_cast<const float4*>(sx + q * kFew);
+#pragma unroll
+          for (int c = 0; c < kFew; c += 16) {
+            uint32_t d[16];
+            tc_ld16(src + (uint32_t)c, d);
+            if (c + 16 == kFew) {
+              tc_fence_before();
+              if (lane == 0) mbar_arrive(tempty_bar(acc));
+            }
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+              const float4 s = s4[(c + j) / 4];
+              sum[c + j] = fmaf(__uint_as_float(d[j]), s.x * w, sum[c + j]);
+              sum[c + j + 1] = fmaf(__uint_as_float(d[j + 1]), s.y * w, sum[c + j + 1]);
+              sum[c + j + 2] = fmaf(__uint_as_float(d[j + 2]), s.z * w, sum[c + j + 2]);
+              sum[c + j + 3] = fmaf(__uint_as_float(d[j + 3]), s.w * w, sum[c + j + 3]);
+            }
+          }
+          if (++acc == kFewAccs) { acc = 0; acc_phase ^= 1u; }
+        }
+      }
+      if (!ok) break;
+      if (live) {
+        T* out = static_cast<T*>(p.out) + v;
+#pragma unroll
+        for (int j = 0; j < kFew; ++j)
+          if (j < p.N) store_f(out + j * p.ld_out, sum[j]);
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {
+    if (threadIdx.x == 0 && p.status != nullptr) atomicOr(p.status, MRL_DEV_TIMEOUT);
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);  // let copies and MMAs still in flight land before the CTA goes
+    __syncthreads();
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  }
+}
+
 // Tensor map of a row-major matrix of codes [rows, cols], read in tiles of box_rows x 128; zeros beyond its ends.
 int make_code_map(CUtensorMap* map, const void* base, long long rows, int cols, long long ld, int box_rows) {
   EncodeTiledFn fn = encode_fn();
@@ -429,6 +599,25 @@ int launch_product(const CUtensorMap& mx, const CUtensorMap& mw, const ProductAr
   return cudaGetLastError() == cudaSuccess ? MRL_OK : MRL_ERR_CUDA;
 }
 
+template <typename T>
+int launch_few(const void* x8, long long ld_x, const void* w8, long long ld_w, int H, FewArgs a, cudaStream_t st) {
+  static std::atomic<uint64_t> attr_done;
+  int rc = mrl_once_per_device(attr_done, [] {
+    return cudaFuncSetAttribute(product_few_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem);
+  });
+  if (rc != MRL_OK) return rc;
+  const int sms = sm_count(), rounds = (int)(((long long)a.V + (long long)sms * kBM - 1) / ((long long)sms * kBM));
+  a.height = (int)(((long long)a.V + (long long)sms * rounds - 1) / ((long long)sms * rounds));
+  a.tiles = (a.V + a.height - 1) / a.height;
+  CUtensorMap mx, mw;
+  rc = make_code_map(&mx, x8, a.N, H, ld_x, kFew);
+  if (rc == MRL_OK) rc = make_code_map(&mw, w8, a.V, H, ld_w, a.height);
+  if (rc != MRL_OK) return rc;
+  mrl_profile_before(st, "product_few_kernel");
+  product_few_kernel<T><<<a.tiles < sms ? a.tiles : sms, kFewThreads, kFewSmem, st>>>(mx, mw, a);
+  mrl_profile_after(st);
+  return cudaGetLastError() == cudaSuccess ? MRL_OK : MRL_ERR_CUDA;
+}
 bool row_type_ok(int32_t dtype) { return dtype == MRL_BF16 || dtype == MRL_F32; }
 bool on_element(const void* p, int elem) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(elem - 1)) == 0; }
 
@@ -466,6 +655,11 @@ extern "C" int mrl_e4m3_product(const void* x8, int64_t ld_x, const float* x_sca
     return MRL_ERR_INVALID_ARG;
   if (out == x8 || out == w8 || out == x_scales || out == w_scales) return MRL_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int k_blocks = (H + kBlock - 1) / kBlock;
+  if (N <= kFew) {
+    FewArgs f{x_scales, w_scales, out, ld_out, (int)N, V, k_blocks, 0, 0, status};
+    return out_dtype == MRL_BF16 ? launch_few<__nv_bfloat16>(x8, ld_x, w8, ld_w, H, f, st) : launch_few<float>(x8, ld_x, w8, ld_w, H, f, st);
+  }
   CUtensorMap mx, mw;
   int rc = make_code_map(&mx, x8, N, H, ld_x, kBM);
   if (rc == MRL_OK) rc = make_code_map(&mw, w8, V, H, ld_w, kBN);
@@ -478,7 +672,7 @@ extern "C" int mrl_e4m3_product(const void* x8, int64_t ld_x, const float* x_sca
   a.N = N;
   a.ld_out = ld_out;
   a.V = V;
-  a.k_blocks = (H + kBlock - 1) / kBlock;
+  a.k_blocks = k_blocks;
   a.m_tiles = (int)((N + kBM - 1) / kBM);
   a.n_tiles = (V + kBN - 1) / kBN;
   a.group_m = 4096 / kBM;  // rows of x that stay in L2 while the weights pass by
