@@ -119,7 +119,7 @@ extern "C" {
 #define MRL_WS_RMSNORM_BWD 4            /* N rows of H columns; V, dtype, S unused */
 #define MRL_WS_GRAD_NORM 5              /* a constant; the sizes are unused */
 #define MRL_WS_ADAMW 6                  /* a constant; the sizes are unused */
-#define MRL_WS_DISTILL 7                /* N rows; V, H, dtype, S unused */
+#define MRL_WS_DISTILL 7                /* N rows, S = places of a list (0: MRL_MAX_TOP); V, H, dtype unused */
 
 #define MRL_MAX_TOP 128      /* longest list of a row's top tokens */
 
@@ -648,8 +648,9 @@ int mrl_e4m3_product(const void* x8, int64_t ld_x, const float* x_scales, const 
  * top_logp as the formulas give them (NaN).  NaN logits are never listed; where fewer than `top` tokens can be, top_ids ends in -1, with
  * top_logp -inf.
  * float32 sums; bitwise reproducible for calls of the same N, V, dtype and alignment (few rows are cut among several CTAs: the
- * last bits of lse can differ from those of a larger call; ids never do).  Cost follows the bytes except on rows with
- * more than 2,048 candidates for the list -- rising ones, or long runs of one value at the top -- which are read several times.
+ * last bits of lse can differ from those of a larger call; ids never do).  Cost follows the bytes, except that rows whose logits rise with the
+ * index are read twice and rows with long runs of one value at the top (more than 1,024 tokens that the list's last place is among) some
+ * eight times.
  * One output at least has to be given.  N = 0 is a no-op.  V > 2^30 -> MRL_ERR_UNSUPPORTED_SHAPE.  MRL_ERR_INVALID_ARG as in mrl_token_logprobs, and for a temperature or top
  * outside its range, an address that is not a multiple of its element, one address for two outputs.
  */
@@ -679,7 +680,7 @@ int mrl_top_logprobs(const void* logits, int32_t dtype, int64_t N, int32_t V, in
  *   row_kl     [device] float32 [N], nullable
  *   loss       [device] float32 [1]
  *   stats      [device] int64 [2], nullable: valid rows, refused rows (both added to under MRL_FLAG_ACCUMULATE_LOSS)
- *   workspace: mrl_workspace_bytes(MRL_WS_DISTILL, N, 0, 0, 0, 0)
+ *   workspace: mrl_workspace_bytes(MRL_WS_DISTILL, N, 0, 0, 0, top)
  * A row is valid if its mask is on, its list has a used place and is not refused.  Refused (and flagged): an id >= V
  * (MRL_DEV_BAD_TOKEN_ID), a token twice, a log-prob of NaN or +inf (MRL_DEV_BAD_LIST).  Rows that are not valid: row_kl 0, gradient 0.
  * Where the learner leaves the rest nothing -- every token is listed, or the others are masked with -inf or the type's lowest

@@ -7,7 +7,7 @@ size_t mrl_thl_workspace_bytes(long long total_words);
 size_t mrl_rmsnorm_bwd_workspace_bytes(long long N, int H);
 size_t mrl_grad_norm_workspace_bytes();
 size_t mrl_adamw_workspace_bytes();
-size_t mrl_distill_workspace_bytes(long long N);
+size_t mrl_distill_workspace_bytes(long long N, int top);
 
 extern "C" size_t mrl_workspace_bytes(int32_t which, int64_t N, int32_t V, int32_t H, int32_t dtype, int32_t S) {
   (void)dtype;
@@ -28,7 +28,7 @@ extern "C" size_t mrl_workspace_bytes(int32_t which, int64_t N, int32_t V, int32
     case MRL_WS_ADAMW:
       return mrl_adamw_workspace_bytes();
     case MRL_WS_DISTILL:
-      return mrl_distill_workspace_bytes(N);
+      return mrl_distill_workspace_bytes(N, S);
     default:
       return 0;
   }

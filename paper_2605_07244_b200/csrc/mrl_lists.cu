@@ -1276,12 +1276,12 @@ struct DistillWs {
   int2 *counts, *sums;
   size_t bytes;
 };
-DistillWs carve(void* ws, long long N) {
+DistillWs carve(void* ws, long long N, int top) {
   MrlCarver c(ws);
   DistillWs w;
   w.records = c.take<ListRecord>((size_t)N);
   w.factors = c.take<RowFactors>((size_t)N);
-  w.z = c.take<float>((size_t)N * kTop);
+  w.z = c.take<float>((size_t)N * top);
   w.term = c.take<double>((size_t)N);
   w.counts = c.take<int2>((size_t)((N + kListRows - 1) / kListRows));
   w.sums = c.take<int2>(kCounts);
@@ -1296,7 +1296,10 @@ float scale_of(float temperature) { return (float)(1.4426950408889634 / (double)
 
 }  // namespace
 
-size_t mrl_distill_workspace_bytes(long long N) { return N > 0 ? carve(nullptr, N).bytes : 0; }
+size_t mrl_distill_workspace_bytes(long long N, int top) {
+  if (N <= 0 || top > kTop) return 0;
+  return carve(nullptr, N, top > 0 ? top : kTop).bytes;
+}
 
 extern "C" int mrl_top_logprobs(const void* logits, int32_t dtype, int64_t N, int32_t V, int64_t ld, const int32_t* ids,
                                 const uint8_t* mask, float temperature, int32_t top, float* logp, float* lse, float* entropy,
@@ -1358,9 +1361,9 @@ extern "C" int mrl_distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64
     return MRL_ERR_INVALID_ARG;
   if (dlogits == logits && ld_out != ld && N > 1) return MRL_ERR_INVALID_ARG;
   if (row_kl != nullptr && (row_kl == loss || row_kl == row_weight || row_kl == top_logp)) return MRL_ERR_INVALID_ARG;
-  if (workspace == nullptr || workspace_bytes < mrl_distill_workspace_bytes(N)) return MRL_ERR_WORKSPACE_TOO_SMALL;
+  if (workspace == nullptr || workspace_bytes < mrl_distill_workspace_bytes(N, top)) return MRL_ERR_WORKSPACE_TOO_SMALL;
   if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return MRL_ERR_INVALID_ARG;
-  const DistillWs w = carve(workspace, N);
+  const DistillWs w = carve(workspace, N, top);
   const int blocks = (int)((N + kListRows - 1) / kListRows);
   const bool bf16 = dtype == MRL_BF16;
   DistillArgs a{logits, dlogits, ld, ld_out, N, V, top, top_ids, top_logp, mask, row_weight, *dp, scale_of(dp->temperature), 0.0, row_kl,

@@ -380,8 +380,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
               }
             } else {
               const T* staged = reinterpret_cast<const T*>(after + 256 + (warp - 4) * kOutWarp);
-              for (int r = 0; r < rows; ++r)
-                if (lane < kCols && c + lane < cols) out[r * p.ld_out + c + lane] = staged[r * (kOutRow / sizeof(T)) + lane];
+              const int col = lane % kCols;  // (of float32 two rows at a time)
+#pragma unroll 4
+              for (int r = lane / kCols; r < rows; r += 32 / kCols)
+                if (c + col < cols) out[r * p.ld_out + c + col] = staged[r * (kOutRow / sizeof(T)) + col];
             }
             __syncwarp();
           }
