@@ -649,8 +649,7 @@ int mrl_e4m3_product(const void* x8, int64_t ld_x, const float* x_scales, const 
  * top_logp -inf.
  * float32 sums; bitwise reproducible for calls of the same N, V, dtype and alignment (few rows are cut among several CTAs: the
  * last bits of lse can differ from those of a larger call; ids never do).  Cost follows the bytes, except that rows whose logits rise with the
- * index are read twice and rows with long runs of one value at the top (more than 1,024 tokens that the list's last place is among) some
- * eight times.
+ * index and rows with more than 1,024 tokens of one value, the list's last place among them, are read once or twice more.
  * One output at least has to be given.  N = 0 is a no-op.  V > 2^30 -> MRL_ERR_UNSUPPORTED_SHAPE.  MRL_ERR_INVALID_ARG as in mrl_token_logprobs, and for a temperature or top
  * outside its range, an address that is not a multiple of its element, one address for two outputs.
  */

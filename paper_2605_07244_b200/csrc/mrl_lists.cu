@@ -265,111 +265,48 @@ struct TopShared {
   Sums part[kMaxParts], red[kTopWarps];
   uint4 held[2 * kHeld];         // the first of them
   int vec[kNoted];               // vectors noted
-  uint32_t hist[256], pick[4], pick2[2 * kTopWarps], n_vec, n_cand, n_list, n_pool;
+  uint32_t pick2[2 * kTopWarps], n_vec, n_cand, n_list, n_pool;
 };
 // (CTA 0 of a row that several share) what is left of the candidates of all
 constexpr int kPool = kMaxParts * kFew;
 
-// The largest digit d (of 256) such that at least `want` counts lie at or above it; `want` becomes what is wanted of d itself.
-__device__ __forceinline__ int pick_digit(TopShared& sh, uint32_t& want) {
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    uint32_t above = 0;
-    int d = 255;
-    for (; d > 0 && above + sh.hist[d] < want; --d) above += sh.hist[d];
-    sh.pick[0] = (uint32_t)d;
-    sh.pick[1] = want - above;
-  }
-  __syncthreads();
-  want = sh.pick[1];
-  return (int)sh.pick[0];
-}
-__device__ __forceinline__ void count_digit(uint32_t* hist, bool on, uint32_t digit) {
-  const unsigned who = __ballot_sync(0xffffffffu, on);
-  if (who == 0) return;
-  int same;
-  const uint32_t d = __shfl_sync(0xffffffffu, digit, __ffs(who) - 1);
-  same = __all_sync(0xffffffffu, !on || digit == d);  // (long runs of one value: one addition a warp)
-  if (same) {
-    if ((threadIdx.x & 31) == __ffs(who) - 1) atomicAdd(&hist[d], (uint32_t)__popc(who));
-  } else if (on) {
-    atomicAdd(&hist[digit], 1u);
-  }
-}
-
-// Calls f(z, index in the part) for every element of a part, with all threads of a warp together; z is NaN where a thread has none.
-template <typename T, typename F>
-__device__ __forceinline__ void each_element(const Part<T>& part, F f) {
-  const int tid = threadIdx.x;
-  f(tid < part.head ? load_f<T>(part.z + tid) : NAN, tid);
-  f(tid < part.tail ? load_f<T>(part.z + part.n - part.tail + tid) : NAN, part.n - part.tail + tid);
-#pragma unroll 1
-  for (int r = 0; r < part.vecs; r += kTopThreads) {
-    const bool on = r + tid < part.vecs;
-    const int at = part.head + (r + tid) * kVecElems<T>;
-    const Vec v = on ? load_vec(part.z + at) : no_vec<T>();
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if constexpr (sizeof(T) == 2) {
-        f(on ? bf16lo_to_f32(v.w[j]) : NAN, at + 2 * j);
-        f(on ? bf16hi_to_f32(v.w[j]) : NAN, at + 2 * j + 1);
-      } else {
-        f(on ? __uint_as_float(v.w[j]) : NAN, at + j);
-      }
-    }
-  }
-}
-
-// The `top` largest keys of a part by 256-way counting: a pass for each eight bits of the last one's value, then of its index up to which tokens of that
-// value are listed, and one that collects.  For rows with more than kCap tokens that are not below the last floor: long runs of one value at the top.  Reads
-// the row six (bf16) to eight times.
+// Adds the first `want` tokens of a part whose logits are `z` to its candidates.
 template <typename T>
-__device__ void select_top(const Part<T> part, int top, TopShared& sh) {
-  Key last = 0;
-  uint32_t want = (uint32_t)top;
-#pragma unroll 1
-  for (int shift = 56; shift >= 0; shift -= 8) {
-    if (sizeof(T) == 2 && (shift == 40 || shift == 32)) {  // a bf16's ordinal ends in sixteen zeros, or ones
-      if (!(last >> 63)) last |= (Key)0xff << shift;
-      continue;
-    }
-    for (int i = threadIdx.x; i < 256; i += kTopThreads) sh.hist[i] = 0;
-    __syncthreads();
-    each_element<T>(part, [&](float z, int i) {
-      const Key key = key_of(z, part.first + i);
-      count_digit(sh.hist, (key >> 32) != 0 && (shift == 56 || (key >> (shift + 8)) == (last >> (shift + 8))), (uint32_t)(key >> shift) & 255u);
-    });
-    last |= (Key)pick_digit(sh, want) << shift;
-  }
-  if (threadIdx.x == 0) sh.n_cand = 0;
-  __syncthreads();
-  each_element<T>(part, [&](float z, int i) {
-    const Key key = key_of(z, part.first + i);
-    if (key >= last) sh.cand[min(atomicAdd(&sh.n_cand, 1u), (uint32_t)(kCap - 1))] = key;
-  });
-  __syncthreads();
-}
-
-// Adds the first `want` tokens of -inf of a part to its candidates (all others are there).
-template <typename T>
-__device__ __noinline__ void add_masked(const Part<T> part, int want, TopShared& sh) {
+__device__ __noinline__ void add_equal(const T* part, int n, int first, float z, int want, TopShared& sh) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll 1
-  for (int r = 0; r < part.n && want > 0; r += kTopThreads) {
+  for (int r = 0; r < n && want > 0; r += kTopThreads) {
     const int i = r + threadIdx.x;
-    const bool masked = i < part.n && load_f<T>(part.z + i) == -INFINITY;
-    const unsigned who = __ballot_sync(0xffffffffu, masked);
-    if (lane == 0) sh.hist[warp] = (uint32_t)__popc(who);
+    const bool equal = i < n && load_f<T>(part + i) == z;
+    const unsigned who = __ballot_sync(0xffffffffu, equal);
+    if (lane == 0) sh.pick2[warp] = (uint32_t)__popc(who);
     __syncthreads();
     int before = __popc(who & ((1u << lane) - 1)), all = 0;
     for (int w = 0; w < kTopWarps; ++w) {
-      before += w < warp ? (int)sh.hist[w] : 0;
-      all += (int)sh.hist[w];
+      before += w < warp ? (int)sh.pick2[w] : 0;
+      all += (int)sh.pick2[w];
     }
-    if (masked && before < want) sh.cand[atomicAdd(&sh.n_cand, 1u)] = key_of(-INFINITY, part.first + i);
+    if (equal && before < want) sh.cand[atomicAdd(&sh.n_cand, 1u)] = key_of(z, first + i);
     want -= all;
     __syncthreads();
   }
+}
+
+// The ordinal of the `want`th largest of kCap candidates.
+__device__ __forceinline__ uint32_t nth_ordinal(const Key* cand, int want) {
+  constexpr int kEach = kCap / kTopThreads;
+  uint32_t mine[kEach], found = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) mine[i] = (uint32_t)(cand[i * kTopThreads + threadIdx.x] >> 32);
+#pragma unroll 1
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t next = found | (1u << bit);
+    int total = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) total += __syncthreads_count(mine[i] >= next);
+    if (total >= want) found = next;
+  }
+  return found;
 }
 
 // Copies the keys that can be among the `top` largest of `from` to `to` (of CTA `rank`, behind what its counter says is there): at most kFew,
@@ -456,6 +393,41 @@ __device__ __forceinline__ uint32_t not_below(const Vec& v, float floor) {
   return bits;
 }
 
+// Candidates: what is not below `least_z`.  Behind kCap of them each takes an earlier one's place, by a hash of its index.  The vectors that were noted are
+// read; where too many were (a row that rises) all are, once more.  At 16 kCap it is clear that the floor has to rise, and the rest is left (a row of one
+// value, 2,048 x 151,936 bf16, top 20: 841 -> 307 us; random values 130).
+template <typename T>
+__device__ __forceinline__ void collect(const Part<T>& part, float z_head, float z_tail, float least_z, TopShared& sh) {
+  const int tid = threadIdx.x;
+  auto push = [&](float z, int index) {
+    if (z >= least_z) {
+      const uint32_t at = atomicAdd(&sh.n_cand, 1u);
+      if (at < kCap) sh.cand[at] = key_of(z, part.first + index);
+      else atomicExch(&sh.cand[((uint32_t)index * 2654435769u) / (0xffffffffu / kCap + 1)], key_of(z, part.first + index));
+    }
+  };
+  if (tid < part.head) push(z_head, tid);
+  if (tid < part.tail) push(z_tail, part.n - part.tail + tid);
+  const bool all = sh.n_vec > kNoted;
+  const int noted = all ? part.vecs : (int)sh.n_vec;
+  for (int k = tid; k < noted && *(volatile uint32_t*)&sh.n_cand < 16 * kCap; k += kTopThreads) {
+    const int at = all ? k : sh.vec[k];
+    Vec v;
+    if (!all && k < kHeld) {
+      const uint4 a = sh.held[k], b = sh.held[kHeld + k];
+      v = Vec{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+    } else {
+      v = load_vec(part.body() + (size_t)at * kVecBytes);
+    }
+    uint32_t bits = not_below<T>(v, least_z);
+#pragma unroll 1
+    for (; bits != 0; bits &= bits - 1) {
+      const int e = __ffs(bits) - 1;
+      push(element<T>(v, e), part.head + at * kVecElems<T> + e);
+    }
+  }
+}
+
 template <typename T, bool kEnt>
 __global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArgs p) {
   __shared__ TopShared sh;
@@ -539,47 +511,36 @@ __global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArg
         }
       }
   }
+  a = block_sums<kTopThreads>(a, sh.red);
   int n = 0;
   if (p.top > 0) {
-    best = fmaxf(best, z_tail);
-    floor = floor_of<T>(kth_ordinal<T>(ordinal(best), p.top, p.top / 4, sh.pick2));  // (barriers: the vectors are noted)
-    auto push = [&](float z, int index) {
-      if (z >= floor) {
-        const uint32_t at = atomicAdd(&sh.n_cand, 1u);
-        if (at < kCap) sh.cand[at] = key_of(z, part.first + index);
-      }
-    };
-    if (tid < part.head) push(z_head, tid);
-    if (tid < part.tail) push(z_tail, part.n - part.tail + tid);
-    // (too many noted -- a row that rises: all vectors, once more)
-    const bool all = sh.n_vec > kNoted;
-    const int noted = all ? part.vecs : (int)sh.n_vec;
-    for (int k = tid; k < noted; k += kTopThreads) {
-      const int at = all ? k : sh.vec[k];
-      Vec v;
-      if (!all && k < kHeld) {
-        const uint4 a = sh.held[k], b = sh.held[kHeld + k];
-        v = Vec{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
-      } else {
-        v = load_vec(part.body() + (size_t)at * kVecBytes);
-      }
-      uint32_t bits = not_below<T>(v, floor);
+    uint32_t least = kth_ordinal<T>(ordinal(fmaxf(best, z_tail)), p.top, p.top / 4, sh.pick2);  // (barriers: the vectors are noted)
+    float crowd = -INFINITY;
+    // More candidates than there is room for: the `top`th value of the kCap that were kept is the next floor, or what is above it, where that is the floor
+    // already and so is what crowds the list.  Two rounds drop kCap - top of them at least.
 #pragma unroll 1
-      for (; bits != 0; bits &= bits - 1) {
-        const int e = __ffs(bits) - 1;
-        push(element<T>(v, e), part.head + at * kVecElems<T> + e);
+    for (;;) {
+      collect<T>(part, z_head, z_tail, floor_of<T>(least), sh);
+      __syncthreads();
+      n = (int)sh.n_cand;
+      if (n <= kCap) break;
+      const uint32_t higher = nth_ordinal(sh.cand, p.top);
+      if (floor_of<T>(higher) > floor_of<T>(least)) {
+        least = higher;
+      } else {
+        crowd = floor_of<T>(least);
+        least = sizeof(T) == 2 ? ((ordinal(crowd) >> 16) + 1) << 16 : ordinal(crowd) + 1;
       }
-    }
-  }
-  a = block_sums<kTopThreads>(a, sh.red);  // (a barrier: the candidates are there)
-  if (p.top > 0) {
-    const int found = (int)sh.n_cand;
-    if (found > kCap) select_top<T>(part, p.top, sh);
-    if (found < min(p.top, part.n)) {
       __syncthreads();  // (all have read the number)
-      add_masked<T>(part, p.top - found, sh);
+      if (tid == 0) sh.n_cand = 0;
+      __syncthreads();
     }
-    n = (int)sh.n_cand;
+    // Masked tokens, or those of the value that crowds, from the front.
+    if (n < min(p.top, part.n)) {
+      __syncthreads();
+      add_equal<T>(part.z, part.n, part.first, crowd, p.top - n, sh);
+      n = (int)sh.n_cand;
+    }
   }
   if (parts > 1) {
     cluster_wait();

@@ -132,6 +132,30 @@ def test_special_rows(dtype, V, top, N):
         check(z[-3:], {k: v[-3:] if torch.is_tensor(v) else v for k, v in got.items()}, None, None, 1.0, top)
 
 
+def crowded_rows(V, dtype, N):
+    """Rows where more tokens than a list of candidates holds are near its last place."""
+    g = torch.Generator().manual_seed(V + 1)
+    low = torch.finfo(dtype).min
+    rising = torch.arange(V).float() * 2.0 ** -14
+    ten = torch.full((V,), low)
+    ten[torch.randperm(V, generator=g)[:10]] = torch.randn(10, generator=g)
+    few_values = torch.randint(-2, 3, (V,), generator=g).float()
+    crowd = torch.where(torch.rand(V, generator=g) < 0.7, torch.tensor(0.5), torch.randn(V, generator=g) * 0.2)
+    bands = torch.randn(V, generator=g) + torch.where((torch.arange(V) // 8) % 256 < 150, 100.0, 0.0)
+    signs = torch.where(torch.rand(V, generator=g) < 0.5, torch.tensor(-0.0), torch.tensor(0.0))
+    below = -1.0 - torch.rand(V, generator=g) * 2.0 ** -6
+    out = [rising, -rising, rising.flip(0) * 3, ten, few_values, crowd, bands, signs, below, -few_values.abs()]
+    return torch.stack(out + [torch.randn(V, generator=g) for _ in range(max(0, N - len(out)))]).to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V,top,N", [(40001, 128, 0), (151936, 20, 0), (151936, 128, 310), (20011, 100, 310)])
+def test_crowded_rows(dtype, V, top, N):
+    z = crowded_rows(V, dtype, N)
+    got = run(z, z.view(-1), None, None, 1.0, top)
+    check(z[:10], {k: v[:10] if torch.is_tensor(v) else v for k, v in got.items()}, None, None, 1.0, top)
+
+
 def test_bad_ids_and_masks():
     z, flat = rows(6, 5000, torch.bfloat16, 1)
     ids = torch.tensor([0, -1, 4999, 5000, 7, 2 ** 31 - 1], dtype=torch.int32)
