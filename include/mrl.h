@@ -623,7 +623,7 @@ int mrl_e4m3_quantize(const void* x, int64_t ld_x, int32_t dtype, int64_t N, int
  *   out       [device] out_dtype [N, ld_out], MRL_BF16 or MRL_F32
  *   status    [device] int32 [1], nullable
  * x8 and w8 have to start on 16 bytes, with row strides (of more than one row) that are multiples of 16 (else MRL_ERR_INVALID_ARG); what lies between
- * column H and the stride is not read.  Any N, H <= 2^24, V.  Bitwise reproducible; a row's result does not depend on the other rows, but its
+ * column H and the stride is not read.  H <= 2^24, V <= 2^30.  Bitwise reproducible; a row's result does not depend on the other rows, but its
  * last bits may on N.  N = 0 is a no-op.  No gradient: what is scored here is frozen.
  */
 int mrl_e4m3_product(const void* x8, int64_t ld_x, const float* x_scales, const void* w8, int64_t ld_w,

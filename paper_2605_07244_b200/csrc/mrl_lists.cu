@@ -976,7 +976,12 @@ __device__ __forceinline__ Totals rest_of_row(Sums& a, bool& low, const DistillA
   }
   low = a.s == 0.f;
   if (!low) return Totals{(double)a.m, a.s, 0.f};
-  return low_sums<T, kThreads>(zrow, p.V, p.c, sh.red, sh.ids, p.top);
+  const Totals t = low_sums<T, kThreads>(zrow, p.V, p.c, sh.red, sh.ids, p.top);
+  if (parts > 1) {  // (the whole row was read: no CTA may write its gradient over it before all have)
+    cluster_arrive();
+    cluster_wait();
+  }
+  return t;
 }
 
 // kShifted: outputs need not start on the same bytes of 32 as their inputs.  (A kernel of its own: code that a row runs through once comes from far, some 30 cycles

@@ -649,7 +649,7 @@ extern "C" int mrl_e4m3_product(const void* x8, int64_t ld_x, const float* x_sca
                                 int32_t* status, void* stream) {
   if (!row_type_ok(out_dtype)) return MRL_ERR_UNSUPPORTED_DTYPE;
   if (N < 0 || H < 1 || V < 1 || ld_x < H || ld_w < H || ld_out < V) return MRL_ERR_INVALID_ARG;
-  if (H > (1 << 24) || N > 0x7fffffffll) return MRL_ERR_UNSUPPORTED_SHAPE;
+  if (H > (1 << 24) || V > (1 << 30) || N > 0x7fffffffll) return MRL_ERR_UNSUPPORTED_SHAPE;
   if (N == 0) return MRL_OK;
   if (x8 == nullptr || x_scales == nullptr || w8 == nullptr || w_scales == nullptr || out == nullptr) return MRL_ERR_INVALID_ARG;
   if (!on_element(x8, 16) || !on_element(w8, 16) || (N > 1 && ld_x % 16 != 0) || (V > 1 && ld_w % 16 != 0)) return MRL_ERR_INVALID_ARG;

@@ -167,6 +167,28 @@ def test_extreme_logits(kind, dtype):
     assert got["dz"][3].isfinite().all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kind", sorted(KINDS))
+@pytest.mark.parametrize("N", [1, 6, 310])
+def test_low_rows_of_several_blocks_in_place(N, kind, dtype):
+    V, low = 100003, torch.finfo(dtype).min
+    g = torch.Generator().manual_seed(N)
+    z = torch.randn(N, V, generator=g).to(dtype)
+    z[::2] = low
+    z[::2, 99990:] = 0.75 * low       # what the rest of these rows has is far from its first parts
+    z[4::6] = -math.inf
+    z[4::6, :8] = torch.randn(8, generator=g).to(dtype)
+    z[4::6, 50000] = low
+    ids = torch.arange(8, dtype=torch.int32).expand(N, 8).contiguous()
+    logq = torch.log_softmax(torch.randn(N, 9, generator=g), 1)[:, :8].contiguous()
+    dp = params(kind, denominator=5.0)
+    a = run(z, z.view(-1), ids, logq, None, None, dp)
+    for _ in range(3):
+        b = run(z, z.view(-1), ids, logq, None, None, dp, in_place=True)
+        assert torch.equal(a["dz"].view(torch.uint8), b["dz"].view(torch.uint8))
+        assert torch.equal(a["row_kl"].view(torch.int32), b["row_kl"].view(torch.int32))
+
+
 def test_refused_lists_and_empty_rows():
     z, flat = rows(9, 2000, torch.bfloat16, 5)
     ids, logq = lists(z, 70, 1, unused=False)

@@ -41,6 +41,7 @@ def test_product_refusals(lib):
     assert call(xs=0x40002) == 1 and call(out=THIRD + 1) == 1 and call(dtype=B.F32, out=THIRD + 2) == 1 and call(out=FAKE) == 1
     big = (1 << 24) + 16
     assert call(H=big, ld_x=big, ld_w=big) == 7 and call(N=1 << 31) == 7
+    assert call(V=(1 << 30) + 1, ld_out=1 << 31) == 7
     assert call(N=0, x=None) == 0
 
 
