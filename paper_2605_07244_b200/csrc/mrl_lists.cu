@@ -610,7 +610,7 @@ __global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArg
 // Three kernels.  list_kernel: which rows count, and what a row's list gives by itself.  distill_kernel: the rows of logits, the bulk of the work.  finish_kernel: the
 // gradient of the listed tokens, and the loss.
 constexpr int kRowOff = 0, kRowValid = 1, kRowRefused = 2;
-constexpr int kListThreads = 512, kListRows = kListThreads / 32;  // of a CTA of list_kernel: a warp per row
+constexpr int kListThreads = 256, kListRows = kListThreads / 32;  // of a CTA of list_kernel: a warp per row
 constexpr int kPlaces = kTop / 32;                 // places of a lane
 
 // Of a row's list.  With x_k = z_k / T, xs the largest of them, e_k = exp(x_k - xs), q_k the teacher's probabilities:
@@ -702,14 +702,16 @@ __global__ void __launch_bounds__(kListThreads) list_kernel(const DistillArgs p)
     }
     const int used = (p.top + 31) / 32;
 #pragma unroll 1
-    for (int o = 0; o < 32; ++o) {
+    for (int o = 0; o <= 16; ++o) {  // (of two lanes one is at most 16 ahead of the other)
 #pragma unroll
       for (int q = 0; q < kPlaces; ++q) {
         if (q >= used) break;
         const int other = __shfl_sync(0xffffffffu, id[q], (lane + o) & 31);
 #pragma unroll
-        for (int j = 0; j < kPlaces; ++j)
+        for (int j = 0; j < kPlaces; ++j) {
+          if (j >= used) break;
           if (other >= 0 && other == id[j] && !(o == 0 && j == q)) bad |= MRL_DEV_BAD_LIST;
+        }
       }
     }
     bad = __reduce_or_sync(0xffffffffu, bad);
@@ -1015,7 +1017,6 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillArgs 
   // shared memory: bits of the body's vectors | parked vectors | staging
   using Bits = typename std::conditional<sizeof(T) == 2, uint16_t, uint8_t>::type;
   Bits* bits = reinterpret_cast<Bits*>(dyn);
-  let_next_start();
 
   if (tid >= kStream) {
     // ---- the last warp: the list
@@ -1028,6 +1029,7 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillArgs 
       l[i] = k < p.top ? p.top_logp[row * p.top + k] : -INFINITY;
     }
     wait_for_previous();
+    let_next_start();  // (behind the wait: what list_kernel wrote is there when finish_kernel starts)
     // (a word of the record a lane, and the counts: they come together)
     constexpr int kRecordWords = (int)sizeof(ListRecord) / 4;
     const int stat = p.records[row].stat, word = reinterpret_cast<const int*>(p.records + row)[lane % kRecordWords];
@@ -1099,6 +1101,7 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillArgs 
   const float z_head = tid < part.head ? load_f<T>(part.z + tid) : -INFINITY;
   const float z_tail = tid < part.tail ? load_f<T>(part.z + part.n - part.tail + tid) : -INFINITY;
   wait_for_previous();
+  let_next_start();
   const int stat = p.records[row].stat;
   uint4* planes = dyn + p.bit_words / 4;
   for (int i = tid; i < p.bit_words / 4; i += kStream) dyn[i] = make_uint4(0, 0, 0, 0);
@@ -1199,26 +1202,49 @@ template <typename T>
 __global__ void __launch_bounds__(1024) finish_kernel(const DistillArgs p) {
   __shared__ double red[32];
   __shared__ int2 redc[32];
-  wait_for_previous();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (blockIdx.x > 0) {
     const long long row = (long long)(blockIdx.x - 1) * 32 + warp;
-    if (row >= p.N || p.records[row].stat != kRowValid) return;
+    // what is known before the rows are done: list_kernel's results (from L2: it ended before distill_kernel's CTAs let this kernel start)
+    const bool valid = row < p.N && __ldcg(&p.records[row].stat) == kRowValid;
+    int id[kPlaces];
+    double x[kPlaces], ln_q[kPlaces], e[kPlaces];
+    if (valid) {
+      const double xs = __ldcg(&p.records[row].xs), ln_one = __ldcg(&p.records[row].ln_one);
+#pragma unroll
+      for (int i = 0; i < kPlaces; ++i) {
+        const int k = i * 32 + lane;
+        id[i] = -1;
+        if (k >= p.top) continue;
+        id[i] = p.top_ids[row * p.top + k];
+        const float l = p.top_logp[row * p.top + k];
+        if (l == -INFINITY) id[i] = -1;
+        x[i] = ((double)__ldcg(p.z + row * p.top + k) * (double)p.c - xs) * p.nat;
+        ln_q[i] = (double)l - ln_one;
+      }
+#pragma unroll
+      for (int i = 0; i < kPlaces; ++i)
+        if (id[i] >= 0) {
+          e[i] = exp(x[i]);
+          if (p.dp.direction == MRL_DISTILL_FORWARD) ln_q[i] = exp(ln_q[i]);  // (q itself)
+        }
+    }
+    wait_for_previous();
+    if (!valid) return;
     const RowFactors r = p.factors[row];
-    const double xs = p.records[row].xs, ln_one = p.records[row].ln_one;
     T* out = static_cast<T*>(p.dlogits) + row * p.ld_out;
-    for (int k = lane; k < p.top; k += 32) {
-      const int id = p.top_ids[row * p.top + k];
-      const float l = p.top_logp[row * p.top + k];
-      if (id < 0 || l == -INFINITY) continue;
-      const double x = ((double)p.z[row * p.top + k] * (double)p.c - xs) * p.nat, ln_q = (double)l - ln_one, pk = exp(x) * (double)r.p_of_e;
+#pragma unroll
+    for (int i = 0; i < kPlaces; ++i) {
+      if (id[i] < 0) continue;
+      const double pk = e[i] * (double)r.p_of_e;
       double g;
-      if (p.dp.direction == MRL_DISTILL_REVERSE) g = pk != 0.0 ? pk * (x - ln_q + r.shift - r.kl) : 0.0;
-      else g = r.mass * pk - exp(ln_q);
-      store_f(out + id, r.scale != 0.0 ? (float)(g * r.scale) : 0.f);
+      if (p.dp.direction == MRL_DISTILL_REVERSE) g = pk != 0.0 ? pk * (x[i] - ln_q[i] + r.shift - r.kl) : 0.0;
+      else g = r.mass * pk - ln_q[i];
+      store_f(out + id[i], r.scale != 0.0 ? (float)(g * r.scale) : 0.f);
     }
     return;
   }
+  wait_for_previous();
   double v = 0.0;
   for (long long i = threadIdx.x; i < p.N; i += 1024) v += p.term[i];
   v = warp_sum(v);
