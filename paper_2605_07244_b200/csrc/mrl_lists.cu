@@ -13,7 +13,6 @@ namespace {
 
 using namespace mrl;
 
-constexpr int kTopThreads = 256, kTopCtas = 5;          // threads, and CTAs an SM, of the top tokens
 constexpr int kThreads = 512, kWarps = kThreads / 32;  // two CTAs an SM
 constexpr int kTop = MRL_MAX_TOP;
 constexpr int kMaxParts = 8;                            // CTAs that share a row
@@ -109,8 +108,9 @@ int launch_rows(void (*kernel)(Params...), long long N, int parts, int threads, 
   cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cfg.attrs = attr;
-  cfg.numAttrs = behind ? 2 : 1;
+  // (CTAs of a launch with a cluster's attribute, be the cluster one CTA, start at half the rate: 47,360 rows of 2,722 bf16 260 us instead of 143)
+  cfg.attrs = parts > 1 ? attr : attr + 1;
+  cfg.numAttrs = (behind ? 1 : 0) + (parts > 1 ? 1 : 0);
   return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? MRL_OK : MRL_ERR_CUDA;
 }
 
@@ -256,33 +256,43 @@ __device__ __forceinline__ Key key_of(float z, int index) { return ((Key)ordinal
 
 constexpr int kUnroll = 3;       // vectors of a thread and group
 constexpr int kSecondFloor = 3;  // the group behind which the floor is set again
-constexpr int kTopWarps = kTopThreads / 32;
-constexpr int kNoted = 2048, kHeld = 320, kCap = 1024;  // vectors noted, those of them whose elements are held, and candidates, of a CTA
-constexpr int kFew = 256;        // keys that are put in order by counting
+// What a CTA of kT threads holds.  256 threads take rows of any length; fewer take short rows, a thread's share of which is six vectors at most.
+template <int kT>
+struct TopSize {
+  static constexpr bool kAny = kT == 256;
+  static constexpr int kCtas = kAny ? 5 : 1280 / kT;        // an SM
+  static constexpr int kWarps = kT / 32;
+  static constexpr int kNoted = kAny ? 2048 : 6 * kT;       // vectors noted
+  static constexpr int kHeld = kAny ? 320 : kT;             // those of them whose elements are held
+  static constexpr int kCap = kAny ? 1024 : 512;            // candidates
+  static constexpr int kFew = kT;                           // keys that are put in order by counting
+};
+template <int kT>
 struct TopShared {
-  Key cand[kCap];                // candidates of this CTA
-  Key list[kFew];                // what is left of them, or (CTA 0) of the pool
-  Sums part[kMaxParts], red[kTopWarps];
-  uint4 held[2 * kHeld];         // the first of them
-  alignas(16) int vec[kNoted];   // vectors noted; then what puts the list in order
-  uint32_t pick2[2 * kTopWarps], n_vec, n_cand, n_list, n_pool;
+  using Size = TopSize<kT>;
+  Key cand[Size::kCap];                // candidates of this CTA
+  Key list[Size::kFew];                // what is left of them, or (CTA 0) of the pool
+  Sums part[Size::kAny ? kMaxParts : 1], red[Size::kWarps];
+  uint4 held[2 * Size::kHeld];         // the first vectors noted
+  alignas(16) int vec[Size::kNoted];   // vectors noted; then what puts the list in order
+  uint32_t pick2[2 * Size::kWarps], n_vec, n_cand, n_list, n_pool;
 };
 // (CTA 0 of a row that several share) what is left of the candidates of all
-constexpr int kPool = kMaxParts * kFew;
+constexpr int kPool = kMaxParts * TopSize<256>::kFew;
 
 // Adds the first `want` tokens of a part whose logits are `z` to its candidates.
-template <typename T>
-__device__ __noinline__ void add_equal(const T* part, int n, int first, float z, int want, TopShared& sh) {
+template <typename T, int kT>
+__device__ __noinline__ void add_equal(const T* part, int n, int first, float z, int want, TopShared<kT>& sh) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll 1
-  for (int r = 0; r < n && want > 0; r += kTopThreads) {
+  for (int r = 0; r < n && want > 0; r += kT) {
     const int i = r + threadIdx.x;
     const bool equal = i < n && load_f<T>(part + i) == z;
     const unsigned who = __ballot_sync(0xffffffffu, equal);
     if (lane == 0) sh.pick2[warp] = (uint32_t)__popc(who);
     __syncthreads();
     int before = __popc(who & ((1u << lane) - 1)), all = 0;
-    for (int w = 0; w < kTopWarps; ++w) {
+    for (int w = 0; w < kT / 32; ++w) {
       before += w < warp ? (int)sh.pick2[w] : 0;
       all += (int)sh.pick2[w];
     }
@@ -292,12 +302,13 @@ __device__ __noinline__ void add_equal(const T* part, int n, int first, float z,
   }
 }
 
-// The ordinal of the `want`th largest of kCap candidates.
+// The ordinal of the `want`th largest of a full list of candidates.
+template <int kT>
 __device__ __forceinline__ uint32_t nth_ordinal(const Key* cand, int want) {
-  constexpr int kEach = kCap / kTopThreads;
+  constexpr int kEach = TopSize<kT>::kCap / kT;
   uint32_t mine[kEach], found = 0;
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) mine[i] = (uint32_t)(cand[i * kTopThreads + threadIdx.x] >> 32);
+  for (int i = 0; i < kEach; ++i) mine[i] = (uint32_t)(cand[i * kT + threadIdx.x] >> 32);
 #pragma unroll 1
   for (int bit = 31; bit >= 0; --bit) {
     const uint32_t next = found | (1u << bit);
@@ -311,19 +322,19 @@ __device__ __forceinline__ uint32_t nth_ordinal(const Key* cand, int want) {
 
 // Copies the keys that can be among the `top` largest of `from` to `to` (of CTA `rank`, behind what its counter says is there): at most kFew,
 // and all of the `top` largest among them.  Bits are settled from above until few enough are left.
-template <int kMost>
+template <int kMost, int kT>
 __device__ __noinline__ void keep_largest(const Key* from, int n, int top, Key* to, uint32_t* n_to) {
-  constexpr int kEach = kMost / kTopThreads;
+  constexpr int kEach = kMost / kT, kFew = TopSize<kT>::kFew;
   Key mine[kEach];
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) mine[i] = i * kTopThreads + threadIdx.x < n ? from[i * kTopThreads + threadIdx.x] : 0;
+  for (int i = 0; i < kEach; ++i) mine[i] = i * kT + threadIdx.x < n ? from[i * kT + threadIdx.x] : 0;
   Key least = 1;
   if (n > kFew) {
     least = 0;
     for (int bit = 63; bit >= 0; --bit) {
       const Key next = least | ((Key)1 << bit);
       int total = __syncthreads_count(mine[0] >= next);
-      if (n > kTopThreads) {
+      if (n > kT) {
 #pragma unroll
         for (int i = 1; i < kEach; ++i) total += __syncthreads_count(mine[i] >= next);
       }
@@ -339,14 +350,15 @@ __device__ __noinline__ void keep_largest(const Key* from, int n, int top, Key* 
 constexpr uint32_t kLowest = 0x00800000u;  // the ordinal above that of -inf
 // An ordinal, kLowest at least, that `want` threads at least do not fall below with theirs, and `more` + 2 others if that can be.  Bits are settled from above, from
 // the first that the threads differ in.
-template <typename T>
+template <typename T, int kT>
 __device__ __forceinline__ uint32_t kth_ordinal(uint32_t mine, int want, int more, uint32_t* red) {
+  constexpr int kWarps = kT / 32;
   uint32_t high = __reduce_max_sync(0xffffffffu, mine), low = __reduce_min_sync(0xffffffffu, mine);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (lane == 0) red[warp] = high, red[kTopWarps + warp] = low;
+  if (lane == 0) red[warp] = high, red[kWarps + warp] = low;
   __syncthreads();
-  high = __reduce_max_sync(0xffffffffu, red[lane % kTopWarps]);
-  low = __reduce_min_sync(0xffffffffu, red[kTopWarps + lane % kTopWarps]);
+  high = __reduce_max_sync(0xffffffffu, red[lane % kWarps]);
+  low = __reduce_min_sync(0xffffffffu, red[kWarps + lane % kWarps]);
   if (high == low) {
     __syncthreads();  // (`red` may be used again)
     return max(low, kLowest);
@@ -396,8 +408,9 @@ __device__ __forceinline__ uint32_t not_below(const Vec& v, float floor) {
 // Candidates: what is not below `least_z`.  Behind kCap of them each takes an earlier one's place, by a hash of its index.  The vectors that were noted are
 // read; where too many were (a row that rises) all are, once more.  At 16 kCap it is clear that the floor has to rise, and the rest is left (a row of one
 // value, 2,048 x 151,936 bf16, top 20: 841 -> 307 us; random values 130).
-template <typename T>
-__device__ __forceinline__ void collect(const Part<T>& part, float z_head, float z_tail, float least_z, TopShared& sh) {
+template <typename T, int kT>
+__device__ __forceinline__ void collect(const Part<T>& part, float z_head, float z_tail, float least_z, TopShared<kT>& sh) {
+  constexpr int kCap = TopSize<kT>::kCap, kNoted = TopSize<kT>::kNoted, kHeld = TopSize<kT>::kHeld;
   const int tid = threadIdx.x;
   auto push = [&](float z, int index) {
     if (z >= least_z) {
@@ -408,9 +421,9 @@ __device__ __forceinline__ void collect(const Part<T>& part, float z_head, float
   };
   if (tid < part.head) push(z_head, tid);
   if (tid < part.tail) push(z_tail, part.n - part.tail + tid);
-  const bool all = sh.n_vec > kNoted;
+  const bool all = TopSize<kT>::kAny && sh.n_vec > kNoted;
   const int noted = all ? part.vecs : (int)sh.n_vec;
-  for (int k = tid; k < noted && *(volatile uint32_t*)&sh.n_cand < 16 * kCap; k += kTopThreads) {
+  for (int k = tid; k < noted && *(volatile uint32_t*)&sh.n_cand < 16 * kCap; k += kT) {
     const int at = all ? k : sh.vec[k];
     Vec v;
     if (!all && k < kHeld) {
@@ -428,21 +441,22 @@ __device__ __forceinline__ void collect(const Part<T>& part, float z_head, float
   }
 }
 
-template <typename T, bool kEnt>
-__global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArgs p) {
-  __shared__ TopShared sh;
+template <typename T, bool kEnt, int kT>
+__global__ void __launch_bounds__(kT, TopSize<kT>::kCtas) top_kernel(const TopArgs p) {
+  using Size = TopSize<kT>;
+  __shared__ TopShared<kT> sh;
   const int tid = threadIdx.x;
-  int parts, rank;
-  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  int parts = 1, rank = 0;
+  if (Size::kAny) {
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  }
   const long long row = blockIdx.x / (unsigned)parts;
   const T* zrow = static_cast<const T*>(p.logits) + row * p.ld;
   const int id = p.ids != nullptr ? p.ids[row] : 0;
-  const bool on = p.mask == nullptr || p.mask[row] != 0, good = id >= 0 && id < p.V;
-  if (!on || !good) {  // (all CTAs of the row)
-    if (rank != 0) return;
+  auto none = [&](bool bad_id) {
     if (tid == 0) {
-      if (on && p.status != nullptr) atomicOr(p.status, MRL_DEV_BAD_TOKEN_ID);
+      if (bad_id && p.status != nullptr) atomicOr(p.status, MRL_DEV_BAD_TOKEN_ID);
       if (p.logp != nullptr) p.logp[row] = 0.f;
       if (p.lse != nullptr) p.lse[row] = 0.f;
       if (kEnt) p.entropy[row] = 0.f;
@@ -451,6 +465,9 @@ __global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArg
       p.top_ids[row * p.top + tid] = -1;
       p.top_logp[row * p.top + tid] = 0.f;
     }
+  };
+  if (p.mask != nullptr && p.mask[row] == 0) {  // (all CTAs of the row)
+    if (rank == 0) none(false);
     return;
   }
   if (tid == 0) sh.n_vec = sh.n_cand = sh.n_list = sh.n_pool = 0;
@@ -468,13 +485,13 @@ __global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArg
   // so that `top` threads at least have an element there, each at least one.  The largest element of each thread sets the last floor behind the last
   // group in the same way, a tight one, and what is not below it is taken from the vectors noted: the first are held in shared memory, others read again.
   float best = z_head, floor = floor_of<T>(kLowest);
-  const int groups = max(1, (part.vecs + kTopThreads * kUnroll - 1) / (kTopThreads * kUnroll));
+  const int groups = max(1, (part.vecs + kT * kUnroll - 1) / (kT * kUnroll));
 #pragma unroll 1
   for (int g = 0; g < groups; ++g) {
-    const int v0 = g * kTopThreads * kUnroll + tid;
+    const int v0 = g * kT * kUnroll + tid;
     Vec v[kUnroll];
 #pragma unroll
-    for (int i = 0; i < kUnroll; ++i) v[i] = v0 + i * kTopThreads < part.vecs ? load_vec(body + (size_t)(v0 - tid + i * kTopThreads) * kVecBytes) : no_vec<T>();
+    for (int i = 0; i < kUnroll; ++i) v[i] = v0 + i * kT < part.vecs ? load_vec(body + (size_t)(v0 - tid + i * kT) * kVecBytes) : no_vec<T>();
     float high[kUnroll], most = best;
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i) {
@@ -488,7 +505,7 @@ __global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArg
     Sums2 more{0, 0};
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i)
-      if (v0 + i * kTopThreads < part.vecs) sums_add<T, kEnt, false>(more, v[i], c2, m2);
+      if (v0 + i * kT < part.vecs) sums_add<T, kEnt, false>(more, v[i], c2, m2);
     float2 s = split_f2(more.s), u = split_f2(more.u);
     if (kEnt && !(u.x + u.y == u.x + u.y)) {  // 0 * inf: masked logits among them (or NaN, which it stays)
       more = Sums2{0, 0};
@@ -499,32 +516,33 @@ __global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArg
     a.s += s.x + s.y;
     a.u += u.x + u.y;
     if (p.top == 0) continue;
-    if (g == 0 || (g == kSecondFloor && g + 1 < groups)) floor = floor_of<T>(kth_ordinal<T>(ordinal(best), p.top, p.top / 4, sh.pick2));
+    if (g == 0 || (g == kSecondFloor && g + 1 < groups)) floor = floor_of<T>(kth_ordinal<T, kT>(ordinal(best), p.top, p.top / 4, sh.pick2));
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i)
       if (high[i] >= floor) {
         const uint32_t at = atomicAdd(&sh.n_vec, 1u);
-        if (at < kNoted) sh.vec[at] = v0 + i * kTopThreads;
-        if (at < kHeld) {
+        if (at < Size::kNoted) sh.vec[at] = v0 + i * kT;
+        if (at < Size::kHeld) {
           sh.held[at] = make_uint4(v[i].w[0], v[i].w[1], v[i].w[2], v[i].w[3]);
-          sh.held[kHeld + at] = make_uint4(v[i].w[4], v[i].w[5], v[i].w[6], v[i].w[7]);
+          sh.held[Size::kHeld + at] = make_uint4(v[i].w[4], v[i].w[5], v[i].w[6], v[i].w[7]);
         }
       }
   }
-  a = block_sums<kTopThreads>(a, sh.red);
+  a = block_sums<kT>(a, sh.red);
   int n = 0;
   if (p.top > 0) {
-    uint32_t least = kth_ordinal<T>(ordinal(fmaxf(best, z_tail)), p.top, p.top / 16, sh.pick2);  // (barriers: the vectors are noted)
+    // (barriers: the vectors are noted; with one group the floor is the last one already)
+    uint32_t least = groups == 1 ? max(ordinal(floor), kLowest) : kth_ordinal<T, kT>(ordinal(fmaxf(best, z_tail)), p.top, p.top / 16, sh.pick2);
     float crowd = -INFINITY;
     // More candidates than there is room for: the `top`th value of the kCap that were kept is the next floor, or what is above it, where that is the floor
     // already and so is what crowds the list.  Two rounds drop kCap - top of them at least.
 #pragma unroll 1
     for (;;) {
-      collect<T>(part, z_head, z_tail, floor_of<T>(least), sh);
+      collect<T, kT>(part, z_head, z_tail, floor_of<T>(least), sh);
       __syncthreads();
       n = (int)sh.n_cand;
-      if (n <= kCap) break;
-      const uint32_t higher = nth_ordinal(sh.cand, p.top);
+      if (n <= Size::kCap) break;
+      const uint32_t higher = nth_ordinal<kT>(sh.cand, p.top);
       if (floor_of<T>(higher) > floor_of<T>(least)) {
         least = higher;
       } else {
@@ -538,35 +556,38 @@ __global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArg
     // Masked tokens, or those of the value that crowds, from the front.
     if (n < min(p.top, part.n)) {
       __syncthreads();
-      add_equal<T>(part.z, part.n, part.first, crowd, p.top - n, sh);
+      add_equal<T, kT>(part.z, part.n, part.first, crowd, p.top - n, sh);
       n = (int)sh.n_cand;
     }
   }
   if (parts > 1) {
     cluster_wait();
     if (tid == 0) *in_cta(&sh.part[rank], 0) = a;
-    if (n > 0) keep_largest<kCap>(sh.cand, n, p.top, in_cta(pool, 0), in_cta(&sh.n_pool, 0));
+    if (n > 0) keep_largest<Size::kCap, kT>(sh.cand, n, p.top, in_cta(pool, 0), in_cta(&sh.n_pool, 0));
     cluster_arrive();
     cluster_wait();
     if (rank != 0) return;
     a = sh.part[0];
     for (int k = 1; k < parts; ++k) a = sums_merge(a, sh.part[k]);
     n = (int)sh.n_pool;
-    if (n > 0) keep_largest<kPool>(pool, n, p.top, sh.list, &sh.n_list);
+    if (n > 0) keep_largest<kPool, kT>(pool, n, p.top, sh.list, &sh.n_list);
   } else if (n > 0) {
-    keep_largest<kCap>(sh.cand, n, p.top, sh.list, &sh.n_list);
+    keep_largest<Size::kCap, kT>(sh.cand, n, p.top, sh.list, &sh.n_list);
+  }
+  if (id < 0 || id >= p.V) {  // (asked here, so that the row's loads do not wait for the id's)
+    none(true);
+    return;
   }
   __syncthreads();
   n = (int)sh.n_list;
   Totals t{(double)a.m, a.s, a.u};
   const bool low = t.s == 0.f;
-  if (low) t = low_sums<T, kTopThreads>(zrow, p.V, p.c, sh.red, nullptr, 0);
+  if (low) t = low_sums<T, kT>(zrow, p.V, p.c, sh.red, nullptr, 0);
   const float ln_s = t.s == 0.f ? NAN : logf(t.s), nat = (float)p.nat;
   // In order: a key's place is the number of larger ordinals, and of lower indices among those that share that place.  (64-bit keys compared as they are, four
   // threads a key: 2,051 x 50,021 float32, top 128, 123 us against 110.)
-  static_assert(kFew == kTopThreads, "a key a thread");
   uint32_t* ordinals = reinterpret_cast<uint32_t*>(sh.vec);
-  uint32_t *shared_by = ordinals + kFew, *low_half = shared_by + kFew;
+  uint32_t *shared_by = ordinals + kT, *low_half = shared_by + kT;
   const Key key = tid < n ? sh.list[tid] : 0;
   const uint32_t mine = (uint32_t)(key >> 32);
   ordinals[tid] = mine;
@@ -594,13 +615,13 @@ __global__ void __launch_bounds__(kTopThreads, kTopCtas) top_kernel(const TopArg
       p.top_logp[row * p.top + at] = low || x < -FLT_MAX ? (float)(((double)z * (double)p.c - t.x0) * p.nat - (double)ln_s) : fmaf(x, nat, -ln_s);
     }
   }
-  if (tid == kTopThreads - 32) {  // (a warp that has hardly any keys)
+  if (tid == kT - 32) {  // (a warp that has hardly any keys)
     const double ln_s64 = t.s == 0.f ? NAN : log((double)t.s);
     if (p.lse != nullptr) p.lse[row] = (float)(t.x0 * p.nat + ln_s64);
     if (p.logp != nullptr) p.logp[row] = (float)(((double)load_f<T>(zrow + id) * (double)p.c - t.x0) * p.nat - ln_s64);
     if (kEnt) p.entropy[row] = (float)(ln_s64 - (double)t.u / (double)t.s * p.nat);
   }
-  for (int k = n + tid; k < p.top; k += kTopThreads) {
+  for (int k = n + tid; k < p.top; k += kT) {
     p.top_ids[row * p.top + k] = -1;
     p.top_logp[row * p.top + k] = -INFINITY;
   }
@@ -1330,10 +1351,18 @@ extern "C" int mrl_top_logprobs(const void* logits, int32_t dtype, int64_t N, in
   const TopArgs a{logits, ld, V, ids, mask, c, 1.0 / ((double)c * (double)temperature), top, logp, lse, entropy, top_logp, top_ids, status};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool bf16 = dtype == MRL_BF16, ent = entropy != nullptr;
-  const int parts = parts_of(N, (long long)V * (bf16 ? 2 : 4), kTopCtas);
+  const long long row_bytes = (long long)V * (bf16 ? 2 : 4);
+  const int parts = parts_of(N, row_bytes, TopSize<256>::kCtas);
+  // Short rows, more of them than CTAs of 256 threads fit: CTAs of fewer threads, if these give a floor (half of them at least above it).  (4,756 rows of 2,722
+  // bf16, top 4: 60 us with 256 threads, 35 with 64; 20,000 of 1,000 float32, top 20: 209 and 117.)
+  const int threads = N <= TopSize<256>::kCtas * 148 || row_bytes > 6 * 128 * kVecBytes || top > 64 ? 256 : row_bytes > 6 * 64 * kVecBytes || top > 32 ? 128 : 64;
+  using Kernel = void (*)(TopArgs);
+  const Kernel kernels[3][4] = {
+      {top_kernel<float, false, 256>, top_kernel<float, true, 256>, top_kernel<__nv_bfloat16, false, 256>, top_kernel<__nv_bfloat16, true, 256>},
+      {top_kernel<float, false, 128>, top_kernel<float, true, 128>, top_kernel<__nv_bfloat16, false, 128>, top_kernel<__nv_bfloat16, true, 128>},
+      {top_kernel<float, false, 64>, top_kernel<float, true, 64>, top_kernel<__nv_bfloat16, false, 64>, top_kernel<__nv_bfloat16, true, 64>}};
   mrl_profile_before(st, "top_kernel");
-  const int rc = launch_rows(bf16 ? (ent ? top_kernel<__nv_bfloat16, true> : top_kernel<__nv_bfloat16, false>)
-                                  : (ent ? top_kernel<float, true> : top_kernel<float, false>), N, parts, kTopThreads,
+  const int rc = launch_rows(kernels[threads == 256 ? 0 : threads == 128 ? 1 : 2][2 * bf16 + ent], N, parts, threads,
                              parts > 1 ? kPool * sizeof(Key) : 0, false, st, a);
   mrl_profile_after(st);
   return rc;
