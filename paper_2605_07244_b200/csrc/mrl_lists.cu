@@ -256,13 +256,13 @@ __device__ __forceinline__ Key key_of(float z, int index) { return ((Key)ordinal
 
 constexpr int kUnroll = 3;       // vectors of a thread and group
 constexpr int kSecondFloor = 3;  // the group behind which the floor is set again
-// What a CTA of kT threads holds.  256 threads take rows of any length; fewer take short rows, a thread's share of which is six vectors at most.
+// What a CTA of kT threads holds.  256 threads take any rows, and those that several CTAs share; 128 and 64 shorter ones.
 template <int kT>
 struct TopSize {
   static constexpr bool kAny = kT == 256;
   static constexpr int kCtas = kAny ? 5 : 1280 / kT;        // an SM
   static constexpr int kWarps = kT / 32;
-  static constexpr int kNoted = kAny ? 2048 : 6 * kT;       // vectors noted
+  static constexpr int kNoted = kT >= 128 ? 2048 : 384;     // vectors noted
   static constexpr int kHeld = kAny ? 320 : kT;             // those of them whose elements are held
   static constexpr int kCap = kAny ? 1024 : 512;            // candidates
   static constexpr int kFew = kT;                           // keys that are put in order by counting
@@ -421,7 +421,7 @@ __device__ __forceinline__ void collect(const Part<T>& part, float z_head, float
   };
   if (tid < part.head) push(z_head, tid);
   if (tid < part.tail) push(z_tail, part.n - part.tail + tid);
-  const bool all = TopSize<kT>::kAny && sh.n_vec > kNoted;
+  const bool all = sh.n_vec > kNoted;
   const int noted = all ? part.vecs : (int)sh.n_vec;
   for (int k = tid; k < noted && *(volatile uint32_t*)&sh.n_cand < 16 * kCap; k += kT) {
     const int at = all ? k : sh.vec[k];
@@ -1353,9 +1353,10 @@ extern "C" int mrl_top_logprobs(const void* logits, int32_t dtype, int64_t N, in
   const bool bf16 = dtype == MRL_BF16, ent = entropy != nullptr;
   const long long row_bytes = (long long)V * (bf16 ? 2 : 4);
   const int parts = parts_of(N, row_bytes, TopSize<256>::kCtas);
-  // Short rows, more of them than CTAs of 256 threads fit: CTAs of fewer threads, if these give a floor (half of them at least above it).  (4,756 rows of 2,722
-  // bf16, top 4: 60 us with 256 threads, 35 with 64; 20,000 of 1,000 float32, top 20: 209 and 117.)
-  const int threads = N <= TopSize<256>::kCtas * 148 || row_bytes > 6 * 128 * kVecBytes || top > 64 ? 256 : row_bytes > 6 * 64 * kVecBytes || top > 32 ? 128 : 64;
+  // More rows than CTAs of 256 threads fit at a time: of fewer threads for shorter rows, so that a row's loads and those of more others are under way during
+  // its selection, if half of the threads can be above a floor.  (6,000 rows of 30,000 bf16, top 20: 114 us with 256 threads, 98 with 128; 2,051 of 50,021 float32 88 and
+  // 97.  4,756 rows of 2,722 bf16, top 4: 60 with 256, 35 with 64; 2,790 of 6,301 float32 35 with 128.)
+  const int threads = N <= TopSize<256>::kCtas * 148 || row_bytes > 128 * 1024 || top > 64 ? 256 : row_bytes > 12 * 1024 || top > 32 ? 128 : 64;
   using Kernel = void (*)(TopArgs);
   const Kernel kernels[3][4] = {
       {top_kernel<float, false, 256>, top_kernel<float, true, 256>, top_kernel<__nv_bfloat16, false, 256>, top_kernel<__nv_bfloat16, true, 256>},

@@ -132,6 +132,24 @@ def test_special_rows(dtype, V, top, N):
         check(z[-3:], {k: v[-3:] if torch.is_tensor(v) else v for k, v in got.items()}, None, None, 1.0, top)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V,top,N", [(40, 32, 800), (1003, 32, 900), (1003, 64, 900), (2722, 4, 1500), (3001, 33, 760), (9001, 64, 790), (24001, 20, 745),
+                                     (32768, 64, 741), (3000, 128, 800)])
+def test_short_rows_of_many(V, top, N, dtype):
+    """More rows than are worked on at a time: special, crowded and plain ones, with bad ids and masked rows among them."""
+    z = torch.cat([special_rows(V, dtype, 0), crowded_rows(V, dtype, 0), rows(N - 27, V, dtype, V)[0]])
+    ids = torch.randint(0, V, (N,), generator=torch.Generator().manual_seed(2), dtype=torch.int32)
+    mask = torch.ones(N, dtype=torch.uint8)
+    ids[40], ids[50], mask[60], mask[61], ids[61] = V, -1, 0, 0, V
+    got = run(z, z.reshape(-1), ids, mask, 1.0, top)
+    assert got["status"] == B.DEV_BAD_TOKEN_ID
+    fine = torch.ones(N, dtype=torch.bool)
+    fine[[40, 50, 60, 61]] = False
+    check(z[fine], {k: v[fine] if torch.is_tensor(v) else v for k, v in got.items()}, ids[fine], mask[fine], 1.0, top)
+    for k in ("logp", "lse", "entropy", "top"):
+        assert not bool(got[k][~fine].any())
+
+
 def crowded_rows(V, dtype, N):
     """Rows where more tokens than a list of candidates holds are near its last place."""
     g = torch.Generator().manual_seed(V + 1)
