@@ -13,7 +13,6 @@ namespace {
 
 using namespace mrl;
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;  // two CTAs an SM
 constexpr int kTop = MRL_MAX_TOP;
 constexpr int kMaxParts = 8;                            // CTAs that share a row
 
@@ -835,15 +834,26 @@ __global__ void __launch_bounds__(1024) counts_kernel(const int2* __restrict__ f
 // are parked in shared memory, the rest comes from L2.  (A small load takes some 3 us while all others stream: what a row needs besides its logits is asked for
 // together with its first vectors.)
 constexpr int kDistillUnroll = 4;
-constexpr int kStream = kThreads - 32;  // threads that work on the logits; the last warp works on the list (in float64: with vectors in its registers too it would spill)
-// Shared memory of a CTA: bits, parked vectors, staging of outputs that start off 16 bytes from their inputs.  What it leaves is L1, which holds the
-// loads in flight.
-constexpr size_t kDistillSmem = 68 * 1024;
-constexpr uint32_t kStageRow = kVecBytes * 32, kStageBytes = kWarps * kStageRow;
+// CTAs of kT threads: 512 for rows of any length, and those that several CTAs share; 128 for short ones.
+constexpr uint32_t kStageRow = kVecBytes * 32;
+template <int kT>
+struct DistillSize {
+  static constexpr bool kAny = kT == 512;
+  static constexpr int kCtas = 1024 / kT;   // an SM
+  static constexpr int kStream = kT - 32;   // threads that work on the logits; the last warp works on the list (in float64: with vectors in its registers too it would spill)
+  // Shared memory of a CTA: bits, parked vectors, staging of outputs that start off 16 bytes from their inputs.  What it leaves is L1, which holds the
+  // loads in flight.
+  static constexpr size_t kSmem = kT * 136;
+  static constexpr uint32_t kStageBytes = kT / 32 * kStageRow;
+};
+// Bytes of a row up to which 128 threads work on it, where rows are more than CTAs of 512 fit: loads, sums and barriers of more rows overlap (20,000 rows of 1,000
+// float32 302 -> 110 us, 2,000 of 32,003 bf16 93 -> 75; of 20,000 float32, 80 KB, 77 and 78; of 32,768 105 and 122).
+constexpr long long kShortRow = 64 * 1024;
 constexpr double kNoRest = -700.0;  // ln p_r below which the learner gives the rest nothing: masks, of -inf or of the type's lowest value
 
+template <int kT>
 struct DistillShared {
-  Sums part[kMaxParts], red[kWarps];
+  Sums part[DistillSize<kT>::kAny ? kMaxParts : 1], red[kT / 32];
   float of_rest;
   uint32_t head_bits, tail_bits;
   int ids[kTop];
@@ -990,7 +1000,7 @@ __device__ __forceinline__ void store_shifted(char* out, const Vec& v, int count
   }
 }
 
-template <typename T>
+template <typename T, int kStream>
 __device__ void zero_part(T* out, int n) {
   const int head = min(n, (int)((0u - (uint32_t)reinterpret_cast<uintptr_t>(out)) & 15) / (int)sizeof(T));
   const int pieces = (n - head) / (16 / (int)sizeof(T)), tail0 = head + pieces * (16 / (int)sizeof(T));
@@ -1000,9 +1010,9 @@ __device__ void zero_part(T* out, int n) {
 }
 
 // The sums over the rest of a row from those of this thread, over all CTAs of the row; `low`: their offset is not a.m.  Called by all threads.
-template <typename T>
-__device__ __forceinline__ Totals rest_of_row(Sums& a, bool& low, const DistillArgs& p, const T* zrow, int parts, int rank, DistillShared& sh) {
-  a = block_sums<kThreads>(a, sh.red);
+template <typename T, int kT>
+__device__ __forceinline__ Totals rest_of_row(Sums& a, bool& low, const DistillArgs& p, const T* zrow, int parts, int rank, DistillShared<kT>& sh) {
+  a = block_sums<kT>(a, sh.red);
   if (parts > 1) {
     cluster_wait();
     if ((int)threadIdx.x < parts) *in_cta(&sh.part[rank], threadIdx.x) = a;
@@ -1013,7 +1023,7 @@ __device__ __forceinline__ Totals rest_of_row(Sums& a, bool& low, const DistillA
   }
   low = a.s == 0.f;
   if (!low) return Totals{(double)a.m, a.s, 0.f};
-  const Totals t = low_sums<T, kThreads>(zrow, p.V, p.c, sh.red, sh.ids, p.top);
+  const Totals t = low_sums<T, kT>(zrow, p.V, p.c, sh.red, sh.ids, p.top);
   if (parts > 1) {  // (the whole row was read: no CTA may write its gradient over it before all have)
     cluster_arrive();
     cluster_wait();
@@ -1023,14 +1033,17 @@ __device__ __forceinline__ Totals rest_of_row(Sums& a, bool& low, const DistillA
 
 // kShifted: outputs need not start on the same bytes of 32 as their inputs.  (A kernel of its own: code that a row runs through once comes from far, some 30 cycles
 // an instruction, if the loops leave no room for it near the SM.)
-template <typename T, bool kShifted>
-__global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillArgs p) {
+template <typename T, bool kShifted, int kT>
+__global__ void __launch_bounds__(kT, DistillSize<kT>::kCtas) distill_kernel(const DistillArgs p) {
+  constexpr int kStream = DistillSize<kT>::kStream;
   extern __shared__ uint4 dyn[];
-  __shared__ DistillShared sh;
+  __shared__ DistillShared<kT> sh;
   const int tid = threadIdx.x, lane = tid & 31;
-  int parts, rank;
-  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  int parts = 1, rank = 0;
+  if (DistillSize<kT>::kAny) {
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  }
   const long long row = blockIdx.x / (unsigned)parts;
   const T* zrow = static_cast<const T*>(p.logits) + row * p.ld;
   const Part<T> part(zrow, p.V, parts, rank);
@@ -1086,7 +1099,7 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillArgs 
     const float scale_f = (float)scale, nat_hi = (float)p.nat, nat_lo = (float)(p.nat - (double)nat_hi);
     Sums a = sums_empty();
     bool low;
-    const Totals rest = rest_of_row<T>(a, low, p, zrow, parts, rank, sh);
+    const Totals rest = rest_of_row<T, kT>(a, low, p, zrow, parts, rank, sh);
     if (lane == 0) {
       float f = 0.f;
       if (scale != 0.0 && rest.s != 0.f)
@@ -1094,7 +1107,7 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillArgs 
       sh.of_rest = f;
     }
     __syncwarp();
-    if (out != nullptr) asm volatile("bar.arrive 1, %0;" ::"n"(kThreads) : "memory");
+    if (out != nullptr) asm volatile("bar.arrive 1, %0;" ::"n"(kT) : "memory");
     RowFactors r = distill_row(rec.list, rest, p.nat, p.dp);
     r.scale = scale;
     if (lane == 0 && rank == 0) {
@@ -1128,7 +1141,7 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillArgs 
   for (int i = tid; i < p.bit_words / 4; i += kStream) dyn[i] = make_uint4(0, 0, 0, 0);
   if (tid == 0) sh.head_bits = sh.tail_bits = 0;
   if (stat != kRowValid) {  // (all CTAs of the row)
-    if (out != nullptr) zero_part(out, part.n);
+    if (out != nullptr) zero_part<T, kStream>(out, part.n);
     return;
   }
   __syncthreads();
@@ -1167,12 +1180,12 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const DistillArgs 
     a.s += s.x + s.y;
   }
   bool low;
-  const double x0 = rest_of_row<T>(a, low, p, zrow, parts, rank, sh).x0;
+  const double x0 = rest_of_row<T, kT>(a, low, p, zrow, parts, rank, sh).x0;
   if (out == nullptr) return;
-  asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");  // the list warp has the factor
+  asm volatile("bar.sync 1, %0;" ::"n"(kT) : "memory");  // the list warp has the factor
   const float of_rest = sh.of_rest;
   if (of_rest == 0.f) {
-    zero_part(out, part.n);
+    zero_part<T, kStream>(out, part.n);
     return;
   }
   if (low) {
@@ -1415,32 +1428,41 @@ extern "C" int mrl_distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64
     a.counts = w.sums;
     a.n_counts = kCounts;
   }
+  const long long row_bytes = (long long)V * elem;
+  const int threads = N > DistillSize<512>::kCtas * 148 && row_bytes <= kShortRow ? 128 : 512;
   // Rows of 512 KB or more are shared by two CTAs, so that the rows in flight still fit L2 between the passes.
-  int parts = parts_of(N, (long long)V * elem, 2);
-  if (parts == 1 && (long long)V * elem >= 512 * 1024) parts = 2;
+  int parts = parts_of(N, row_bytes, DistillSize<512>::kCtas);
+  if (parts == 1 && row_bytes >= 512 * 1024) parts = 2;
   const long long off = static_cast<const char*>(dlogits) - static_cast<const char*>(logits);
   const bool shifted = dlogits != nullptr && (off % kVecBytes != 0 || (N > 1 && (ld_out - ld) * elem % kVecBytes != 0));
   a.bit_words = (int)mrl_align_up((size_t)((V + parts - 1) / parts + 16 + 31) / 32, 4);
-  const size_t fixed = (size_t)a.bit_words * 4 + (shifted ? kStageBytes : 0);
-  if (dlogits != nullptr && fixed < kDistillSmem) a.park_slots = (int)((kDistillSmem - fixed) / (kStream * kVecBytes)) * kStream;
+  const size_t stage = threads == 128 ? DistillSize<128>::kStageBytes : DistillSize<512>::kStageBytes, room = threads == 128 ? DistillSize<128>::kSmem : DistillSize<512>::kSmem;
+  const size_t fixed = (size_t)a.bit_words * 4 + (shifted ? stage : 0);
+  const int movers = threads - 32;
+  if (dlogits != nullptr && fixed < room) a.park_slots = (int)((room - fixed) / (movers * kVecBytes)) * movers;
   const size_t smem = fixed + (size_t)a.park_slots * kVecBytes;
   using Kernel = void (*)(const DistillArgs);
-  const Kernel kernels[4] = {distill_kernel<__nv_bfloat16, false>, distill_kernel<__nv_bfloat16, true>, distill_kernel<float, false>,
-                             distill_kernel<float, true>};
+  const Kernel kernels[2][4] = {{distill_kernel<__nv_bfloat16, false, 512>, distill_kernel<__nv_bfloat16, true, 512>, distill_kernel<float, false, 512>,
+                                 distill_kernel<float, true, 512>},
+                                {distill_kernel<__nv_bfloat16, false, 128>, distill_kernel<__nv_bfloat16, true, 128>, distill_kernel<float, false, 128>,
+                                 distill_kernel<float, true, 128>}};
   static std::atomic<uint64_t> attr_done;
   int rc = mrl_once_per_device(attr_done, [&] {
-    // the carve-out that two CTAs an SM need, as a percentage of the 228 KB it can give: the rest stays L1
-    constexpr int kCarve = (int)((2 * (kDistillSmem + 4096) * 100 + 228 * 1024 - 1) / (228 * 1024));
-    for (const Kernel k : kernels) {
-      cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-      if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, kCarve);
+    // the carve-out that an SM's CTAs need, as a percentage of the 228 KB it can give: the rest stays L1
+    auto carve_out = [](size_t ctas, size_t bytes) { return (int)((ctas * bytes * 100 + 228 * 1024 - 1) / (228 * 1024)); };
+    for (int i = 0; i < 8; ++i) {
+      const Kernel k = kernels[i >> 2][i & 3];
+      cudaError_t e = i < 4 ? cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) : cudaSuccess;
+      if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout,
+                                 i < 4 ? carve_out(DistillSize<512>::kCtas, DistillSize<512>::kSmem + 4096) : carve_out(DistillSize<128>::kCtas, DistillSize<128>::kSmem + 2048));
       if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
   });
   if (rc != MRL_OK) return rc;
   mrl_profile_before(st, "distill_kernel");
-  rc = launch_rows(kernels[(bf16 ? 0 : 2) + shifted], N, parts, kThreads, smem, true, st, a);
+  rc = launch_rows(kernels[threads == 128][(bf16 ? 0 : 2) + shifted], N, parts, threads, smem, true, st, a);
   mrl_profile_after(st);
   if (rc != MRL_OK) return rc;
   const unsigned ctas = dlogits != nullptr ? 1 + (unsigned)((N + 31) / 32) : 1;

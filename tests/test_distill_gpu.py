@@ -189,6 +189,28 @@ def test_low_rows_of_several_blocks_in_place(N, kind, dtype):
         assert torch.equal(a["row_kl"].view(torch.int32), b["row_kl"].view(torch.int32))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kind", sorted(KINDS))
+@pytest.mark.parametrize("V,top,pad,offset", [(33, 8, 0, 0), (1003, 20, 3, 1), (9001, 128, 0, 0), (16000, 33, 0, 0)])
+def test_short_rows_of_many(V, top, pad, offset, kind, dtype):
+    N, low = 420, torch.finfo(dtype).min
+    z, flat = rows(N, V, dtype, V, pad, offset)
+    ids, logq = lists(z, top, 4)
+    free = torch.ones(N, V, dtype=torch.bool)
+    for r in range(0, N, 7):                # rows whose unlisted tokens are masked, one way and the other, some but for a few
+        free[r][ids[r][ids[r] >= 0].long()] = False
+        free[r, :V // 9 if r % 14 else 0] = False
+        z[r][free[r]] = -math.inf if r % 21 else low
+    g = torch.Generator().manual_seed(V)
+    weight = torch.rand(N, generator=g) + 0.5
+    mask = (torch.rand(N, generator=g) < 0.9).to(torch.uint8)
+    dp = params(kind, 1.0, 0.7)
+    a = run(z, flat, ids, logq, mask, weight, dp)
+    check(z, a, ids, logq, mask, weight, dp)
+    b = run(z, flat, ids, logq, mask, weight, dp, in_place=True)
+    assert torch.equal(a["dz"].view(torch.uint8), b["dz"].view(torch.uint8)) and torch.equal(a["row_kl"], b["row_kl"]) and a["loss"] == b["loss"]
+
+
 def test_refused_lists_and_empty_rows():
     z, flat = rows(9, 2000, torch.bfloat16, 5)
     ids, logq = lists(z, 70, 1, unused=False)
