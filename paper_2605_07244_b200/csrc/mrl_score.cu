@@ -408,14 +408,19 @@ product_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
 }
 
 // ------------------------------------------------------------------------------------------ product of few rows
-// Up to 16 rows of x: bound by the weights' bytes.  The weights take the tensor core's 128 lanes here and the rows of x its columns, so that a CTA keeps a deep
+// Up to 32 rows of x: bound by the weights' bytes.  The weights take the tensor core's 128 lanes here and the rows of x its columns, so that a CTA keeps a deep
 // ring of weights alone on its way; a thread sums one weight row's outputs.  Tiles are as high as makes all CTAs work on the same number of
 // them (151,936 rows: 9 of 115 on each of 148 SMs instead of 8 or 9 of 128).
 constexpr int kFewThreads = 192, kFewAccs = 8;  // warps: copies, issue, four that sum; accumulators, one K-block each
-constexpr int kFew = 16;                        // (of 17 rows 129 us against 126 with the tiles above, of 64, with as many columns, 154 against 130)
-constexpr uint32_t kFewStage = kATile + kFew * kBlock;
-constexpr int kFewStages = (int)(200 * 1024 / kFewStage);
-constexpr size_t kFewSmem = (size_t)kFewStages * kFewStage + 1024 /* alignment */ + 512 /* barriers */ + 4 * 4 * kFew * 4 /* scales of x */;
+// (with as many columns as rows, 64 of them 158 us at 64 rows against 131 with the tiles above, 32 of them 118 at 24 rows against 131)
+constexpr int kMostFew = 32;
+template <int kFew>
+struct FewSize {
+  static constexpr uint32_t kStage = kATile + kFew * kBlock;
+  // (one token's 622 MB of weights, their copies in 200 KB of stages an SM 118 us, in 183 115, in 146 to 164 112, in 110 115)
+  static constexpr int kStages = (int)(150 * 1024 / kStage);
+  static constexpr size_t kSmem = (size_t)kStages * kStage + 1024 /* alignment */ + 512 /* barriers */ + 4 * 4 * kFew * 4 /* scales of x */;
+};
 
 struct FewArgs {
   const float *x_scales, *w_scales;
@@ -425,9 +430,11 @@ struct FewArgs {
   int32_t* status;
 };
 
-template <typename T>
+template <typename T, int kFew>
 __global__ void __launch_bounds__(kFewThreads, 1)
 product_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const FewArgs p) {
+  constexpr int kFewStages = FewSize<kFew>::kStages;
+  constexpr uint32_t kFewStage = FewSize<kFew>::kStage;
   constexpr uint32_t kIdesc = (1u << 4) | ((uint32_t)(kFew >> 3) << 17) | ((uint32_t)(kBM >> 4) << 24);
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = smem_addr(smem_raw), tiles = (raw + 1023u) & ~1023u;
@@ -508,9 +515,9 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
       const int within = quad * 32 + lane, v = t * p.height + within;
       const bool live = within < p.height && v < p.V;
       const float* ws = p.w_scales + (live ? (long long)(v / kBlock) * p.k_blocks : 0);
-      float sum[kFew];
+      f2 sum[kFew / 2];
 #pragma unroll
-      for (int j = 0; j < kFew; ++j) sum[j] = 0.f;
+      for (int j = 0; j < kFew / 2; ++j) sum[j] = 0;
 #pragma unroll 1
       for (int kb0 = 0; kb0 < p.k_blocks && ok; kb0 += 4) {
         float sw[4];
@@ -529,6 +536,7 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
           if (!ok) break;
           tc_fence_after();
           const float w = q == 0 ? sw[0] : q == 1 ? sw[1] : q == 2 ? sw[2] : sw[3];
+          const f2 w2 = make_f2(w, w);
           const uint32_t src = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * kFew);
           const float4* s4 = reinterpret_cast<const float4*>(sx + q * kFew);
 #pragma unroll
@@ -542,10 +550,9 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
 #pragma unroll
             for (int j = 0; j < 16; j += 4) {
               const float4 s = s4[(c + j) / 4];
-              sum[c + j] = fmaf(__uint_as_float(d[j]), s.x * w, sum[c + j]);
-              sum[c + j + 1] = fmaf(__uint_as_float(d[j + 1]), s.y * w, sum[c + j + 1]);
-              sum[c + j + 2] = fmaf(__uint_as_float(d[j + 2]), s.z * w, sum[c + j + 2]);
-              sum[c + j + 3] = fmaf(__uint_as_float(d[j + 3]), s.w * w, sum[c + j + 3]);
+              f2* to = sum + (c + j) / 2;
+              to[0] = fma_f2(make_f2(__uint_as_float(d[j]), __uint_as_float(d[j + 1])), mul_f2(make_f2(s.x, s.y), w2), to[0]);
+              to[1] = fma_f2(make_f2(__uint_as_float(d[j + 2]), __uint_as_float(d[j + 3])), mul_f2(make_f2(s.z, s.w), w2), to[1]);
             }
           }
           if (++acc == kFewAccs) { acc = 0; acc_phase ^= 1u; }
@@ -555,8 +562,11 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
       if (live) {
         T* out = static_cast<T*>(p.out) + v;
 #pragma unroll
-        for (int j = 0; j < kFew; ++j)
-          if (j < p.N) store_f(out + j * p.ld_out, sum[j]);
+        for (int j = 0; j < kFew; j += 2) {
+          const float2 u = split_f2(sum[j / 2]);
+          if (j < p.N) store_f(out + j * p.ld_out, u.x);
+          if (j + 1 < p.N) store_f(out + (j + 1) * p.ld_out, u.y);
+        }
       }
     }
   }
@@ -603,11 +613,11 @@ int launch_product(const CUtensorMap& mx, const CUtensorMap& mw, const ProductAr
   return cudaGetLastError() == cudaSuccess ? MRL_OK : MRL_ERR_CUDA;
 }
 
-template <typename T>
+template <typename T, int kFew>
 int launch_few(const void* x8, long long ld_x, const void* w8, long long ld_w, int H, FewArgs a, cudaStream_t st) {
   static std::atomic<uint64_t> attr_done;
   int rc = mrl_once_per_device(attr_done, [] {
-    return cudaFuncSetAttribute(product_few_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem);
+    return cudaFuncSetAttribute(product_few_kernel<T, kFew>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FewSize<kFew>::kSmem);
   });
   if (rc != MRL_OK) return rc;
   const int sms = sm_count(), rounds = (int)(((long long)a.V + (long long)sms * kBM - 1) / ((long long)sms * kBM));
@@ -618,7 +628,7 @@ int launch_few(const void* x8, long long ld_x, const void* w8, long long ld_w, i
   if (rc == MRL_OK) rc = make_code_map(&mw, w8, a.V, H, ld_w, a.height);
   if (rc != MRL_OK) return rc;
   mrl_profile_before(st, "product_few_kernel");
-  product_few_kernel<T><<<a.tiles < sms ? a.tiles : sms, kFewThreads, kFewSmem, st>>>(mx, mw, a);
+  product_few_kernel<T, kFew><<<a.tiles < sms ? a.tiles : sms, kFewThreads, FewSize<kFew>::kSmem, st>>>(mx, mw, a);
   mrl_profile_after(st);
   return cudaGetLastError() == cudaSuccess ? MRL_OK : MRL_ERR_CUDA;
 }
@@ -660,9 +670,11 @@ extern "C" int mrl_e4m3_product(const void* x8, int64_t ld_x, const float* x_sca
   if (out == x8 || out == w8 || out == x_scales || out == w_scales) return MRL_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int k_blocks = (H + kBlock - 1) / kBlock;
-  if (N <= kFew) {
-    FewArgs f{x_scales, w_scales, out, ld_out, (int)N, V, k_blocks, 0, 0, status};
-    return out_dtype == MRL_BF16 ? launch_few<__nv_bfloat16>(x8, ld_x, w8, ld_w, H, f, st) : launch_few<float>(x8, ld_x, w8, ld_w, H, f, st);
+  if (N <= kMostFew) {
+    const FewArgs f{x_scales, w_scales, out, ld_out, (int)N, V, k_blocks, 0, 0, status};
+    if (out_dtype == MRL_BF16)
+      return N <= 16 ? launch_few<__nv_bfloat16, 16>(x8, ld_x, w8, ld_w, H, f, st) : launch_few<__nv_bfloat16, 32>(x8, ld_x, w8, ld_w, H, f, st);
+    return N <= 16 ? launch_few<float, 16>(x8, ld_x, w8, ld_w, H, f, st) : launch_few<float, 32>(x8, ld_x, w8, ld_w, H, f, st);
   }
   CUtensorMap mx, mw;
   int rc = make_code_map(&mx, x8, N, H, ld_x, kBM);

@@ -99,7 +99,7 @@ def check(out, x8, xs, w8, ws):
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("N,H,V", [(1, 1, 1), (1, 128, 129), (2, 16, 300), (5, 4096, 1000), (17, 130, 255), (64, 256, 256), (65, 384, 700),
                                    (127, 1003, 513), (128, 512, 4096), (200, 1024, 2000), (777, 1003, 5003), (300, 4096, 151), (1, 8192, 40000),
-                                   (1000, 640, 777)])
+                                   (1000, 640, 777), (16, 1003, 5000), (18, 2048, 20001), (31, 130, 30001), (32, 4096, 19000), (33, 512, 300)])
 def test_product(N, H, V, dtype):
     x8, xs, w8, ws = operands(N, H, V, N + H + V)
     wide = torch.full((N + 2, V + 3), 5.0, dtype=dtype, device="cuda")
