@@ -440,6 +440,31 @@ __device__ __forceinline__ void collect(const Part<T>& part, float z_head, float
   }
 }
 
+// As kth_ordinal, of the largest elements of the quarters of each thread's vector: where a row has hardly more vectors than its list has places.
+// (Those of whole vectors would be no floor, and all tokens candidates: 8,192 rows of 1,000 bf16, top 64: 141 us, this way 68.)
+template <typename T, int kT>
+__device__ __noinline__ uint32_t kth_of_quarters(const Vec v, int want) {
+  uint32_t mine[4], found = 0;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    float high;
+    if constexpr (sizeof(T) == 2)
+      high = fmaxf(fmaxf(bf16lo_to_f32(v.w[2 * q]), bf16hi_to_f32(v.w[2 * q])), fmaxf(bf16lo_to_f32(v.w[2 * q + 1]), bf16hi_to_f32(v.w[2 * q + 1])));
+    else
+      high = fmaxf(__uint_as_float(v.w[2 * q]), __uint_as_float(v.w[2 * q + 1]));
+    mine[q] = ordinal(high);
+  }
+  for (int bit = 31; bit >= (sizeof(T) == 2 ? 16 : 0); --bit) {
+    const uint32_t next = found | (1u << bit);
+    int n = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) n += __syncthreads_count(mine[q] >= next);
+    if (n >= want) found = next;
+    if (n >= want && n <= want + want / 4 + 2) break;
+  }
+  return max(found, kLowest);
+}
+
 template <typename T, bool kEnt, int kT>
 __global__ void __launch_bounds__(kT, TopSize<kT>::kCtas) top_kernel(const TopArgs p) {
   using Size = TopSize<kT>;
@@ -515,7 +540,8 @@ __global__ void __launch_bounds__(kT, TopSize<kT>::kCtas) top_kernel(const TopAr
     a.s += s.x + s.y;
     a.u += u.x + u.y;
     if (p.top == 0) continue;
-    if (g == 0 || (g == kSecondFloor && g + 1 < groups)) floor = floor_of<T>(kth_ordinal<T, kT>(ordinal(best), p.top, p.top / 4, sh.pick2));
+    if (part.vecs <= kT && 2 * p.top > part.vecs) floor = floor_of<T>(kth_of_quarters<T, kT>(v[0], p.top));
+    else if (g == 0 || (g == kSecondFloor && g + 1 < groups)) floor = floor_of<T>(kth_ordinal<T, kT>(ordinal(best), p.top, p.top / 4, sh.pick2));
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i)
       if (high[i] >= floor) {
