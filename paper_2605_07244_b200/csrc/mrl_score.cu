@@ -127,8 +127,12 @@ __global__ void __launch_bounds__(256) quantize_row_kernel(const QuantizeArgs p)
   for (int i = 0; i < kRowPieces; ++i) {
     const long long b = first + i * kGroups;
     float peak = piece[i].peak();
+    if constexpr (kLanes == 32) {
+      peak = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(peak)));  // (not negative: in the order of its bits)
+    } else {
 #pragma unroll
-    for (int o = kLanes / 2; o > 0; o >>= 1) peak = fmaxf(peak, __shfl_xor_sync(0xffffffffu, peak, o));
+      for (int o = kLanes / 2; o > 0; o >>= 1) peak = fmaxf(peak, __shfl_xor_sync(0xffffffffu, peak, o));
+    }
     const float scale = e4m3_scale(peak), inv = 1.0f / scale;
     if (b < total && lane == 0) p.scales[b] = scale;
     piece[i].store(p.codes + row[i] * p.ld_codes, col[i], p.H, inv, p.words);
