@@ -411,15 +411,12 @@ template <typename T, int kT>
 __device__ __forceinline__ void collect(const Part<T>& part, float z_head, float z_tail, float least_z, TopShared<kT>& sh) {
   constexpr int kCap = TopSize<kT>::kCap, kNoted = TopSize<kT>::kNoted, kHeld = TopSize<kT>::kHeld;
   const int tid = threadIdx.x;
-  auto push = [&](float z, int index) {
-    if (z >= least_z) {
-      const uint32_t at = atomicAdd(&sh.n_cand, 1u);
-      if (at < kCap) sh.cand[at] = key_of(z, part.first + index);
-      else atomicExch(&sh.cand[((uint32_t)index * 2654435769u) / (0xffffffffu / kCap + 1)], key_of(z, part.first + index));
-    }
+  auto put = [&](uint32_t at, float z, int index) {
+    if (at < kCap) sh.cand[at] = key_of(z, part.first + index);
+    else atomicExch(&sh.cand[((uint32_t)index * 2654435769u) / (0xffffffffu / kCap + 1)], key_of(z, part.first + index));
   };
-  if (tid < part.head) push(z_head, tid);
-  if (tid < part.tail) push(z_tail, part.n - part.tail + tid);
+  if (tid < part.head && z_head >= least_z) put(atomicAdd(&sh.n_cand, 1u), z_head, tid);
+  if (tid < part.tail && z_tail >= least_z) put(atomicAdd(&sh.n_cand, 1u), z_tail, part.n - part.tail + tid);
   const bool all = sh.n_vec > kNoted;
   const int noted = all ? part.vecs : (int)sh.n_vec;
   for (int k = tid; k < noted && *(volatile uint32_t*)&sh.n_cand < 16 * kCap; k += kT) {
@@ -432,10 +429,11 @@ __device__ __forceinline__ void collect(const Part<T>& part, float z_head, float
       v = load_vec(part.body() + (size_t)at * kVecBytes);
     }
     uint32_t bits = not_below<T>(v, least_z);
+    uint32_t place = bits != 0 ? atomicAdd(&sh.n_cand, (uint32_t)__popc(bits)) : 0;
 #pragma unroll 1
     for (; bits != 0; bits &= bits - 1) {
       const int e = __ffs(bits) - 1;
-      push(element<T>(v, e), part.head + at * kVecElems<T> + e);
+      put(place++, element<T>(v, e), part.head + at * kVecElems<T> + e);
     }
   }
 }
@@ -542,16 +540,22 @@ __global__ void __launch_bounds__(kT, TopSize<kT>::kCtas) top_kernel(const TopAr
     if (p.top == 0) continue;
     if (part.vecs <= kT && 2 * p.top > part.vecs) floor = floor_of<T>(kth_of_quarters<T, kT>(v[0], p.top));
     else if (g == 0 || (g == kSecondFloor && g + 1 < groups)) floor = floor_of<T>(kth_ordinal<T, kT>(ordinal(best), p.top, p.top / 4, sh.pick2));
+    int hits = 0;
 #pragma unroll
-    for (int i = 0; i < kUnroll; ++i)
-      if (high[i] >= floor) {
-        const uint32_t at = atomicAdd(&sh.n_vec, 1u);
-        if (at < Size::kNoted) sh.vec[at] = v0 + i * kT;
-        if (at < Size::kHeld) {
-          sh.held[at] = make_uint4(v[i].w[0], v[i].w[1], v[i].w[2], v[i].w[3]);
-          sh.held[Size::kHeld + at] = make_uint4(v[i].w[4], v[i].w[5], v[i].w[6], v[i].w[7]);
+    for (int i = 0; i < kUnroll; ++i) hits += high[i] >= floor;
+    if (hits != 0) {
+      uint32_t at = atomicAdd(&sh.n_vec, (uint32_t)hits);
+#pragma unroll
+      for (int i = 0; i < kUnroll; ++i)
+        if (high[i] >= floor) {
+          if (at < Size::kNoted) sh.vec[at] = v0 + i * kT;
+          if (at < Size::kHeld) {
+            sh.held[at] = make_uint4(v[i].w[0], v[i].w[1], v[i].w[2], v[i].w[3]);
+            sh.held[Size::kHeld + at] = make_uint4(v[i].w[4], v[i].w[5], v[i].w[6], v[i].w[7]);
+          }
+          ++at;
         }
-      }
+    }
   }
   a = block_sums<kT>(a, sh.red);
   int n = 0;
@@ -596,15 +600,18 @@ __global__ void __launch_bounds__(kT, TopSize<kT>::kCtas) top_kernel(const TopAr
     for (int k = 1; k < parts; ++k) a = sums_merge(a, sh.part[k]);
     n = (int)sh.n_pool;
     if (n > 0) keep_largest<kPool, kT>(pool, n, p.top, sh.list, &sh.n_list);
-  } else if (n > 0) {
+  } else if (n > Size::kFew) {
     keep_largest<Size::kCap, kT>(sh.cand, n, p.top, sh.list, &sh.n_list);
   }
+  const bool few = parts == 1 && n <= Size::kFew;  // the candidates are the list
   if (id < 0 || id >= p.V) {  // (asked here, so that the row's loads do not wait for the id's)
     none(true);
     return;
   }
-  __syncthreads();
-  n = (int)sh.n_list;
+  if (!few) {
+    __syncthreads();
+    n = (int)sh.n_list;
+  }
   Totals t{(double)a.m, a.s, a.u};
   const bool low = t.s == 0.f;
   if (low) t = low_sums<T, kT>(zrow, p.V, p.c, sh.red, nullptr, 0);
@@ -613,7 +620,7 @@ __global__ void __launch_bounds__(kT, TopSize<kT>::kCtas) top_kernel(const TopAr
   // threads a key: 2,051 x 50,021 float32, top 128, 123 us against 110.)
   uint32_t* ordinals = reinterpret_cast<uint32_t*>(sh.vec);
   uint32_t *shared_by = ordinals + kT, *low_half = shared_by + kT;
-  const Key key = tid < n ? sh.list[tid] : 0;
+  const Key key = tid < n ? (few ? sh.cand : sh.list)[tid] : 0;
   const uint32_t mine = (uint32_t)(key >> 32);
   ordinals[tid] = mine;
   shared_by[tid] = 0;
