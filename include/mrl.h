@@ -647,8 +647,8 @@ int mrl_e4m3_product(const void* x8, int64_t ld_x, const float* x_scales, const 
  * are listed after all others, by their index); a row of nothing else, one with NaN or with +inf: lse, logp, entropy and
  * top_logp as the formulas give them (NaN).  NaN logits are never listed; where fewer than `top` tokens can be, top_ids ends in -1, with
  * top_logp -inf.
- * float32 sums; bitwise reproducible for calls of the same N, V, dtype and alignment (few rows are cut among several CTAs: the
- * last bits of lse can differ from those of a larger call; ids never do).  Cost follows the bytes, except that rows whose logits rise with the
+ * float32 sums; bitwise reproducible for calls of the same N, V, dtype, top and alignment (few rows are cut among several CTAs, and
+ * many short ones worked on by smaller ones: the last bits of lse can differ from those of another call; ids never do).  Cost follows the bytes, except that rows whose logits rise with the
  * index and rows with more than 1,024 tokens of one value, the list's last place among them, are read once or twice more.
  * One output at least has to be given.  N = 0 is a no-op.  V > 2^30 -> MRL_ERR_UNSUPPORTED_SHAPE.  MRL_ERR_INVALID_ARG as in mrl_token_logprobs, and for a temperature or top
  * outside its range, an address that is not a multiple of its element, one address for two outputs.
@@ -686,7 +686,7 @@ int mrl_top_logprobs(const void* logits, int32_t dtype, int64_t N, int32_t V, in
  * value: ln p_r < -700 -- there is no rest: its term is left out (q_r = 0).  A listed token with z = -inf makes the forward KL infinite, its
  * gradient is finite; NaN, +inf and rows of -inf alone give NaN.
  * The rows' sums are float32, a row's KL and the sum over the rows float64 in a fixed order: bitwise reproducible for calls
- * of the same N, V, dtype and alignment.  N = 0: loss (and stats) are zeroed unless accumulated.  V > 2^20 -> MRL_ERR_UNSUPPORTED_SHAPE; other
+ * of the same N, V, dtype and alignment (other N: other last bits).  N = 0: loss (and stats) are zeroed unless accumulated.  V > 2^20 -> MRL_ERR_UNSUPPORTED_SHAPE; other
  * errors as in mrl_policy_loss_fwd_bwd and mrl_top_logprobs.
  */
 int mrl_distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64_t N, int32_t V, int64_t ld, const int32_t* top_ids,
