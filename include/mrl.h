@@ -649,7 +649,8 @@ int mrl_e4m3_product(const void* x8, int64_t ld_x, const float* x_scales, const 
  * top_logp -inf.
  * float32 sums; bitwise reproducible for calls of the same N, V, dtype, top and alignment (few rows are cut among several CTAs, and
  * many short ones worked on by smaller ones: the last bits of lse can differ from those of another call; ids never do).  Cost follows the bytes, except that rows whose logits rise with the
- * index and rows with more than 1,024 tokens of one value, the list's last place among them, are read once or twice more.
+ * index and rows with more than 1,024 tokens of one value, the list's last place among them, are read once or twice more, and rows
+ * without a logit above -1.4e9 T (rows masked throughout) or with one above 1.4e9 T twice more by single elements.
  * One output at least has to be given.  N = 0 is a no-op.  V > 2^30 -> MRL_ERR_UNSUPPORTED_SHAPE.  MRL_ERR_INVALID_ARG as in mrl_token_logprobs, and for a temperature or top
  * outside its range, an address that is not a multiple of its element, one address for two outputs.
  */

@@ -1,8 +1,9 @@
 // Top tokens and learning from them: mrl_top_logprobs and mrl_distill_loss_fwd_bwd.
 //
-// Both read rows of logits against a running (m, s): m the largest of z c, c = log2(e) / T, and s = sum_v 2^(z_v c - m).  m starts at the
-// lowest float, not at -inf, so that -inf - m stays -inf and a NaN always reaches the sum.  s = 0: nothing but -inf, or logits so low that z c
-// leaves float32 (rows masked throughout with the type's lowest value): those are summed again against their largest logit itself.
+// Both read rows of logits against a running (m, s): m the largest of z c, c = log2(e) / T, and s = sum_v 2^(z_v c - m), each exponent one multiply-add.
+// m is rounded and z c there is not, so the largest exponent is the product's rounding error: 64 at most where |z c| < 2^31, but thousands and up beyond (a mask
+// of -1e10: 440), where 2^t is infinite or 0.  So m starts at -2^31: what lies below (masks of -1e10, -1e30, of the type's lowest value, -inf) adds 0, and a NaN
+// always reaches the sum.  A row with nothing above -2^31, or with z c above 2^31, is summed again against its largest logit itself.
 #include <float.h>
 
 #include <type_traits>
@@ -126,7 +127,10 @@ __device__ __forceinline__ U* in_cta(U* p, int rank) {
 struct Sums {
   float m, s, u;  // u = sum_v 2^(t_v) t_v, t_v = z_v c - m
 };
-__device__ __forceinline__ Sums sums_empty() { return Sums{-FLT_MAX, 0.f, 0.f}; }
+constexpr float kFar = 2147483648.f;  // 2^31
+__device__ __forceinline__ Sums sums_empty() { return Sums{-kFar, 0.f, 0.f}; }
+// Is the row to be summed again, against its largest logit?
+__device__ __forceinline__ bool sums_far(Sums a) { return a.s == 0.f || a.m >= kFar; }
 // s and u over a higher maximum: u' = sum 2^(t + d) (t + d) with d = m - m'
 __device__ __forceinline__ Sums sums_raise(Sums a, float m) {
   const float d = a.m - m, f = ex2_approx(d);                       // (NaN for two infinities)
@@ -204,8 +208,8 @@ struct Totals {
   double x0;
   float s, u;
 };
-// The sums of a row whose s above is 0, against its largest logit: 2^((z - zm) c); without the `n` tokens of `ids`.  Called by the block; slow, and hardly
-// ever needed.  (Plain arguments: what a lambda takes by reference is copied to every thread's stack before the kernel begins, 250 MB for 1,480 rows.)
+// The sums of a row that is sums_far, against its largest logit: 2^((z - zm) c); without the `n` tokens of `ids`.  Called by the block; slow: two reads by
+// single elements, and each token is compared with each of `ids`.  (Plain arguments: what a lambda takes by reference is copied to every thread's stack before the kernel begins, 250 MB for 1,480 rows.)
 template <typename T, int kT>
 __device__ __noinline__ Totals low_sums(const T* z, int V, float c, Sums* red, const int* ids, int n) {
   auto listed = [&](int v) {
@@ -613,7 +617,7 @@ __global__ void __launch_bounds__(kT, TopSize<kT>::kCtas) top_kernel(const TopAr
     n = (int)sh.n_list;
   }
   Totals t{(double)a.m, a.s, a.u};
-  const bool low = t.s == 0.f;
+  const bool low = sums_far(a);
   if (low) t = low_sums<T, kT>(zrow, p.V, p.c, sh.red, nullptr, 0);
   const float ln_s = t.s == 0.f ? NAN : logf(t.s), nat = (float)p.nat;
   // In order: a key's place is the number of larger ordinals, and of lower indices among those that share that place.  (64-bit keys compared as they are, four
@@ -1042,7 +1046,7 @@ __device__ void zero_part(T* out, int n) {
   if (tail0 + (int)threadIdx.x < n) store_f(out + tail0 + threadIdx.x, 0.f);
 }
 
-// The sums over the rest of a row from those of this thread, over all CTAs of the row; `low`: their offset is not a.m.  Called by all threads.
+// The sums over the rest of a row from those of this thread, over all CTAs of the row; `low`: sums_far, their offset is not a.m.  Called by all threads.
 template <typename T, int kT>
 __device__ __forceinline__ Totals rest_of_row(Sums& a, bool& low, const DistillArgs& p, const T* zrow, int parts, int rank, DistillShared<kT>& sh) {
   a = block_sums<kT>(a, sh.red);
@@ -1054,7 +1058,7 @@ __device__ __forceinline__ Totals rest_of_row(Sums& a, bool& low, const DistillA
     a = sh.part[0];
     for (int k = 1; k < parts; ++k) a = sums_merge(a, sh.part[k]);
   }
-  low = a.s == 0.f;
+  low = sums_far(a);
   if (!low) return Totals{(double)a.m, a.s, 0.f};
   const Totals t = low_sums<T, kT>(zrow, p.V, p.c, sh.red, sh.ids, p.top);
   if (parts > 1) {  // (the whole row was read: no CTA may write its gradient over it before all have)
