@@ -683,8 +683,8 @@ int mrl_top_logprobs(const void* logits, int32_t dtype, int64_t N, int32_t V, in
  *   workspace: mrl_workspace_bytes(MRL_WS_DISTILL, N, 0, 0, 0, top)
  * A row is valid if its mask is on, its list has a used place and is not refused.  Refused (and flagged): an id >= V
  * (MRL_DEV_BAD_TOKEN_ID), a token twice, a log-prob of NaN or +inf (MRL_DEV_BAD_LIST).  Rows that are not valid: row_kl 0, gradient 0.
- * Where the learner leaves the rest nothing -- every token is listed, or the others are masked with -inf or the type's lowest
- * value: ln p_r < -700 -- there is no rest: its term is left out (q_r = 0).  A listed token with z = -inf makes the forward KL infinite, its
+ * Where every token is listed, or the others are masked -- the largest of their logits is -2^26 or less (-1e8, the type's lowest value, -inf) and
+ * ln p_r < -700 -- there is no rest: its term is left out (q_r = 0).  A listed token with z = -inf makes the forward KL infinite, its
  * gradient is finite; NaN, +inf and rows of -inf alone give NaN.
  * The rows' sums are float32, a row's KL and the sum over the rows float64 in a fixed order: bitwise reproducible for calls
  * of the same N, V, dtype and alignment (other N: other last bits).  N = 0: loss (and stats) are zeroed unless accumulated.  V > 2^20 -> MRL_ERR_UNSUPPORTED_SHAPE; other

@@ -17,7 +17,8 @@ F64 = torch.float64
 E4M3_MAX = 448.0
 SCALE_MIN = 2.0 ** -126
 BLOCK = 128
-NO_REST = -700.0        # ln p_r below which the learner gives the rest nothing
+NO_REST = -700.0        # ln p_r below which the learner gives the rest nothing, if it is masked:
+MASK = -2.0 ** 26       # the largest of its logits is this or less
 
 
 def _w(t):
@@ -76,7 +77,7 @@ def distill_row(z, ids, logps, temperature, reverse, rest_event, floor):
     p = x.exp() / total
     ln_p = x - total.log()
     ln_p_rest = float(torch.logsumexp(x[outside], 0) - total.log()) if bool(outside.any()) else -math.inf
-    has_rest = ln_p_rest >= NO_REST
+    has_rest = ln_p_rest > -math.inf and not (ln_p_rest < NO_REST and float(z[outside].max()) <= MASK)
     p_rest = math.exp(ln_p_rest) if has_rest else 0.0
     within = torch.zeros(V, dtype=F64)                                      # softmax over the rest
     if has_rest:

@@ -886,7 +886,10 @@ struct DistillSize {
 // Bytes of a row up to which 128 threads work on it, where rows are more than CTAs of 512 fit: loads, sums and barriers of more rows overlap (20,000 rows of 1,000
 // float32 302 -> 110 us, 2,000 of 32,003 bf16 93 -> 75; of 20,000 float32, 80 KB, 77 and 78; of 32,768 105 and 122).
 constexpr long long kShortRow = 64 * 1024;
-constexpr double kNoRest = -700.0;  // ln p_r below which the learner gives the rest nothing: masks, of -inf or of the type's lowest value
+// A rest whose largest logit (x0 in units of z c) is a mask, kMask or less, and which the learner leaves nothing, is no event.  What else has a small p_r is one,
+// however small: at T = 0.01 logits 8 apart make ln p_r = -800.  (A power of two, so that it is exact times c.)
+constexpr double kNoRest = -700.0, kMask = -67108864.0;
+__device__ __forceinline__ bool masked_away(double ln_p_rest, double x0, float c) { return ln_p_rest < kNoRest && x0 <= kMask * (double)c; }
 
 template <int kT>
 struct DistillShared {
@@ -921,12 +924,12 @@ __device__ __forceinline__ float rest_factor(const ListRecord& list, Sums a, flo
   const float in_list = list.sum_e_f * of_list, in_rest = a.s * of_rest, total = in_list + in_rest;
   const float p_rest = in_rest / total;
   if (dp.rest != MRL_REST_EVENT) return p_rest;
-  if (!(p_rest >= 1e-30f) && p_rest == p_rest) {  // is there a rest?  ln p_r below kNoRest
+  if (!(p_rest >= 1e-30f) && p_rest == p_rest) {  // is there a rest?
     const double ln_p_rest = (double)logf(a.s / total) - (d > 0.f ? (double)d * (double)nat_hi : 0.0);
-    if (ln_p_rest < kNoRest) return 0.f;
+    if (masked_away(ln_p_rest, (double)a.m, c)) return 0.f;
   }
   if (dp.direction == MRL_DISTILL_FORWARD) return fmaf(list.mass_f + list.q_rest_f, p_rest, -list.q_rest_f);
-  if (in_list == 0.f) return 0.f;  // (a list masked away: d may be -inf)
+  if (in_list == 0.f || p_rest == 0.f) return 0.f;  // (a list masked away, or one logit far above all: d may be infinite)
   int whole = (int)(__float_as_uint(a.s) >> 23) - 127;  // ln s = whole ln 2 + ln part
   float part = __uint_as_float((__float_as_uint(a.s) & 0x007fffffu) | 0x3f800000u);
   if (part > 1.41421356f) part *= 0.5f, ++whole;
@@ -938,7 +941,7 @@ __device__ __forceinline__ float rest_factor(const ListRecord& list, Sums a, flo
 }
 
 // A row's KL, and what its listed tokens' gradient takes
-__device__ __forceinline__ RowFactors distill_row(const ListRecord& list, Totals rest, double nat, const mrl_distill_params& dp) {
+__device__ __forceinline__ RowFactors distill_row(const ListRecord& list, Totals rest, float c, double nat, const mrl_distill_params& dp) {
   const bool event = dp.rest == MRL_REST_EVENT, any_rest = rest.s != 0.f;
   const double m = any_rest ? fmax(list.xs, rest.x0) : list.xs, below = list.xs - m, below_rest = rest.x0 - m;
   const float of_list = exp_of(below, nat), in_rest = any_rest ? rest.s * exp_of(below_rest, nat) : 0.f;
@@ -948,7 +951,7 @@ __device__ __forceinline__ RowFactors distill_row(const ListRecord& list, Totals
   r.shift = below * nat - ln_total;
   r.p_of_e = of_list / total;
   const double ln_p_rest = any_rest ? ln_of(rest.s) + below_rest * nat - ln_total : -INFINITY;
-  const bool has_rest = !(ln_p_rest < kNoRest);
+  const bool has_rest = any_rest && !masked_away(ln_p_rest, rest.x0, c);
   r.mass = list.mass;
   const float p_rest = has_rest ? in_rest / total : 0.f;
   r.of_rest = p_rest;
@@ -1140,12 +1143,12 @@ __global__ void __launch_bounds__(kT, DistillSize<kT>::kCtas) distill_kernel(con
     if (lane == 0) {
       float f = 0.f;
       if (scale != 0.0 && rest.s != 0.f)
-        f = (low ? distill_row(rec.list, rest, p.nat, p.dp).of_rest : rest_factor(rec.list, a, p.c, nat_hi, nat_lo, p.dp)) / rest.s * scale_f;
+        f = (low ? distill_row(rec.list, rest, p.c, p.nat, p.dp).of_rest : rest_factor(rec.list, a, p.c, nat_hi, nat_lo, p.dp)) / rest.s * scale_f;
       sh.of_rest = f;
     }
     __syncwarp();
     if (out != nullptr) asm volatile("bar.arrive 1, %0;" ::"n"(kT) : "memory");
-    RowFactors r = distill_row(rec.list, rest, p.nat, p.dp);
+    RowFactors r = distill_row(rec.list, rest, p.c, p.nat, p.dp);
     r.scale = scale;
     if (lane == 0 && rank == 0) {
       p.factors[row] = r;
