@@ -252,7 +252,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
       }
     }
   } else if (warp == 1) {
-    // (the whole warp goes through the loop, so that addresses and descriptors stay in uniform registers; one lane issues)
+    // (The whole warp goes through the loop, so that addresses and descriptors stay in uniform registers; one lane issues.  Nothing in the loop is for whole
+    // warps, so a lane may leave it by itself when a wait runs out.)
     const bool issuer = elect_one();
     int stage = 0, acc = 0;
     uint32_t phase = 0, acc_phase = 0;
@@ -312,8 +313,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         }
       };
       load_scales(0);
-      if (!mbar_wait(tfull_bar(acc), acc_phase, abort_flag)) { ok = false; break; }
-      __syncwarp();
+      if (!mbar_wait_warp(tfull_bar(acc), acc_phase, abort_flag)) { ok = false; break; }
       tc_fence_after();
       uint32_t v[2][32];  // the 32 columns that are added and the 32 on their way
       tc_ld32_start(mine + (uint32_t)(acc * kBN), v[0]);
@@ -329,19 +329,18 @@ product_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         const uint32_t src = mine + (uint32_t)(acc * kBN), last = tempty_bar(acc);
         acc ^= 1;
         if (acc == 0) acc_phase ^= 1u;
-        bool ready = false;
+        bool ready = false;  // in all lanes alike
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           tc_ld32_wait(v[c & 1]);
           if (c < 3) {
             tc_ld32_start(src + (uint32_t)(32 * (c + 1)), v[(c & 1) ^ 1]);
-            if (c == 2) ready = mbar_test(tfull_bar(acc), acc_phase);
+            if (c == 2) ready = __all_sync(0xffffffffu, mbar_test(tfull_bar(acc), acc_phase));
           } else {  // read: the accumulator may be written again
             tc_fence_before();
             if (lane == 0) mbar_arrive(last);
             if (kb + 1 < p.k_blocks) {
-              if (!ready) ok = mbar_wait(tfull_bar(acc), acc_phase, abort_flag);
-              __syncwarp();
+              if (!ready) ok = mbar_wait_warp(tfull_bar(acc), acc_phase, abort_flag);
               if (!ok) break;
               tc_fence_after();
               tc_ld32_start(mine + (uint32_t)(acc * kBN), v[0]);
@@ -535,8 +534,7 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         __syncwarp();
 #pragma unroll 1
         for (int q = 0; q < 4 && kb0 + q < p.k_blocks; ++q) {
-          ok = mbar_wait(tfull_bar(acc), acc_phase, abort_flag);
-          ok = __all_sync(0xffffffffu, ok);
+          ok = mbar_wait_warp(tfull_bar(acc), acc_phase, abort_flag);
           if (!ok) break;
           tc_fence_after();
           const float w = q == 0 ? sw[0] : q == 1 ? sw[1] : q == 2 ? sw[2] : sw[3];

@@ -67,6 +67,11 @@ __device__ __forceinline__ bool mbar_wait2(uint32_t bar, uint32_t parity, uint32
   if (ok != 0) return true;
   return mbar_wait(bar, parity, abort_flag) && mbar_wait(bar2, parity2, abort_flag);
 }
+// The same for a whole warp: true in all of its lanes or in none (each polls for itself, so that one may see the barrier and another the flag), for what follows
+// is for whole warps: __syncwarp and the aligned tcgen05 instructions.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+}
 // True in one lane of a converged warp, in a way that the compiler knows to be one.
 __device__ __forceinline__ bool elect_one() {
   uint32_t one;
