@@ -598,8 +598,8 @@ int mrl_adamw_step(const mrl_tensor_slot* slots, int32_t n_slots, const mrl_adam
  * mrl_e4m3_quantize -- a matrix as e4m3 codes with one float32 scale per block of block_rows x 128 elements:
  *   scales[a, b] = max(max over the block of |x| / 448, 2^-126),   codes[t, i] = e4m3(x[t, i] / scales[a, b])
  * to nearest even (where x / scale is within 2^-22 of itself of the border between two codes, either may come); the blocks at
- * the ends may be short.  NaN gives the code of NaN, infinities 448; the maxima pass over NaN, an infinite one gives an infinite
- * scale and codes of zero (NaN for the infinite elements).
+ * the ends may be short.  NaN gives the code of NaN; the maxima pass over NaN, an infinite one gives an infinite scale and codes of zero (NaN for
+ * the infinite elements).
  *
  *   x          [device] dtype [N, ld_x], MRL_BF16 or MRL_F32
  *   block_rows 128 (weights of mrl_e4m3_product) or 1 (its rows)
@@ -614,7 +614,10 @@ int mrl_e4m3_quantize(const void* x, int64_t ld_x, int32_t dtype, int64_t N, int
 /*
  * mrl_e4m3_product -- rows times weights, both in e4m3 codes with a scale for each block of 128 columns:
  *   out[t, v] = sum over blocks b of  x_scales[t, b] w_scales[v / 128, b]  sum over i in b of  x8[t, i] w8[v, i]
- * The inner sums are the tensor cores' (float32 accumulators), the outer one is float32, rounded once to the output's type.
+ * The inner sums are the tensor cores' (float32 accumulators), the outer one is float32, rounded once to the output's type.  The two scales of a block are
+ * multiplied first, in float32: their product has to lie from 2^-126 up to 2^127, as it does for scales of mrl_e4m3_quantize where the two blocks' largest
+ * magnitudes have a product from 2^-108 up to 2^144.  Below, an output loses bits or is 0; above, it is infinite or NaN.  Blocks of zeros, of scale 2^-126, add 0
+ * beside any finite scale.
  *
  *   x8        [device] uint8 [N, ld_x]   e4m3 codes: those of mrl_rmsnorm_residual_fwd (group 128) or of mrl_e4m3_quantize
  *   x_scales  [device] float32 [N, ceil(H / 128)], contiguous
@@ -686,9 +689,11 @@ int mrl_top_logprobs(const void* logits, int32_t dtype, int64_t N, int32_t V, in
  * Where every token is listed, or the others are masked -- the largest of their logits is -2^26 or less (-1e8, the type's lowest value, -inf) and
  * ln p_r < -700 -- there is no rest: its term is left out (q_r = 0).  A listed token with z = -inf makes the forward KL infinite, its
  * gradient is finite; NaN, +inf and rows of -inf alone give NaN.
- * The rows' sums are float32, a row's KL and the sum over the rows float64 in a fixed order: bitwise reproducible for calls
- * of the same N, V, dtype and alignment (other N: other last bits).  N = 0: loss (and stats) are zeroed unless accumulated.  V > 2^20 -> MRL_ERR_UNSUPPORTED_SHAPE; other
- * errors as in mrl_policy_loss_fwd_bwd and mrl_top_logprobs.
+ * The rows' sums, and the probabilities and logarithms taken from them, are float32; a row's KL is added up from these in float64, and so are the rows, in a
+ * fixed order: bitwise reproducible for calls of the same N, V, dtype and alignment (other N: other last bits).
+ * Cost follows the bytes, except that a row whose other tokens are all below -1.4e9 T (masked away, as in constrained decoding), or one of them above 1.4e9 T, is
+ * read twice more by single elements, each compared with the list.
+ * N = 0: loss (and stats) are zeroed unless accumulated.  V > 2^20 -> MRL_ERR_UNSUPPORTED_SHAPE; other errors as in mrl_policy_loss_fwd_bwd and mrl_top_logprobs.
  */
 int mrl_distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64_t N, int32_t V, int64_t ld, const int32_t* top_ids,
                              const float* top_logp, int32_t top, const uint8_t* mask, const float* row_weight,
