@@ -3,7 +3,8 @@
 // Both read rows of logits against a running (m, s): m the largest of z c, c = log2(e) / T, and s = sum_v 2^(z_v c - m), each exponent one multiply-add.
 // m is rounded and z c there is not, so the largest exponent is the product's rounding error: 64 at most where |z c| < 2^31, but thousands and up beyond (a mask
 // of -1e10: 440), where 2^t is infinite or 0.  So m starts at -2^31: what lies below (masks of -1e10, -1e30, of the type's lowest value, -inf) adds 0, and a NaN
-// always reaches the sum.  A row with nothing above -2^31, or with z c above 2^31, is summed again against its largest logit itself.
+// always reaches the sum.  A row whose s is 0 is summed again against its largest logit itself: one with nothing above -2^31, and one with z c of
+// 2^31 or more, whose s is made 0.
 #include <float.h>
 
 #include <type_traits>
@@ -129,8 +130,6 @@ struct Sums {
 };
 constexpr float kFar = 2147483648.f;  // 2^31
 __device__ __forceinline__ Sums sums_empty() { return Sums{-kFar, 0.f, 0.f}; }
-// Is the row to be summed again, against its largest logit?
-__device__ __forceinline__ bool sums_far(Sums a) { return a.s == 0.f || a.m >= kFar; }
 // s and u over a higher maximum: u' = sum 2^(t + d) (t + d) with d = m - m'
 __device__ __forceinline__ Sums sums_raise(Sums a, float m) {
   const float d = a.m - m, f = ex2_approx(d);                       // (NaN for two infinities)
@@ -172,8 +171,9 @@ __device__ __forceinline__ void sums_add(Sums& a, float z, float c) {
   if (m > a.m) a = sums_raise(a, m);
   sums_term<true, true>(z, c, a.m, a.s, a.u);
 }
-// Over the block, in a fixed order; every thread gets the result.  The maximum first, so that each thread rescales once.
-template <int kT>
+// Over the block, in a fixed order; every thread gets the result.  The maximum first, so that each thread rescales once.  (kRaw: whatever the maximum; otherwise
+// s = 0 where it is kFar or more.)
+template <int kT, bool kRaw = false>
 __device__ __forceinline__ Sums block_sums(Sums a, Sums* red) {
   constexpr int kWarps = kT / 32;
   float m = a.m;
@@ -185,7 +185,7 @@ __device__ __forceinline__ Sums block_sums(Sums a, Sums* red) {
   m = lane < kWarps ? red[lane].m : -FLT_MAX;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  a = sums_raise(a, m);
+  a = !kRaw && m >= kFar ? Sums{FLT_MAX, 0.f, 0.f} : sums_raise(a, m);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
@@ -208,7 +208,7 @@ struct Totals {
   double x0;
   float s, u;
 };
-// The sums of a row that is sums_far, against its largest logit: 2^((z - zm) c); without the `n` tokens of `ids`.  Called by the block; slow: two reads by
+// The sums of a row whose s above is 0, against its largest logit: 2^((z - zm) c); without the `n` tokens of `ids`.  Called by the block; slow: two reads by
 // single elements, and each token is compared with each of `ids`.  (Plain arguments: what a lambda takes by reference is copied to every thread's stack before the kernel begins, 250 MB for 1,480 rows.)
 template <typename T, int kT>
 __device__ __noinline__ Totals low_sums(const T* z, int V, float c, Sums* red, const int* ids, int n) {
@@ -222,12 +222,12 @@ __device__ __noinline__ Totals low_sums(const T* z, int V, float c, Sums* red, c
     if (!listed(v)) zm = fmaxf(zm, load_f<T>(z + v));
   Sums a{zm, 0.f, 0.f};
   __syncthreads();
-  zm = block_sums<kT>(a, red).m;
+  zm = block_sums<kT, true>(a, red).m;
   a = Sums{0.f, 0.f, 0.f};
   for (int v = threadIdx.x; v < V; v += kT)
     if (!listed(v)) sums_term<true, true>(load_f<T>(z + v) - zm, c, 0.f, a.s, a.u);
   __syncthreads();
-  a = block_sums<kT>(a, red);
+  a = block_sums<kT, true>(a, red);
   return Totals{(double)zm * (double)c, a.s, a.u};
 }
 
@@ -617,7 +617,7 @@ __global__ void __launch_bounds__(kT, TopSize<kT>::kCtas) top_kernel(const TopAr
     n = (int)sh.n_list;
   }
   Totals t{(double)a.m, a.s, a.u};
-  const bool low = sums_far(a);
+  const bool low = t.s == 0.f;
   if (low) t = low_sums<T, kT>(zrow, p.V, p.c, sh.red, nullptr, 0);
   const float ln_s = t.s == 0.f ? NAN : logf(t.s), nat = (float)p.nat;
   // In order: a key's place is the number of larger ordinals, and of lower indices among those that share that place.  (64-bit keys compared as they are, four
@@ -1049,7 +1049,7 @@ __device__ void zero_part(T* out, int n) {
   if (tail0 + (int)threadIdx.x < n) store_f(out + tail0 + threadIdx.x, 0.f);
 }
 
-// The sums over the rest of a row from those of this thread, over all CTAs of the row; `low`: sums_far, their offset is not a.m.  Called by all threads.
+// The sums over the rest of a row from those of this thread, over all CTAs of the row; `low`: their offset is not a.m.  Called by all threads.
 template <typename T, int kT>
 __device__ __forceinline__ Totals rest_of_row(Sums& a, bool& low, const DistillArgs& p, const T* zrow, int parts, int rank, DistillShared<kT>& sh) {
   a = block_sums<kT>(a, sh.red);
@@ -1061,7 +1061,7 @@ __device__ __forceinline__ Totals rest_of_row(Sums& a, bool& low, const DistillA
     a = sh.part[0];
     for (int k = 1; k < parts; ++k) a = sums_merge(a, sh.part[k]);
   }
-  low = sums_far(a);
+  low = a.s == 0.f;
   if (!low) return Totals{(double)a.m, a.s, 0.f};
   const Totals t = low_sums<T, kT>(zrow, p.V, p.c, sh.red, sh.ids, p.top);
   if (parts > 1) {  // (the whole row was read: no CTA may write its gradient over it before all have)
