@@ -211,10 +211,14 @@ struct Lse2 {
 
 __device__ __forceinline__ Lse2 lse2_empty() { return Lse2{-INFINITY, 0.f}; }
 
+// A sum carried to a higher maximum, f = 2^(old - new).  The maximum is a rounded product and the terms' exponents are not, so beyond 2^31 a sum over masks
+// alone (-1e10, -1e30) can be infinite: it counts nothing beside a maximum that makes f 0.  (A NaN stays one.)
+__device__ __forceinline__ float carried(float s, float f) { return f == 0.f && fabsf(s) == INFINITY ? 0.f : s * f; }
+
 __device__ __forceinline__ Lse2 lse2_merge(Lse2 a, Lse2 b) {
   float m = fmaxf(a.m, b.m);
   if (m == -INFINITY) return Lse2{m, 0.f};
-  return Lse2{m, a.s * ex2_approx(a.m - m) + b.s * ex2_approx(b.m - m)};
+  return Lse2{m, carried(a.s, ex2_approx(a.m - m)) + carried(b.s, ex2_approx(b.m - m))};
 }
 
 __device__ __forceinline__ Lse2 lse2_warp_reduce(Lse2 v) {

@@ -343,8 +343,8 @@ __global__ void __launch_bounds__(kT, 1024 / kT) row_stream_kernel(const RowPara
     const float m_new = fmaxf(m_run, vmax * MRL_LOG2E);
     if (m_new > m_run) {  // also the first group (m_run = -inf, s_run = 0)
       const float f = mrl::ex2_approx(m_run - m_new);
-      s_run *= f;
-      if (kEnt) u_run *= f;
+      s_run = mrl::carried(s_run, f);
+      if (kEnt) u_run = mrl::carried(u_run, f);
       m_run = m_new;
     }
     if (m_run != -INFINITY) {
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(kT, 1024 / kT) row_stream_kernel(const RowPara
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   const float rescale = m_run != -INFINITY ? mrl::ex2_approx(m_run - m) : 0.f;
-  float sum = s_run * rescale, usum = kEnt ? u_run * rescale : 0.f;
+  float sum = mrl::carried(s_run, rescale), usum = kEnt ? mrl::carried(u_run, rescale) : 0.f;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -400,7 +400,7 @@ __global__ void __launch_bounds__(kT, 1024 / kT) row_stream_kernel(const RowPara
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) tm = fmaxf(tm, __shfl_xor_sync(0xffffffffu, tm, o));
     const float wscale = wm != -INFINITY ? mrl::ex2_approx(wm - tm) : 0.f;
-    float ts = ws * wscale, tu = (kEnt && lane < kWarpsT) ? red[64 + lane] * wscale : 0.f;
+    float ts = mrl::carried(ws, wscale), tu = (kEnt && lane < kWarpsT) ? mrl::carried(red[64 + lane], wscale) : 0.f;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       ts += __shfl_xor_sync(0xffffffffu, ts, o);
@@ -424,8 +424,8 @@ __global__ void __launch_bounds__(kT, 1024 / kT) row_stream_kernel(const RowPara
         if (got) {  // rank order, so both CTAs form the same sums
           const float4 a = xchg[0], b = xchg[1];
           tm = fmaxf(a.x, b.x);
-          ts = (a.x != -INFINITY ? a.y * mrl::ex2_approx(a.x - tm) : 0.f) +
-               (b.x != -INFINITY ? b.y * mrl::ex2_approx(b.x - tm) : 0.f);
+          ts = (a.x != -INFINITY ? mrl::carried(a.y, mrl::ex2_approx(a.x - tm)) : 0.f) +
+               (b.x != -INFINITY ? mrl::carried(b.y, mrl::ex2_approx(b.x - tm)) : 0.f);
           zt = a.w != 0.f ? a.z : (b.w != 0.f ? b.z : 0.f);
         } else if (p.status != nullptr) {
           atomicOr(p.status, MRL_DEV_TIMEOUT);
