@@ -267,6 +267,7 @@ int mrl_group_advantages(const float* rewards, const int32_t* seq_len, int32_t P
  *   lse    [device] float32 [N], nullable; 0 on those rows
  *   workspace: mrl_workspace_bytes(MRL_WS_TOKEN_LOGPROBS, ...) (currently 0; may be NULL then)
  *
+ * Logits of -inf, and finite masks of any size (-1e9, -1e30, the type's lowest value) in a row with other logits, add 0.
  * float32 accumulation; results are bitwise reproducible from run to run.
  * N = 0 is a no-op.  V < 1, ld < V, N < 0, a null required pointer -> MRL_ERR_INVALID_ARG.
  */

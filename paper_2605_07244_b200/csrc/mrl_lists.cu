@@ -209,7 +209,7 @@ struct Totals {
   float s, u;
 };
 // The sums of a row whose s above is 0, against its largest logit: 2^((z - zm) c); without the `n` tokens of `ids`.  Called by the block; slow: two reads by
-// single elements, and each token is compared with each of `ids`.  (Plain arguments: what a lambda takes by reference is copied to every thread's stack before the kernel begins, 250 MB for 1,480 rows.)
+// single elements, and each token is compared with each of `ids` (distillation of 8,192 x 128,256 bf16 whose unlisted tokens are all masked: 779 -> 1,940 to 2,410 us).  (Plain arguments: what a lambda takes by reference is copied to every thread's stack before the kernel begins, 250 MB for 1,480 rows.)
 template <typename T, int kT>
 __device__ __noinline__ Totals low_sums(const T* z, int V, float c, Sums* red, const int* ids, int n) {
   auto listed = [&](int v) {

@@ -13,7 +13,7 @@ __device__ __forceinline__ void store_f(__nv_bfloat16* p, float v) { *p = __floa
 // ------------------------------------------------------------------------------------------ quantizer
 // A block's elements stay in registers between its maximum and its codes: one read, one write.  Bound by HBM (151,936 x 4,096 bf16 287 us, 6.5 TB/s).
 // kWide: 16 bytes of a row by one load, and their codes by one store.  Otherwise (rows off 16 bytes) four elements by single loads, and four codes by
-// one store where the codes' rows allow it.
+// one store where the codes' rows allow it: bound by issue (18,223 x 9,602 bf16 168 us, half of the copy rate, 86 % of the issue slots busy).
 template <typename T, bool kWide>
 struct Piece {
   static constexpr int kElems = kWide ? 16 / (int)sizeof(T) : 4, kWords = kElems * (int)sizeof(T) / 4;
@@ -157,9 +157,9 @@ int launch_quantize(const QuantizeArgs& a, int rows, cudaStream_t st) {
 // One CTA per SM works through tiles of 128 rows x 256 weights.  Warp 0 brings K-blocks of 128 codes (one 128-byte swizzle row) into a
 // ring by TMA, one thread of warp 1 multiplies each into one of two accumulators in tensor memory -- never two blocks into the same,
 // for each block has its own scale -- and eight warps add scale * accumulator to sums in registers, 128 columns (so one scale) of one
-// row a thread, while the next block is multiplied.  A block takes 827 cycles (stamps; 4,096 x 151,936 x 4,096 2.26 ms): 512 are the tensor core's, its
-// operands alone come in 715 (48 KB from L2), additions and loads out of tensor memory take the rest.  Pairs of CTAs, which share the weights' tile, 5.6 ms: an
-// arrival across the pair for every block; sixteen warps of 64 columns 2.96.
+// row a thread, while the next block is multiplied.  A block takes 827 cycles (stamps; 4,096 x 151,936 x 4,096 2.6 to 2.7 ms in repeated calls, 2.3 ms alone): 512 are the tensor core's, its
+// operands alone come in 715 (48 KB from L2), additions and loads out of tensor memory take the rest.  Pairs of CTAs, which share the weights' tile, 5.6 ms: each
+// block waited for an arrival across the pair; sixteen warps of 64 columns 2.96.
 constexpr int kBM = 128, kBN = 256;
 constexpr int kStages = 4, kEpiWarps = 8, kProductThreads = 128 + 32 * kEpiWarps;
 // registers of a thread: 168 at launch, moved from the first warpgroup (copies, issue) to the two that hold sums (128 x 40 + 256 x 232)
