@@ -654,7 +654,7 @@ int mrl_e4m3_product(const void* x8, int64_t ld_x, const float* x_scales, const 
  * float32 sums; bitwise reproducible for calls of the same N, V, dtype, top and alignment (few rows are cut among several CTAs, and
  * many short ones worked on by smaller ones: the last bits of lse can differ from those of another call; ids never do).  Cost follows the bytes, except that rows whose logits rise with the
  * index and rows with more than 1,024 tokens of one value, the list's last place among them, are read once or twice more, and rows
- * without a logit above -1.4e9 T (rows masked throughout) or with one above 1.4e9 T twice more by single elements.
+ * without a logit above some -1.5e9 T (rows masked throughout) or with one above 1.5e9 T twice more by single elements.
  * One output at least has to be given.  N = 0 is a no-op.  V > 2^30 -> MRL_ERR_UNSUPPORTED_SHAPE.  MRL_ERR_INVALID_ARG as in mrl_token_logprobs, and for a temperature or top
  * outside its range, an address that is not a multiple of its element, one address for two outputs.
  */
@@ -692,7 +692,7 @@ int mrl_top_logprobs(const void* logits, int32_t dtype, int64_t N, int32_t V, in
  * gradient is finite; NaN, +inf and rows of -inf alone give NaN.
  * The rows' sums, and the probabilities and logarithms taken from them, are float32; a row's KL is added up from these in float64, and so are the rows, in a
  * fixed order: bitwise reproducible for calls of the same N, V, dtype and alignment (other N: other last bits).
- * Cost follows the bytes, except that a row whose other tokens are all below -1.4e9 T (masked away, as in constrained decoding), or one of them above 1.4e9 T, is
+ * Cost follows the bytes, except that a row whose other tokens are all below some -1.5e9 T (masked away, as in constrained decoding), or one of them above 1.5e9 T, is
  * read twice more by single elements, each compared with the list.
  * N = 0: loss (and stats) are zeroed unless accumulated.  V > 2^20 -> MRL_ERR_UNSUPPORTED_SHAPE; other errors as in mrl_policy_loss_fwd_bwd and mrl_top_logprobs.
  */
